@@ -46,6 +46,7 @@ enum {
 };
 
 enum { HH_F32 = 0, HH_BF16 = 1 };                       /* weight / KV element type */
+enum { HH_F16 = 2 };                                    /* a further row type of the hh_kv4 calls */
 /*
  * Weight formats.  HH_WF_DTYPE: the weights are used as loaded (cfg.dtype).
  * HH_WF_Q4G32 (bf16 models only): the paper's mouth model runs 4-bit weights
@@ -243,6 +244,157 @@ void hh_destroy(hh_ctx* ctx);
  * src must be device memory, 16-byte aligned, bytes a positive multiple of
  * 16; otherwise HH_ERR_INVALID_ARG. */
 hh_status hh_read_probe(const void* src, size_t bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * A paged cache in 4 bits: its operators on the caller's own device memory.
+ *
+ * The KV cache's memory grows with the window (Sec. 6.6); held in 4 bits it
+ * is 72 bytes a position and kv head where fp16 takes 256.  Pages hold 16
+ * positions, heads have 64 dimensions, as in a context's cache.
+ *
+ * Values.  Keys and values are quantized in groups of 32 consecutive
+ * dimensions of one position and head (two groups a row): the scale s is
+ * max|x| / 7 (fp32 division), rounded to nearest even to 8 significant bits
+ * and to a multiple of 2^-24, at most 2720; the code is
+ * c = clamp(rint(x / s), -7, 7) (fp32 division, ties to even; 0 where s is
+ * 0); the value is c * s, which fp16 holds exactly.  Magnitudes above 19,040
+ * saturate.  A key or value row (64 dimensions) with an infinity or NaN has
+ * NaN as both its scales: what attends it is NaN, as it would be unquantized.
+ *
+ * Pages.  One page of one kv head is a block of 1,152 bytes; a page is
+ * n_kv_heads blocks in head order, a pool n_pages pages.  With n = c + 8 the
+ * block's nibbles (j = 0 the lowest of a 16-bit word) and fp16 scales are:
+ *   keys    bytes 0 .. 511: the code of (slot, dimension 32 t + 8 g + 2 j + h)
+ *           is nibble j of the 16-bit word 4 (16 g + slot) + 2 t + h;
+ *   values  bytes 512 .. 1023: the code of (slot, dimension 4 r + j) is
+ *           nibble j of the word 4 (16 (slot / 4) + r) + slot % 4;
+ *   scales  bytes 1024 .. 1087: keys, at [slot][group];
+ *           bytes 1088 .. 1151: values, at [group][slot].
+ *
+ * All calls enqueue on hip_stream (NULL: the null stream), which must belong
+ * to the current device, as must all memory; none of them synchronizes,
+ * allocates or keeps anything, so a caller may capture them into a graph.
+ * Pointers of the two descriptions below are read by the device when the
+ * call's kernels run, the descriptions themselves during the call.
+ * ------------------------------------------------------------------------ */
+
+typedef struct {
+  void* pool;                 /* device, 16-byte aligned: n_pages * n_kv_heads * 1152 bytes */
+  const int32_t* page_table;  /* device [table_rows][max_pages]: page ids in [0, n_pages)   */
+  int32_t n_pages, n_kv_heads;
+  int32_t max_pages;          /* columns of the page table                                  */
+  int32_t table_rows;
+} hh_kv4_pool;
+
+/* Rows of one or more sequences, each sequence's consecutive: sequence s has
+ * rows row_start[s] .. row_start[s + 1] - 1, at positions first_pos[s],
+ * first_pos[s] + 1, ...  A row at a negative position is padding: it has no
+ * key, and nothing to attend to. */
+typedef struct {
+  const int32_t* row_start;   /* device [n_seqs + 1], or NULL: one row each, row s          */
+  const int32_t* first_pos;   /* device [n_seqs]                                            */
+  const int32_t* table_row;   /* device [n_seqs] rows of the page table, or NULL: row s     */
+  int32_t n_seqs;
+  int32_t n_rows;             /* rows of the buffers                                        */
+  int32_t max_rows;           /* at least the longest sequence's rows (1 without row_start) */
+} hh_kv4_rows;
+
+/*
+ * Quantize key and value rows into their pages.
+ *  k, v      device, 16-byte aligned, [n_rows][n_kv_heads][64] of `dtype`
+ *            (HH_F32, HH_F16, HH_BF16) with k_stride and v_stride elements
+ *            from row to row (multiples of 16 bytes, at least n_kv_heads * 64),
+ *            so rows may be columns of a wider matrix.
+ *  rope      NULL, or device [rope_len][32][2] fp32, 16-byte aligned: cos and
+ *            sin of position and pair; keys are then rotated at their positions
+ *            (pairs i, i + 32), in 64 bits rounded once to fp32, before they
+ *            are quantized.
+ * Only the slots of the given positions are written.  Rows whose position is
+ * negative, or past the page table's max_pages * 16 or rope_len, are skipped.
+ * Two rows of one call must not have the same place in the cache.
+ * Errors: INVALID_ARG (NULL or misaligned pointers, a size < 1, a stride, an
+ * element type), UNSUPPORTED (more than 2^31 - 1 work items), HIP.
+ */
+hh_status hh_kv4_append(const hh_kv4_pool* pool, const hh_kv4_rows* rows, const void* k, const void* v, int32_t dtype,
+                        int64_t k_stride, int64_t v_stride, const float* rope, int32_t rope_len, void* hip_stream);
+
+/* The values that the pages hold for the given rows, into k and v (as in
+ * hh_kv4_append; c * s rounded to nearest even to `dtype`).  Rows at
+ * positions that have no page are set to 0.  Errors as hh_kv4_append's. */
+hh_status hh_kv4_read(const hh_kv4_pool* pool, const hh_kv4_rows* rows, void* k, void* v, int32_t dtype,
+                      int64_t k_stride, int64_t v_stride, void* hip_stream);
+
+/* Bytes of device memory that hh_kv4_attention needs for these sizes (their
+ * pointers are not read): 0 or more. */
+hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows* rows, int32_t n_heads, size_t* bytes);
+
+/*
+ * Causal grouped-query attention over the pages: the row at position p attends
+ * to the keys at positions 0 .. p of its sequence's page table row (its own
+ * included: append first), query head j to kv head j / (n_heads / n_kv_heads).
+ *   out = sum_t w_t v_t,  w = softmax_t(scale * q . k_t)
+ *  q, out    device, 16-byte aligned, [n_rows][n_heads][64] of q_dtype and
+ *            out_dtype, strides as above (at least n_heads * 64); out must not
+ *            overlap q.  n_heads is a multiple of n_kv_heads.
+ *  scale     finite, > 0.
+ *  rope      NULL, or as above: queries are rotated at their positions first
+ *            (in fp32).
+ *  workspace device, 256-byte aligned, hh_kv4_attention_workspace() bytes (NULL
+ *            if that is 0); its contents need not be kept or cleared, and calls
+ *            that may run at the same time need one each.
+ * Rows at negative positions give 0; rows of `out` in no sequence are left as
+ * they are.  Positions past max_pages * 16 - 1 are taken as that.  Sums and
+ * softmax are fp32; with an fp32 `out` the products take fp16 pairs (22 bits)
+ * of queries and weights, with a 16-bit one the weights are single fp16 numbers,
+ * 2^-12 off at most.  Equal calls give equal bits.
+ * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
+ * UNSUPPORTED (more than 2^31 - 1 workgroups), HIP.
+ */
+hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, const void* q, int32_t q_dtype,
+                           int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len,
+                           void* out, int32_t out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                           void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Pages of any paged cache: n_layers pools of n_pages pages of page_bytes, a
+ * pool every layer_stride bytes from `pool` (device, 16-byte aligned;
+ * page_bytes and layer_stride multiples of 16; layer_stride at least
+ * n_pages * page_bytes where there are several layers).  Streams, devices and
+ * captures as above.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Copy page src[i] to page dst[i] in every layer, i < n: a fork's last page, a
+ * stream's pages to another pool position.
+ *  src, dst  host, page ids, read during the call.  A page may be the source of
+ *            several copies.
+ * Errors: INVALID_ARG (NULL or misaligned pointers, sizes, an id out of range,
+ * a destination that is listed twice or is a source), OOM (host memory), HIP.
+ */
+hh_status hh_kv_copy_pages(void* pool, int32_t n_layers, int64_t layer_stride, int64_t page_bytes, int32_t n_pages,
+                           int32_t n, const int32_t* src, const int32_t* dst, void* hip_stream);
+
+/* Bytes of device memory hh_kv_compact needs for a pool of n_pages pages. */
+hh_status hh_kv_compact_workspace(int32_t n_pages, size_t* bytes);
+
+/*
+ * Move the live pages to the lowest ids, on the device, so that what lies
+ * behind them can be given back.  A page is live if an entry
+ * page_table[r][i], i < ceil(lengths[r] / 16), names it (several may: shared
+ * pages stay shared).  With L live pages, the live pages with ids >= L go, in
+ * ascending order, to the free ids < L in ascending order; no other page is
+ * touched, and the entries are rewritten.  Entries past a row's length stay as
+ * they are; entries out of range name no page and stay as well.
+ *  page_table  device [table_rows][max_pages].
+ *  lengths     device [table_rows], positions held by each row.
+ *  live        device, receives L.
+ *  workspace   device, 256-byte aligned, hh_kv_compact_workspace() bytes, one
+ *              for each call that may run at the same time; contents as above.
+ * Errors: INVALID_ARG, UNSUPPORTED (n_pages over 2^20), HIP.
+ */
+hh_status hh_kv_compact(void* pool, int32_t n_layers, int64_t layer_stride, int64_t page_bytes, int32_t n_pages,
+                        int32_t* page_table, int32_t table_rows, int32_t max_pages, const int32_t* lengths,
+                        int32_t* live, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Message of the last error on this context ("" if none); never NULL. */
 const char* hh_last_error(const hh_ctx* ctx);

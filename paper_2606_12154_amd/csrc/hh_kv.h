@@ -1,0 +1,67 @@
+// Launchers of the 4-bit paged cache's kernels (k_kv4.hip) and of the page
+// kernels (k_pages.hip); arguments have been checked by the callers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace hh {
+
+constexpr int kKv4Block = 1152;  // bytes of one (page, kv head): codes 512 + 512, scales 64 + 64
+
+enum RowType { kRowF32 = 0, kRowBF16 = 1, kRowF16 = 2 };
+
+struct Kv4Pool {
+  unsigned char* pool;
+  const int* table;
+  int n_pages, hkv, max_pages, table_rows;
+};
+
+// row_start and table_row may be null: one row each, table row s.
+struct Kv4Rows {
+  const int* row_start;
+  const int* first_pos;
+  const int* table_row;
+  int n_seqs, n_rows, max_rows;
+};
+
+// fp32 (cos, sin) at [position][pair], or null.
+struct RopeTable {
+  const float2* at;
+  int len;
+};
+
+struct Kv4Attend {
+  const void* q;
+  void* out;
+  int64_t q_stride, out_stride;
+  int q_type, out_type, hq;
+  float scale;
+  RopeTable rope;
+  float* part;  // workspace: split outputs and statistics
+};
+
+hipError_t kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
+                      int64_t k_stride, int64_t v_stride, RopeTable rope);
+hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
+                    int64_t v_stride);
+// Workgroups of the append and read kernels, and of the attention kernel:
+// callers refuse what does not fit a launch.
+int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R);
+int64_t kv4_attend_groups(const Kv4Pool& P, const Kv4Rows& R, int hq);
+size_t kv4_attend_workspace(const Kv4Pool& P, const Kv4Rows& R, int hq);
+hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A);
+
+// n_layers pools of pages of `bytes` (a multiple of 16), layer_stride bytes apart.
+struct PagePool {
+  unsigned char* pool;
+  int64_t layer_stride, bytes;
+  int n_layers, n_pages;
+};
+hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst);
+size_t compact_workspace(int n_pages);
+hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int table_rows, int max_pages,
+                         const int* lengths, int* live, void* ws);
+
+}  // namespace hh

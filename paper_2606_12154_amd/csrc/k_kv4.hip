@@ -1,0 +1,778 @@
+// A paged KV cache in 4 bits: quantizing rows into pages, reading them back,
+// and causal grouped-query attention over the pages (gfx950).
+//
+// Values are c * s: c an integer in -7 .. 7, s a scale of at most 8
+// significant bits for 32 dimensions of one position and head, a multiple of
+// 2^-24 of at most 2720.  Hence c * s and 24 s are fp16 numbers, and with a
+// code's nibble n = c + 8 in bits 6 .. 9 of 0x4c00 (16 + n as fp16) one packed
+// fp16 FMA, (16 + n) s - 24 s, gives two values without a rounding: a shift, an
+// and-or and an FMA for two elements.
+//
+// The block of a (page, head) is laid out so that a lane's 8 bytes are what it
+// needs as an operand of mfma_f32_16x16x32_f16 (lane l: row or column l % 16,
+// contraction elements 8 (l / 16) .. + 7), with no transposition:
+//   keys    lane l holds slot l % 16, dimensions 8 (l / 16) .. + 7 of each half;
+//   values  lane l holds slots 4 (l / 16) .. + 3, dimensions 4 (l % 16) .. + 3.
+// The scores of two pages, S^T[slot][query] (accumulator: column l % 16, rows
+// 4 (l / 16) + i), leave each lane with the slots of both pages that its value
+// bytes hold; with the contraction of O^T[dim][query] += V^T P^T taken in that
+// order, weights go from accumulators to operands within their lanes.
+#include "hh_device.h"
+#include "hh_kv.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace hh {
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kKeyScales = 1024, kValueScales = 1088;  // byte offsets in a block
+constexpr float kMaxScale = 2720.f;
+
+// ------------------------------------------------------------------ rows and types
+
+struct Seq {
+  int row0, n, first, trow;  // rows row0 .. row0 + n - 1 at positions first ..
+};
+
+// The sequence's rows, kept inside the buffers whatever the device arrays say.
+__device__ __forceinline__ Seq load_seq(const Kv4Pool& P, const Kv4Rows& R, int s) {
+  Seq q;
+  const int a = R.row_start ? R.row_start[s] : s, b = R.row_start ? R.row_start[s + 1] : s + 1;
+  q.row0 = min(max(a, 0), R.n_rows);
+  q.n = min(max(min(b, R.n_rows) - q.row0, 0), R.max_rows);
+  q.first = max(min(R.first_pos[s], 1 << 30), -(1 << 30));
+  q.trow = R.table_row ? R.table_row[s] : s;
+  // No such table row: every position is padding.
+  if (q.trow < 0 || q.trow >= P.table_rows) {
+    q.trow = 0;
+    q.first = -(1 << 30);
+  }
+  return q;
+}
+
+__device__ __forceinline__ const unsigned char* block_of(const Kv4Pool& P, const int* row, int page, int head) {
+  const int id = row[page];
+  // An id outside the pool reads its first page.
+  return P.pool + ((size_t)((unsigned)id < (unsigned)P.n_pages ? id : 0) * P.hkv + head) * kKv4Block;
+}
+
+// N elements (N * size a multiple of 8 bytes, 8-byte aligned) as fp32.
+template <int N>
+__device__ __forceinline__ void load_row(const void* p, size_t at, int type, float* f) {
+  if (type == kRowF32) {
+    const f32x4* s = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + at);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const f32x4 v = s[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[4 * i + j] = v[j];
+    }
+    return;
+  }
+  unsigned w[N / 2];
+  const u32x2* s = reinterpret_cast<const u32x2*>(static_cast<const unsigned short*>(p) + at);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    const u32x2 v = s[i];
+    w[2 * i] = v[0];
+    w[2 * i + 1] = v[1];
+  }
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    if (type == kRowF16) {
+      const f16x2 h = __builtin_bit_cast(f16x2, w[i]);
+      f[2 * i] = (float)h[0];
+      f[2 * i + 1] = (float)h[1];
+    } else {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+}
+
+__device__ __forceinline__ unsigned pack16(float a, float b, int type) {
+  if (type == kRowF16) return __builtin_bit_cast(unsigned, f16x2{(_Float16)a, (_Float16)b});
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b});
+}
+
+template <int N>
+__device__ __forceinline__ void store_row(void* p, size_t at, int type, const float* f) {
+  if (type == kRowF32) {
+    f32x4* d = reinterpret_cast<f32x4*>(static_cast<float*>(p) + at);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) d[i] = f32x4{f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]};
+    return;
+  }
+  u32x2* d = reinterpret_cast<u32x2*>(static_cast<unsigned short*>(p) + at);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i)
+    d[i] = u32x2{pack16(f[4 * i], f[4 * i + 1], type), pack16(f[4 * i + 2], f[4 * i + 3], type)};
+}
+
+// ------------------------------------------------------------------ append and read
+
+// Scale of a group whose largest magnitude is a (finite).
+__device__ __forceinline__ float group_scale(float a) {
+  const float t = a / 7.0f;
+  if (t < 0x1p-17f) return rintf(t * 0x1p24f) * 0x1p-24f;
+  const unsigned u = __float_as_uint(t);
+  return fminf(__uint_as_float((u + 0x7fffu + ((u >> 16) & 1u)) & 0xffff0000u), kMaxScale);
+}
+
+__device__ __forceinline__ unsigned code_of(float x, float s) {
+  if (!(s > 0.f)) return 8u;  // a zero scale, or NaN
+  return (unsigned)((int)fminf(fmaxf(rintf(x / s), -7.f), 7.f) + 8);
+}
+
+__device__ __forceinline__ unsigned short half_bits(float s) {
+  return __builtin_bit_cast(unsigned short, (_Float16)s);
+}
+
+// One wave has one (page, head) of one sequence: the rows of the call that lie
+// in that page.  Keys: lane (slot r, quarter g) has the 16 dimensions of its 8
+// code bytes, which are whole rotation pairs (i, i + 32); values: lane (r, g)
+// the 4 slots x 4 dimensions of its own.  A page that the rows fill is written
+// 8 bytes a lane; in one that they fill partly a lane writes its slots alone.
+__global__ __launch_bounds__(256) void k_kv4_append(Kv4Pool P, Kv4Rows R, const void* __restrict__ k,
+                                                    const void* __restrict__ v, int type, int64_t ks, int64_t vs,
+                                                    RopeTable rope, int tiles) {
+  const int lane = threadIdx.x & 63;
+  int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int head = (int)(w % P.hkv);
+  w /= P.hkv;
+  const int tile = (int)(w % tiles);
+  w /= tiles;
+  if (w >= R.n_seqs) return;
+  const Seq q = load_seq(P, R, (int)w);
+  const int lo = max(q.first, 0);
+  int hi = min(q.first + q.n, P.max_pages * kPage);
+  if (rope.at) hi = min(hi, rope.len);
+  const int page = lo / kPage + tile;
+  if (page * kPage >= hi) return;
+  const int id = P.table[(size_t)q.trow * P.max_pages + page];
+  if ((unsigned)id >= (unsigned)P.n_pages) return;
+  unsigned char* blk = P.pool + ((size_t)id * P.hkv + head) * kKv4Block;
+  const int r = lane & 15, g = lane >> 4;
+
+  {
+    const int pos = page * kPage + r;
+    const bool mine = pos >= lo && pos < hi;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    if (mine) {
+      const size_t at = (size_t)(q.row0 + (pos - q.first)) * ks + head * 64 + 8 * g;
+      load_row<8>(k, at, type, x);
+      load_row<8>(k, at + 32, type, x + 8);
+      if (rope.at) {
+        const float2* cs = rope.at + (size_t)pos * 32 + 8 * g;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 t = cs[i];
+          const double a = x[i], b = x[8 + i], c = t.x, s = t.y;
+          x[i] = (float)(a * c - b * s);
+          x[8 + i] = (float)(b * c + a * s);
+        }
+      }
+    }
+    float top[2] = {0.f, 0.f};
+    int bad = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      top[i >> 3] = fmaxf(top[i >> 3], fabsf(x[i]));
+      bad |= !(fabsf(x[i]) < INFINITY);
+    }
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+      top[0] = fmaxf(top[0], __shfl_xor(top[0], o, 64));
+      top[1] = fmaxf(top[1], __shfl_xor(top[1], o, 64));
+      bad |= __shfl_xor(bad, o, 64);
+    }
+    unsigned word[2], sc = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float s = bad ? NAN : group_scale(top[t]);
+      unsigned d = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        d |= code_of(x[8 * t + 2 * j], s) << (4 * j);
+        d |= code_of(x[8 * t + 2 * j + 1], s) << (4 * j + 16);
+      }
+      word[t] = d;
+      sc |= (unsigned)half_bits(s) << (16 * t);
+    }
+    if (mine) {
+      *reinterpret_cast<u32x2*>(blk + 8 * lane) = u32x2{word[0], word[1]};
+      if (g == 0) *reinterpret_cast<unsigned*>(blk + kKeyScales + 4 * r) = sc;
+    }
+  }
+
+  unsigned short code[4], sc[4];
+  bool mine[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int slot = 4 * g + i, pos = page * kPage + slot;
+    mine[i] = pos >= lo && pos < hi;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (mine[i]) load_row<4>(v, (size_t)(q.row0 + (pos - q.first)) * vs + head * 64 + 4 * r, type, x);
+    float top = 0.f;
+    int bad = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      top = fmaxf(top, fabsf(x[j]));
+      bad |= !(fabsf(x[j]) < INFINITY);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      top = fmaxf(top, __shfl_xor(top, o, 64));
+      bad |= __shfl_xor(bad, o, 64);
+    }
+    bad |= __shfl_xor(bad, 8, 64);
+    const float s = bad ? NAN : group_scale(top);
+    unsigned d = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) d |= code_of(x[j], s) << (4 * j);
+    code[i] = (unsigned short)d;
+    sc[i] = half_bits(s);
+  }
+  unsigned short* vb = reinterpret_cast<unsigned short*>(blk + 512) + 4 * lane;
+  unsigned short* vsc = reinterpret_cast<unsigned short*>(blk + kValueScales) + (r >> 3) * 16 + 4 * g;
+  if (mine[0] && mine[3]) {
+    *reinterpret_cast<u32x2*>(vb) =
+        u32x2{code[0] | (unsigned)code[1] << 16, code[2] | (unsigned)code[3] << 16};
+    if ((r & 7) == 0)
+      *reinterpret_cast<u32x2*>(vsc) = u32x2{sc[0] | (unsigned)sc[1] << 16, sc[2] | (unsigned)sc[3] << 16};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (mine[i]) {
+        vb[i] = code[i];
+        if ((r & 7) == 0) vsc[i] = sc[i];
+      }
+  }
+}
+
+// The same lanes the other way round.  Tiles are counted from the page of the
+// first position, which may be negative: such rows, and those past the page
+// table, are set to zero.
+__global__ __launch_bounds__(256) void k_kv4_read(Kv4Pool P, Kv4Rows R, void* __restrict__ k, void* __restrict__ v,
+                                                  int type, int64_t ks, int64_t vs, int tiles) {
+  const int lane = threadIdx.x & 63;
+  int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int head = (int)(w % P.hkv);
+  w /= P.hkv;
+  const int tile = (int)(w % tiles);
+  w /= tiles;
+  if (w >= R.n_seqs) return;
+  const Seq q = load_seq(P, R, (int)w);
+  const int page = (q.first >> 4) + tile;  // floor
+  const int hi = q.first + q.n;
+  if (page * kPage >= hi) return;
+  const bool held = page >= 0 && page < P.max_pages;
+  const unsigned char* blk =
+      block_of(P, P.table + (size_t)q.trow * P.max_pages, held ? page : 0, head);
+  const int r = lane & 15, g = lane >> 4;
+
+  {
+    const int pos = page * kPage + r;
+    if (pos >= q.first && pos < hi) {
+      const u32x2 word = *reinterpret_cast<const u32x2*>(blk + 8 * lane);
+      const unsigned sc = *reinterpret_cast<const unsigned*>(blk + kKeyScales + 4 * r);
+      const f16x2 s = __builtin_bit_cast(f16x2, sc);
+      const size_t at = (size_t)(q.row0 + (pos - q.first)) * ks + head * 64 + 8 * g;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int c = (int)(word[t] >> (4 * (e >> 1) + 16 * (e & 1)) & 15u) - 8;
+          x[e] = held ? (float)c * (float)s[t] : 0.f;
+        }
+        store_row<8>(k, at + 32 * t, type, x);
+      }
+    }
+  }
+  const u32x2 word = *reinterpret_cast<const u32x2*>(blk + 512 + 8 * lane);
+  const u32x2 sc = *reinterpret_cast<const u32x2*>(blk + kValueScales + (r >> 3) * 32 + 8 * g);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int pos = page * kPage + 4 * g + i;
+    if (pos < q.first || pos >= hi) continue;
+    const unsigned both = sc[i >> 1];
+    const f16x2 s = __builtin_bit_cast(f16x2, both);
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = (int)(word[i >> 1] >> (16 * (i & 1) + 4 * j) & 15u) - 8;
+      x[j] = held ? (float)c * (float)s[i & 1] : 0.f;
+    }
+    store_row<4>(v, (size_t)(q.row0 + (pos - q.first)) * vs + head * 64 + 4 * r, type, x);
+  }
+}
+
+// Pages that max_rows consecutive positions can touch.
+int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
+
+// ------------------------------------------------------------------ attention
+
+// Operand columns are (row, query head of the kv head's group) pairs, row-major:
+// column c of a sequence is row c / G, head c % G.
+struct Plan {
+  int nq;      // 16-column tiles of a wave
+  int wk;      // waves of a workgroup that share the columns and split the keys (4), or 1
+  int tiles;   // column tiles (workgroups) a sequence and kv head
+  int splits;  // key splits over workgroups
+};
+
+Plan plan_of(const Kv4Pool& P, const Kv4Rows& R, int hq) {
+  const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv);
+  Plan p;
+  p.nq = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+  const int64_t t4 = (cols + 63) / 64, seqs = (int64_t)R.n_seqs * P.hkv;
+  p.wk = (t4 + 3) / 4 * seqs >= 512 ? 1 : 4;
+  const int64_t tiles = p.wk == 1 ? (cols + 64 * p.nq - 1) / (64 * p.nq) : (cols + 16 * p.nq - 1) / (16 * p.nq);
+  p.tiles = (int)std::min<int64_t>(tiles, 1 << 30);
+  const int64_t groups = tiles * seqs;
+  const int most = (P.max_pages + 31) / 32;  // at least 32 pages each
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1023 + groups) / groups, most, 128}));
+  if (p.wk == 1) p.splits = 1;
+  return p;
+}
+
+// Pages of a split, given the pages that a column tile attends to.
+__device__ __forceinline__ int split_pages(int np, int splits) {
+  const int pairs = (np + 1) >> 1;
+  return 2 * ((pairs + splits - 1) / splits);
+}
+
+struct PageRegs {
+  u32x2 k, v, vs;
+  unsigned ks;
+};
+
+__device__ __forceinline__ void load_page(PageRegs& r, const unsigned char* blk, int lane) {
+  r.k = *reinterpret_cast<const u32x2*>(blk + 8 * lane);
+  r.v = *reinterpret_cast<const u32x2*>(blk + 512 + 8 * lane);
+  r.ks = *reinterpret_cast<const unsigned*>(blk + kKeyScales + 4 * (lane & 15));
+  r.vs = *reinterpret_cast<const u32x2*>(blk + kValueScales + ((lane & 15) >> 3) * 32 + 8 * (lane >> 4));
+}
+
+// Nibble j of both halves of w as 16 + n.
+template <int J>
+__device__ __forceinline__ f16x2 codes16(unsigned w) {
+  const unsigned x = J < 2 ? w << (6 - 4 * J) : w >> (4 * J - 6);
+  return __builtin_bit_cast(f16x2, (x & 0x03c003c0u) | 0x4c004c00u);
+}
+
+__device__ __forceinline__ f16x8 join8(f16x2 a, f16x2 b, f16x2 c, f16x2 d) {
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// 8 keys' elements of one dword under one scale.
+__device__ __forceinline__ f16x8 key_frag(unsigned w, f16x2 s, f16x2 b) {
+  return join8(__builtin_elementwise_fma(codes16<0>(w), s, b), __builtin_elementwise_fma(codes16<1>(w), s, b),
+               __builtin_elementwise_fma(codes16<2>(w), s, b), __builtin_elementwise_fma(codes16<3>(w), s, b));
+}
+
+// Dimension 4 r + J of the lane's 4 slots in each of two pages.
+template <int J>
+__device__ __forceinline__ f16x8 value_frag(u32x2 wa, u32x2 wb, const f16x2* s, const f16x2* b) {
+  return join8(__builtin_elementwise_fma(codes16<J>(wa[0]), s[0], b[0]),
+               __builtin_elementwise_fma(codes16<J>(wa[1]), s[1], b[1]),
+               __builtin_elementwise_fma(codes16<J>(wb[0]), s[2], b[2]),
+               __builtin_elementwise_fma(codes16<J>(wb[1]), s[3], b[3]));
+}
+
+// What the weights are scaled by, as an exponent: a weight is at most
+// 2^(kOffset + kSlack) (the maximum that they are taken against is raised once
+// scores lead it by more than kSlack), so fp16 holds it, and down to 2^-31 of
+// the row's largest.
+constexpr float kOffset = 7.f, kSlack = 8.f;
+
+// QT, PT: fp16 terms of queries and of weights.  Queries are scaled by a power of
+// two that puts a row's largest element into [2^13, 2^14), so that one term holds any
+// 16-bit query and two hold 22 bits of an fp32 one.
+template <int NQ, int QT, int PT, int WK>
+__global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  unsigned b = blockIdx.x;
+  const int head = b % (unsigned)P.hkv;
+  b /= (unsigned)P.hkv;
+  const int split = b % (unsigned)splits;
+  b /= (unsigned)splits;
+  // The last tiles have the most keys: they go first.
+  const int tile = tiles - 1 - (int)(b % (unsigned)tiles);
+  const Seq s = load_seq(P, R, b / (unsigned)tiles);
+  const int G = A.hq / P.hkv;
+  const int cols = s.n * G;  // below 2^31 with a tile to spare (kv4_attend_groups)
+  const int c0 = (tile * (WK == 1 ? 4 : 1) + (WK == 1 ? wave : 0)) * (16 * NQ);
+  if (c0 >= cols) return;
+  // Keys of the tile's first and last row.
+  const int most = P.max_pages * kPage;
+  const int row_a = c0 / G, row_b = (min(c0 + 16 * NQ, cols) - 1) / G;
+  const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
+  const int np = (some_see + kPage - 1) / kPage;
+  const int per = split_pages(np, splits);
+  const int p0 = split * per, p1 = min(p0 + per, np);
+  const bool joined = per < np;  // several splits have keys
+  if (split > 0 && p0 >= np) return;
+
+  // ---- queries
+  f16x8 qh[NQ][2], ql[QT == 2 ? NQ : 1][2];
+  float qs[NQ];  // scores to powers of two
+  int lim[NQ];   // keys that the column sees
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    const int c = c0 + 16 * t + r;
+    const bool real = c < cols;
+    const int row = real ? c / G : row_a, j = real ? c % G : 0;
+    lim[t] = real ? min(max(s.first + row + 1, 0), most) : 0;
+    float x[16];
+    const size_t at = (size_t)(s.row0 + row) * A.q_stride + (head * G + j) * 64 + 8 * g;
+    load_row<8>(A.q, at, A.q_type, x);
+    load_row<8>(A.q, at + 32, A.q_type, x + 8);
+    if (A.rope.at) {
+      const int pos = min(max(s.first + row, 0), A.rope.len - 1);
+      const f32x4* cs = reinterpret_cast<const f32x4*>(A.rope.at + (size_t)pos * 32 + 8 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 w = cs[i];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float a = x[2 * i + e], bb = x[8 + 2 * i + e], co = w[2 * e], si = w[2 * e + 1];
+          x[2 * i + e] = a * co - bb * si;
+          x[8 + 2 * i + e] = bb * co + a * si;
+        }
+      }
+    }
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    int e = 0;
+    if (top > 0.f && top < INFINITY) e = 14 - __builtin_amdgcn_frexp_expf(top);
+    qs[t] = fmaxf(__builtin_amdgcn_ldexpf(A.scale * 1.4426950408889634f, -e), 1e-37f);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float y = real ? __builtin_amdgcn_ldexpf(x[i], e) : 0.f;
+      const _Float16 h = (_Float16)y;
+      qh[t][i >> 3][i & 7] = h;
+      if constexpr (QT == 2) ql[t][i >> 3][i & 7] = (_Float16)(y - (float)h);
+    }
+  }
+
+  // ---- keys and values
+  f32x4 o[NQ][4], sum[NQ];
+  float base[NQ], raise[NQ];  // weights are 2^(S qs - base); a score above raise raises it
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    base[t] = 0.f;
+    raise[t] = -INFINITY;
+  }
+  const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+  const int* row = P.table + (size_t)s.trow * P.max_pages;
+
+  auto fetch = [&](PageRegs* pr, int p) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_page(pr[i], block_of(P, row, min(p + i, np - 1), head), lane);
+  };
+
+  auto step = [&](const PageRegs* pr, int p, auto masked) {
+    constexpr bool MASK = decltype(masked)::value;
+    f16x8 kf[2][2];
+    f16x2 vsc[4], vbi[4];
+    unsigned nan4 = 0;  // MASK: the lane's 8 value slots whose scale is NaN
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f16x2 sc = __builtin_bit_cast(f16x2, pr[i].ks);
+      const f16x2 s0 = {sc[0], sc[0]}, s1 = {sc[1], sc[1]};
+      const f16x2 m24 = {(_Float16)-24, (_Float16)-24};
+      kf[i][0] = key_frag(pr[i].k[0], s0, s0 * m24);
+      kf[i][1] = key_frag(pr[i].k[1], s1, s1 * m24);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        unsigned w = pr[i].vs[h];
+        if constexpr (MASK) {
+          // Values that no row of the tile sees may be anything; a NaN that
+          // only some rows see must not reach the others as 0 x NaN, so it
+          // goes through the scores.
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const int slot = (p + i) * kPage + 4 * g + 2 * h + z;
+            const unsigned bits = w >> (16 * z) & 0xffffu;
+            const bool bad = (bits & 0x7c00u) == 0x7c00u;
+            if (bad || slot >= some_see) w &= z ? 0x0000ffffu : 0xffff0000u;
+            if (bad) nan4 |= 1u << (4 * i + 2 * h + z);
+          }
+        }
+        const f16x2 sv = __builtin_bit_cast(f16x2, w);
+        vsc[2 * i + h] = sv;
+        vbi[2 * i + h] = sv * f16x2{(_Float16)-24, (_Float16)-24};
+      }
+    }
+    if constexpr (MASK) {
+      // Either group of a value row may hold the NaN: lanes r and r ^ 8.
+      nan4 |= (unsigned)__shfl_xor((int)nan4, 8, 64);
+    }
+    f16x8 vf[4];
+    vf[0] = value_frag<0>(pr[0].v, pr[1].v, vsc, vbi);
+    vf[1] = value_frag<1>(pr[0].v, pr[1].v, vsc, vbi);
+    vf[2] = value_frag<2>(pr[0].v, pr[1].v, vsc, vbi);
+    vf[3] = value_frag<3>(pr[0].v, pr[1].v, vsc, vbi);
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      f32x4 sc[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (QT == 2) {
+          sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], ql[t][0], sc[i], 0, 0, 0);
+          sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], ql[t][1], sc[i], 0, 0, 0);
+        }
+        sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], qh[t][0], sc[i], 0, 0, 0);
+        sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], qh[t][1], sc[i], 0, 0, 0);
+      }
+      if constexpr (MASK) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int slot = (p + i) * kPage + 4 * g + e;
+            const float x = nan4 >> (4 * i + e) & 1u ? NAN : sc[i][e];
+            sc[i][e] = slot < lim[t] ? x : -INFINITY;
+          }
+      }
+      float mx = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3]));
+      mx = fmaxf(mx, fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      if (__builtin_amdgcn_ballot_w64(mx > raise[t])) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        if (mx > raise[t] || (raise[t] > -INFINITY && fmaf(mx, qs[t], -base[t]) > kOffset)) {
+          const float nb = mx * qs[t] - kOffset;
+          const float f = raise[t] > -INFINITY ? __builtin_amdgcn_exp2f(base[t] - nb) : 0.f;
+          base[t] = nb;
+          raise[t] = mx + kSlack / qs[t];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[t][j] *= f;
+          sum[t] *= f;
+        }
+      }
+      f16x8 ph, pl;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(sc[i][e], qs[t], -base[t]));
+          const _Float16 h = (_Float16)w;
+          ph[4 * i + e] = h;
+          if constexpr (PT == 2) pl[4 * i + e] = (_Float16)(w - (float)h);
+        }
+      if constexpr (PT == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], pl, o[t][j], 0, 0, 0);
+        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl, sum[t], 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], ph, o[t][j], 0, 0, 0);
+      // Weights are summed as they enter the products.
+      sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph, sum[t], 0, 0, 0);
+    }
+  };
+
+  {
+    PageRegs cur[2], nxt[2];
+    int p = p0 + (WK == 1 ? 0 : 2 * wave);
+    constexpr int STEP = WK == 1 ? 2 : 8;
+    if (p < p1) fetch(cur, p);
+    while (p < p1) {
+      const int pn = p + STEP;
+      if (pn < p1) fetch(nxt, pn);
+      if ((p + 2) * kPage <= all_see) step(cur, p, std::false_type());
+      else step(cur, p, std::true_type());
+      cur[0] = nxt[0];
+      cur[1] = nxt[1];
+      p = pn;
+    }
+  }
+
+  // ---- output of 16 consecutive dimensions of column c, or the split's part
+  auto put = [&](int c, int d0, auto n_const, const float* x, float l, float m) {
+    constexpr int N = decltype(n_const)::value;
+    if (c >= cols) return;
+    const int rw = s.row0 + c / G, hd = head * G + c % G;
+    if (joined) {
+      const size_t at = ((size_t)split * R.n_rows + rw) * A.hq + hd;
+      float* dst = A.part + at * 64 + d0;
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i)
+        *reinterpret_cast<f32x4*>(dst + 4 * i) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+      if (d0 == 0) {
+        float2* ml = reinterpret_cast<float2*>(A.part + (size_t)splits * R.n_rows * A.hq * 64) + at;
+        *ml = make_float2(m, l);
+      }
+      return;
+    }
+    float y[N];
+    const float inv = l == 0.f ? 0.f : 1.0f / l;  // nothing to attend to: 0
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = x[i] * inv;
+    store_row<N>(A.out, (size_t)rw * A.out_stride + hd * 64 + d0, A.out_type, y);
+  };
+
+  if constexpr (WK == 1) {
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[4 * i + j] = o[t][j][i];
+      put(c0 + 16 * t + r, 16 * g, std::integral_constant<int, 16>(), x, sum[t][0],
+          raise[t] > -INFINITY ? base[t] : -INFINITY);
+    }
+  } else {
+    // Join the four waves: wave w takes dimensions 16 g + 4 w .. + 3.
+    __shared__ f32x4 lo[4][4][64];
+    __shared__ float2 ls[4][64];
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      if (t) __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{o[t][0][i], o[t][1][i], o[t][2][i], o[t][3][i]};
+      ls[wave][lane] = make_float2(raise[t] > -INFINITY ? base[t] : -INFINITY, sum[t][0]);
+      __syncthreads();
+      float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) m = fmaxf(m, ls[w][lane].x);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float2 z = ls[w][lane];
+        // A wave without a finite score adds 0, or NaN if it saw one.
+        const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
+        const f32x4 y = lo[w][wave][lane];
+        l += f * z.y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+      }
+      put(c0 + 16 * t + r, 16 * g + 4 * wave, std::integral_constant<int, 4>(), x, l, m);
+    }
+  }
+}
+
+// Joins the splits of one (row, head): lane l has dimension l; the four waves
+// of a workgroup have four of them.
+__global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
+  const int lane = threadIdx.x & 63;
+  int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int hd = (int)(w % A.hq);
+  w /= A.hq;
+  const int i = (int)(w % R.max_rows);
+  w /= R.max_rows;
+  if (w >= R.n_seqs) return;
+  const Seq s = load_seq(P, R, (int)w);
+  if (i >= s.n) return;
+  // The pages of the row's column tile, as the attention kernel cut them.
+  const int G = A.hq / P.hkv;
+  const int cols = s.n * G, c0 = (i * G + hd % G) / tile_cols * tile_cols;
+  const int row_b = (min(c0 + tile_cols, cols) - 1) / G;
+  const int some_see = min(max(s.first + row_b + 1, 0), P.max_pages * kPage);
+  const int np = (some_see + kPage - 1) / kPage;
+  const int per = split_pages(np, splits);
+  if (per >= np) return;
+  const int n = (np + per - 1) / per;
+  const size_t at = (size_t)(s.row0 + i) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
+  const float2* ml = reinterpret_cast<const float2*>(A.part + (size_t)splits * step * 64) + at;
+  float m = -INFINITY;
+  for (int k = lane; k < n; k += 64) m = fmaxf(m, ml[k * step].x);
+  m = wave_max(m);
+  float l = 0.f, x = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < n; ++k) {
+    const float2 z = ml[k * step];
+    const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
+    l += f * z.y;
+    x += f * A.part[(k * step + at) * 64 + lane];
+  }
+  const float y = l == 0.f ? 0.f : x * (1.0f / l);
+  const size_t to = (size_t)(s.row0 + i) * A.out_stride + hd * 64 + lane;
+  if (A.out_type == kRowF32) static_cast<float*>(A.out)[to] = y;
+  else static_cast<unsigned short*>(A.out)[to] = (unsigned short)pack16(y, 0.f, A.out_type);
+}
+
+template <int NQ, int QT, int PT>
+void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Plan& p) {
+  const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
+  if constexpr (NQ == 4) {
+    if (p.wk == 1) {
+      k_kv4_attend<NQ, QT, PT, 1><<<groups, 256, 0, st>>>(P, R, A, p.tiles, p.splits);
+      return;
+    }
+  }
+  k_kv4_attend<NQ, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, p.tiles, p.splits);
+}
+
+template <int QT, int PT>
+void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Plan& p) {
+  if (p.nq == 1) launch_attend<1, QT, PT>(st, P, R, A, p);
+  else if (p.nq == 2) launch_attend<2, QT, PT>(st, P, R, A, p);
+  else launch_attend<4, QT, PT>(st, P, R, A, p);
+}
+
+}  // namespace
+
+int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R) {
+  return ((int64_t)R.n_seqs * row_tiles(R) * P.hkv + 3) / 4;
+}
+
+hipError_t kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
+                      int64_t k_stride, int64_t v_stride, RopeTable rope) {
+  k_kv4_append<<<(unsigned)kv4_row_groups(P, R), 256, 0, st>>>(P, R, k, v, type, k_stride, v_stride, rope, row_tiles(R));
+  return hipGetLastError();
+}
+
+hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
+                    int64_t v_stride) {
+  k_kv4_read<<<(unsigned)kv4_row_groups(P, R), 256, 0, st>>>(P, R, k, v, type, k_stride, v_stride, row_tiles(R));
+  return hipGetLastError();
+}
+
+int64_t kv4_attend_groups(const Kv4Pool& P, const Kv4Rows& R, int hq) {
+  // Columns are counted in 32 bits.
+  const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv);
+  if (cols > INT32_MAX - 1024) return cols;
+  const Plan p = plan_of(P, R, hq);
+  const int64_t join = p.splits > 1 ? ((int64_t)R.n_seqs * R.max_rows * hq + 3) / 4 : 0;
+  return std::max((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits, join);
+}
+
+size_t kv4_attend_workspace(const Kv4Pool& P, const Kv4Rows& R, int hq) {
+  const Plan p = plan_of(P, R, hq);
+  return p.splits > 1 ? (size_t)p.splits * R.n_rows * hq * (64 + 2) * sizeof(float) : 0;
+}
+
+hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A) {
+  const Plan p = plan_of(P, R, A.hq);
+  // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers.
+  if (A.out_type == kRowF32) launch_attend<2, 2>(st, P, R, A, p);
+  else if (A.q_type == kRowF32 || A.rope.at) launch_attend<2, 1>(st, P, R, A, p);
+  else launch_attend<1, 1>(st, P, R, A, p);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && p.splits > 1) {
+    const int64_t waves = (int64_t)R.n_seqs * R.max_rows * A.hq;
+    k_kv4_join<<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace hh

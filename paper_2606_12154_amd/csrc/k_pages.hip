@@ -1,0 +1,205 @@
+// Pages of a paged cache: copies between pages and compaction of a pool, in
+// every layer at once.  Both only move bytes; a layer's pool holds its pages
+// one after the other.
+#include "hh_device.h"
+#include "hh_kv.h"
+
+#include <algorithm>
+
+namespace hh {
+namespace {
+
+// Copies go in pieces of 4 KiB, one a wave (four 16-byte loads a lane in
+// flight); pieces of a page are whole but for its last.
+constexpr int kPiece = 4096;
+
+__device__ __forceinline__ void copy_piece(const unsigned char* __restrict__ src, unsigned char* __restrict__ dst,
+                                           int64_t bytes, int piece) {
+  const int lane = threadIdx.x & 63;
+  const int64_t off = (int64_t)piece * kPiece + lane * 16;
+  u32x4 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (off + i * 1024 < bytes) v[i] = *reinterpret_cast<const u32x4*>(src + off + i * 1024);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (off + i * 1024 < bytes) *reinterpret_cast<u32x4*>(dst + off + i * 1024) = v[i];
+}
+
+// Pairs travel as kernel arguments (at most 4 KiB of them a launch).
+constexpr int kPairs = 480;
+struct PairArgs {
+  int n;
+  int src[kPairs], dst[kPairs];
+};
+
+__global__ __launch_bounds__(256) void k_copy_pages(PagePool P, int pieces, PairArgs a) {
+  int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int piece = (int)(w % pieces);
+  w /= pieces;
+  const int pair = (int)(w % a.n), layer = (int)(w / a.n);
+  if (layer >= P.n_layers) return;
+  unsigned char* base = P.pool + layer * P.layer_stride;
+  copy_piece(base + a.src[pair] * P.bytes, base + a.dst[pair] * P.bytes, P.bytes, piece);
+}
+
+// ------------------------------------------------------------------ compaction
+
+constexpr int kPlanThreads = 1024;
+constexpr int kMaxPlanPages = 1 << 20;  // one bit each in LDS: 128 KiB
+
+// Sum of v over the threads before this one; total: over all of them.
+__device__ __forceinline__ int exclusive_scan(int v, int* red, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) red[wave] = x;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    if (w < wave) before += red[w];
+    total += red[w];
+  }
+  __syncthreads();
+  return before + x - v;
+}
+
+// One workgroup finds the live pages (a bit each in LDS), their count, and the
+// moves: live pages behind the count, in order, to the free ones before it.
+// moves: [0] their number, then sources, destinations and the new id of every
+// page that moves.
+__global__ __launch_bounds__(kPlanThreads) void k_compact_plan(int n_pages, const int* __restrict__ table, int rows,
+                                                               int max_pages, const int* __restrict__ lengths,
+                                                               int* __restrict__ live, int* moves) {
+  extern __shared__ unsigned bits[];
+  __shared__ int red[kPlanThreads / 64];
+  const int t = threadIdx.x, words = (n_pages + 31) / 32;
+  for (int i = t; i < words; i += kPlanThreads) bits[i] = 0u;
+  __syncthreads();
+  const int wave = t >> 6, lane = t & 63;
+  for (int r = wave; r < rows; r += kPlanThreads / 64) {
+    const int held = min((max(lengths[r], 0) + (int64_t)kPage - 1) / kPage, (int64_t)max_pages);
+    for (int i = lane; i < held; i += 64) {
+      const int id = table[(size_t)r * max_pages + i];
+      if ((unsigned)id < (unsigned)n_pages) atomicOr(&bits[id >> 5], 1u << (id & 31));
+    }
+  }
+  __syncthreads();
+  // Thread t has words w0 .. w1 - 1.
+  const int per = (words + kPlanThreads - 1) / kPlanThreads;
+  const int w0 = min(t * per, words), w1 = min(w0 + per, words);
+  int mine = 0;
+  for (int i = w0; i < w1; ++i) mine += __popc(bits[i]);
+  int count, moved, holes;
+  exclusive_scan(mine, red, count);
+  // Bits of word i for the ids at or behind the count.
+  auto behind = [&](int i) { return i * 32 >= count ? ~0u : i * 32 + 32 <= count ? 0u : ~0u << (count - i * 32); };
+  int from = 0, to = 0;
+  for (int i = w0; i < w1; ++i) {
+    from += __popc(bits[i] & behind(i));
+    to += __popc(~bits[i] & ~behind(i));
+  }
+  int a = exclusive_scan(from, red, moved), b = exclusive_scan(to, red, holes);
+  int* src = moves + 1;
+  int* dst = src + n_pages;
+  int* to_id = dst + n_pages;
+  for (int i = w0; i < w1; ++i) {
+    for (unsigned m = bits[i] & behind(i); m; m &= m - 1) src[a++] = i * 32 + __ffs(m) - 1;
+    for (unsigned m = ~bits[i] & ~behind(i); m; m &= m - 1) dst[b++] = i * 32 + __ffs(m) - 1;
+  }
+  __threadfence_block();
+  __syncthreads();
+  for (int i = t; i < moved; i += kPlanThreads) to_id[src[i]] = dst[i];
+  if (t == 0) {
+    moves[0] = moved;
+    *live = count;
+  }
+}
+
+// The first move_groups workgroups copy, the others rewrite the page tables.
+__global__ __launch_bounds__(256) void k_compact_move(PagePool P, int pieces, const int* __restrict__ moves,
+                                                      int move_groups, int* __restrict__ table, int rows,
+                                                      int max_pages, const int* __restrict__ lengths,
+                                                      const int* __restrict__ live) {
+  const int* src = moves + 1;
+  const int* dst = src + P.n_pages;
+  const int* to_id = dst + P.n_pages;
+  if ((int)blockIdx.x < move_groups) {
+    const int n = moves[0];
+    const int64_t all = (int64_t)n * pieces * P.n_layers;
+    for (int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); w < all;
+         w += (int64_t)move_groups * 4) {
+      const int64_t rest = w / pieces;
+      const int i = (int)(rest % n), layer = (int)(rest / n);
+      unsigned char* base = P.pool + layer * P.layer_stride;
+      copy_piece(base + src[i] * P.bytes, base + dst[i] * P.bytes, P.bytes, (int)(w % pieces));
+    }
+    return;
+  }
+  const int count = *live;
+  const int group = blockIdx.x - move_groups, groups = gridDim.x - move_groups;
+  for (int r = group; r < rows; r += groups) {
+    const int held = min((max(lengths[r], 0) + (int64_t)kPage - 1) / kPage, (int64_t)max_pages);
+    for (int i = threadIdx.x; i < held; i += 256) {
+      const size_t at = (size_t)r * max_pages + i;
+      const int id = table[at];
+      if (id >= count && id < P.n_pages) table[at] = to_id[id];
+    }
+  }
+}
+
+int pieces_of(const PagePool& P) { return (int)((P.bytes + kPiece - 1) / kPiece); }
+
+}  // namespace
+
+hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst) {
+  const int pieces = pieces_of(P);
+  // Pairs of a launch, so that its workgroups stay within a grid.
+  const int64_t each = (int64_t)pieces * P.n_layers;
+  const int most = (int)std::max<int64_t>(1, std::min<int64_t>(kPairs, ((int64_t)1 << 31) / each));
+  for (int o = 0; o < n; o += most) {
+    PairArgs a;
+    a.n = std::min(most, n - o);
+    for (int i = 0; i < a.n; ++i) {
+      a.src[i] = src[o + i];
+      a.dst[i] = dst[o + i];
+    }
+    k_copy_pages<<<(unsigned)((a.n * each + 3) / 4), 256, 0, st>>>(P, pieces, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+size_t compact_workspace(int n_pages) { return ((size_t)1 + 3 * (size_t)n_pages) * sizeof(int); }
+
+hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int table_rows, int max_pages,
+                         const int* lengths, int* live, void* ws) {
+  int* moves = static_cast<int*>(ws);
+  const size_t lds = (size_t)(P.n_pages + 31) / 32 * 4;
+  static_assert(kMaxPlanPages / 8 + 1024 <= 160 * 1024, "LDS");
+  if (lds > 48 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_compact_plan),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, kMaxPlanPages / 8);
+    if (e != hipSuccess) return e;
+  }
+  k_compact_plan<<<1, kPlanThreads, lds, st>>>(P.n_pages, table, table_rows, max_pages, lengths, live, moves);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int pieces = pieces_of(P);
+  // At most half the pool moves; the loop takes what is left beyond 2,048 workgroups.
+  const int64_t most = ((int64_t)P.n_pages / 2 + 1) * pieces * P.n_layers;
+  const int move_groups = (int)std::min<int64_t>((most + 3) / 4, 2048);
+  const int table_groups = std::min(table_rows, 256);
+  k_compact_move<<<move_groups + table_groups, 256, 0, st>>>(P, pieces, moves, move_groups, table, table_rows,
+                                                             max_pages, lengths, live);
+  return hipGetLastError();
+}
+
+}  // namespace hh

@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_float, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, byref, c_float, c_int32, c_int64, c_size_t, c_void_p
 
 import numpy as np
 
@@ -19,14 +19,16 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhh.so")
 
 HH_OK, HH_ERR_INVALID_ARG, HH_ERR_OOM, HH_ERR_CONTEXT_FULL = 0, -1, -2, -3
 HH_ERR_NOT_LOADED, HH_ERR_HIP, HH_ERR_UNSUPPORTED = -4, -5, -6
-HH_F32, HH_BF16 = 0, 1
+HH_F32, HH_BF16, HH_F16 = 0, 1, 2
 HH_LOGITS_NONE, HH_LOGITS_LAST, HH_LOGITS_ALL = 0, 1, 2
 HH_WF_DTYPE, HH_WF_Q4G32 = 0, 1
 
 EXPORTED = ["hh_workspace_size", "hh_create", "hh_load_weights", "hh_prefill", "hh_prefill_batch", "hh_decode_step",
             "hh_decode_step_noalloc", "hh_reset", "hh_stream_length", "hh_read_argmax", "hh_destroy", "hh_last_error",
             "hh_q4g32_quantize", "hh_router_create", "hh_router_query", "hh_router_route",
-            "hh_router_size", "hh_router_destroy", "hh_render_marker", "hh_read_probe"]
+            "hh_router_size", "hh_router_destroy", "hh_render_marker", "hh_read_probe",
+            "hh_kv4_append", "hh_kv4_read", "hh_kv4_attention_workspace", "hh_kv4_attention", "hh_kv_copy_pages",
+            "hh_kv_compact_workspace", "hh_kv_compact"]
 
 
 class hh_config(ctypes.Structure):
@@ -36,6 +38,16 @@ class hh_config(ctypes.Structure):
         ("tied_embeddings", c_int32), ("dtype", c_int32), ("max_streams", c_int32),
         ("max_context", c_int32), ("page_size", c_int32), ("max_prefill", c_int32),
         ("weight_format", c_int32)]
+
+
+class hh_kv4_pool(ctypes.Structure):
+    _fields_ = [("pool", c_void_p), ("page_table", c_void_p), ("n_pages", c_int32), ("n_kv_heads", c_int32),
+                ("max_pages", c_int32), ("table_rows", c_int32)]
+
+
+class hh_kv4_rows(ctypes.Structure):
+    _fields_ = [("row_start", c_void_p), ("first_pos", c_void_p), ("table_row", c_void_p), ("n_seqs", c_int32),
+                ("n_rows", c_int32), ("max_rows", c_int32)]
 
 
 class HHError(RuntimeError):
@@ -55,7 +67,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     if not os.path.exists(path):
         raise RuntimeError(f"HIP library not built: {path} (run paper_2606_12154_amd/build.py)")
     lib = ctypes.CDLL(path)
-    i32p = POINTER(c_int32)
+    i32p, poolp, rowsp = POINTER(c_int32), POINTER(hh_kv4_pool), POINTER(hh_kv4_rows)
     sig = {
         "hh_workspace_size": ([POINTER(hh_config), POINTER(c_size_t)], c_int32),
         "hh_create": ([POINTER(hh_config), c_void_p, c_size_t, c_void_p, POINTER(c_void_p)], c_int32),
@@ -77,6 +89,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "hh_router_destroy": ([c_void_p], None),
         "hh_render_marker": ([ctypes.c_char_p, c_void_p, ctypes.c_int64, POINTER(ctypes.c_int64)], c_int32),
         "hh_read_probe": ([c_void_p, c_size_t, c_void_p], c_int32),
+        "hh_kv4_append": ([poolp, rowsp, c_void_p, c_void_p, c_int32, c_int64, c_int64, c_void_p, c_int32, c_void_p],
+                          c_int32),
+        "hh_kv4_read": ([poolp, rowsp, c_void_p, c_void_p, c_int32, c_int64, c_int64, c_void_p], c_int32),
+        "hh_kv4_attention_workspace": ([poolp, rowsp, c_int32, POINTER(c_size_t)], c_int32),
+        "hh_kv4_attention": ([poolp, rowsp, c_void_p, c_int32, c_int64, c_int32, c_float, c_void_p, c_int32, c_void_p,
+                              c_int32, c_int64, c_void_p, c_size_t, c_void_p], c_int32),
+        "hh_kv_copy_pages": ([c_void_p, c_int32, c_int64, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p],
+                             c_int32),
+        "hh_kv_compact_workspace": ([c_int32, POINTER(c_size_t)], c_int32),
+        "hh_kv_compact": ([c_void_p, c_int32, c_int64, c_int64, c_int32, c_void_p, c_int32, c_int32, c_void_p, c_void_p,
+                           c_void_p, c_size_t, c_void_p], c_int32),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -167,6 +190,55 @@ def hh_q4g32_quantize(src_ptr: int, rows: int, K: int, dst_ptr: int, hip_stream:
 
 def hh_read_probe(src_ptr: int, nbytes: int, hip_stream: int) -> None:
     _check(None, load_library().hh_read_probe(c_void_p(src_ptr), nbytes, c_void_p(hip_stream)))
+
+
+def hh_kv4_append(pool: hh_kv4_pool, rows: hh_kv4_rows, k_ptr, v_ptr, dtype: int, k_stride: int, v_stride: int,
+                  rope_ptr, rope_len: int, hip_stream) -> None:
+    _check(None, load_library().hh_kv4_append(byref(pool), byref(rows), k_ptr, v_ptr, dtype, k_stride, v_stride,
+                                              rope_ptr, rope_len, hip_stream))
+
+
+def hh_kv4_read(pool: hh_kv4_pool, rows: hh_kv4_rows, k_ptr, v_ptr, dtype: int, k_stride: int, v_stride: int,
+                hip_stream) -> None:
+    _check(None, load_library().hh_kv4_read(byref(pool), byref(rows), k_ptr, v_ptr, dtype, k_stride, v_stride,
+                                            hip_stream))
+
+
+def hh_kv4_attention_workspace(pool: hh_kv4_pool, rows: hh_kv4_rows, n_heads: int) -> int:
+    n = c_size_t()
+    _check(None, load_library().hh_kv4_attention_workspace(byref(pool), byref(rows), n_heads, byref(n)))
+    return n.value
+
+
+def hh_kv4_attention(pool: hh_kv4_pool, rows: hh_kv4_rows, q_ptr, q_dtype: int, q_stride: int, n_heads: int,
+                     scale: float, rope_ptr, rope_len: int, out_ptr, out_dtype: int, out_stride: int, workspace_ptr,
+                     workspace_bytes: int, hip_stream) -> None:
+    _check(None, load_library().hh_kv4_attention(byref(pool), byref(rows), q_ptr, q_dtype, q_stride, n_heads, scale,
+                                                 rope_ptr, rope_len, out_ptr, out_dtype, out_stride, workspace_ptr,
+                                                 workspace_bytes, hip_stream))
+
+
+def hh_kv_copy_pages(pool_ptr, n_layers: int, layer_stride: int, page_bytes: int, n_pages: int, src, dst,
+                     hip_stream) -> None:
+    src, dst = (np.ascontiguousarray(x, dtype=np.int32) for x in (src, dst))
+    if src.shape != dst.shape or src.ndim != 1:
+        raise ValueError("src and dst must list the same number of pages")
+    _check(None, load_library().hh_kv_copy_pages(pool_ptr, n_layers, layer_stride, page_bytes, n_pages, len(src),
+                                                 src.ctypes.data, dst.ctypes.data, hip_stream))
+
+
+def hh_kv_compact_workspace(n_pages: int) -> int:
+    n = c_size_t()
+    _check(None, load_library().hh_kv_compact_workspace(n_pages, byref(n)))
+    return n.value
+
+
+def hh_kv_compact(pool_ptr, n_layers: int, layer_stride: int, page_bytes: int, n_pages: int, table_ptr,
+                  table_rows: int, max_pages: int, lengths_ptr, live_ptr, workspace_ptr, workspace_bytes: int,
+                  hip_stream) -> None:
+    _check(None, load_library().hh_kv_compact(pool_ptr, n_layers, layer_stride, page_bytes, n_pages, table_ptr,
+                                              table_rows, max_pages, lengths_ptr, live_ptr, workspace_ptr,
+                                              workspace_bytes, hip_stream))
 
 
 def _text(s) -> bytes:
