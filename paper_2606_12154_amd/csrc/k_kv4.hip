@@ -355,18 +355,19 @@ struct PageRegs {
   unsigned ks;
 };
 
-__device__ __forceinline__ void load_page(PageRegs& r, const unsigned char* blk, int lane) {
+__device__ __forceinline__ void load_page(PageRegs& r, const unsigned char* blk, unsigned lane) {
   r.k = *reinterpret_cast<const u32x2*>(blk + 8 * lane);
-  r.v = *reinterpret_cast<const u32x2*>(blk + 512 + 8 * lane);
-  r.ks = *reinterpret_cast<const unsigned*>(blk + kKeyScales + 4 * (lane & 15));
-  r.vs = *reinterpret_cast<const u32x2*>(blk + kValueScales + ((lane & 15) >> 3) * 32 + 8 * (lane >> 4));
+  r.v = *reinterpret_cast<const u32x2*>(blk + (512 + 8 * lane));
+  r.ks = *reinterpret_cast<const unsigned*>(blk + (kKeyScales + 4 * (lane & 15)));
+  r.vs = *reinterpret_cast<const u32x2*>(blk + (kValueScales + (lane & 8) * 4 + 8 * (lane >> 4)));
 }
 
-// Nibble j of both halves of w as 16 + n.
+// Nibble j of both halves of w as 16 + n.  The mask comes in a vector register:
+// with both constants in scalar ones and-or would be two instructions.
 template <int J>
-__device__ __forceinline__ f16x2 codes16(unsigned w) {
+__device__ __forceinline__ f16x2 codes16(unsigned w, unsigned mask) {
   const unsigned x = J < 2 ? w << (6 - 4 * J) : w >> (4 * J - 6);
-  return __builtin_bit_cast(f16x2, (x & 0x03c003c0u) | 0x4c004c00u);
+  return __builtin_bit_cast(f16x2, (x & mask) | 0x4c004c00u);
 }
 
 __device__ __forceinline__ f16x8 join8(f16x2 a, f16x2 b, f16x2 c, f16x2 d) {
@@ -374,31 +375,32 @@ __device__ __forceinline__ f16x8 join8(f16x2 a, f16x2 b, f16x2 c, f16x2 d) {
 }
 
 // 8 keys' elements of one dword under one scale.
-__device__ __forceinline__ f16x8 key_frag(unsigned w, f16x2 s, f16x2 b) {
-  return join8(__builtin_elementwise_fma(codes16<0>(w), s, b), __builtin_elementwise_fma(codes16<1>(w), s, b),
-               __builtin_elementwise_fma(codes16<2>(w), s, b), __builtin_elementwise_fma(codes16<3>(w), s, b));
+__device__ __forceinline__ f16x8 key_frag(unsigned w, unsigned mask, f16x2 s, f16x2 b) {
+  return join8(__builtin_elementwise_fma(codes16<0>(w, mask), s, b), __builtin_elementwise_fma(codes16<1>(w, mask), s, b),
+               __builtin_elementwise_fma(codes16<2>(w, mask), s, b), __builtin_elementwise_fma(codes16<3>(w, mask), s, b));
 }
 
 // Dimension 4 r + J of the lane's 4 slots in each of two pages.
 template <int J>
-__device__ __forceinline__ f16x8 value_frag(u32x2 wa, u32x2 wb, const f16x2* s, const f16x2* b) {
-  return join8(__builtin_elementwise_fma(codes16<J>(wa[0]), s[0], b[0]),
-               __builtin_elementwise_fma(codes16<J>(wa[1]), s[1], b[1]),
-               __builtin_elementwise_fma(codes16<J>(wb[0]), s[2], b[2]),
-               __builtin_elementwise_fma(codes16<J>(wb[1]), s[3], b[3]));
+__device__ __forceinline__ f16x8 value_frag(u32x2 wa, u32x2 wb, unsigned mask, const f16x2* s, const f16x2* b) {
+  return join8(__builtin_elementwise_fma(codes16<J>(wa[0], mask), s[0], b[0]),
+               __builtin_elementwise_fma(codes16<J>(wa[1], mask), s[1], b[1]),
+               __builtin_elementwise_fma(codes16<J>(wb[0], mask), s[2], b[2]),
+               __builtin_elementwise_fma(codes16<J>(wb[1], mask), s[3], b[3]));
 }
 
-// What the weights are scaled by, as an exponent: a weight is at most
-// 2^(kOffset + kSlack) (the maximum that they are taken against is raised once
-// scores lead it by more than kSlack), so fp16 holds it, and down to 2^-31 of
-// the row's largest.
+// Weights are 2^(S qs - base): base puts a column's largest score so far at
+// 2^kOffset, and is raised once a score passes 2^(kOffset + kSlack), so that fp16
+// holds every weight, down to 2^-31 of the row's largest.  Raising it rarely
+// leaves the step without reductions across lanes.
 constexpr float kOffset = 7.f, kSlack = 8.f;
 
 // QT, PT: fp16 terms of queries and of weights.  Queries are scaled by a power of
 // two that puts a row's largest element into [2^13, 2^14), so that one term holds any
 // 16-bit query and two hold 22 bits of an fp32 one.
 template <int NQ, int QT, int PT, int WK>
-__global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4 : NQ == 2 ? 3 : 2))) void
+k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   unsigned b = blockIdx.x;
@@ -470,22 +472,20 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
 
   // ---- keys and values
   f32x4 o[NQ][4], sum[NQ];
-  float base[NQ], raise[NQ];  // weights are 2^(S qs - base); a score above raise raises it
+  float base[NQ];
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     base[t] = 0.f;
-    raise[t] = -INFINITY;
   }
   const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+  const f16x2 m24 = {(_Float16)-24, (_Float16)-24};
+  unsigned mask;
+  asm("v_mov_b32 %0, 0x03c003c0" : "=v"(mask));
   const int* row = P.table + (size_t)s.trow * P.max_pages;
-
-  auto fetch = [&](PageRegs* pr, int p) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) load_page(pr[i], block_of(P, row, min(p + i, np - 1), head), lane);
-  };
+  bool first = true;
 
   auto step = [&](const PageRegs* pr, int p, auto masked) {
     constexpr bool MASK = decltype(masked)::value;
@@ -496,9 +496,8 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
     for (int i = 0; i < 2; ++i) {
       const f16x2 sc = __builtin_bit_cast(f16x2, pr[i].ks);
       const f16x2 s0 = {sc[0], sc[0]}, s1 = {sc[1], sc[1]};
-      const f16x2 m24 = {(_Float16)-24, (_Float16)-24};
-      kf[i][0] = key_frag(pr[i].k[0], s0, s0 * m24);
-      kf[i][1] = key_frag(pr[i].k[1], s1, s1 * m24);
+      kf[i][0] = key_frag(pr[i].k[0], mask, s0, s0 * m24);
+      kf[i][1] = key_frag(pr[i].k[1], mask, s1, s1 * m24);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         unsigned w = pr[i].vs[h];
@@ -517,7 +516,7 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
         }
         const f16x2 sv = __builtin_bit_cast(f16x2, w);
         vsc[2 * i + h] = sv;
-        vbi[2 * i + h] = sv * f16x2{(_Float16)-24, (_Float16)-24};
+        vbi[2 * i + h] = sv * m24;
       }
     }
     if constexpr (MASK) {
@@ -525,10 +524,10 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
       nan4 |= (unsigned)__shfl_xor((int)nan4, 8, 64);
     }
     f16x8 vf[4];
-    vf[0] = value_frag<0>(pr[0].v, pr[1].v, vsc, vbi);
-    vf[1] = value_frag<1>(pr[0].v, pr[1].v, vsc, vbi);
-    vf[2] = value_frag<2>(pr[0].v, pr[1].v, vsc, vbi);
-    vf[3] = value_frag<3>(pr[0].v, pr[1].v, vsc, vbi);
+    vf[0] = value_frag<0>(pr[0].v, pr[1].v, mask, vsc, vbi);
+    vf[1] = value_frag<1>(pr[0].v, pr[1].v, mask, vsc, vbi);
+    vf[2] = value_frag<2>(pr[0].v, pr[1].v, mask, vsc, vbi);
+    vf[3] = value_frag<3>(pr[0].v, pr[1].v, mask, vsc, vbi);
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
       f32x4 sc[2];
@@ -542,41 +541,39 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
         sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], qh[t][0], sc[i], 0, 0, 0);
         sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], qh[t][1], sc[i], 0, 0, 0);
       }
-      if constexpr (MASK) {
+      float x[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int slot = (p + i) * kPage + 4 * g + e;
-            const float x = nan4 >> (4 * i + e) & 1u ? NAN : sc[i][e];
-            sc[i][e] = slot < lim[t] ? x : -INFINITY;
-          }
+      for (int i = 0; i < 8; ++i) {
+        x[i] = fmaf(sc[i >> 2][i & 3], qs[t], -base[t]);
+        if constexpr (MASK) {
+          if (nan4 >> i & 1u) x[i] = NAN;
+          if ((p + (i >> 2)) * kPage + 4 * g + (i & 3) >= lim[t]) x[i] = -INFINITY;
+        }
       }
-      float mx = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3]));
-      mx = fmaxf(mx, fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-      if (__builtin_amdgcn_ballot_w64(mx > raise[t])) {
+      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      // A wave's first pages set the base: a column that sees none of them
+      // sees none of the later ones either.
+      if (first || __builtin_amdgcn_ballot_w64(mx > kOffset + kSlack)) {
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        if (mx > raise[t] || (raise[t] > -INFINITY && fmaf(mx, qs[t], -base[t]) > kOffset)) {
-          const float nb = mx * qs[t] - kOffset;
-          const float f = raise[t] > -INFINITY ? __builtin_amdgcn_exp2f(base[t] - nb) : 0.f;
-          base[t] = nb;
-          raise[t] = mx + kSlack / qs[t];
+        float up = mx > -INFINITY ? mx - kOffset : 0.f;
+        if (!first) up = fmaxf(up, 0.f);
+        const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
+        base[t] += up;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) o[t][j] *= f;
-          sum[t] *= f;
-        }
+        for (int i = 0; i < 8; ++i) x[i] -= up;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[t][j] *= f;
+        sum[t] *= f;
       }
       f16x8 ph, pl;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(sc[i][e], qs[t], -base[t]));
-          const _Float16 h = (_Float16)w;
-          ph[4 * i + e] = h;
-          if constexpr (PT == 2) pl[4 * i + e] = (_Float16)(w - (float)h);
-        }
+      for (int i = 0; i < 8; ++i) {
+        const float w = __builtin_amdgcn_exp2f(x[i]);
+        const _Float16 h = (_Float16)w;
+        ph[i] = h;
+        if constexpr (PT == 2) pl[i] = (_Float16)(w - (float)h);
+      }
       if constexpr (PT == 2) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], pl, o[t][j], 0, 0, 0);
@@ -587,25 +584,66 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
       // Weights are summed as they enter the products.
       sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph, sum[t], 0, 0, 0);
     }
+    first = false;
   };
 
   {
-    PageRegs cur[2], nxt[2];
-    int p = p0 + (WK == 1 ? 0 : 2 * wave);
     constexpr int STEP = WK == 1 ? 2 : 8;
-    if (p < p1) fetch(cur, p);
-    while (p < p1) {
-      const int pn = p + STEP;
-      if (pn < p1) fetch(nxt, pn);
-      if ((p + 2) * kPage <= all_see) step(cur, p, std::false_type());
-      else step(cur, p, std::true_type());
-      cur[0] = nxt[0];
-      cur[1] = nxt[1];
-      p = pn;
+    int p = p0 + (WK == 1 ? 0 : 2 * wave);
+    if (p < p1) {
+      // Loads run one step ahead, page ids two; what would lie behind the wave's
+      // last step is its last step again (no branch around loads, whose
+      // waits would then have to assume that it was not taken).
+      const int last = p + (p1 - 1 - p) / STEP * STEP;
+      auto ids = [&](int q, unsigned* id) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const unsigned x = (unsigned)row[min(min(q, last) + i, np - 1)];
+          id[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
+        }
+      };
+      auto fetch = [&](PageRegs* pr, const unsigned* id) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          load_page(pr[i], P.pool + ((size_t)id[i] * (unsigned)P.hkv + (unsigned)head) * kKv4Block, (unsigned)lane);
+      };
+      const int full = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
+      PageRegs a[2], c[2];
+      unsigned id[2];
+      ids(p, id);
+      fetch(a, id);
+      ids(p + STEP, id);
+      bool swapped = false;
+      while (p < full) {
+        fetch(c, id);
+        ids(p + 2 * STEP, id);
+        step(a, p, std::false_type());
+        p += STEP;
+        if (p >= full) {
+          swapped = true;
+          break;
+        }
+        fetch(a, id);
+        ids(p + 2 * STEP, id);
+        step(c, p, std::false_type());
+        p += STEP;
+      }
+      if (swapped) {
+        a[0] = c[0];
+        a[1] = c[1];
+      }
+      while (p < p1) {
+        fetch(c, id);
+        ids(p + 2 * STEP, id);
+        step(a, p, std::true_type());
+        a[0] = c[0];
+        a[1] = c[1];
+        p += STEP;
+      }
     }
   }
 
-  // ---- output of 16 consecutive dimensions of column c, or the split's part
+  // ---- output of N consecutive dimensions of column c, or the split's part
   auto put = [&](int c, int d0, auto n_const, const float* x, float l, float m) {
     constexpr int N = decltype(n_const)::value;
     if (c >= cols) return;
@@ -638,7 +676,7 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[4 * i + j] = o[t][j][i];
       put(c0 + 16 * t + r, 16 * g, std::integral_constant<int, 16>(), x, sum[t][0],
-          raise[t] > -INFINITY ? base[t] : -INFINITY);
+          sum[t][0] == 0.f ? -INFINITY : base[t]);
     }
   } else {
     // Join the four waves: wave w takes dimensions 16 g + 4 w .. + 3.
@@ -649,7 +687,8 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
       if (t) __syncthreads();
 #pragma unroll
       for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{o[t][0][i], o[t][1][i], o[t][2][i], o[t][3][i]};
-      ls[wave][lane] = make_float2(raise[t] > -INFINITY ? base[t] : -INFINITY, sum[t][0]);
+      // A wave whose keys the column does not see has no base.
+      ls[wave][lane] = make_float2(sum[t][0] == 0.f ? -INFINITY : base[t], sum[t][0]);
       __syncthreads();
       float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -657,7 +696,6 @@ __global__ __launch_bounds__(256) void k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Att
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const float2 z = ls[w][lane];
-        // A wave without a finite score adds 0, or NaN if it saw one.
         const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
         const f32x4 y = lo[w][wave][lane];
         l += f * z.y;
