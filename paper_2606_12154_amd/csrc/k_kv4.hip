@@ -94,6 +94,35 @@ __device__ __forceinline__ void load_row(const void* p, size_t at, int type, flo
   }
 }
 
+// 8 elements at each of two places, in flight (raw) and as fp32.
+struct RawRow {
+  u32x4 w[4];
+};
+__device__ __forceinline__ void load_raw(RawRow& r, const void* p, size_t at, size_t next, int type) {
+  if (type == kRowF32) {
+    const u32x4* a = reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + at);
+    const u32x4* b = reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + next);
+    r.w[0] = a[0];
+    r.w[1] = a[1];
+    r.w[2] = b[0];
+    r.w[3] = b[1];
+  } else {
+    r.w[0] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(p) + at);
+    r.w[1] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(p) + next);
+    r.w[2] = r.w[3] = u32x4{0u, 0u, 0u, 0u};
+  }
+}
+__device__ __forceinline__ void raw_values(const RawRow& r, int type, float* f) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const unsigned full = r.w[i >> 2][i & 3], word = r.w[i >> 3][(i >> 1) & 3];
+    const unsigned half = i & 1 ? word >> 16 : word & 0xffffu;
+    f[i] = type == kRowF32 ? __uint_as_float(full)
+           : type == kRowF16 ? (float)__builtin_bit_cast(_Float16, (unsigned short)half)
+                             : __uint_as_float(half << 16);
+  }
+}
+
 __device__ __forceinline__ unsigned pack16(float a, float b, int type) {
   if (type == kRowF16) return __builtin_bit_cast(unsigned, f16x2{(_Float16)a, (_Float16)b});
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -322,6 +351,8 @@ int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
 
 // Operand columns are (row, query head of the kv head's group) pairs, row-major:
 // column c of a sequence is row c / G, head c % G.
+constexpr int kMaxSplits = 128;
+
 struct Plan {
   int nq;      // 16-column tiles of a wave
   int wk;      // waves of a workgroup that share the columns and split the keys (4), or 1
@@ -339,7 +370,7 @@ Plan plan_of(const Kv4Pool& P, const Kv4Rows& R, int hq) {
   p.tiles = (int)std::min<int64_t>(tiles, 1 << 30);
   const int64_t groups = tiles * seqs;
   const int most = (P.max_pages + 31) / 32;  // at least 32 pages each
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1023 + groups) / groups, most, 128}));
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1023 + groups) / groups, most, kMaxSplits}));
   if (p.wk == 1) p.splits = 1;
   return p;
 }
@@ -425,31 +456,61 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   const bool joined = per < np;  // several splits have keys
   if (split > 0 && p0 >= np) return;
 
+  // ---- what the first step needs goes out before the queries are worked on
+  const int* row = P.table + (size_t)s.trow * P.max_pages;
+  constexpr int STEP = WK == 1 ? 2 : 8;
+  int p = p0 + (WK == 1 ? 0 : 2 * wave);
+  // Loads run one step ahead, page ids two; what would lie behind the wave's
+  // last step is its last step again (no branch around loads, whose waits would
+  // then have to assume that it was not taken).
+  const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
+  auto ids = [&](int q, unsigned* id) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned x = (unsigned)row[max(min(min(q, last) + i, np - 1), 0)];
+      id[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
+    }
+  };
+  auto fetch = [&](PageRegs* pr, const unsigned* id) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      load_page(pr[i], P.pool + ((size_t)id[i] * (unsigned)P.hkv + (unsigned)head) * kKv4Block, (unsigned)lane);
+  };
+  RawRow raw[NQ];
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    const int c = min(c0 + 16 * t + r, cols - 1), rw = c / G, j = c - rw * G;
+    const size_t at = (size_t)(s.row0 + rw) * A.q_stride + (head * G + j) * 64 + 8 * g;
+    load_raw(raw[t], A.q, at, at + 32, A.q_type);
+  }
+  PageRegs a[2], c[2];
+  unsigned id[2];
+  ids(p, id);
+  fetch(a, id);
+  ids(p + STEP, id);
+
   // ---- queries
   f16x8 qh[NQ][2], ql[QT == 2 ? NQ : 1][2];
   float qs[NQ];  // scores to powers of two
   int lim[NQ];   // keys that the column sees
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
-    const int c = c0 + 16 * t + r;
-    const bool real = c < cols;
-    const int row = real ? c / G : row_a, j = real ? c % G : 0;
-    lim[t] = real ? min(max(s.first + row + 1, 0), most) : 0;
+    const int cc = c0 + 16 * t + r;
+    const bool real = cc < cols;
+    const int pos = s.first + min(cc, cols - 1) / G;
+    lim[t] = real ? min(max(pos + 1, 0), most) : 0;
     float x[16];
-    const size_t at = (size_t)(s.row0 + row) * A.q_stride + (head * G + j) * 64 + 8 * g;
-    load_row<8>(A.q, at, A.q_type, x);
-    load_row<8>(A.q, at + 32, A.q_type, x + 8);
+    raw_values(raw[t], A.q_type, x);
     if (A.rope.at) {
-      const int pos = min(max(s.first + row, 0), A.rope.len - 1);
-      const f32x4* cs = reinterpret_cast<const f32x4*>(A.rope.at + (size_t)pos * 32 + 8 * g);
+      const f32x4* cs = reinterpret_cast<const f32x4*>(A.rope.at + (size_t)min(max(pos, 0), A.rope.len - 1) * 32 + 8 * g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const f32x4 w = cs[i];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float a = x[2 * i + e], bb = x[8 + 2 * i + e], co = w[2 * e], si = w[2 * e + 1];
-          x[2 * i + e] = a * co - bb * si;
-          x[8 + 2 * i + e] = bb * co + a * si;
+          const float u = x[2 * i + e], v = x[8 + 2 * i + e], co = w[2 * e], si = w[2 * e + 1];
+          x[2 * i + e] = u * co - v * si;
+          x[8 + 2 * i + e] = v * co + u * si;
         }
       }
     }
@@ -484,7 +545,6 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   const f16x2 m24 = {(_Float16)-24, (_Float16)-24};
   unsigned mask;
   asm("v_mov_b32 %0, 0x03c003c0" : "=v"(mask));
-  const int* row = P.table + (size_t)s.trow * P.max_pages;
   bool first = true;
 
   auto step = [&](const PageRegs* pr, int p, auto masked) {
@@ -528,6 +588,9 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
     vf[1] = value_frag<1>(pr[0].v, pr[1].v, mask, vsc, vbi);
     vf[2] = value_frag<2>(pr[0].v, pr[1].v, mask, vsc, vbi);
     vf[3] = value_frag<3>(pr[0].v, pr[1].v, mask, vsc, vbi);
+    // Scores of all columns first: the check below is the step's only branch, so
+    // products and exponentials of different columns can overlap around it.
+    float x[NQ][8], high = -INFINITY;
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
       f32x4 sc[2];
@@ -541,19 +604,24 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
         sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], qh[t][0], sc[i], 0, 0, 0);
         sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], qh[t][1], sc[i], 0, 0, 0);
       }
-      float x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = fmaf(sc[i >> 2][i & 3], qs[t], -base[t]);
+        x[t][i] = fmaf(sc[i >> 2][i & 3], qs[t], -base[t]);
         if constexpr (MASK) {
-          if (nan4 >> i & 1u) x[i] = NAN;
-          if ((p + (i >> 2)) * kPage + 4 * g + (i & 3) >= lim[t]) x[i] = -INFINITY;
+          if (nan4 >> i & 1u) x[t][i] = NAN;
+          if ((p + (i >> 2)) * kPage + 4 * g + (i & 3) >= lim[t]) x[t][i] = -INFINITY;
         }
+        high = fmaxf(high, x[t][i]);
       }
-      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      // A wave's first pages set the base: a column that sees none of them
-      // sees none of the later ones either.
-      if (first || __builtin_amdgcn_ballot_w64(mx > kOffset + kSlack)) {
+    }
+    // A wave's first pages set the base: a column that sees none of them sees
+    // none of the later ones either.
+    if (first || __builtin_amdgcn_ballot_w64(high > kOffset + kSlack)) {
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) {
+        float mx = x[t][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[t][i]);
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
         float up = mx > -INFINITY ? mx - kOffset : 0.f;
@@ -561,15 +629,18 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
         const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
         base[t] += up;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] -= up;
+        for (int i = 0; i < 8; ++i) x[t][i] -= up;
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[t][j] *= f;
         sum[t] *= f;
       }
+    }
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
       f16x8 ph, pl;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float w = __builtin_amdgcn_exp2f(x[i]);
+        const float w = __builtin_amdgcn_exp2f(x[t][i]);
         const _Float16 h = (_Float16)w;
         ph[i] = h;
         if constexpr (PT == 2) pl[i] = (_Float16)(w - (float)h);
@@ -588,66 +659,41 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   };
 
   {
-    constexpr int STEP = WK == 1 ? 2 : 8;
-    int p = p0 + (WK == 1 ? 0 : 2 * wave);
-    if (p < p1) {
-      // Loads run one step ahead, page ids two; what would lie behind the wave's
-      // last step is its last step again (no branch around loads, whose
-      // waits would then have to assume that it was not taken).
-      const int last = p + (p1 - 1 - p) / STEP * STEP;
-      auto ids = [&](int q, unsigned* id) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const unsigned x = (unsigned)row[min(min(q, last) + i, np - 1)];
-          id[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
-        }
-      };
-      auto fetch = [&](PageRegs* pr, const unsigned* id) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          load_page(pr[i], P.pool + ((size_t)id[i] * (unsigned)P.hkv + (unsigned)head) * kKv4Block, (unsigned)lane);
-      };
-      const int full = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
-      PageRegs a[2], c[2];
-      unsigned id[2];
-      ids(p, id);
+    const int full = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
+    bool swapped = false;
+    while (p < full) {
+      fetch(c, id);
+      ids(p + 2 * STEP, id);
+      step(a, p, std::false_type());
+      p += STEP;
+      if (p >= full) {
+        swapped = true;
+        break;
+      }
       fetch(a, id);
-      ids(p + STEP, id);
-      bool swapped = false;
-      while (p < full) {
-        fetch(c, id);
-        ids(p + 2 * STEP, id);
-        step(a, p, std::false_type());
-        p += STEP;
-        if (p >= full) {
-          swapped = true;
-          break;
-        }
-        fetch(a, id);
-        ids(p + 2 * STEP, id);
-        step(c, p, std::false_type());
-        p += STEP;
-      }
-      if (swapped) {
-        a[0] = c[0];
-        a[1] = c[1];
-      }
-      while (p < p1) {
-        fetch(c, id);
-        ids(p + 2 * STEP, id);
-        step(a, p, std::true_type());
-        a[0] = c[0];
-        a[1] = c[1];
-        p += STEP;
-      }
+      ids(p + 2 * STEP, id);
+      step(c, p, std::false_type());
+      p += STEP;
+    }
+    if (swapped) {
+      a[0] = c[0];
+      a[1] = c[1];
+    }
+    while (p < p1) {
+      fetch(c, id);
+      ids(p + 2 * STEP, id);
+      step(a, p, std::true_type());
+      a[0] = c[0];
+      a[1] = c[1];
+      p += STEP;
     }
   }
 
   // ---- output of N consecutive dimensions of column c, or the split's part
-  auto put = [&](int c, int d0, auto n_const, const float* x, float l, float m) {
+  auto put = [&](int col, int d0, auto n_const, const float* x, float l, float m) {
     constexpr int N = decltype(n_const)::value;
-    if (c >= cols) return;
-    const int rw = s.row0 + c / G, hd = head * G + c % G;
+    if (col >= cols) return;
+    const int rw = s.row0 + col / G, hd = head * G + col % G;
     if (joined) {
       const size_t at = ((size_t)split * R.n_rows + rw) * A.hq + hd;
       float* dst = A.part + at * 64 + d0;
@@ -707,17 +753,18 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   }
 }
 
-// Joins the splits of one (row, head): lane l has dimension l; the four waves
-// of a workgroup have four of them.
+// Joins the splits of a (row, head): WAVES waves have it, lane l dimensions
+// 4 (l % 16) .. + 3 of every (4 WAVES)-th split, so that all loads are in flight
+// at once.  Many splits (few rows) take four waves, up to 16 splits one.
+template <int WAVES>
 __global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
-  const int lane = threadIdx.x & 63;
-  int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int hd = (int)(w % A.hq);
-  w /= A.hq;
-  const int i = (int)(w % R.max_rows);
-  w /= R.max_rows;
-  if (w >= R.n_seqs) return;
-  const Seq s = load_seq(P, R, (int)w);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned b = WAVES == 4 ? blockIdx.x : blockIdx.x * 4u + wave;
+  const int part_of = WAVES == 4 ? wave : 0;
+  const int hd = b % (unsigned)A.hq, i = b / (unsigned)A.hq % (unsigned)R.max_rows;
+  const unsigned sq = b / (unsigned)A.hq / (unsigned)R.max_rows;
+  if (sq >= (unsigned)R.n_seqs) return;
+  const Seq s = load_seq(P, R, sq);
   if (i >= s.n) return;
   // The pages of the row's column tile, as the attention kernel cut them.
   const int G = A.hq / P.hkv;
@@ -730,21 +777,63 @@ __global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Atten
   const int n = (np + per - 1) / per;
   const size_t at = (size_t)(s.row0 + i) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
   const float2* ml = reinterpret_cast<const float2*>(A.part + (size_t)splits * step * 64) + at;
-  float m = -INFINITY;
-  for (int k = lane; k < n; k += 64) m = fmaxf(m, ml[k * step].x);
-  m = wave_max(m);
-  float l = 0.f, x = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < n; ++k) {
-    const float2 z = ml[k * step];
-    const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
-    l += f * z.y;
-    x += f * A.part[(k * step + at) * 64 + lane];
+  const float* part = A.part + at * 64 + 4 * (lane & 15);
+  constexpr int N = WAVES == 4 ? kMaxSplits / 16 : 4;  // loads of a lane
+  f32x4 y[N];
+  float2 z[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int sp = (k * WAVES + part_of) * 4 + (lane >> 4);
+    y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    z[k] = make_float2(-INFINITY, 0.f);
+    if (sp < n) {
+      z[k] = ml[sp * step];
+      y[k] = *reinterpret_cast<const f32x4*>(part + sp * step * 64);
+    }
   }
-  const float y = l == 0.f ? 0.f : x * (1.0f / l);
-  const size_t to = (size_t)(s.row0 + i) * A.out_stride + hd * 64 + lane;
-  if (A.out_type == kRowF32) static_cast<float*>(A.out)[to] = y;
-  else static_cast<unsigned short*>(A.out)[to] = (unsigned short)pack16(y, 0.f, A.out_type);
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < N; ++k) m = fmaxf(m, z[k].x);
+  m = fmaxf(m, __shfl_xor(m, 16, 64));
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  float x[5] = {0.f, 0.f, 0.f, 0.f, 0.f};  // 4 dimensions and the sum of weights, against m
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const float f = z[k].x > -INFINITY ? __builtin_amdgcn_exp2f(z[k].x - m) : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] += f * y[k][j];
+    x[4] += f * z[k].y;
+  }
+#pragma unroll
+  for (int j = 0; j < 5; ++j) {
+    x[j] += __shfl_xor(x[j], 16, 64);
+    x[j] += __shfl_xor(x[j], 32, 64);
+  }
+  if constexpr (WAVES == 4) {
+    __shared__ float xs[4][6][16];
+    if (lane < 16) {
+#pragma unroll
+      for (int j = 0; j < 5; ++j) xs[wave][j][lane] = x[j];
+      xs[wave][5][lane] = m;
+    }
+    __syncthreads();
+    if (wave) return;
+    const int d = lane & 15;
+    m = fmaxf(fmaxf(xs[0][5][d], xs[1][5][d]), fmaxf(xs[2][5][d], xs[3][5][d]));
+#pragma unroll
+    for (int j = 0; j < 5; ++j) x[j] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mw = xs[w][5][d], f = mw > -INFINITY ? __builtin_amdgcn_exp2f(mw - m) : 0.f;
+#pragma unroll
+      for (int j = 0; j < 5; ++j) x[j] += f * xs[w][j][d];
+    }
+  }
+  if (lane >= 16) return;
+  const float inv = x[4] == 0.f ? 0.f : 1.0f / x[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] *= inv;
+  store_row<4>(A.out, (size_t)(s.row0 + i) * A.out_stride + hd * 64 + 4 * lane, A.out_type, x);
 }
 
 template <int NQ, int QT, int PT>
@@ -789,7 +878,7 @@ int64_t kv4_attend_groups(const Kv4Pool& P, const Kv4Rows& R, int hq) {
   const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv);
   if (cols > INT32_MAX - 1024) return cols;
   const Plan p = plan_of(P, R, hq);
-  const int64_t join = p.splits > 1 ? ((int64_t)R.n_seqs * R.max_rows * hq + 3) / 4 : 0;
+  const int64_t join = p.splits > 1 ? (int64_t)R.n_seqs * R.max_rows * hq : 0;
   return std::max((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits, join);
 }
 
@@ -800,14 +889,16 @@ size_t kv4_attend_workspace(const Kv4Pool& P, const Kv4Rows& R, int hq) {
 
 hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A) {
   const Plan p = plan_of(P, R, A.hq);
-  // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers.
+  // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers, whose
+  // rounding to 11 bits is an eighth of a bf16 output's.
   if (A.out_type == kRowF32) launch_attend<2, 2>(st, P, R, A, p);
-  else if (A.q_type == kRowF32 || A.rope.at) launch_attend<2, 1>(st, P, R, A, p);
+  else if (A.out_type == kRowF16 && (A.q_type == kRowF32 || A.rope.at)) launch_attend<2, 1>(st, P, R, A, p);
   else launch_attend<1, 1>(st, P, R, A, p);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
-    const int64_t waves = (int64_t)R.n_seqs * R.max_rows * A.hq;
-    k_kv4_join<<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
+    const int64_t outs = (int64_t)R.n_seqs * R.max_rows * A.hq;
+    if (p.splits > 16) k_kv4_join<4><<<(unsigned)outs, 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
+    else k_kv4_join<1><<<(unsigned)((outs + 3) / 4), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
     e = hipGetLastError();
   }
   return e;
