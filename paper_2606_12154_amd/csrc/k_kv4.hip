@@ -43,7 +43,7 @@ __device__ __forceinline__ Seq load_seq(const Kv4Pool& P, const Kv4Rows& R, int 
   Seq q;
   const int a = R.row_start ? R.row_start[s] : s, b = R.row_start ? R.row_start[s + 1] : s + 1;
   q.row0 = min(max(a, 0), R.n_rows);
-  q.n = min(max(min(b, R.n_rows) - q.row0, 0), R.max_rows);
+  q.n = min(max(min(max(b, 0), R.n_rows) - q.row0, 0), R.max_rows);
   q.first = max(min(R.first_pos[s], 1 << 30), -(1 << 30));
   q.trow = R.table_row ? R.table_row[s] : s;
   // No such table row: every position is padding.
@@ -351,7 +351,7 @@ int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
 
 // Operand columns are (row, query head of the kv head's group) pairs, row-major:
 // column c of a sequence is row c / G, head c % G.
-constexpr int kMaxSplits = 128;
+constexpr int kMaxSplits = 64;
 
 struct Plan {
   int nq;      // 16-column tiles of a wave
@@ -369,8 +369,9 @@ Plan plan_of(const Kv4Pool& P, const Kv4Rows& R, int hq) {
   const int64_t tiles = p.wk == 1 ? (cols + 64 * p.nq - 1) / (64 * p.nq) : (cols + 16 * p.nq - 1) / (16 * p.nq);
   p.tiles = (int)std::min<int64_t>(tiles, 1 << 30);
   const int64_t groups = tiles * seqs;
-  const int most = (P.max_pages + 31) / 32;  // at least 32 pages each
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1023 + groups) / groups, most, kMaxSplits}));
+  const int64_t target = p.nq == 1 ? 1024 : p.nq == 2 ? 768 : 512;
+  const int64_t most = P.max_pages <= 64 ? 1 : P.max_pages / 16;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(target - 1 + groups) / groups, most, kMaxSplits}));
   if (p.wk == 1) p.splits = 1;
   return p;
 }
@@ -753,37 +754,37 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   }
 }
 
-// Joins the splits of a (row, head): WAVES waves have it, lane l dimensions
-// 4 (l % 16) .. + 3 of every (4 WAVES)-th split, so that all loads are in flight
-// at once.  Many splits (few rows) take four waves, up to 16 splits one.
-template <int WAVES>
-__global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const unsigned b = WAVES == 4 ? blockIdx.x : blockIdx.x * 4u + wave;
-  const int part_of = WAVES == 4 ? wave : 0;
-  const int hd = b % (unsigned)A.hq, i = b / (unsigned)A.hq % (unsigned)R.max_rows;
-  const unsigned sq = b / (unsigned)A.hq / (unsigned)R.max_rows;
-  if (sq >= (unsigned)R.n_seqs) return;
-  const Seq s = load_seq(P, R, sq);
-  if (i >= s.n) return;
-  // The pages of the row's column tile, as the attention kernel cut them.
-  const int G = A.hq / P.hkv;
-  const int cols = s.n * G, c0 = (i * G + hd % G) / tile_cols * tile_cols;
+// Splits that hold keys of column c's tile in a sequence (as the attention
+// kernel cut them); 1: the attention kernel wrote the output.
+__device__ __forceinline__ int splits_of(const Kv4Pool& P, const Seq& s, int G, int c, int tile_cols, int splits) {
+  const int cols = s.n * G, c0 = c / tile_cols * tile_cols;
   const int row_b = (min(c0 + tile_cols, cols) - 1) / G;
   const int some_see = min(max(s.first + row_b + 1, 0), P.max_pages * kPage);
-  const int np = (some_see + kPage - 1) / kPage;
-  const int per = split_pages(np, splits);
-  if (per >= np) return;
-  const int n = (np + per - 1) / per;
+  const int np = (some_see + kPage - 1) / kPage, per = split_pages(np, splits);
+  return per >= np ? 1 : (np + per - 1) / per;
+}
+
+// Joins the splits of few (row, head)s, a workgroup each: lane l of wave w has
+// dimensions 4 (l % 16) .. + 3 of splits 4 w + l / 16, + 16, ...: all loads are
+// in flight at once.
+__global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned b = blockIdx.x, row = b / (unsigned)A.hq;
+  const int hd = b - row * A.hq, i = row % (unsigned)R.max_rows;
+  const Seq s = load_seq(P, R, row / (unsigned)R.max_rows);
+  if (i >= s.n) return;
+  const int G = A.hq / P.hkv;
+  const int n = splits_of(P, s, G, i * G + hd % G, tile_cols, splits);
+  if (n == 1) return;
   const size_t at = (size_t)(s.row0 + i) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
   const float2* ml = reinterpret_cast<const float2*>(A.part + (size_t)splits * step * 64) + at;
   const float* part = A.part + at * 64 + 4 * (lane & 15);
-  constexpr int N = WAVES == 4 ? kMaxSplits / 16 : 4;  // loads of a lane
+  constexpr int N = kMaxSplits / 16;  // loads of a lane
   f32x4 y[N];
   float2 z[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    const int sp = (k * WAVES + part_of) * 4 + (lane >> 4);
+    const int sp = k * 16 + wave * 4 + (lane >> 4);
     y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
     z[k] = make_float2(-INFINITY, 0.f);
     if (sp < n) {
@@ -809,31 +810,69 @@ __global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Atten
     x[j] += __shfl_xor(x[j], 16, 64);
     x[j] += __shfl_xor(x[j], 32, 64);
   }
-  if constexpr (WAVES == 4) {
-    __shared__ float xs[4][6][16];
-    if (lane < 16) {
+  __shared__ float xs[4][6][16];
+  if (lane < 16) {
 #pragma unroll
-      for (int j = 0; j < 5; ++j) xs[wave][j][lane] = x[j];
-      xs[wave][5][lane] = m;
-    }
-    __syncthreads();
-    if (wave) return;
-    const int d = lane & 15;
-    m = fmaxf(fmaxf(xs[0][5][d], xs[1][5][d]), fmaxf(xs[2][5][d], xs[3][5][d]));
-#pragma unroll
-    for (int j = 0; j < 5; ++j) x[j] = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float mw = xs[w][5][d], f = mw > -INFINITY ? __builtin_amdgcn_exp2f(mw - m) : 0.f;
-#pragma unroll
-      for (int j = 0; j < 5; ++j) x[j] += f * xs[w][j][d];
-    }
+    for (int j = 0; j < 5; ++j) xs[wave][j][lane] = x[j];
+    xs[wave][5][lane] = m;
   }
-  if (lane >= 16) return;
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+  m = fmaxf(fmaxf(xs[0][5][lane], xs[1][5][lane]), fmaxf(xs[2][5][lane], xs[3][5][lane]));
+#pragma unroll
+  for (int j = 0; j < 5; ++j) x[j] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float mw = xs[w][5][lane], f = mw > -INFINITY ? __builtin_amdgcn_exp2f(mw - m) : 0.f;
+#pragma unroll
+    for (int j = 0; j < 5; ++j) x[j] += f * xs[w][j][lane];
+  }
   const float inv = x[4] == 0.f ? 0.f : 1.0f / x[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) x[j] *= inv;
   store_row<4>(A.out, (size_t)(s.row0 + i) * A.out_stride + hd * 64 + 4 * lane, A.out_type, x);
+}
+
+// Up to 16 splits of many (row, head)s, 16 lanes each: lane l of them has
+// split l's statistics and dimensions 4 l .. + 3.
+__global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
+  const int l16 = threadIdx.x & 15;
+  const unsigned b = blockIdx.x * 16u + (threadIdx.x >> 4), row = b / (unsigned)A.hq;
+  const int hd = b - row * A.hq, i = row % (unsigned)R.max_rows;
+  const unsigned sq = row / (unsigned)R.max_rows;
+  // (No early return: the lanes of a wave exchange below.)
+  const bool in = sq < (unsigned)R.n_seqs;
+  const Seq s = load_seq(P, R, in ? sq : 0);
+  const int G = A.hq / P.hkv;
+  const int n = in && i < s.n ? splits_of(P, s, G, i * G + hd % G, tile_cols, splits) : 1;
+  const size_t at = (size_t)(s.row0 + (n > 1 ? i : 0)) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
+  const float2* ml = reinterpret_cast<const float2*>(A.part + (size_t)splits * step * 64) + at;
+  const float* part = A.part + at * 64 + 4 * l16;
+  float2 z = make_float2(-INFINITY, 0.f);
+  if (n > 1 && l16 < n) z = ml[l16 * step];
+  const float m = row_max16(z.x);
+  const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
+  const float l = row_sum16(f * z.y);
+  float x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < splits; k0 += 4) {
+    f32x4 y[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (n > 1 && k0 + k < n) y[k] = *reinterpret_cast<const f32x4*>(part + (k0 + k) * step * 64);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float w = __shfl(f, (k0 + k) & 15, 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] += w * y[k][j];
+    }
+  }
+  if (n == 1) return;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] *= inv;
+  store_row<4>(A.out, (size_t)(s.row0 + i) * A.out_stride + hd * 64 + 4 * l16, A.out_type, x);
 }
 
 template <int NQ, int QT, int PT>
@@ -897,8 +936,8 @@ hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const 
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
     const int64_t outs = (int64_t)R.n_seqs * R.max_rows * A.hq;
-    if (p.splits > 16) k_kv4_join<4><<<(unsigned)outs, 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
-    else k_kv4_join<1><<<(unsigned)((outs + 3) / 4), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
+    if (p.splits > 16) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
+    else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
     e = hipGetLastError();
   }
   return e;
