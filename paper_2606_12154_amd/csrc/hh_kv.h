@@ -46,12 +46,19 @@ hipError_t kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const 
                       int64_t k_stride, int64_t v_stride, RopeTable rope);
 hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
                     int64_t v_stride);
-// Workgroups of the append and read kernels, and of the attention kernel:
-// callers refuse what does not fit a launch.
-int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R);
-int64_t kv4_attend_groups(const Kv4Pool& P, const Kv4Rows& R, int hq);
-size_t kv4_attend_workspace(const Kv4Pool& P, const Kv4Rows& R, int hq);
-hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A);
+int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R);  // their workgroups: callers refuse what does not fit a grid
+
+// How the attention of these sizes is cut up.
+struct Kv4Plan {
+  int nq;      // 16-column tiles of a wave
+  int wk;      // waves of a workgroup that share the columns and split the keys (4), or 1
+  int tiles;   // column tiles (workgroups) a sequence and kv head
+  int splits;  // key splits over workgroups
+  int64_t groups;    // the larger grid: callers refuse what does not fit
+  size_t workspace;  // bytes
+};
+Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq);
+hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
 
 // n_layers pools of pages of `bytes` (a multiple of 16), layer_stride bytes apart.
 struct PagePool {

@@ -21,6 +21,7 @@
 #include "hh_kv.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace hh {
@@ -145,17 +146,30 @@ __device__ __forceinline__ void store_row(void* p, size_t at, int type, const fl
 
 // ------------------------------------------------------------------ append and read
 
-// Scale of a group whose largest magnitude is a (finite).
-__device__ __forceinline__ float group_scale(float a) {
-  const float t = a / 7.0f;
-  if (t < 0x1p-17f) return rintf(t * 0x1p24f) * 0x1p-24f;
-  const unsigned u = __float_as_uint(t);
-  return fminf(__uint_as_float((u + 0x7fffu + ((u >> 16) & 1u)) & 0xffff0000u), kMaxScale);
+// x / s as a division rounds it, wherever that decides: a reciprocal and one
+// correction by the residual.  The quotient's distance from the middle between
+// two fp32 numbers is 0 or at least 1/510 of their distance (s has 8 significant bits,
+// and 7 has 3), and 0 only for a power of two, whose reciprocal is exact; the
+// corrected quotient is 2^-22 off.
+__device__ __forceinline__ float quotient(float x, float s, float r) {
+  const float q = x * r;
+  return fmaf(fmaf(-q, s, x), r, q);
 }
 
-__device__ __forceinline__ unsigned code_of(float x, float s) {
-  if (!(s > 0.f)) return 8u;  // a zero scale, or NaN
-  return (unsigned)((int)fminf(fmaxf(rintf(x / s), -7.f), 7.f) + 8);
+// Scale of a group whose largest magnitude is a (finite).
+__device__ __forceinline__ float group_scale(float a) {
+  const float t = quotient(a, 7.0f, 1.0f / 7.0f);
+  const unsigned u = __float_as_uint(t);
+  const float s = fminf(__uint_as_float((u + 0x7fffu + ((u >> 16) & 1u)) & 0xffff0000u), kMaxScale);
+  return t < 0x1p-17f ? rintf(t * 0x1p24f) * 0x1p-24f : s;
+}
+
+// Reciprocal of a scale; 0, and hence code 0, for a zero scale or NaN.
+__device__ __forceinline__ float scale_rcp(float s) { return s > 0.f ? __builtin_amdgcn_rcpf(s) : 0.f; }
+
+// n = c + 8 of a finite x: r is scale_rcp(s); s is finite.
+__device__ __forceinline__ unsigned code_of(float x, float s, float r) {
+  return (unsigned)((int)fminf(fmaxf(rintf(quotient(x, s, r)), -7.f), 7.f) + 8);
 }
 
 __device__ __forceinline__ unsigned short half_bits(float s) {
@@ -171,13 +185,11 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Pool P, Kv4Rows R, const 
                                                     const void* __restrict__ v, int type, int64_t ks, int64_t vs,
                                                     RopeTable rope, int tiles) {
   const int lane = threadIdx.x & 63;
-  int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int head = (int)(w % P.hkv);
-  w /= P.hkv;
-  const int tile = (int)(w % tiles);
-  w /= tiles;
-  if (w >= R.n_seqs) return;
-  const Seq q = load_seq(P, R, (int)w);
+  const int head = blockIdx.y * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (head >= P.hkv) return;
+  const unsigned sq = blockIdx.x / (unsigned)tiles;
+  const int tile = blockIdx.x - sq * tiles;
+  const Seq q = load_seq(P, R, sq);
   const int lo = max(q.first, 0);
   int hi = min(q.first + q.n, P.max_pages * kPage);
   if (rope.at) hi = min(hi, rope.len);
@@ -225,15 +237,16 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Pool P, Kv4Rows R, const 
     unsigned word[2], sc = 0;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const float s = bad ? NAN : group_scale(top[t]);
+      // (A row that is not finite: codes of 0.)
+      const float s = bad ? 0.f : group_scale(top[t]), rs = scale_rcp(s);
       unsigned d = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        d |= code_of(x[8 * t + 2 * j], s) << (4 * j);
-        d |= code_of(x[8 * t + 2 * j + 1], s) << (4 * j + 16);
+        d |= code_of(bad ? 0.f : x[8 * t + 2 * j], s, rs) << (4 * j);
+        d |= code_of(bad ? 0.f : x[8 * t + 2 * j + 1], s, rs) << (4 * j + 16);
       }
       word[t] = d;
-      sc |= (unsigned)half_bits(s) << (16 * t);
+      sc |= (bad ? 0x7e00u : (unsigned)half_bits(s)) << (16 * t);
     }
     if (mine) {
       *reinterpret_cast<u32x2*>(blk + 8 * lane) = u32x2{word[0], word[1]};
@@ -262,12 +275,12 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Pool P, Kv4Rows R, const 
       bad |= __shfl_xor(bad, o, 64);
     }
     bad |= __shfl_xor(bad, 8, 64);
-    const float s = bad ? NAN : group_scale(top);
+    const float s = bad ? 0.f : group_scale(top), rs = scale_rcp(s);
     unsigned d = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) d |= code_of(x[j], s) << (4 * j);
+    for (int j = 0; j < 4; ++j) d |= code_of(bad ? 0.f : x[j], s, rs) << (4 * j);
     code[i] = (unsigned short)d;
-    sc[i] = half_bits(s);
+    sc[i] = bad ? 0x7e00u : half_bits(s);
   }
   unsigned short* vb = reinterpret_cast<unsigned short*>(blk + 512) + 4 * lane;
   unsigned short* vsc = reinterpret_cast<unsigned short*>(blk + kValueScales) + (r >> 3) * 16 + 4 * g;
@@ -292,13 +305,11 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Pool P, Kv4Rows R, const 
 __global__ __launch_bounds__(256) void k_kv4_read(Kv4Pool P, Kv4Rows R, void* __restrict__ k, void* __restrict__ v,
                                                   int type, int64_t ks, int64_t vs, int tiles) {
   const int lane = threadIdx.x & 63;
-  int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int head = (int)(w % P.hkv);
-  w /= P.hkv;
-  const int tile = (int)(w % tiles);
-  w /= tiles;
-  if (w >= R.n_seqs) return;
-  const Seq q = load_seq(P, R, (int)w);
+  const int head = blockIdx.y * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (head >= P.hkv) return;
+  const unsigned sq = blockIdx.x / (unsigned)tiles;
+  const int tile = blockIdx.x - sq * tiles;
+  const Seq q = load_seq(P, R, sq);
   const int page = (q.first >> 4) + tile;  // floor
   const int hi = q.first + q.n;
   if (page * kPage >= hi) return;
@@ -353,27 +364,32 @@ int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
 // column c of a sequence is row c / G, head c % G.
 constexpr int kMaxSplits = 64;
 
-struct Plan {
-  int nq;      // 16-column tiles of a wave
-  int wk;      // waves of a workgroup that share the columns and split the keys (4), or 1
-  int tiles;   // column tiles (workgroups) a sequence and kv head
-  int splits;  // key splits over workgroups
-};
-
-Plan plan_of(const Kv4Pool& P, const Kv4Rows& R, int hq) {
-  const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv);
-  Plan p;
-  p.nq = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
-  const int64_t t4 = (cols + 63) / 64, seqs = (int64_t)R.n_seqs * P.hkv;
-  p.wk = (t4 + 3) / 4 * seqs >= 512 ? 1 : 4;
-  const int64_t tiles = p.wk == 1 ? (cols + 64 * p.nq - 1) / (64 * p.nq) : (cols + 16 * p.nq - 1) / (16 * p.nq);
-  p.tiles = (int)std::min<int64_t>(tiles, 1 << 30);
-  const int64_t groups = tiles * seqs;
-  const int64_t target = p.nq == 1 ? 1024 : p.nq == 2 ? 768 : 512;
-  const int64_t most = P.max_pages <= 64 ? 1 : P.max_pages / 16;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(target - 1 + groups) / groups, most, kMaxSplits}));
-  if (p.wk == 1) p.splits = 1;
-  return p;
+// Key splits of `groups` (sequence, kv head, column tile)s over up to `pages`
+// pages, by the time that they would take, in ns.  Measured (32 query heads on
+// 8): a workgroup that is alone on its CU takes 65 ns a page with one column tile, 120
+// with four; four (two) of them there, as many as fit, 150 (187) each.  What
+// comes before and after the pages is 4.5 us, and 0.5 more for each neighbour; the
+// join 2.8 us, and its reads.  So one sequence of 700 positions is not split (7.6
+// us against 8.4), 8,192 take 32 splits (8.9; 16 splits 10.7), 32 sequences of
+// 4,000 take 4 (22.4; unsplit 31.3), 64 of 1,500 none (19.0; 2 splits 19.5),
+// 256 rows behind 30,000 positions 4 (92; 2 splits 118, 8 splits 99).
+int splits_for(int nq, int64_t groups, int pages, int64_t outputs) {
+  const double page = nq == 1 ? 65 : nq == 2 ? 90 : 120, more = nq == 1 ? 28 : nq == 2 ? 50 : 67;
+  const int fit = nq == 1 ? 4 : nq == 2 ? 3 : 2;
+  const int most = std::max(1, std::min(kMaxSplits, pages / 8));
+  int best = 1;
+  double best_ns = 0;
+  for (int s = 1; s <= most; ++s) {
+    const double k = std::ceil((double)groups * s / 256), here = std::min<double>(k, fit);
+    const double each = (page + more * (here - 1)) * std::max(1.0, k / fit);
+    double ns = 4500 * std::ceil(k / fit) + 500 * (here - 1) + each * std::ceil((double)pages / s);
+    if (s > 1) ns += 2800 + 0.066 * (double)outputs * s;
+    if (s == 1 || ns < best_ns) {
+      best = s;
+      best_ns = ns;
+    }
+  }
+  return best;
 }
 
 // Pages of a split, given the pages that a column tile attends to.
@@ -444,7 +460,7 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   const int tile = tiles - 1 - (int)(b % (unsigned)tiles);
   const Seq s = load_seq(P, R, b / (unsigned)tiles);
   const int G = A.hq / P.hkv;
-  const int cols = s.n * G;  // below 2^31 with a tile to spare (kv4_attend_groups)
+  const int cols = s.n * G;  // below 2^31 with a tile to spare (kv4_plan)
   const int c0 = (tile * (WK == 1 ? 4 : 1) + (WK == 1 ? wave : 0)) * (16 * NQ);
   if (c0 >= cols) return;
   // Keys of the tile's first and last row.
@@ -876,7 +892,7 @@ __global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4
 }
 
 template <int NQ, int QT, int PT>
-void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Plan& p) {
+void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
   if constexpr (NQ == 4) {
     if (p.wk == 1) {
@@ -888,7 +904,7 @@ void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4
 }
 
 template <int QT, int PT>
-void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Plan& p) {
+void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   if (p.nq == 1) launch_attend<1, QT, PT>(st, P, R, A, p);
   else if (p.nq == 2) launch_attend<2, QT, PT>(st, P, R, A, p);
   else launch_attend<4, QT, PT>(st, P, R, A, p);
@@ -896,38 +912,42 @@ void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4
 
 }  // namespace
 
-int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R) {
-  return ((int64_t)R.n_seqs * row_tiles(R) * P.hkv + 3) / 4;
+int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R) { return (int64_t)R.n_seqs * row_tiles(R); }
+
+// A wave a (page, head), up to four heads a workgroup.
+static dim3 row_grid(const Kv4Pool& P, const Kv4Rows& R) {
+  return dim3((unsigned)kv4_row_groups(P, R), (unsigned)((P.hkv + 3) / 4));
 }
+static unsigned row_threads(const Kv4Pool& P) { return 64u * std::min(P.hkv, 4); }
 
 hipError_t kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
                       int64_t k_stride, int64_t v_stride, RopeTable rope) {
-  k_kv4_append<<<(unsigned)kv4_row_groups(P, R), 256, 0, st>>>(P, R, k, v, type, k_stride, v_stride, rope, row_tiles(R));
+  k_kv4_append<<<row_grid(P, R), row_threads(P), 0, st>>>(P, R, k, v, type, k_stride, v_stride, rope, row_tiles(R));
   return hipGetLastError();
 }
 
 hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
                     int64_t v_stride) {
-  k_kv4_read<<<(unsigned)kv4_row_groups(P, R), 256, 0, st>>>(P, R, k, v, type, k_stride, v_stride, row_tiles(R));
+  k_kv4_read<<<row_grid(P, R), row_threads(P), 0, st>>>(P, R, k, v, type, k_stride, v_stride, row_tiles(R));
   return hipGetLastError();
 }
 
-int64_t kv4_attend_groups(const Kv4Pool& P, const Kv4Rows& R, int hq) {
-  // Columns are counted in 32 bits.
-  const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv);
-  if (cols > INT32_MAX - 1024) return cols;
-  const Plan p = plan_of(P, R, hq);
+Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq) {
+  Kv4Plan p;
+  const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), seqs = (int64_t)R.n_seqs * P.hkv;
+  p.nq = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+  p.wk = (cols + 255) / 256 * seqs >= 512 ? 1 : 4;
+  const int64_t tiles = p.wk == 1 ? (cols + 255) / 256 : (cols + 16 * p.nq - 1) / (16 * p.nq);
+  p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
+  p.splits = p.wk == 1 ? 1 : splits_for(p.nq, tiles * seqs, P.max_pages, (int64_t)R.n_rows * hq);
   const int64_t join = p.splits > 1 ? (int64_t)R.n_seqs * R.max_rows * hq : 0;
-  return std::max((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits, join);
+  // (Columns are counted in 32 bits.)
+  p.groups = cols > INT32_MAX - 1024 ? cols : std::max(seqs * tiles * p.splits, join);
+  p.workspace = p.splits > 1 ? (size_t)p.splits * R.n_rows * hq * (64 + 2) * sizeof(float) : 0;
+  return p;
 }
 
-size_t kv4_attend_workspace(const Kv4Pool& P, const Kv4Rows& R, int hq) {
-  const Plan p = plan_of(P, R, hq);
-  return p.splits > 1 ? (size_t)p.splits * R.n_rows * hq * (64 + 2) * sizeof(float) : 0;
-}
-
-hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A) {
-  const Plan p = plan_of(P, R, A.hq);
+hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers, whose
   // rounding to 11 bits is an eighth of a bf16 output's.
   if (A.out_type == kRowF32) launch_attend<2, 2>(st, P, R, A, p);

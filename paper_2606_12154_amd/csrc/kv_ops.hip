@@ -101,8 +101,9 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
   Kv4Pool P;
   Kv4Rows R;
   if (!bytes || !describe(pool, rows, &P, &R) || n_heads < 1 || n_heads % P.hkv != 0) return HH_ERR_INVALID_ARG;
-  if (kv4_attend_groups(P, R, n_heads) > INT32_MAX) return HH_ERR_UNSUPPORTED;
-  *bytes = kv4_attend_workspace(P, R, n_heads);
+  const Kv4Plan plan = kv4_plan(P, R, n_heads);
+  if (plan.groups > INT32_MAX) return HH_ERR_UNSUPPORTED;
+  *bytes = plan.workspace;
   return HH_OK;
 }
 
@@ -122,9 +123,9 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
   if (!aligned(q, 16) || !aligned(out, 16) || !row_stride(q_stride, n, q_size) || !row_stride(out_stride, n, out_size) ||
       !(scale > 0.f) || !std::isfinite(scale))
     return HH_ERR_INVALID_ARG;
-  if (kv4_attend_groups(P, R, n_heads) > INT32_MAX) return HH_ERR_UNSUPPORTED;
-  const size_t need = kv4_attend_workspace(P, R, n_heads);
-  if (need && (!aligned(workspace, 256) || workspace_bytes < need)) return HH_ERR_INVALID_ARG;
+  const Kv4Plan plan = kv4_plan(P, R, n_heads);
+  if (plan.groups > INT32_MAX) return HH_ERR_UNSUPPORTED;
+  if (plan.workspace && (!aligned(workspace, 256) || workspace_bytes < plan.workspace)) return HH_ERR_INVALID_ARG;
   A.q = q;
   A.out = out;
   A.q_stride = q_stride;
@@ -132,7 +133,7 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
   A.hq = n_heads;
   A.scale = scale;
   A.part = static_cast<float*>(workspace);
-  return from_hip(kv4_attend(static_cast<hipStream_t>(hip_stream), P, R, A));
+  return from_hip(kv4_attend(static_cast<hipStream_t>(hip_stream), P, R, A, plan));
 }
 
 hh_status hh_kv_copy_pages(void* pool, int32_t n_layers, int64_t layer_stride, int64_t page_bytes, int32_t n_pages,
