@@ -61,6 +61,15 @@ enum { HH_F16 = 2 };                                    /* a further row type of
  * computes with the values q * s.
  */
 enum { HH_WF_DTYPE = 0, HH_WF_Q4G32 = 1 };
+/*
+ * Added to a weight format (either, of either dtype): the context keeps its
+ * KV cache in 4 bits, in the pages of hh_kv4_append below, quantized as keys
+ * (rotated) and values are produced.  72 bytes a position and kv head take the place of
+ * fp16's 256 (fp32's 512).  Prompts and decode steps run as otherwise, batch-1 steps
+ * through the kernels of the multi-stream ones; hh_decode_step_noalloc gives
+ * HH_ERR_UNSUPPORTED.  A context is created with one or the other cache.
+ */
+enum { HH_KV_Q4 = 0x100 };
 enum { HH_LOGITS_NONE = 0, HH_LOGITS_LAST = 1, HH_LOGITS_ALL = 2 };
 
 /*
@@ -80,7 +89,7 @@ typedef struct {
   int32_t max_prefill;       /* rows per prefill pass; 0 means max_context.
                                 Longer prompts are processed in passes.      */
   int32_t weight_format;     /* HH_WF_DTYPE or HH_WF_Q4G32 (dtype HH_BF16,
-                                d_model % 32 == 0)                           */
+                                d_model % 32 == 0); + HH_KV_Q4               */
 } hh_config;
 
 typedef struct hh_ctx hh_ctx;
@@ -205,6 +214,40 @@ hh_status hh_decode_step_noalloc(hh_ctx* ctx, int32_t stream_id, const int32_t* 
  * Also clears the context's record of a failed decode step (see
  * hh_decode_step). */
 hh_status hh_reset(hh_ctx* ctx, int32_t stream_id);
+
+/*
+ * Fork a stream: each listed stream becomes a copy of stream src -- its
+ * positions, pending token and argmax history -- and goes on by itself.  Full KV
+ * pages are shared between the streams until each drops them; the partly
+ * filled last page is copied.  What the listed streams held is dropped.  So
+ * several answers to one prompt, or prompts with a common beginning, take one
+ * prompt evaluation of it.
+ *  dst  host, n distinct stream ids other than src.
+ * Only enqueues.  Errors: INVALID_ARG (an id out of range, repeated or src, n
+ * outside 1..max_streams - 1), OOM (host memory), HIP.
+ */
+hh_status hh_fork(hh_ctx* ctx, int32_t src, int32_t n, const int32_t* dst);
+
+/*
+ * Cut a stream to its first `length` positions and free the KV pages behind
+ * them (a page that another stream shares stays; one that this stream will
+ * write to again is copied first).  The stream's pending token becomes the argmax recorded at
+ * position length - 1; where none was (inside a prompt), the next
+ * decode step of the stream must be given its token.  length 0 is as
+ * hh_reset of the stream, but for the record of a failed step.
+ * Only enqueues.  Errors: INVALID_ARG (an id out of range, length < 0 or past
+ * the stream's), HIP.
+ */
+hh_status hh_truncate(hh_ctx* ctx, int32_t stream_id, int32_t length);
+
+/*
+ * Move the KV pages that streams hold to the lowest page ids (hh_kv_compact's
+ * rule), in every layer; results do not change.  After it the pages that are
+ * in use, *pages_in_use of them (may be NULL), lie together at the start of each layer's
+ * pool.  Only enqueues.  Errors: UNSUPPORTED (over 2^20 pages), OOM (host
+ * memory), HIP.
+ */
+hh_status hh_compact(hh_ctx* ctx, int32_t* pages_in_use);
 
 /* Current length (positions held in the KV cache) of a stream. */
 hh_status hh_stream_length(const hh_ctx* ctx, int32_t stream_id, int32_t* length);

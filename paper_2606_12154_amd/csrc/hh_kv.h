@@ -57,7 +57,8 @@ struct Kv4Plan {
   int64_t groups;    // the larger grid: callers refuse what does not fit
   size_t workspace;  // bytes
 };
-Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq);
+// pages: a bound of the pages that a sequence holds; most_bytes: of the workspace.
+Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes = SIZE_MAX);
 hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
 
 // n_layers pools of pages of `bytes` (a multiple of 16), layer_stride bytes apart.
@@ -67,8 +68,20 @@ struct PagePool {
   int n_layers, n_pages;
 };
 hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst);
+constexpr int kMaxCompactPages = 1 << 20;  // one bit each in LDS: 128 KiB
 size_t compact_workspace(int n_pages);
 hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int table_rows, int max_pages,
                          const int* lengths, int* live, void* ws);
+
+// ---- a context's streams (hh_fork, hh_truncate)
+// Streams ids[0 .. n) become the first len positions of stream src: page-table
+// entries of its full pages, then last[i] (where given) for the partly filled one;
+// position, pending token and argmax history.
+hipError_t fork_streams(hipStream_t st, int src, int n, const int* ids, const int* last, int len, int max_ctx,
+                        int max_pages, int* table, int* pos, int* pending, unsigned long long* slot, int* hist);
+// Stream s ends at len > 0: its pending token is the argmax of position len - 1.
+hipError_t truncate_stream(hipStream_t st, int s, int len, int max_ctx, int* pos, int* pending, const int* hist);
+// p[0 .. n) = 0, as a kernel (a graph's replays may clear memory only so).
+void zero_floats(hipStream_t st, float* p, size_t n);
 
 }  // namespace hh

@@ -364,6 +364,9 @@ int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
 // column c of a sequence is row c / G, head c % G.
 constexpr int kMaxSplits = 64;
 
+// Workspace of s splits: 64 dimensions, base and sum of weights each.
+size_t split_bytes(int s, int64_t outputs) { return (size_t)s * (size_t)outputs * (64 + 2) * sizeof(float); }
+
 // Key splits of `groups` (sequence, kv head, column tile)s over up to `pages`
 // pages, by the time that they would take, in ns.  Measured (32 query heads on
 // 8): a workgroup that is alone on its CU takes 65 ns a page with one column tile, 120
@@ -373,13 +376,13 @@ constexpr int kMaxSplits = 64;
 // us against 8.4), 8,192 take 32 splits (8.9; 16 splits 10.7), 32 sequences of
 // 4,000 take 4 (22.4; unsplit 31.3), 64 of 1,500 none (19.0; 2 splits 19.5),
 // 256 rows behind 30,000 positions 4 (92; 2 splits 118, 8 splits 99).
-int splits_for(int nq, int64_t groups, int pages, int64_t outputs) {
+int splits_for(int nq, int64_t groups, int pages, int64_t outputs, size_t most_bytes) {
   const double page = nq == 1 ? 65 : nq == 2 ? 90 : 120, more = nq == 1 ? 28 : nq == 2 ? 50 : 67;
   const int fit = nq == 1 ? 4 : nq == 2 ? 3 : 2;
   const int most = std::max(1, std::min(kMaxSplits, pages / 8));
   int best = 1;
   double best_ns = 0;
-  for (int s = 1; s <= most; ++s) {
+  for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= most_bytes); ++s) {
     const double k = std::ceil((double)groups * s / 256), here = std::min<double>(k, fit);
     const double each = (page + more * (here - 1)) * std::max(1.0, k / fit);
     double ns = 4500 * std::ceil(k / fit) + 500 * (here - 1) + each * std::ceil((double)pages / s);
@@ -932,18 +935,19 @@ hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k,
   return hipGetLastError();
 }
 
-Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq) {
+Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes) {
   Kv4Plan p;
   const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), seqs = (int64_t)R.n_seqs * P.hkv;
   p.nq = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
   p.wk = (cols + 255) / 256 * seqs >= 512 ? 1 : 4;
   const int64_t tiles = p.wk == 1 ? (cols + 255) / 256 : (cols + 16 * p.nq - 1) / (16 * p.nq);
   p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-  p.splits = p.wk == 1 ? 1 : splits_for(p.nq, tiles * seqs, P.max_pages, (int64_t)R.n_rows * hq);
+  const int64_t outputs = (int64_t)R.n_rows * hq;
+  p.splits = p.wk == 1 ? 1 : splits_for(p.nq, tiles * seqs, pages, outputs, most_bytes);
   const int64_t join = p.splits > 1 ? (int64_t)R.n_seqs * R.max_rows * hq : 0;
   // (Columns are counted in 32 bits.)
   p.groups = cols > INT32_MAX - 1024 ? cols : std::max(seqs * tiles * p.splits, join);
-  p.workspace = p.splits > 1 ? (size_t)p.splits * R.n_rows * hq * (64 + 2) * sizeof(float) : 0;
+  p.workspace = p.splits > 1 ? split_bytes(p.splits, outputs) : 0;
   return p;
 }
 

@@ -46,7 +46,6 @@ __global__ __launch_bounds__(256) void k_copy_pages(PagePool P, int pieces, Pair
 // ------------------------------------------------------------------ compaction
 
 constexpr int kPlanThreads = 1024;
-constexpr int kMaxPlanPages = 1 << 20;  // one bit each in LDS: 128 KiB
 
 // Sum of v over the threads before this one; total: over all of them.
 __device__ __forceinline__ int exclusive_scan(int v, int* red, int& total) {
@@ -154,6 +153,46 @@ __global__ __launch_bounds__(256) void k_compact_move(PagePool P, int pieces, co
   }
 }
 
+// ------------------------------------------------------------------ streams
+
+constexpr int kForks = 62;
+struct ForkArgs {
+  int n, has_last;
+  int ids[kForks], last[kForks];
+};
+
+// One row of workgroups a fork; nothing that it reads does it write.
+__global__ __launch_bounds__(256) void k_fork_streams(int src, int len, int max_ctx, int max_pages, ForkArgs a,
+                                                      int* __restrict__ table, int* __restrict__ pos,
+                                                      int* __restrict__ pending, unsigned long long* __restrict__ slot,
+                                                      int* __restrict__ hist) {
+  const int s = a.ids[blockIdx.y], full = len / kPage;
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < len) hist[(size_t)s * max_ctx + i] = hist[(size_t)src * max_ctx + i];
+  if (i < full) table[(size_t)s * max_pages + i] = table[(size_t)src * max_pages + i];
+  if (i == 0) {
+    if (a.has_last) table[(size_t)s * max_pages + full] = a.last[blockIdx.y];
+    pos[s] = len;
+    pending[s] = pending[src];
+    slot[s] = 0ull;
+  }
+}
+
+__global__ void k_truncate_stream(int s, int len, int max_ctx, int* __restrict__ pos, int* __restrict__ pending,
+                                  const int* __restrict__ hist) {
+  pos[s] = len;
+  pending[s] = hist[(size_t)s * max_ctx + len - 1];
+}
+
+__global__ __launch_bounds__(256) void k_zero_floats(float* __restrict__ p, size_t n) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i + 4 <= n) {
+    *reinterpret_cast<f32x4*>(p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+  } else {
+    for (size_t j = i; j < n; ++j) p[j] = 0.f;
+  }
+}
+
 int pieces_of(const PagePool& P) { return (int)((P.bytes + kPiece - 1) / kPiece); }
 
 }  // namespace
@@ -183,10 +222,10 @@ hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int tabl
                          const int* lengths, int* live, void* ws) {
   int* moves = static_cast<int*>(ws);
   const size_t lds = (size_t)(P.n_pages + 31) / 32 * 4;
-  static_assert(kMaxPlanPages / 8 + 1024 <= 160 * 1024, "LDS");
+  static_assert(kMaxCompactPages / 8 + 1024 <= 160 * 1024, "LDS");
   if (lds > 48 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_compact_plan),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, kMaxPlanPages / 8);
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, kMaxCompactPages / 8);
     if (e != hipSuccess) return e;
   }
   k_compact_plan<<<1, kPlanThreads, lds, st>>>(P.n_pages, table, table_rows, max_pages, lengths, live, moves);
@@ -200,6 +239,33 @@ hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int tabl
   k_compact_move<<<move_groups + table_groups, 256, 0, st>>>(P, pieces, moves, move_groups, table, table_rows,
                                                              max_pages, lengths, live);
   return hipGetLastError();
+}
+
+hipError_t fork_streams(hipStream_t st, int src, int n, const int* ids, const int* last, int len, int max_ctx,
+                        int max_pages, int* table, int* pos, int* pending, unsigned long long* slot, int* hist) {
+  for (int o = 0; o < n; o += kForks) {
+    ForkArgs a{};
+    a.n = std::min(kForks, n - o);
+    a.has_last = last != nullptr;
+    for (int i = 0; i < a.n; ++i) {
+      a.ids[i] = ids[o + i];
+      a.last[i] = last ? last[o + i] : 0;
+    }
+    const dim3 grid((unsigned)std::max(1, (len + 255) / 256), (unsigned)a.n);
+    k_fork_streams<<<grid, 256, 0, st>>>(src, len, max_ctx, max_pages, a, table, pos, pending, slot, hist);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t truncate_stream(hipStream_t st, int s, int len, int max_ctx, int* pos, int* pending, const int* hist) {
+  k_truncate_stream<<<1, 1, 0, st>>>(s, len, max_ctx, pos, pending, hist);
+  return hipGetLastError();
+}
+
+void zero_floats(hipStream_t st, float* p, size_t n) {
+  if (n > 0) k_zero_floats<<<(unsigned)((n + 1023) / 1024), 256, 0, st>>>(p, n);
 }
 
 }  // namespace hh

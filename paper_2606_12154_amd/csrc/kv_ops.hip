@@ -101,7 +101,7 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
   Kv4Pool P;
   Kv4Rows R;
   if (!bytes || !describe(pool, rows, &P, &R) || n_heads < 1 || n_heads % P.hkv != 0) return HH_ERR_INVALID_ARG;
-  const Kv4Plan plan = kv4_plan(P, R, n_heads);
+  const Kv4Plan plan = kv4_plan(P, R, n_heads, P.max_pages);
   if (plan.groups > INT32_MAX) return HH_ERR_UNSUPPORTED;
   *bytes = plan.workspace;
   return HH_OK;
@@ -123,7 +123,7 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
   if (!aligned(q, 16) || !aligned(out, 16) || !row_stride(q_stride, n, q_size) || !row_stride(out_stride, n, out_size) ||
       !(scale > 0.f) || !std::isfinite(scale))
     return HH_ERR_INVALID_ARG;
-  const Kv4Plan plan = kv4_plan(P, R, n_heads);
+  const Kv4Plan plan = kv4_plan(P, R, n_heads, P.max_pages);
   if (plan.groups > INT32_MAX) return HH_ERR_UNSUPPORTED;
   if (plan.workspace && (!aligned(workspace, 256) || workspace_bytes < plan.workspace)) return HH_ERR_INVALID_ARG;
   A.q = q;
@@ -161,7 +161,7 @@ hh_status hh_kv_copy_pages(void* pool, int32_t n_layers, int64_t layer_stride, i
 
 hh_status hh_kv_compact_workspace(int32_t n_pages, size_t* bytes) {
   if (!bytes || n_pages < 1) return HH_ERR_INVALID_ARG;
-  if (n_pages > 1 << 20) return HH_ERR_UNSUPPORTED;
+  if (n_pages > kMaxCompactPages) return HH_ERR_UNSUPPORTED;
   *bytes = compact_workspace(n_pages);
   return HH_OK;
 }
@@ -173,7 +173,7 @@ hh_status hh_kv_compact(void* pool, int32_t n_layers, int64_t layer_stride, int6
   if (!page_pool(pool, n_layers, layer_stride, page_bytes, n_pages, &P) || !aligned(page_table, 4) || table_rows < 1 ||
       max_pages < 1 || max_pages > 1 << 26 || !aligned(lengths, 4) || !aligned(live, 4))
     return HH_ERR_INVALID_ARG;
-  if (n_pages > 1 << 20) return HH_ERR_UNSUPPORTED;
+  if (n_pages > kMaxCompactPages) return HH_ERR_UNSUPPORTED;
   if (!aligned(workspace, 256) || workspace_bytes < compact_workspace(n_pages)) return HH_ERR_INVALID_ARG;
   return from_hip(compact_pages(static_cast<hipStream_t>(hip_stream), P, page_table, table_rows, max_pages, lengths,
                                 live, workspace));

@@ -12,6 +12,7 @@
 #include <cstring>
 #include <map>
 #include <mutex>
+#include <new>
 #include <string>
 #include <tuple>
 #include <type_traits>
@@ -19,6 +20,7 @@
 
 #include "hh.h"
 #include "hh_kernels.h"
+#include "hh_kv.h"
 
 using namespace hh;
 
@@ -28,6 +30,7 @@ constexpr int kSplitMax = 64;   // attention splits per (row, kv head) in decode
 constexpr int kLogitRows = 64;  // rows of the logits staging buffer (prefill ALL)
 constexpr int kSplitRows = 1024;  // rows of one many-row LM head launch
 constexpr int kMaxStepWG = 1024; // upper bound on persistent decode-step workgroups
+constexpr size_t kKv4Work = (size_t)16 << 20;  // split outputs of the 4-bit cache's attention (it takes as many splits as fit)
 
 size_t al(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -60,10 +63,25 @@ struct Layout {
   // between launches; in the zero-initialised range) and row sums of squares.
   size_t nrm_cnt, nrm_ss;
   int nrm_ncnt;
+  // 4-bit caches: fp32 rows of the QKV product, the pass's sequences (row
+  // starts, first positions, streams) and the attention's split outputs.
+  bool kv4;
+  size_t qkv32, seqs, kv4_work;
+  size_t page_bytes;  // one layer's page
+  size_t compact, lengths;  // hh_compact's lists, and the streams' lengths
   size_t total;
 };
 
-bool config_supported(const hh_config& c, std::string& why) {
+// The cache's format travels in weight_format (HH_KV_Q4); the rest of the runtime
+// sees the weights' format alone.
+hh_config without_kv(hh_config c) {
+  c.weight_format &= ~HH_KV_Q4;
+  return c;
+}
+bool wants_kv4(const hh_config& c) { return (c.weight_format & HH_KV_Q4) != 0; }
+
+bool config_supported(const hh_config& asked, std::string& why) {
+  const hh_config c = without_kv(asked);
   if (c.n_layers < 0 || c.d_model <= 0 || c.n_heads <= 0 || c.n_kv_heads <= 0 || c.ffn_dim <= 0 || c.vocab < 2 ||
       c.max_streams < 1 || c.max_context < 1 || c.max_prefill < 0) {
     why = "non-positive dimension in config";
@@ -116,8 +134,10 @@ int* step_err_word(const hh_config& g, const StepWords& w) {
 // Bytes of a matrix's 4-bit codes as operand tiles (its scales follow them).
 size_t q4_tile_codes(size_t rows, size_t K) { return (rows + 15) / 16 * 16 * K / 2; }
 
-Layout make_layout(const hh_config& c) {
+Layout make_layout(const hh_config& asked) {
+  const hh_config c = without_kv(asked);
   Layout L{};
+  L.kv4 = wants_kv4(asked);
   const bool bf = c.dtype == HH_BF16;
   L.ew = bf ? 2 : 4;
   L.ekv = bf ? 2 : 4;
@@ -204,7 +224,8 @@ Layout make_layout(const hh_config& c) {
   }
   L.final_norm = take(d * 4);
   L.rope = take((size_t)c.max_context * 32 * sizeof(float2));
-  L.kv = take((size_t)c.n_layers * L.n_pages * 2 * c.n_kv_heads * kPage * 64 * L.ekv);
+  L.page_bytes = L.kv4 ? (size_t)c.n_kv_heads * kKv4Block : (size_t)2 * c.n_kv_heads * kPage * 64 * L.ekv;
+  L.kv = take((size_t)c.n_layers * L.n_pages * L.page_bytes);
   L.page_table = take((size_t)c.max_streams * L.max_pages * 4);
   L.pos = take((size_t)c.max_streams * 4);
   L.pending = take((size_t)c.max_streams * 4);
@@ -244,6 +265,13 @@ Layout make_layout(const hh_config& c) {
   L.split = take(2 * sr * d * 2);
   L.row_scale = take(sr * 4);
   L.nrm_ss = take((size_t)32 * (d / 64) * 4);
+  L.compact = take(compact_workspace(L.n_pages));
+  L.lengths = take((size_t)c.max_streams * 4);
+  if (L.kv4) {
+    L.qkv32 = take(R * L.nqkv * 4);
+    L.seqs = take((3 * (size_t)c.max_streams + 1) * 4);
+    L.kv4_work = take(kKv4Work);
+  }
   L.total = off;
   return L;
 }
@@ -287,8 +315,13 @@ struct hh_ctx {
   std::vector<int> len;
   std::vector<std::vector<int>> pages;
   std::vector<int> free_pages;
+  std::vector<int> refs;  // streams that hold a page
+  // Whether a position's argmax is recorded (last rows of prompts, decode
+  // steps), and whether the stream's pending token is one of them.
+  std::vector<std::vector<unsigned char>> recorded;
+  std::vector<char> pending_known;
   std::vector<int> uploaded_streams;  // row_stream contents last uploaded for decode
-  std::map<std::tuple<int, int, int>, hipGraphExec_t> graphs;
+  std::map<std::tuple<int, int, int, int>, hipGraphExec_t> graphs;
 
   template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(arena + off); }
   hh_status fail(hh_status s, const std::string& m) {
@@ -339,6 +372,27 @@ WTiles head_tiles(const hh_ctx* c) {
 
 KvLayout kv_layout(const hh_ctx* c) { return KvLayout{c->L.n_pages, c->cfg.n_kv_heads, c->L.max_pages}; }
 
+// What a pass over rows of a 4-bit cache needs: the cache (layer 0), the rows'
+// sequences on the device, and how their attention is cut up.
+struct Kv4Pass {
+  Kv4Pool pool;
+  Kv4Rows rows;
+  Kv4Plan plan;
+};
+
+// n_seqs sequences of up to max_rows rows, n_rows in all, over up to `pages`
+// pages; starts null: one row each.
+Kv4Pass kv4_pass(const hh_ctx* c, int n_seqs, int n_rows, int max_rows, const int* starts, const int* first_pos,
+                 const int* streams, int pages) {
+  const Layout& L = c->L;
+  Kv4Pass p;
+  p.pool = Kv4Pool{c->at<unsigned char>(L.kv), c->at<int>(L.page_table), L.n_pages, c->cfg.n_kv_heads, L.max_pages,
+                   c->cfg.max_streams};
+  p.rows = Kv4Rows{starts, first_pos, streams, n_seqs, n_rows, max_rows};
+  p.plan = kv4_plan(p.pool, p.rows, c->cfg.n_heads, std::min(pages, L.max_pages), kKv4Work);
+  return p;
+}
+
 // Enqueue the transformer layers + head for n rows whose bookkeeping
 // (row_stream, row_pos, x) has been prepared.  decode_gemv: batch-1 weight
 // streaming path; otherwise the MFMA GEMM path.  s_max: attention splits
@@ -348,7 +402,7 @@ KvLayout kv_layout(const hh_ctx* c) { return KvLayout{c->L.n_pages, c->cfg.n_kv_
 // query-block pairs are in L.items.
 template <typename TW, typename TKV, typename TM>
 void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row, float* logits,
-                    int prefill_stream = -1, int prefill_pos = 0, int n_items = 0) {
+                    int prefill_stream = -1, int prefill_pos = 0, int n_items = 0, const Kv4Pass* pass = nullptr) {
   using DK = DecodeKernels<TW, TKV, TM>;
   using GK = GemmKernels<TM, TKV>;
   const hh_config& g = c->cfg;
@@ -372,8 +426,9 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
   // reads it (RowNorm); `pending`: h holds x * gain and the row sums of
   // squares are in nrm_ss, not yet applied.  (For prompt rows the large-tile
   // kernels' arrival chain cost as much as the norm pass it replaced.)
+  // (4-bit caches take the QKV product's rows whole, without such a scale.)
   const bool rnorm = sizeof(TM) == 2 && !decode_gemv && prefill_stream < 0 && head_row == -1 &&
-                     L.tiled && GK::norm_fusable(d) && d % 256 == 0 && d <= 2048 && c->row_norm;
+                     !L.kv4 && L.tiled && GK::norm_fusable(d) && d % 256 == 0 && d <= 2048 && c->row_norm;
   float* nss = rnorm ? c->at<float>(L.nrm_ss) : nullptr;
   int* ncnt = rnorm ? c->at<int>(L.nrm_cnt) : nullptr;
   RowNorm rn_use;
@@ -401,7 +456,7 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
       if (!fuse) DK::rmsnorm_rows(st, n, x, an, eps, d, h);
       else if (l == 0) GK::rmsnorm(st, n, x, d, an, eps, h);
       // Prefill rows of one stream with an fp16 cache use MFMA flash attention.
-      const bool flash = prefill_stream >= 0 && sizeof(TKV) == 2 &&
+      const bool flash = !L.kv4 && prefill_stream >= 0 && sizeof(TKV) == 2 &&
                          flash_prefill_supported(hq / hkv, c->cfg.max_context,
                                                  (size_t)kl.n_pages * 2 * hkv * kPage * kHeadDim);
       // Flash attention reads only the fp16 queries.
@@ -417,7 +472,30 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
       // over the QKV split-K reduction, rotation and KV append.
       const bool fold = prefill_stream < 0 && head_row == -1;
       QkvFold<TKV> qf;
-      if (fold) {
+      if (L.kv4) {
+        // The product's rows in fp32 (it adds, so they start at zero); keys are
+        // rotated and quantized as they go into their pages, queries rotated as
+        // the attention reads them.
+        float* rows = c->at<float>(L.qkv32);
+        zero_floats(st, rows, (size_t)n * L.nqkv);
+        GK::resid(st, gws, h, n, c->at<TM>(L.wqkvM[l]), d, L.nqkv, ws, rows, nullptr, 0.f, nullptr, tq);
+        Kv4Pool pool = pass->pool;
+        pool.pool += (size_t)l * L.n_pages * L.page_bytes;
+        const RopeTable rt{rope, g.max_context};
+        (void)kv4_append(st, pool, pass->rows, rows + hq * 64, rows + (hq + hkv) * 64, kRowF32, L.nqkv, L.nqkv, rt);
+        Kv4Attend a{};
+        a.q = rows;
+        a.out = oM;
+        a.q_stride = L.nqkv;
+        a.out_stride = hq * 64;
+        a.q_type = kRowF32;
+        a.out_type = sizeof(TM) == 2 ? kRowF16 : kRowF32;
+        a.hq = hq;
+        a.scale = 0.125f;
+        a.rope = rt;
+        a.part = c->at<float>(L.kv4_work);
+        (void)kv4_attend(st, pool, pass->rows, a, pass->plan);
+      } else if (fold) {
         const int sp = GK::qkv_deferred(st, gws, h, n, c->at<TM>(L.wqkvM[l]), d, hq, hkv, ws, rs, rp, rope, q, kv, kl, l,
                                         pt, tq,
                                         pending ? rn_use : RowNorm());
@@ -426,7 +504,9 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
         GK::qkv(st, gws, h, n, c->at<TM>(L.wqkvM[l]), d, hq, hkv, ws, rs, rp, rope, flash ? nullptr : q,
                 flash ? c->at<TM>(L.qM) : nullptr, kv, kl, l, pt, tq);
       }
-      if (flash) {
+      if (L.kv4) {
+        // (attended above)
+      } else if (flash) {
         if constexpr (sizeof(TKV) == 2)
           flash_prefill(st, reinterpret_cast<const _Float16*>(c->at<TM>(L.qM)), reinterpret_cast<const _Float16*>(kv),
                         kl, l, pt, prefill_stream, prefill_pos, n, hq, hkv, reinterpret_cast<_Float16*>(oM));
@@ -477,8 +557,9 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
 }
 
 // One decode step for n rows (row_stream already on the device).
+// pages: a bound of the rows' cached pages (how a 4-bit cache's attention is cut up).
 template <typename TW, typename TKV, typename TM>
-void enqueue_decode(hh_ctx* c, int n, bool feed, bool want_logits) {
+void enqueue_decode(hh_ctx* c, int n, bool feed, bool want_logits, int pages) {
   const Layout& L = c->L;
   using DK = DecodeKernels<TW, TKV, TM>;
   DK::prep_embed(c->stream, n, -1, feed ? c->at<int>(L.feed) : nullptr, c->at<int>(L.row_stream),
@@ -486,8 +567,11 @@ void enqueue_decode(hh_ctx* c, int n, bool feed, bool want_logits) {
                  c->at<unsigned long long>(L.slot), c->at<TW>(L.embed), c->at<float>(L.x), c->cfg.d_model);
   // The batch-1 GEMV kernels read the model's own (bf16) matrices, which a
   // 4-bit model does not compute with: it takes the MFMA path at one row.
-  const bool gemv = n == 1 && c->cfg.weight_format == HH_WF_DTYPE;
-  enqueue_layers<TW, TKV, TM>(c, n, gemv, kSplitMax, -1, want_logits ? c->at<float>(L.logits) : nullptr);
+  // So do steps on a 4-bit cache, which those kernels do not read.
+  const bool gemv = n == 1 && c->cfg.weight_format == HH_WF_DTYPE && !L.kv4;
+  Kv4Pass pass{};
+  if (L.kv4) pass = kv4_pass(c, n, n, 1, nullptr, c->at<int>(L.row_pos), c->at<int>(L.row_stream), pages);
+  enqueue_layers<TW, TKV, TM>(c, n, gemv, kSplitMax, -1, want_logits ? c->at<float>(L.logits) : nullptr, -1, 0, 0, &pass);
   finalize(c->stream, 0, n, c->at<int>(L.row_stream), c->at<int>(L.row_pos), c->at<unsigned long long>(L.slot),
            c->at<int>(L.pending), c->at<int>(L.hist), c->at<int>(L.pos), c->cfg.max_context);
 }
@@ -546,6 +630,7 @@ hipError_t setup_step_tables_q4(hh_ctx* c) {
 }
 
 hipError_t setup_step_kernel(hh_ctx* c) {
+  if (c->L.kv4) return hipSuccess;  // it reads fp16 and fp32 caches
   if (c->cfg.dtype == HH_BF16) {
     if (c->cfg.weight_format == HH_WF_Q4G32) {
       // Without the 4-bit kernel (other shapes) the fp16 one streams the
@@ -616,21 +701,39 @@ hh_status launch_step(hh_ctx* c, int s, bool feed, bool want_logits, const StepW
   return HH_OK;
 }
 
+// A free page, held by one stream.
+int take_page(hh_ctx* c) {
+  const int p = c->free_pages.back();
+  c->free_pages.pop_back();
+  c->refs[p] = 1;
+  return p;
+}
+// One stream less holds page p.
+void drop_page(hh_ctx* c, int p) {
+  if (--c->refs[p] == 0) c->free_pages.push_back(p);
+}
+
 // Make sure stream s owns pages for positions [0, new_len); upload new entries.
+// (The page that holds the stream's last position, if it is not full, is the
+// stream's alone: hh_fork and hh_truncate copy such a page.)
 hh_status ensure_pages(hh_ctx* c, int s, int new_len) {
   const int need = (new_len + kPage - 1) / kPage;
   std::vector<int>& pg = c->pages[s];
   const int first_new = (int)pg.size();
   if (need <= first_new) return HH_OK;
   if ((int)c->free_pages.size() < need - first_new) return c->fail(HH_ERR_CONTEXT_FULL, "KV page pool exhausted");
-  for (int i = first_new; i < need; ++i) {
-    pg.push_back(c->free_pages.back());
-    c->free_pages.pop_back();
-  }
+  for (int i = first_new; i < need; ++i) pg.push_back(take_page(c));
   int* dst = c->at<int>(c->L.page_table) + (size_t)s * c->L.max_pages + first_new;
   put_ints(c->stream, dst, pg.data() + first_new, need - first_new);
   HIPCHK(c, hipGetLastError());
   return HH_OK;
+}
+
+// n more positions of stream s, the last one's argmax recorded and pending.
+void note_rows(hh_ctx* c, int s, int n) {
+  c->recorded[s].resize(c->recorded[s].size() + n, 0);
+  c->recorded[s].back() = 1;
+  c->pending_known[s] = 1;
 }
 
 // LM head + greedy key of row `row` of x into logits (optional) and the
@@ -723,7 +826,14 @@ hh_status do_prefill(hh_ctx* c, int s, const int32_t* tokens, int n, int mode, f
     DK::prep_embed(st, P, s, c->at<int>(L.feed), c->at<int>(L.row_stream), c->at<int>(L.row_pos), c->at<int>(L.pos),
                    c->at<int>(L.pending), c->at<unsigned long long>(L.slot), c->at<TW>(L.embed), c->at<float>(L.x),
                    c->cfg.d_model);
-    enqueue_layers<TW, TKV, TM>(c, P, false, 1, -2, nullptr, s, c->len[s] + r0);
+    Kv4Pass pass{};
+    if (L.kv4) {
+      const int starts[2] = {0, P};
+      put_ints(st, c->at<int>(L.seqs), starts, 2);
+      pass = kv4_pass(c, 1, P, P, c->at<int>(L.seqs), c->at<int>(L.row_pos), c->at<int>(L.row_stream),
+                      (c->len[s] + r0 + P + kPage - 1) / kPage);
+    }
+    enqueue_layers<TW, TKV, TM>(c, P, false, 1, -2, nullptr, s, c->len[s] + r0, 0, &pass);
     unsigned long long* slot = c->at<unsigned long long>(L.slot);
     if (mode == HH_LOGITS_ALL) {
       // Device memory of this GPU is written directly, anything else through
@@ -749,6 +859,7 @@ hh_status do_prefill(hh_ctx* c, int s, const int32_t* tokens, int n, int mode, f
   }
   if (next) HIPCHK(c, hipMemcpyAsync(next, c->at<int>(L.pending) + s, sizeof(int), hipMemcpyDefault, st));
   c->len[s] += n;
+  note_rows(c, s, n);
   return HH_OK;
 }
 
@@ -806,7 +917,7 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
     // fp16 caches: MFMA attention over each stream's rows where it is the
     // faster one (flash_packed_wins).
     std::vector<FlashItem> items;
-    if (sizeof(TKV) == 2 &&
+    if (sizeof(TKV) == 2 && !L.kv4 &&
         flash_prefill_supported(g.n_heads / g.n_kv_heads, g.max_context,
                                 (size_t)L.n_pages * 2 * g.n_kv_heads * kPage * kHeadDim)) {
       PackedRows pr;
@@ -833,7 +944,28 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
     HIPCHK(c, hipMemcpyAsync(c->at<int>(L.feed), tk.data(), R * sizeof(int), hipMemcpyHostToDevice, st));
     DK::prep_embed(st, R, -2, c->at<int>(L.feed), row_stream, row_pos, c->at<int>(L.pos), c->at<int>(L.pending),
                    slot, c->at<TW>(L.embed), x, d);
-    enqueue_layers<TW, TKV, TM>(c, R, false, 1, -2, nullptr, -1, 0, (int)items.size());
+    Kv4Pass pass{};
+    if (L.kv4) {
+      std::vector<int> starts, first, streams;
+      int most = 1, keys = 1;
+      for (int r = 0; r < R; ++r) {
+        if (r == 0 || rs[r] != rs[r - 1]) {
+          starts.push_back(r);
+          first.push_back(rp[r]);
+          streams.push_back(rs[r]);
+        }
+        most = std::max(most, r + 1 - starts.back());
+        keys = std::max(keys, rp[r] + 1);
+      }
+      const int ns = (int)starts.size();
+      starts.push_back(R);
+      int* seqs = c->at<int>(L.seqs);
+      put_ints(st, seqs, starts.data(), ns + 1);
+      put_ints(st, seqs + ns + 1, first.data(), ns);
+      put_ints(st, seqs + 2 * ns + 1, streams.data(), ns);
+      pass = kv4_pass(c, ns, R, most, seqs, seqs + ns + 1, seqs + 2 * ns + 1, (keys + kPage - 1) / kPage);
+    }
+    enqueue_layers<TW, TKV, TM>(c, R, false, 1, -2, nullptr, -1, 0, (int)items.size(), &pass);
     if (ne > 0) {
       // The streams whose last row the pass held: norm of those rows into
       // rows 0 .. ne - 1 of h, then the head and argmax.
@@ -863,7 +995,10 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
   if (next)
     for (int i = 0; i < n; ++i)
       HIPCHK(c, hipMemcpyAsync(next + i, c->at<int>(L.pending) + ids[i], sizeof(int), hipMemcpyDefault, st));
-  for (int i = 0; i < n; ++i) c->len[ids[i]] += lens[i];
+  for (int i = 0; i < n; ++i) {
+    c->len[ids[i]] += lens[i];
+    note_rows(c, ids[i], lens[i]);
+  }
   return HH_OK;
 }
 
@@ -888,6 +1023,14 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
     HIPCHK(c, hipGetLastError());
   }
   const bool want_logits = logits != nullptr;
+  // A 4-bit cache's attention is cut up for the longest stream's pages, in
+  // powers of two (a graph for each).
+  int pages = 0;
+  if (L.kv4) {
+    int longest = 1;
+    for (int i = 0; i < n; ++i) longest = std::max(longest, c->len[ids[i]] + 1);
+    for (pages = 1; pages * kPage < longest;) pages *= 2;
+  }
   if (n == 1 && (c->step_wg > 0 || words)) {
     // Each step owns 512 epochs (8 phases x 64 layers); epoch 0 is never
     // used, so zero-initialised exchange words never look current.
@@ -906,12 +1049,12 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
       rc = launch_step<TM, TKV>(c, ids[0], tokens != nullptr, want_logits, w);
     if (rc != HH_OK) return rc;
   } else if (c->use_graphs) {
-    auto key = std::make_tuple(n, tokens != nullptr ? 1 : 0, want_logits ? 1 : 0);
+    auto key = std::make_tuple(n, tokens != nullptr ? 1 : 0, want_logits ? 1 : 0, pages);
     auto it = c->graphs.find(key);
     if (it == c->graphs.end()) {
       hipGraph_t graph;
       HIPCHK(c, hipStreamBeginCapture(st, hipStreamCaptureModeRelaxed));
-      enqueue_decode<TW, TKV, TM>(c, n, tokens != nullptr, want_logits);
+      enqueue_decode<TW, TKV, TM>(c, n, tokens != nullptr, want_logits, pages);
       hipError_t e = hipStreamEndCapture(st, &graph);
       if (e != hipSuccess) return c->hip_fail(e, "hipStreamEndCapture");
       hipGraphExec_t exec;
@@ -922,7 +1065,7 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
     }
     HIPCHK(c, hipGraphLaunch(it->second, st));
   } else {
-    enqueue_decode<TW, TKV, TM>(c, n, tokens != nullptr, want_logits);
+    enqueue_decode<TW, TKV, TM>(c, n, tokens != nullptr, want_logits, pages);
     HIPCHK(c, hipGetLastError());
   }
   if (logits)
@@ -939,7 +1082,10 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
         HIPCHK(c, hipMemcpyAsync(next + i, c->at<int>(L.pending) + ids[i], sizeof(int), hipMemcpyDefault, st));
     }
   }
-  for (int i = 0; i < n; ++i) c->len[ids[i]] += 1;
+  for (int i = 0; i < n; ++i) {
+    c->len[ids[i]] += 1;
+    note_rows(c, ids[i], 1);
+  }
   return HH_OK;
 }
 
@@ -947,9 +1093,11 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
 // zero in one launch (the decode-step kernel's error word with clear_error).
 hh_status reset_range(hh_ctx* c, int s0, int n, bool clear_error) {
   for (int s = s0; s < s0 + n; ++s) {
-    for (int p : c->pages[s]) c->free_pages.push_back(p);
+    for (int p : c->pages[s]) drop_page(c, p);
     c->pages[s].clear();
     c->len[s] = 0;
+    c->recorded[s].clear();
+    c->pending_known[s] = 0;
   }
   int* err = clear_error && c->step_wg > 0 ? reinterpret_cast<int*>(c->at<unsigned long long>(c->L.ll) + c->L.ll_words - 8) : nullptr;
   HIPCHK(c, reset_streams(c->stream, s0, n, c->at<int>(c->L.pos), c->at<int>(c->L.pending),
@@ -1030,7 +1178,7 @@ hh_status hh_create(const hh_config* cfg, void* arena, size_t arena_bytes, void*
   Layout L = make_layout(*cfg);
   if (arena_bytes < L.total) return HH_ERR_OOM;
   hh_ctx* c = new hh_ctx();
-  c->cfg = *cfg;
+  c->cfg = without_kv(*cfg);
   c->L = L;
   c->arena = static_cast<char*>(arena);
   c->stream = static_cast<hipStream_t>(hip_stream);
@@ -1050,6 +1198,9 @@ hh_status hh_create(const hh_config* cfg, void* arena, size_t arena_bytes, void*
   c->row_norm = !(rne && rne[0] == '0');
   c->len.assign(cfg->max_streams, 0);
   c->pages.assign(cfg->max_streams, {});
+  c->refs.assign(L.n_pages, 0);
+  c->recorded.assign(cfg->max_streams, {});
+  c->pending_known.assign(cfg->max_streams, 0);
   for (int p = L.n_pages - 1; p >= 0; --p) c->free_pages.push_back(p);
   // RoPE table: angle p * theta^(-2i/64) in fp64, cos/sin rounded to fp32.
   std::vector<float2> rope((size_t)cfg->max_context * 32);
@@ -1267,6 +1418,8 @@ hh_status hh_decode_step(hh_ctx* c, int32_t n, const int32_t* stream_ids, const 
     seen[ids[i]] = 1;
     if (c->len[ids[i]] + 1 > g.max_context) return c->fail(HH_ERR_CONTEXT_FULL, "stream at max_context");
     if (!tokens && c->len[ids[i]] == 0) return c->fail(HH_ERR_INVALID_ARG, "empty stream needs an explicit token");
+    if (!tokens && !c->pending_known[ids[i]])
+      return c->fail(HH_ERR_INVALID_ARG, "no argmax was recorded where the stream was cut: it needs an explicit token");
     if (tokens && (tokens[i] < 0 || tokens[i] >= g.vocab))
       return c->fail(HH_ERR_INVALID_ARG, "token id out of range");
   }
@@ -1300,6 +1453,8 @@ hh_status hh_decode_step_noalloc(hh_ctx* c, int32_t s, const int32_t* token, flo
     return c->fail(HH_ERR_INVALID_ARG, "the context's device is not the current device");
   if (c->len[s] + 1 > g.max_context) return c->fail(HH_ERR_CONTEXT_FULL, "stream at max_context");
   if (!token && c->len[s] == 0) return c->fail(HH_ERR_INVALID_ARG, "empty stream needs an explicit token");
+  if (!token && !c->pending_known[s])
+    return c->fail(HH_ERR_INVALID_ARG, "no argmax was recorded where the stream was cut: it needs an explicit token");
   if (token && (*token < 0 || *token >= g.vocab)) return c->fail(HH_ERR_INVALID_ARG, "token id out of range");
   const int have = (int)c->pages[s].size();
   if ((c->len[s] + 1 + kPage - 1) / kPage > have && c->free_pages.empty())
@@ -1335,6 +1490,137 @@ hh_status hh_reset(hh_ctx* c, int32_t s) {
   // The error word goes with any reset: later steps run again (a stream that
   // recorded -1 keeps it as its pending token until its own reset).
   return s == -1 ? reset_range(c, 0, c->cfg.max_streams, true) : reset_range(c, s, 1, true);
+}
+
+hh_status hh_fork(hh_ctx* c, int32_t src, int32_t n, const int32_t* dst) {
+  if (!c) return HH_ERR_INVALID_ARG;
+  const hh_config& g = c->cfg;
+  const Layout& L = c->L;
+  if (src < 0 || src >= g.max_streams || n < 1 || n >= g.max_streams || !dst)
+    return c->fail(HH_ERR_INVALID_ARG, "need a source and 1..max_streams - 1 streams to fork it to");
+  try {
+    std::vector<char> seen(g.max_streams, 0);
+    seen[src] = 1;
+    for (int i = 0; i < n; ++i) {
+      if (dst[i] < 0 || dst[i] >= g.max_streams) return c->fail(HH_ERR_INVALID_ARG, "stream id out of range");
+      if (seen[dst[i]]) return c->fail(HH_ERR_INVALID_ARG, "stream listed twice, or the source");
+      seen[dst[i]] = 1;
+    }
+    // Full pages are shared; a partly filled last page is copied, since its
+    // stream goes on writing to it.  (There is a free page for each copy: a
+    // stream never has more than its share of the pool.)
+    const int len = c->len[src], full = len / kPage;
+    const bool part = len % kPage != 0;
+    const std::vector<int> shared(c->pages[src].begin(), c->pages[src].begin() + full);
+    std::vector<int> from, to, ids(dst, dst + n);
+    from.reserve(n);
+    to.reserve(n);
+    for (int i = 0; i < n; ++i) {
+      c->pages[dst[i]].reserve(full + 1);
+      c->recorded[dst[i]].reserve(len);
+    }
+    for (int i = 0; i < n; ++i) {
+      const int s = dst[i];
+      for (int p : c->pages[s]) drop_page(c, p);
+      c->pages[s].assign(shared.begin(), shared.end());
+      for (int p : shared) ++c->refs[p];
+      c->recorded[s] = c->recorded[src];
+      c->pending_known[s] = c->pending_known[src];
+      c->len[s] = len;
+    }
+    for (int i = 0; i < n && part; ++i) {
+      from.push_back(c->pages[src][full]);
+      to.push_back(take_page(c));
+      c->pages[dst[i]].push_back(to.back());
+    }
+    const PagePool pool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes, g.n_layers,
+                        L.n_pages};
+    if (part && g.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, n, from.data(), to.data()));
+    HIPCHK(c, fork_streams(c->stream, src, n, ids.data(), part ? to.data() : nullptr, len, g.max_context, L.max_pages,
+                           c->at<int>(L.page_table), c->at<int>(L.pos), c->at<int>(L.pending),
+                           c->at<unsigned long long>(L.slot), c->at<int>(L.hist)));
+  } catch (const std::bad_alloc&) {
+    return HH_ERR_OOM;
+  }
+  return HH_OK;
+}
+
+hh_status hh_truncate(hh_ctx* c, int32_t s, int32_t length) {
+  if (!c) return HH_ERR_INVALID_ARG;
+  const Layout& L = c->L;
+  if (s < 0 || s >= c->cfg.max_streams) return c->fail(HH_ERR_INVALID_ARG, "stream id out of range");
+  if (length < 0 || length > c->len[s]) return c->fail(HH_ERR_INVALID_ARG, "length outside the stream");
+  if (length == 0) return reset_range(c, s, 1, false);
+  if (length == c->len[s]) return HH_OK;
+  std::vector<int>& pg = c->pages[s];
+  const int keep = (length + kPage - 1) / kPage;
+  while ((int)pg.size() > keep) {
+    drop_page(c, pg.back());
+    pg.pop_back();
+  }
+  c->len[s] = length;
+  c->recorded[s].resize(length);
+  c->pending_known[s] = c->recorded[s].back();
+  // The page that the stream writes next must be its own.  (Another stream
+  // holds it too, so a page is free.)
+  if (length % kPage != 0 && c->refs[pg.back()] > 1) {
+    const int from = pg.back(), to = take_page(c);
+    const PagePool pool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes,
+                        c->cfg.n_layers, L.n_pages};
+    drop_page(c, from);
+    pg.back() = to;
+    if (c->cfg.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, 1, &from, &to));
+    put_ints(c->stream, c->at<int>(L.page_table) + (size_t)s * L.max_pages + keep - 1, &to, 1);
+    HIPCHK(c, hipGetLastError());
+  }
+  HIPCHK(c, truncate_stream(c->stream, s, length, c->cfg.max_context, c->at<int>(L.pos), c->at<int>(L.pending),
+                            c->at<int>(L.hist)));
+  return HH_OK;
+}
+
+hh_status hh_compact(hh_ctx* c, int32_t* pages_in_use) {
+  if (!c) return HH_ERR_INVALID_ARG;
+  const hh_config& g = c->cfg;
+  const Layout& L = c->L;
+  if (L.n_pages > kMaxCompactPages) return c->fail(HH_ERR_UNSUPPORTED, "compaction takes at most 2^20 pages");
+  try {
+    // Pages that a stream holds beyond its length (a call that failed for want
+    // of pages) go back first: the device goes by the lengths.
+    for (int s = 0; s < g.max_streams; ++s)
+      while ((int)c->pages[s].size() > (c->len[s] + kPage - 1) / kPage) {
+        drop_page(c, c->pages[s].back());
+        c->pages[s].pop_back();
+      }
+    // The device's rule, mirrored: live pages behind their count, in order, to
+    // the free ones before it.
+    int live = 0;
+    for (int r : c->refs) live += r > 0;
+    std::vector<int> to(L.n_pages), refs(L.n_pages, 0), spare;
+    spare.reserve(L.n_pages);
+    int hole = 0;
+    for (int p = 0; p < L.n_pages; ++p) {
+      to[p] = p;
+      if (p < live || c->refs[p] == 0) continue;
+      while (c->refs[hole] > 0) ++hole;
+      to[p] = hole++;
+    }
+    for (int p = L.n_pages - 1; p >= live; --p) spare.push_back(p);
+    const PagePool pool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes, g.n_layers,
+                        L.n_pages};
+    put_ints(c->stream, c->at<int>(L.lengths), c->len.data(), g.max_streams);
+    HIPCHK(c, hipGetLastError());
+    HIPCHK(c, compact_pages(c->stream, pool, c->at<int>(L.page_table), g.max_streams, L.max_pages, c->at<int>(L.lengths),
+                            c->at<int>(L.scratch_u32), c->at<int>(L.compact)));
+    for (int p = 0; p < L.n_pages; ++p) refs[to[p]] += c->refs[p];
+    for (auto& pg : c->pages)
+      for (int& p : pg) p = to[p];
+    c->refs.swap(refs);
+    c->free_pages.swap(spare);
+    if (pages_in_use) *pages_in_use = live;
+  } catch (const std::bad_alloc&) {
+    return HH_ERR_OOM;
+  }
+  return HH_OK;
 }
 
 hh_status hh_stream_length(const hh_ctx* c, int32_t s, int32_t* length) {

@@ -22,13 +22,14 @@ HH_ERR_NOT_LOADED, HH_ERR_HIP, HH_ERR_UNSUPPORTED = -4, -5, -6
 HH_F32, HH_BF16, HH_F16 = 0, 1, 2
 HH_LOGITS_NONE, HH_LOGITS_LAST, HH_LOGITS_ALL = 0, 1, 2
 HH_WF_DTYPE, HH_WF_Q4G32 = 0, 1
+HH_KV_Q4 = 0x100  # added to a weight format: 4-bit KV cache
 
 EXPORTED = ["hh_workspace_size", "hh_create", "hh_load_weights", "hh_prefill", "hh_prefill_batch", "hh_decode_step",
             "hh_decode_step_noalloc", "hh_reset", "hh_stream_length", "hh_read_argmax", "hh_destroy", "hh_last_error",
             "hh_q4g32_quantize", "hh_router_create", "hh_router_query", "hh_router_route",
             "hh_router_size", "hh_router_destroy", "hh_render_marker", "hh_read_probe",
             "hh_kv4_append", "hh_kv4_read", "hh_kv4_attention_workspace", "hh_kv4_attention", "hh_kv_copy_pages",
-            "hh_kv_compact_workspace", "hh_kv_compact"]
+            "hh_kv_compact_workspace", "hh_kv_compact", "hh_fork", "hh_truncate", "hh_compact"]
 
 
 class hh_config(ctypes.Structure):
@@ -77,6 +78,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "hh_prefill_batch": ([c_void_p, c_int32, i32p, i32p, i32p, c_void_p], c_int32),
         "hh_decode_step_noalloc": ([c_void_p, c_int32, i32p, c_void_p, c_void_p], c_int32),
         "hh_reset": ([c_void_p, c_int32], c_int32),
+        "hh_fork": ([c_void_p, c_int32, c_int32, i32p], c_int32),
+        "hh_truncate": ([c_void_p, c_int32, c_int32], c_int32),
+        "hh_compact": ([c_void_p, i32p], c_int32),
         "hh_stream_length": ([c_void_p, c_int32, i32p], c_int32),
         "hh_read_argmax": ([c_void_p, c_int32, c_int32, c_int32, i32p], c_int32),
         "hh_destroy": ([c_void_p], None),
@@ -161,6 +165,21 @@ def hh_decode_step_noalloc(ctx: int, stream_id: int, token, logits_ptr, next_ptr
 
 def hh_reset(ctx: int, stream_id: int) -> None:
     _check(ctx, load_library().hh_reset(ctx, stream_id))
+
+
+def hh_fork(ctx: int, src: int, dst) -> None:
+    dst = np.ascontiguousarray(dst, dtype=np.int32)
+    _check(ctx, load_library().hh_fork(ctx, src, len(dst), dst.ctypes.data_as(POINTER(c_int32))))
+
+
+def hh_truncate(ctx: int, stream_id: int, length: int) -> None:
+    _check(ctx, load_library().hh_truncate(ctx, stream_id, length))
+
+
+def hh_compact(ctx: int) -> int:
+    n = c_int32()
+    _check(ctx, load_library().hh_compact(ctx, byref(n)))
+    return n.value
 
 
 def hh_stream_length(ctx: int, stream_id: int) -> int:
@@ -299,7 +318,8 @@ def _check(ctx, status: int) -> None:
 
 def make_config(shape, max_streams: int, max_context: int, max_prefill: int = 0,
                 weight_format: int = 0) -> hh_config:
-    """hh_config from a model-shape object (attributes as in synth.ModelShape)."""
+    """hh_config from a model-shape object (attributes as in synth.ModelShape);
+    weight_format: HH_WF_DTYPE or HH_WF_Q4G32, + HH_KV_Q4 for a 4-bit KV cache."""
     return hh_config(shape.n_layers, shape.d_model, shape.n_heads, shape.n_kv_heads, shape.head_dim,
                      shape.ffn_dim, shape.vocab, shape.rms_eps, shape.rope_theta, int(shape.tied),
                      int(shape.dtype), max_streams, max_context, 16, max_prefill, weight_format)
@@ -354,6 +374,17 @@ class Context:
         hh_decode_step(self.ctx, n, stream_ids, tokens, None if buf is None else buf.ctypes.data,
                        None if nxt is None else nxt.ctypes.data)
         return nxt, buf
+
+    def fork(self, src: int, dst) -> None:
+        """Streams dst become copies of stream src (full pages shared)."""
+        hh_fork(self.ctx, src, dst)
+
+    def truncate(self, stream_id: int, length: int) -> None:
+        hh_truncate(self.ctx, stream_id, length)
+
+    def compact(self) -> int:
+        """KV pages in use, moved to the lowest page ids."""
+        return hh_compact(self.ctx)
 
     def reset(self, stream_id: int = -1) -> None:
         hh_reset(self.ctx, stream_id)

@@ -187,3 +187,29 @@ def test_compaction_refuses():
     refused(hh.hh_kv_compact, *{**ok, "pages": (1 << 20) + 1, "n": 1 << 40}.values(), None, status=hh.HH_ERR_UNSUPPORTED)
     refused(hh.hh_kv_compact_workspace, 0)
     refused(hh.hh_kv_compact_workspace, (1 << 20) + 1, status=hh.HH_ERR_UNSUPPORTED)
+
+
+# ------------------------------------------------------------------ contexts with a 4-bit cache
+
+def test_cache_format_in_the_config():
+    import synth
+    for f in (0, hh.HH_WF_Q4G32):
+        n, c = 4, 4096
+        sizes = [hh.hh_workspace_size(hh.make_config(synth.ONE_B, n, c, 512, weight_format=f + k)) for k in (0, hh.HH_KV_Q4)]
+        sh = synth.ONE_B
+        kv = n * c * sh.n_layers * sh.n_kv_heads
+        extra = 512 * (sh.q_dim + 2 * sh.kv_dim) * 4 + (16 << 20)  # the pass's fp32 rows and split outputs
+        assert abs(sizes[0] - sizes[1] - (kv * (256 - 72) - extra)) < 4096
+    for bad in (hh.HH_KV_Q4 + 2, 0x200, -1, hh.HH_KV_Q4 + hh.HH_WF_Q4G32):
+        cfg = hh.make_config(synth.TINY, 2, 128, weight_format=bad)
+        with pytest.raises(hh.HHError) as e:
+            hh.hh_workspace_size(cfg)
+        assert e.value.status == hh.HH_ERR_UNSUPPORTED
+    assert hh.hh_workspace_size(hh.make_config(synth.TINY, 2, 128, weight_format=hh.HH_KV_Q4)) > 0
+
+
+def test_stream_calls_without_a_context():
+    lib = hh.load_library()
+    assert lib.hh_fork(None, 0, 1, None) == hh.HH_ERR_INVALID_ARG
+    assert lib.hh_truncate(None, 0, 0) == hh.HH_ERR_INVALID_ARG
+    assert lib.hh_compact(None, None) == hh.HH_ERR_INVALID_ARG
