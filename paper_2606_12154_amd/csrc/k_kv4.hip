@@ -41,18 +41,36 @@ struct Seq {
 
 // The sequence's rows, kept inside the buffers whatever the device arrays say.
 __device__ __forceinline__ Seq load_seq(const Kv4Pool& P, const Kv4Rows& R, int s) {
+  // (Every pointer read, whether given or not, so that the loads go out together.)
+  const int* starts = (R.row_start ? R.row_start : R.first_pos) + s;
+  const int* rows = (R.table_row ? R.table_row : R.first_pos) + s;
+  const int first = R.first_pos[s], a0 = starts[0], b0 = starts[R.row_start ? 1 : 0], row = rows[0];
+  const int a = R.row_start ? a0 : s, b = R.row_start ? b0 : s + 1;
   Seq q;
-  const int a = R.row_start ? R.row_start[s] : s, b = R.row_start ? R.row_start[s + 1] : s + 1;
   q.row0 = min(max(a, 0), R.n_rows);
   q.n = min(max(min(max(b, 0), R.n_rows) - q.row0, 0), R.max_rows);
-  q.first = max(min(R.first_pos[s], 1 << 30), -(1 << 30));
-  q.trow = R.table_row ? R.table_row[s] : s;
+  q.first = max(min(first, 1 << 30), -(1 << 30));
+  q.trow = R.table_row ? row : s;
   // No such table row: every position is padding.
   if (q.trow < 0 || q.trow >= P.table_rows) {
     q.trow = 0;
     q.first = -(1 << 30);
   }
   return q;
+}
+
+// x / d as a product (x < 2^31): the multiplier is 2^(31 + s) / d rounded up, s the
+// least with 2^s >= d, so it is off by less than 2^s / d of 2^-31.
+struct Div {
+  unsigned mul, shift, d;
+};
+Div div_by(unsigned d) {
+  unsigned s = 0;
+  while ((1u << s) < d) ++s;
+  return Div{(unsigned)((((uint64_t)1 << (31 + s)) + d - 1) / d), s, d};
+}
+__device__ __forceinline__ unsigned operator/(unsigned x, Div v) {
+  return (unsigned)(((uint64_t)x * v.mul) >> 31 >> v.shift);
 }
 
 __device__ __forceinline__ const unsigned char* block_of(const Kv4Pool& P, const int* row, int page, int head) {
@@ -451,24 +469,21 @@ constexpr float kOffset = 7.f, kSlack = 8.f;
 // 16-bit query and two hold 22 bits of an fp32 one.
 template <int NQ, int QT, int PT, int WK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4 : NQ == 2 ? 3 : 2))) void
-k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
+k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  unsigned b = blockIdx.x;
-  const int head = b % (unsigned)P.hkv;
-  b /= (unsigned)P.hkv;
-  const int split = b % (unsigned)splits;
-  b /= (unsigned)splits;
+  const unsigned b1 = blockIdx.x / heads, b2 = b1 / splits_, sq = b2 / tiles_;
+  const int head = blockIdx.x - b1 * heads.d, split = b1 - b2 * splits_.d, splits = splits_.d;
   // The last tiles have the most keys: they go first.
-  const int tile = tiles - 1 - (int)(b % (unsigned)tiles);
-  const Seq s = load_seq(P, R, b / (unsigned)tiles);
-  const int G = A.hq / P.hkv;
+  const int tile = tiles_.d - 1 - (b2 - sq * tiles_.d);
+  const Seq s = load_seq(P, R, sq);
+  const int G = group.d;
   const int cols = s.n * G;  // below 2^31 with a tile to spare (kv4_plan)
   const int c0 = (tile * (WK == 1 ? 4 : 1) + (WK == 1 ? wave : 0)) * (16 * NQ);
   if (c0 >= cols) return;
   // Keys of the tile's first and last row.
   const int most = P.max_pages * kPage;
-  const int row_a = c0 / G, row_b = (min(c0 + 16 * NQ, cols) - 1) / G;
+  const int row_a = (unsigned)c0 / group, row_b = (unsigned)(min(c0 + 16 * NQ, cols) - 1) / group;
   const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
   const int np = (some_see + kPage - 1) / kPage;
   const int per = split_pages(np, splits);
@@ -499,7 +514,7 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   RawRow raw[NQ];
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
-    const int c = min(c0 + 16 * t + r, cols - 1), rw = c / G, j = c - rw * G;
+    const int c = min(c0 + 16 * t + r, cols - 1), rw = (unsigned)c / group, j = c - rw * G;
     const size_t at = (size_t)(s.row0 + rw) * A.q_stride + (head * G + j) * 64 + 8 * g;
     load_raw(raw[t], A.q, at, at + 32, A.q_type);
   }
@@ -517,7 +532,7 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   for (int t = 0; t < NQ; ++t) {
     const int cc = c0 + 16 * t + r;
     const bool real = cc < cols;
-    const int pos = s.first + min(cc, cols - 1) / G;
+    const int pos = s.first + (int)((unsigned)min(cc, cols - 1) / group);
     lim[t] = real ? min(max(pos + 1, 0), most) : 0;
     float x[16];
     raw_values(raw[t], A.q_type, x);
@@ -713,7 +728,8 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tiles, int splits) {
   auto put = [&](int col, int d0, auto n_const, const float* x, float l, float m) {
     constexpr int N = decltype(n_const)::value;
     if (col >= cols) return;
-    const int rw = s.row0 + col / G, hd = head * G + col % G;
+    const int at_row = (unsigned)col / group;
+    const int rw = s.row0 + at_row, hd = head * G + col - at_row * G;
     if (joined) {
       const size_t at = ((size_t)split * R.n_rows + rw) * A.hq + hd;
       float* dst = A.part + at * 64 + d0;
@@ -897,13 +913,14 @@ __global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4
 template <int NQ, int QT, int PT>
 void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
+  const Div heads = div_by(P.hkv), splits = div_by(p.splits), tiles = div_by(p.tiles), group = div_by(A.hq / P.hkv);
   if constexpr (NQ == 4) {
     if (p.wk == 1) {
-      k_kv4_attend<NQ, QT, PT, 1><<<groups, 256, 0, st>>>(P, R, A, p.tiles, p.splits);
+      k_kv4_attend<NQ, QT, PT, 1><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
       return;
     }
   }
-  k_kv4_attend<NQ, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, p.tiles, p.splits);
+  k_kv4_attend<NQ, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
 }
 
 template <int QT, int PT>
