@@ -401,8 +401,8 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
 /* ------------------------------------------------------------------------
  * Pages of any paged cache: n_layers pools of n_pages pages of page_bytes, a
  * pool every layer_stride bytes from `pool` (device, 16-byte aligned;
- * page_bytes and layer_stride multiples of 16; layer_stride at least
- * n_pages * page_bytes where there are several layers).  Streams, devices and
+ * page_bytes and layer_stride multiples of 16, page_bytes at most 64 MiB;
+ * layer_stride at least n_pages * page_bytes where there are several layers).  Streams, devices and
  * captures as above.
  * ------------------------------------------------------------------------ */
 

@@ -67,7 +67,8 @@ struct PagePool {
   int64_t layer_stride, bytes;
   int n_layers, n_pages;
 };
-hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst);
+// once: no page is the source of two copies.
+hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst, bool once);
 constexpr int kMaxCompactPages = 1 << 20;  // one bit each in LDS: 128 KiB
 size_t compact_workspace(int n_pages);
 hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int table_rows, int max_pages,

@@ -9,21 +9,31 @@
 namespace hh {
 namespace {
 
-// Copies go in pieces of 4 KiB, one a wave (four 16-byte loads a lane in
-// flight); pieces of a page are whole but for its last.
-constexpr int kPiece = 4096;
+// Copies go in pieces of 2 KiB, one a wave (two 16-byte loads a lane in flight);
+// pieces of a page are whole but for its last.  What bounds them is memory:
+// written lines are not kept in the caches (63 copies of one 512 KiB page: 8.4 ->
+// 7.1 us), and where pages are read once and are too many for the caches,
+// neither are read ones (1,500 pages of 147 KB: 95.5 -> 92.6 us, 4.8 TB/s of
+// reads and writes; a large plain copy reaches 5.0).  Pieces of 4 KiB took 0.8 us
+// more, of 8 KiB half as long again.
+constexpr int kPiece = 2048;
+constexpr int64_t kCached = (int64_t)64 << 20;  // bytes that may still be in the caches
 
+template <bool ONCE>
 __device__ __forceinline__ void copy_piece(const unsigned char* __restrict__ src, unsigned char* __restrict__ dst,
                                            int64_t bytes, int piece) {
   const int lane = threadIdx.x & 63;
   const int64_t off = (int64_t)piece * kPiece + lane * 16;
-  u32x4 v[4];
+  u32x4 v[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (off + i * 1024 < bytes) v[i] = *reinterpret_cast<const u32x4*>(src + off + i * 1024);
+  for (int i = 0; i < 2; ++i)
+    if (off + i * 1024 < bytes) {
+      const u32x4* p = reinterpret_cast<const u32x4*>(src + off + i * 1024);
+      v[i] = ONCE ? __builtin_nontemporal_load(p) : *p;
+    }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (off + i * 1024 < bytes) *reinterpret_cast<u32x4*>(dst + off + i * 1024) = v[i];
+  for (int i = 0; i < 2; ++i)
+    if (off + i * 1024 < bytes) __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4*>(dst + off + i * 1024));
 }
 
 // Pairs travel as kernel arguments (at most 4 KiB of them a launch).
@@ -33,6 +43,7 @@ struct PairArgs {
   int src[kPairs], dst[kPairs];
 };
 
+template <bool ONCE>
 __global__ __launch_bounds__(256) void k_copy_pages(PagePool P, int pieces, PairArgs a) {
   int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int piece = (int)(w % pieces);
@@ -40,7 +51,7 @@ __global__ __launch_bounds__(256) void k_copy_pages(PagePool P, int pieces, Pair
   const int pair = (int)(w % a.n), layer = (int)(w / a.n);
   if (layer >= P.n_layers) return;
   unsigned char* base = P.pool + layer * P.layer_stride;
-  copy_piece(base + a.src[pair] * P.bytes, base + a.dst[pair] * P.bytes, P.bytes, piece);
+  copy_piece<ONCE>(base + a.src[pair] * P.bytes, base + a.dst[pair] * P.bytes, P.bytes, piece);
 }
 
 // ------------------------------------------------------------------ compaction
@@ -122,6 +133,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(int n_pages, cons
 }
 
 // The first move_groups workgroups copy, the others rewrite the page tables.
+template <bool ONCE>
 __global__ __launch_bounds__(256) void k_compact_move(PagePool P, int pieces, const int* __restrict__ moves,
                                                       int move_groups, int* __restrict__ table, int rows,
                                                       int max_pages, const int* __restrict__ lengths,
@@ -137,7 +149,7 @@ __global__ __launch_bounds__(256) void k_compact_move(PagePool P, int pieces, co
       const int64_t rest = w / pieces;
       const int i = (int)(rest % n), layer = (int)(rest / n);
       unsigned char* base = P.pool + layer * P.layer_stride;
-      copy_piece(base + src[i] * P.bytes, base + dst[i] * P.bytes, P.bytes, (int)(w % pieces));
+      copy_piece<ONCE>(base + src[i] * P.bytes, base + dst[i] * P.bytes, P.bytes, (int)(w % pieces));
     }
     return;
   }
@@ -197,7 +209,8 @@ int pieces_of(const PagePool& P) { return (int)((P.bytes + kPiece - 1) / kPiece)
 
 }  // namespace
 
-hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst) {
+hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst, bool once) {
+  once = once && n * P.bytes * P.n_layers > kCached;
   const int pieces = pieces_of(P);
   // Pairs of a launch, so that its workgroups stay within a grid.
   const int64_t each = (int64_t)pieces * P.n_layers;
@@ -209,7 +222,9 @@ hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, 
       a.src[i] = src[o + i];
       a.dst[i] = dst[o + i];
     }
-    k_copy_pages<<<(unsigned)((a.n * each + 3) / 4), 256, 0, st>>>(P, pieces, a);
+    const unsigned groups = (unsigned)((a.n * each + 3) / 4);
+    if (once) k_copy_pages<true><<<groups, 256, 0, st>>>(P, pieces, a);
+    else k_copy_pages<false><<<groups, 256, 0, st>>>(P, pieces, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -236,8 +251,12 @@ hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int tabl
   const int64_t most = ((int64_t)P.n_pages / 2 + 1) * pieces * P.n_layers;
   const int move_groups = (int)std::min<int64_t>((most + 3) / 4, 2048);
   const int table_groups = std::min(table_rows, 256);
-  k_compact_move<<<move_groups + table_groups, 256, 0, st>>>(P, pieces, moves, move_groups, table, table_rows,
-                                                             max_pages, lengths, live);
+  const unsigned all = move_groups + table_groups;
+  // (Their number is known to the device alone: half of the pool at most.)
+  if (P.n_pages / 2 * P.bytes * P.n_layers > kCached)
+    k_compact_move<true><<<all, 256, 0, st>>>(P, pieces, moves, move_groups, table, table_rows, max_pages, lengths, live);
+  else
+    k_compact_move<false><<<all, 256, 0, st>>>(P, pieces, moves, move_groups, table, table_rows, max_pages, lengths, live);
   return hipGetLastError();
 }
 

@@ -56,7 +56,7 @@ bool rope_table(const float* rope, int32_t len, RopeTable* t) {
 
 bool page_pool(void* pool, int32_t n_layers, int64_t layer_stride, int64_t page_bytes, int32_t n_pages, PagePool* P) {
   if (!aligned(pool, 16) || n_layers < 1 || n_layers > 1 << 16 || n_pages < 1 || page_bytes < 16 ||
-      page_bytes > (int64_t)1 << 30 || page_bytes % 16 != 0)
+      page_bytes > (int64_t)1 << 26 || page_bytes % 16 != 0 || (double)page_bytes * n_pages * n_layers > 0x1p60)
     return false;
   if (n_layers > 1 && (layer_stride % 16 != 0 || layer_stride < page_bytes * n_pages)) return false;
   *P = PagePool{static_cast<unsigned char*>(pool), n_layers > 1 ? layer_stride : 0, page_bytes, n_layers, n_pages};
@@ -153,10 +153,14 @@ hh_status hh_kv_copy_pages(void* pool, int32_t n_layers, int64_t layer_stride, i
     if (seen[dst[i]]) return HH_ERR_INVALID_ARG;
     seen[dst[i]] = 1;
   }
-  for (int32_t i = 0; i < n; ++i)
-    if (seen[src[i]]) return HH_ERR_INVALID_ARG;
+  bool once = true;
+  for (int32_t i = 0; i < n; ++i) {
+    if (seen[src[i]] == 1) return HH_ERR_INVALID_ARG;
+    once = once && seen[src[i]] == 0;
+    seen[src[i]] = 2;
+  }
   if (n == 0) return HH_OK;
-  return from_hip(copy_pages(static_cast<hipStream_t>(hip_stream), P, n, src, dst));
+  return from_hip(copy_pages(static_cast<hipStream_t>(hip_stream), P, n, src, dst, once));
 }
 
 hh_status hh_kv_compact_workspace(int32_t n_pages, size_t* bytes) {

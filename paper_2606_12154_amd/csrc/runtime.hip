@@ -1535,7 +1535,7 @@ hh_status hh_fork(hh_ctx* c, int32_t src, int32_t n, const int32_t* dst) {
     }
     const PagePool pool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes, g.n_layers,
                         L.n_pages};
-    if (part && g.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, n, from.data(), to.data()));
+    if (part && g.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, n, from.data(), to.data(), false));
     HIPCHK(c, fork_streams(c->stream, src, n, ids.data(), part ? to.data() : nullptr, len, g.max_context, L.max_pages,
                            c->at<int>(L.page_table), c->at<int>(L.pos), c->at<int>(L.pending),
                            c->at<unsigned long long>(L.slot), c->at<int>(L.hist)));
@@ -1569,7 +1569,7 @@ hh_status hh_truncate(hh_ctx* c, int32_t s, int32_t length) {
                         c->cfg.n_layers, L.n_pages};
     drop_page(c, from);
     pg.back() = to;
-    if (c->cfg.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, 1, &from, &to));
+    if (c->cfg.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, 1, &from, &to, false));
     put_ints(c->stream, c->at<int>(L.page_table) + (size_t)s * L.max_pages + keep - 1, &to, 1);
     HIPCHK(c, hipGetLastError());
   }
