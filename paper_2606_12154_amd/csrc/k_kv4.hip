@@ -28,6 +28,7 @@ namespace hh {
 namespace {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kKeyScales = 1024, kValueScales = 1088;  // byte offsets in a block
@@ -381,6 +382,8 @@ int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
 // Operand columns are (row, query head of the kv head's group) pairs, row-major:
 // column c of a sequence is row c / G, head c % G.
 constexpr int kMaxSplits = 64;
+constexpr int kRowsTile = 256;  // columns of a workgroup of k_kv4_attend_rows
+constexpr int kRowsNq = 4;
 
 // Workspace of s splits: 64 dimensions, base and sum of weights each.
 size_t split_bytes(int s, int64_t outputs) { return (size_t)s * (size_t)outputs * (64 + 2) * sizeof(float); }
@@ -413,10 +416,11 @@ int splits_for(int nq, int64_t groups, int pages, int64_t outputs, size_t most_b
   return best;
 }
 
-// Pages of a split, given the pages that a column tile attends to.
-__device__ __forceinline__ int split_pages(int np, int splits) {
-  const int pairs = (np + 1) >> 1;
-  return 2 * ((pairs + splits - 1) / splits);
+// Pages of a split, given the pages that a column tile attends to, in units that
+// a workgroup takes at a time.
+__device__ __forceinline__ int split_pages(int np, int splits, int unit) {
+  const int units = (np + unit - 1) / unit;
+  return unit * ((units + splits - 1) / splits);
 }
 
 struct PageRegs {
@@ -438,24 +442,72 @@ __device__ __forceinline__ f16x2 codes16(unsigned w, unsigned mask) {
   const unsigned x = J < 2 ? w << (6 - 4 * J) : w >> (4 * J - 6);
   return __builtin_bit_cast(f16x2, (x & mask) | 0x4c004c00u);
 }
-
-__device__ __forceinline__ f16x8 join8(f16x2 a, f16x2 b, f16x2 c, f16x2 d) {
-  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+__device__ __forceinline__ unsigned code_mask() {
+  unsigned m;
+  asm("v_mov_b32 %0, 0x03c003c0" : "=v"(m));
+  return m;
 }
 
-// 8 keys' elements of one dword under one scale.
-__device__ __forceinline__ f16x8 key_frag(unsigned w, unsigned mask, f16x2 s, f16x2 b) {
-  return join8(__builtin_elementwise_fma(codes16<0>(w, mask), s, b), __builtin_elementwise_fma(codes16<1>(w, mask), s, b),
-               __builtin_elementwise_fma(codes16<2>(w, mask), s, b), __builtin_elementwise_fma(codes16<3>(w, mask), s, b));
+__device__ __forceinline__ f16x2 minus24(f16x2 s) { return s * f16x2{(_Float16)-24, (_Float16)-24}; }
+
+// The lane's 8 keys' elements of one dword under one scale.
+__device__ __forceinline__ f16x8 key_frag(unsigned w, unsigned mask, f16x2 s) {
+  const f16x2 b = minus24(s);
+  const f16x2 x0 = __builtin_elementwise_fma(codes16<0>(w, mask), s, b), x1 = __builtin_elementwise_fma(codes16<1>(w, mask), s, b);
+  const f16x2 x2 = __builtin_elementwise_fma(codes16<2>(w, mask), s, b), x3 = __builtin_elementwise_fma(codes16<3>(w, mask), s, b);
+  return f16x8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
 }
 
-// Dimension 4 r + J of the lane's 4 slots in each of two pages.
+// Dimension 4 r + J of the lane's 4 slots; s, b: their scales, and -24 times.
 template <int J>
-__device__ __forceinline__ f16x8 value_frag(u32x2 wa, u32x2 wb, unsigned mask, const f16x2* s, const f16x2* b) {
-  return join8(__builtin_elementwise_fma(codes16<J>(wa[0], mask), s[0], b[0]),
-               __builtin_elementwise_fma(codes16<J>(wa[1], mask), s[1], b[1]),
-               __builtin_elementwise_fma(codes16<J>(wb[0], mask), s[2], b[2]),
-               __builtin_elementwise_fma(codes16<J>(wb[1], mask), s[3], b[3]));
+__device__ __forceinline__ f16x4 value_frag(u32x2 w, unsigned mask, const f16x2* s, const f16x2* b) {
+  const f16x2 lo = __builtin_elementwise_fma(codes16<J>(w[0], mask), s[0], b[0]);
+  const f16x2 hi = __builtin_elementwise_fma(codes16<J>(w[1], mask), s[1], b[1]);
+  return f16x4{lo[0], lo[1], hi[0], hi[1]};
+}
+
+// A page's operands: keys, and values.  MASK: values that no row of the tile sees
+// (slots from `seen` on) may be anything, and a NaN that only some rows see must
+// not reach the others as 0 x NaN: such values become 0, and bit i of `bad` says that
+// the lane's value slot i is NaN, which then goes through the scores.
+__device__ __forceinline__ void keys_of(u32x2 k, unsigned scales, unsigned mask, f16x8* kf) {
+  const f16x2 s = __builtin_bit_cast(f16x2, scales);
+  const unsigned k0 = k[0], k1 = k[1];
+  kf[0] = key_frag(k0, mask, f16x2{s[0], s[0]});
+  kf[1] = key_frag(k1, mask, f16x2{s[1], s[1]});
+}
+template <bool MASK>
+__device__ __forceinline__ void values_of(u32x2 v, u32x2 scales, unsigned mask, int page, int seen, f16x4* vf,
+                                          unsigned* bad) {
+  f16x2 s[2], b[2];
+  unsigned nan4 = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    unsigned w = scales[h];
+    if constexpr (MASK) {
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int slot = page * kPage + 4 * (int)((threadIdx.x & 63) >> 4) + 2 * h + z;
+        const bool nan = ((w >> (16 * z)) & 0x7c00u) == 0x7c00u;
+        if (nan || slot >= seen) w &= z ? 0x0000ffffu : 0xffff0000u;
+        if (nan) nan4 |= 1u << (2 * h + z);
+      }
+    }
+    s[h] = __builtin_bit_cast(f16x2, w);
+    b[h] = minus24(s[h]);
+  }
+  if constexpr (MASK) {
+    // Either group of a value row may hold the NaN: lanes r and r ^ 8.
+    *bad = nan4 | (unsigned)__shfl_xor((int)nan4, 8, 64);
+  }
+  vf[0] = value_frag<0>(v, mask, s, b);
+  vf[1] = value_frag<1>(v, mask, s, b);
+  vf[2] = value_frag<2>(v, mask, s, b);
+  vf[3] = value_frag<3>(v, mask, s, b);
+}
+
+__device__ __forceinline__ f16x8 join8(f16x4 a, f16x4 b) {
+  return f16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
 // Weights are 2^(S qs - base): base puts a column's largest score so far at
@@ -464,191 +516,122 @@ __device__ __forceinline__ f16x8 value_frag(u32x2 wa, u32x2 wb, unsigned mask, c
 // leaves the step without reductions across lanes.
 constexpr float kOffset = 7.f, kSlack = 8.f;
 
-// QT, PT: fp16 terms of queries and of weights.  Queries are scaled by a power of
-// two that puts a row's largest element into [2^13, 2^14), so that one term holds any
-// 16-bit query and two hold 22 bits of an fp32 one.
-template <int NQ, int QT, int PT, int WK>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4 : NQ == 2 ? 3 : 2))) void
-k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 15, g = lane >> 4;
-  const unsigned b1 = blockIdx.x / heads, b2 = b1 / splits_, sq = b2 / tiles_;
-  const int head = blockIdx.x - b1 * heads.d, split = b1 - b2 * splits_.d, splits = splits_.d;
-  // The last tiles have the most keys: they go first.
-  const int tile = tiles_.d - 1 - (b2 - sq * tiles_.d);
-  const Seq s = load_seq(P, R, sq);
-  const int G = group.d;
-  const int cols = s.n * G;  // below 2^31 with a tile to spare (kv4_plan)
-  const int c0 = (tile * (WK == 1 ? 4 : 1) + (WK == 1 ? wave : 0)) * (16 * NQ);
-  if (c0 >= cols) return;
-  // Keys of the tile's first and last row.
-  const int most = P.max_pages * kPage;
-  const int row_a = (unsigned)c0 / group, row_b = (unsigned)(min(c0 + 16 * NQ, cols) - 1) / group;
-  const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
-  const int np = (some_see + kPage - 1) / kPage;
-  const int per = split_pages(np, splits);
-  const int p0 = split * per, p1 = min(p0 + per, np);
-  const bool joined = per < np;  // several splits have keys
-  if (split > 0 && p0 >= np) return;
+// Where a wave stands: columns c0 .. c0 + 16 NQ - 1 of one (sequence, kv head).
+struct Place {
+  Seq s;
+  int head, G, cols, c0;
+  Div group;
+};
 
-  // ---- what the first step needs goes out before the queries are worked on
-  const int* row = P.table + (size_t)s.trow * P.max_pages;
-  constexpr int STEP = WK == 1 ? 2 : 8;
-  int p = p0 + (WK == 1 ? 0 : 2 * wave);
-  // Loads run one step ahead, page ids two; what would lie behind the wave's
-  // last step is its last step again (no branch around loads, whose waits would
-  // then have to assume that it was not taken).
-  const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
-  auto ids = [&](int q, unsigned* id) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const unsigned x = (unsigned)row[max(min(min(q, last) + i, np - 1), 0)];
-      id[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
-    }
-  };
-  auto fetch = [&](PageRegs* pr, const unsigned* id) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      load_page(pr[i], P.pool + ((size_t)id[i] * (unsigned)P.hkv + (unsigned)head) * kKv4Block, (unsigned)lane);
-  };
-  RawRow raw[NQ];
-#pragma unroll
-  for (int t = 0; t < NQ; ++t) {
-    const int c = min(c0 + 16 * t + r, cols - 1), rw = (unsigned)c / group, j = c - rw * G;
-    const size_t at = (size_t)(s.row0 + rw) * A.q_stride + (head * G + j) * 64 + 8 * g;
-    load_raw(raw[t], A.q, at, at + 32, A.q_type);
-  }
-  PageRegs a[2], c[2];
-  unsigned id[2];
-  ids(p, id);
-  fetch(a, id);
-  ids(p + STEP, id);
-
-  // ---- queries
+// A wave's NQ tiles of 16 columns.  QT, PT: fp16 terms of queries and of weights.
+// Queries (but for fp16 ones) are scaled by a power of two that puts a row's
+// largest element into [2^13, 2^14), so that one term holds any 16-bit query
+// and two hold 22 bits of an fp32 one.
+template <int NQ, int QT, int PT>
+struct Columns {
   f16x8 qh[NQ][2], ql[QT == 2 ? NQ : 1][2];
   float qs[NQ];  // scores to powers of two
   int lim[NQ];   // keys that the column sees
-#pragma unroll
-  for (int t = 0; t < NQ; ++t) {
-    const int cc = c0 + 16 * t + r;
-    const bool real = cc < cols;
-    const int pos = s.first + (int)((unsigned)min(cc, cols - 1) / group);
-    lim[t] = real ? min(max(pos + 1, 0), most) : 0;
-    float x[16];
-    raw_values(raw[t], A.q_type, x);
-    if (A.rope.at) {
-      const f32x4* cs = reinterpret_cast<const f32x4*>(A.rope.at + (size_t)min(max(pos, 0), A.rope.len - 1) * 32 + 8 * g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 w = cs[i];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float u = x[2 * i + e], v = x[8 + 2 * i + e], co = w[2 * e], si = w[2 * e + 1];
-          x[2 * i + e] = u * co - v * si;
-          x[8 + 2 * i + e] = v * co + u * si;
-        }
-      }
-    }
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    int e = 0;
-    if (top > 0.f && top < INFINITY) e = 14 - __builtin_amdgcn_frexp_expf(top);
-    qs[t] = fmaxf(__builtin_amdgcn_ldexpf(A.scale * 1.4426950408889634f, -e), 1e-37f);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float y = real ? __builtin_amdgcn_ldexpf(x[i], e) : 0.f;
-      const _Float16 h = (_Float16)y;
-      qh[t][i >> 3][i & 7] = h;
-      if constexpr (QT == 2) ql[t][i >> 3][i & 7] = (_Float16)(y - (float)h);
-    }
-  }
-
-  // ---- keys and values
   f32x4 o[NQ][4], sum[NQ];
   float base[NQ];
-#pragma unroll
-  for (int t = 0; t < NQ; ++t) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    base[t] = 0.f;
-  }
-  const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
-  const f16x2 m24 = {(_Float16)-24, (_Float16)-24};
-  unsigned mask;
-  asm("v_mov_b32 %0, 0x03c003c0" : "=v"(mask));
-  bool first = true;
+  bool first;
 
-  auto step = [&](const PageRegs* pr, int p, auto masked) {
-    constexpr bool MASK = decltype(masked)::value;
-    f16x8 kf[2][2];
-    f16x2 vsc[4], vbi[4];
-    unsigned nan4 = 0;  // MASK: the lane's 8 value slots whose scale is NaN
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const f16x2 sc = __builtin_bit_cast(f16x2, pr[i].ks);
-      const f16x2 s0 = {sc[0], sc[0]}, s1 = {sc[1], sc[1]};
-      kf[i][0] = key_frag(pr[i].k[0], mask, s0, s0 * m24);
-      kf[i][1] = key_frag(pr[i].k[1], mask, s1, s1 * m24);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        unsigned w = pr[i].vs[h];
-        if constexpr (MASK) {
-          // Values that no row of the tile sees may be anything; a NaN that
-          // only some rows see must not reach the others as 0 x NaN, so it
-          // goes through the scores.
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const int slot = (p + i) * kPage + 4 * g + 2 * h + z;
-            const unsigned bits = w >> (16 * z) & 0xffffu;
-            const bool bad = (bits & 0x7c00u) == 0x7c00u;
-            if (bad || slot >= some_see) w &= z ? 0x0000ffffu : 0xffff0000u;
-            if (bad) nan4 |= 1u << (4 * i + 2 * h + z);
-          }
-        }
-        const f16x2 sv = __builtin_bit_cast(f16x2, w);
-        vsc[2 * i + h] = sv;
-        vbi[2 * i + h] = sv * m24;
-      }
-    }
-    if constexpr (MASK) {
-      // Either group of a value row may hold the NaN: lanes r and r ^ 8.
-      nan4 |= (unsigned)__shfl_xor((int)nan4, 8, 64);
-    }
-    f16x8 vf[4];
-    vf[0] = value_frag<0>(pr[0].v, pr[1].v, mask, vsc, vbi);
-    vf[1] = value_frag<1>(pr[0].v, pr[1].v, mask, vsc, vbi);
-    vf[2] = value_frag<2>(pr[0].v, pr[1].v, mask, vsc, vbi);
-    vf[3] = value_frag<3>(pr[0].v, pr[1].v, mask, vsc, vbi);
-    // Scores of all columns first: the check below is the step's only branch, so
-    // products and exponentials of different columns can overlap around it.
-    float x[NQ][8], high = -INFINITY;
+  // Columns behind the last one repeat it (and are not written).
+  static __device__ __forceinline__ void load(RawRow* raw, const Place& w, const Kv4Attend& A) {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
-      f32x4 sc[2];
+      const int c = min(w.c0 + 16 * t + r, w.cols - 1), rw = (unsigned)c / w.group, j = c - rw * w.G;
+      const size_t at = (size_t)(w.s.row0 + rw) * A.q_stride + (w.head * w.G + j) * 64 + 8 * g;
+      load_raw(raw[t], A.q, at, at + 32, A.q_type);
+    }
+  }
+
+  __device__ __forceinline__ void start(const RawRow* raw, const Place& w, const Kv4Attend& A, int most) {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    first = true;
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      base[t] = 0.f;
+      const int pos = w.s.first + (int)((unsigned)min(w.c0 + 16 * t + r, w.cols - 1) / w.group);
+      lim[t] = min(max(pos + 1, 0), most);
+      if (QT == 1 && A.q_type == kRowF16 && !A.rope.at) {
+        qh[t][0] = __builtin_bit_cast(f16x8, raw[t].w[0]);
+        qh[t][1] = __builtin_bit_cast(f16x8, raw[t].w[1]);
+        qs[t] = fmaxf(A.scale * 1.4426950408889634f, 1e-37f);
+        continue;
+      }
+      float x[16];
+      raw_values(raw[t], A.q_type, x);
+      if (A.rope.at) {
+        const f32x4* cs = reinterpret_cast<const f32x4*>(A.rope.at + (size_t)min(max(pos, 0), A.rope.len - 1) * 32 + 8 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 cw = cs[i];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float u = x[2 * i + e], v = x[8 + 2 * i + e], co = cw[2 * e], si = cw[2 * e + 1];
+            x[2 * i + e] = u * co - v * si;
+            x[8 + 2 * i + e] = v * co + u * si;
+          }
+        }
+      }
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      int e = 0;
+      if (top > 0.f && top < INFINITY) e = 14 - __builtin_amdgcn_frexp_expf(top);
+      qs[t] = fmaxf(__builtin_amdgcn_ldexpf(A.scale * 1.4426950408889634f, -e), 1e-37f);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = __builtin_amdgcn_ldexpf(x[i], e);
+        const _Float16 h = (_Float16)y;
+        qh[t][i >> 3][i & 7] = h;
+        if constexpr (QT == 2) ql[t][i >> 3][i & 7] = (_Float16)(y - (float)h);
+      }
+    }
+  }
+
+  // A step takes two pages: their scores, the scores' weights, the weighted values.
+
+  // kf[page][half of the dimensions].
+  __device__ __forceinline__ void scores(const f16x8 (*kf)[2], f32x4 (*sc)[2]) const {
+#pragma unroll
+    for (int t = 0; t < NQ; ++t)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        sc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         if constexpr (QT == 2) {
-          sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], ql[t][0], sc[i], 0, 0, 0);
-          sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], ql[t][1], sc[i], 0, 0, 0);
+          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], ql[t][0], sc[t][i], 0, 0, 0);
+          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], ql[t][1], sc[t][i], 0, 0, 0);
         }
-        sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], qh[t][0], sc[i], 0, 0, 0);
-        sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], qh[t][1], sc[i], 0, 0, 0);
+        sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], qh[t][0], sc[t][i], 0, 0, 0);
+        sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], qh[t][1], sc[t][i], 0, 0, 0);
       }
+  }
+
+  // MASK: slots past a column's keys, and bad (8 bits, see values_of).  The check
+  // of all columns' scores is the step's only branch.
+  template <bool MASK>
+  __device__ __forceinline__ void weights(const f32x4 (*sc)[2], int page, unsigned bad, f16x8* ph, f16x8* pl) {
+    const int g = (threadIdx.x & 63) >> 4;
+    float x[NQ][8], high = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < NQ; ++t)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[t][i] = fmaf(sc[i >> 2][i & 3], qs[t], -base[t]);
+        x[t][i] = fmaf(sc[t][i >> 2][i & 3], qs[t], -base[t]);
         if constexpr (MASK) {
-          if (nan4 >> i & 1u) x[t][i] = NAN;
-          if ((p + (i >> 2)) * kPage + 4 * g + (i & 3) >= lim[t]) x[t][i] = -INFINITY;
+          if (bad >> i & 1u) x[t][i] = NAN;
+          if ((page + (i >> 2)) * kPage + 4 * g + (i & 3) >= lim[t]) x[t][i] = -INFINITY;
         }
         high = fmaxf(high, x[t][i]);
       }
-    }
     // A wave's first pages set the base: a column that sees none of them sees
     // none of the later ones either.
     if (first || __builtin_amdgcn_ballot_w64(high > kOffset + kSlack)) {
@@ -670,36 +653,145 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
         sum[t] *= f;
       }
     }
+    first = false;
 #pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      f16x8 ph, pl;
+    for (int t = 0; t < NQ; ++t)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float w = __builtin_amdgcn_exp2f(x[t][i]);
         const _Float16 h = (_Float16)w;
-        ph[i] = h;
-        if constexpr (PT == 2) pl[i] = (_Float16)(w - (float)h);
+        ph[t][i] = h;
+        if constexpr (PT == 2) pl[t][i] = (_Float16)(w - (float)h);
       }
+  }
+
+  // vf[dimension of four].  Weights are summed as they enter the products.
+  __device__ __forceinline__ void values(const f16x8* vf, const f16x8* ph, const f16x8* pl) {
+    const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
       if constexpr (PT == 2) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], pl, o[t][j], 0, 0, 0);
-        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl, sum[t], 0, 0, 0);
+        for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], pl[t], o[t][j], 0, 0, 0);
+        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl[t], sum[t], 0, 0, 0);
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], ph, o[t][j], 0, 0, 0);
-      // Weights are summed as they enter the products.
-      sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph, sum[t], 0, 0, 0);
+      for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], ph[t], o[t][j], 0, 0, 0);
+      sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph[t], sum[t], 0, 0, 0);
     }
-    first = false;
-  };
+  }
 
+  // A column that saw no key has no base.
+  __device__ __forceinline__ float base_of(int t) const { return sum[t][0] == 0.f ? -INFINITY : base[t]; }
+};
+
+// N consecutive dimensions of column col, from d0 on: the output, or (joined)
+// the split's part of it, with base m and sum of weights l.
+template <int N>
+__device__ __forceinline__ void put(const Kv4Rows& R, const Kv4Attend& A, const Place& w, int col, int d0, const float* x,
+                                    float l, float m, bool joined, int split, int splits) {
+  if (col >= w.cols) return;
+  const int at_row = (unsigned)col / w.group;
+  const int rw = w.s.row0 + at_row, hd = w.head * w.G + col - at_row * w.G;
+  if (joined) {
+    const size_t at = ((size_t)split * R.n_rows + rw) * A.hq + hd;
+    float* dst = A.part + at * 64 + d0;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      *reinterpret_cast<f32x4*>(dst + 4 * i) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+    if (d0 == 0) {
+      float2* ml = reinterpret_cast<float2*>(A.part + (size_t)splits * R.n_rows * A.hq * 64) + at;
+      *ml = make_float2(m, l);
+    }
+    return;
+  }
+  float y[N];
+  const float inv = l == 0.f ? 0.f : 1.0f / l;  // nothing to attend to: 0
+#pragma unroll
+  for (int i = 0; i < N; ++i) y[i] = x[i] * inv;
+  store_row<N>(A.out, (size_t)rw * A.out_stride + hd * 64 + d0, A.out_type, y);
+}
+
+// Few columns: a workgroup has one tile of 16 NQ of them, and its four waves
+// take the tile's keys in turn (two pages a step) and join at the end.
+template <int NQ, int QT, int PT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4 : NQ == 2 ? 3 : 2))) void
+k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const unsigned b1 = blockIdx.x / heads, b2 = b1 / splits_, sq = b2 / tiles_;
+  const int split = b1 - b2 * splits_.d, splits = splits_.d;
+  // The last tiles have the most keys: they go first.
+  const int tile = tiles_.d - 1 - (b2 - sq * tiles_.d);
+  const Seq s = load_seq(P, R, sq);
+  const int G = group.d, cols = s.n * G;  // below 2^31 with a tile to spare (kv4_plan)
+  const Place w{s, (int)(blockIdx.x - b1 * heads.d), G, cols, tile * (16 * NQ), group};
+  if (w.c0 >= cols) return;
+  // Keys of the tile's first and last row.
+  const int most = P.max_pages * kPage;
+  const int row_a = (unsigned)w.c0 / group, row_b = (unsigned)(min(w.c0 + 16 * NQ, cols) - 1) / group;
+  const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
+  const int np = (some_see + kPage - 1) / kPage;
+  const int per = split_pages(np, splits, 2);
+  const int p0 = split * per, p1 = min(p0 + per, np);
+  const bool joined = per < np;  // several splits have keys
+  if (split > 0 && p0 >= np) return;
+
+  // What the first step needs goes out before the queries are worked on.  Loads
+  // run one step ahead, page ids two; what would lie behind the wave's last
+  // step is its last step again (no branch around loads, whose waits would then have to
+  // assume that it was not taken).
+  const int* row = P.table + (size_t)s.trow * P.max_pages;
+  constexpr int STEP = 8;
+  int p = p0 + 2 * wave;
+  const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
+  auto ids = [&](int q, unsigned* id) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned x = (unsigned)row[max(min(min(q, last) + i, np - 1), 0)];
+      id[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
+    }
+  };
+  auto fetch = [&](PageRegs* pr, const unsigned* id) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      load_page(pr[i], P.pool + ((size_t)id[i] * (unsigned)P.hkv + (unsigned)w.head) * kKv4Block, (unsigned)lane);
+  };
+  RawRow raw[NQ];
+  Columns<NQ, QT, PT> C;
+  C.load(raw, w, A);
+  PageRegs a[2], c[2];
+  unsigned id[2];
+  ids(p, id);
+  fetch(a, id);
+  ids(p + STEP, id);
+  C.start(raw, w, A, most);
+
+  const unsigned mask = code_mask();
+  auto step = [&](const PageRegs* pr, auto masked) {
+    constexpr bool MASK = decltype(masked)::value;
+    f16x8 kf[2][2], vf[4];
+    f16x4 va[4], vb[4];
+    unsigned bad[2] = {0u, 0u};
+    keys_of(pr[0].k, pr[0].ks, mask, kf[0]);
+    keys_of(pr[1].k, pr[1].ks, mask, kf[1]);
+    values_of<MASK>(pr[0].v, pr[0].vs, mask, p, some_see, va, &bad[0]);
+    values_of<MASK>(pr[1].v, pr[1].vs, mask, p + 1, some_see, vb, &bad[1]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vf[j] = join8(va[j], vb[j]);
+    f32x4 sc[NQ][2];
+    f16x8 ph[NQ], pl[NQ];
+    C.scores(kf, sc);
+    C.template weights<MASK>(sc, p, bad[0] | bad[1] << 4, ph, pl);
+    C.values(vf, ph, pl);
+  };
   {
     const int full = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
     bool swapped = false;
     while (p < full) {
       fetch(c, id);
       ids(p + 2 * STEP, id);
-      step(a, p, std::false_type());
+      step(a, std::false_type());
       p += STEP;
       if (p >= full) {
         swapped = true;
@@ -707,7 +799,7 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
       }
       fetch(a, id);
       ids(p + 2 * STEP, id);
-      step(c, p, std::false_type());
+      step(c, std::false_type());
       p += STEP;
     }
     if (swapped) {
@@ -717,99 +809,219 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
     while (p < p1) {
       fetch(c, id);
       ids(p + 2 * STEP, id);
-      step(a, p, std::true_type());
+      step(a, std::true_type());
       a[0] = c[0];
       a[1] = c[1];
       p += STEP;
     }
   }
 
-  // ---- output of N consecutive dimensions of column c, or the split's part
-  auto put = [&](int col, int d0, auto n_const, const float* x, float l, float m) {
-    constexpr int N = decltype(n_const)::value;
-    if (col >= cols) return;
-    const int at_row = (unsigned)col / group;
-    const int rw = s.row0 + at_row, hd = head * G + col - at_row * G;
-    if (joined) {
-      const size_t at = ((size_t)split * R.n_rows + rw) * A.hq + hd;
-      float* dst = A.part + at * 64 + d0;
+  // Join the four waves: wave v takes dimensions 16 g + 4 v .. + 3.
+  __shared__ f32x4 lo[4][4][64];
+  __shared__ float2 ls[4][64];
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i)
-        *reinterpret_cast<f32x4*>(dst + 4 * i) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-      if (d0 == 0) {
-        float2* ml = reinterpret_cast<float2*>(A.part + (size_t)splits * R.n_rows * A.hq * 64) + at;
-        *ml = make_float2(m, l);
-      }
-      return;
+  for (int t = 0; t < NQ; ++t) {
+    if (t) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{C.o[t][0][i], C.o[t][1][i], C.o[t][2][i], C.o[t][3][i]};
+    ls[wave][lane] = make_float2(C.base_of(t), C.sum[t][0]);
+    __syncthreads();
+    float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < 4; ++v) m = fmaxf(m, ls[v][lane].x);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const float2 z = ls[v][lane];
+      const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
+      const f32x4 y = lo[v][wave][lane];
+      l += f * z.y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] += f * y[j];
     }
-    float y[N];
-    const float inv = l == 0.f ? 0.f : 1.0f / l;  // nothing to attend to: 0
-#pragma unroll
-    for (int i = 0; i < N; ++i) y[i] = x[i] * inv;
-    store_row<N>(A.out, (size_t)rw * A.out_stride + hd * 64 + d0, A.out_type, y);
-  };
+    put<4>(R, A, w, w.c0 + 16 * t + r, 16 * g + 4 * wave, x, l, m, joined, split, splits);
+  }
+}
 
-  if constexpr (WK == 1) {
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      float x[16];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[4 * i + j] = o[t][j][i];
-      put(c0 + 16 * t + r, 16 * g, std::integral_constant<int, 16>(), x, sum[t][0],
-          sum[t][0] == 0.f ? -INFINITY : base[t]);
+// Many columns: a workgroup has 256 of them, and all its waves take the same
+// keys, 4 pages a step.  Together they make the pages' operands, for all of
+// them, in LDS (two buffers: a barrier a step).
+template <int NQ, int QT, int PT>
+__global__ __launch_bounds__(4096 / NQ / 4) __attribute__((amdgpu_waves_per_eu(NQ == 4 ? 2 : 4))) void
+k_kv4_attend_rows(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
+  constexpr int WAVES = 16 / NQ;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const unsigned b1 = blockIdx.x / heads, b2 = b1 / splits_, sq = b2 / tiles_;
+  const int split = b1 - b2 * splits_.d, splits = splits_.d;
+  const Seq s = load_seq(P, R, sq);
+  const int G = group.d, cols = s.n * G;
+  // The last tiles have the most keys: they go first.
+  const int t0 = (int)(tiles_.d - 1 - (b2 - sq * tiles_.d)) * kRowsTile;
+  if (t0 >= cols) return;
+  const int c0 = t0 + wave * (16 * NQ);
+  const Place w{s, (int)(blockIdx.x - b1 * heads.d), G, cols, min(c0, cols - 1), group};
+  const bool idle = c0 >= cols;  // such a wave makes operands only
+  // Keys of the workgroup's first and last row, and of the wave's last.
+  const int most = P.max_pages * kPage;
+  const int row_a = (unsigned)t0 / group, row_b = (unsigned)(min(t0 + kRowsTile, cols) - 1) / group;
+  const int row_w = (unsigned)(min(w.c0 + 16 * NQ, cols) - 1) / group;
+  const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
+  const int mine = idle ? 0 : min(max(s.first + row_w + 1, 0), most);
+  const int np = (some_see + kPage - 1) / kPage;
+  const int per = split_pages(np, splits, 4);
+  const int p0 = split * per, p1 = min(p0 + per, np);
+  const bool joined = per < np;
+  if (split > 0 && p0 >= np) return;
+
+  const int* row = P.table + (size_t)s.trow * P.max_pages;
+  // Four waves make a page each; eight, the keys or the values of one.
+  const int page = wave * 4 / WAVES;
+  const bool keys = WAVES == 4 || !(wave & 1), values = WAVES == 4 || (wave & 1);
+  auto page_id = [&](int q) {  // the wave's page of the step at q; behind the last one, any
+    const unsigned x = (unsigned)row[max(min(q + page, np - 1), 0)];
+    return x < (unsigned)P.n_pages ? x : 0u;
+  };
+  struct {
+    u32x2 k, v, vs;
+    unsigned ks;
+  } pr;
+  auto fetch = [&](unsigned id) {
+    const unsigned char* blk = P.pool + ((size_t)id * (unsigned)P.hkv + (unsigned)w.head) * kKv4Block;
+    if (keys) {
+      pr.k = *reinterpret_cast<const u32x2*>(blk + 8 * (unsigned)lane);
+      pr.ks = *reinterpret_cast<const unsigned*>(blk + (kKeyScales + 4 * (unsigned)r));
     }
-  } else {
-    // Join the four waves: wave w takes dimensions 16 g + 4 w .. + 3.
-    __shared__ f32x4 lo[4][4][64];
-    __shared__ float2 ls[4][64];
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      if (t) __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{o[t][0][i], o[t][1][i], o[t][2][i], o[t][3][i]};
-      // A wave whose keys the column does not see has no base.
-      ls[wave][lane] = make_float2(sum[t][0] == 0.f ? -INFINITY : base[t], sum[t][0]);
-      __syncthreads();
-      float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) m = fmaxf(m, ls[w][lane].x);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float2 z = ls[w][lane];
-        const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
-        const f32x4 y = lo[w][wave][lane];
-        l += f * z.y;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+    if (values) {
+      pr.v = *reinterpret_cast<const u32x2*>(blk + (512 + 8 * (unsigned)lane));
+      pr.vs = *reinterpret_cast<const u32x2*>(blk + (kValueScales + (lane & 8) * 4 + 8 * (unsigned)g));
+    }
+  };
+  RawRow raw[NQ];
+  Columns<NQ, QT, PT> C;
+  C.load(raw, w, A);
+  unsigned id = page_id(p0);
+  fetch(id);
+  id = page_id(p0 + 4);
+  C.start(raw, w, A, most);
+
+  // Operands of 4 pages: keys [page][half], values [pair of pages][dimension of four].
+  __shared__ f16x8 kl[3][4][2][64], vl[3][2][4][64];
+  __shared__ unsigned badl[3][4][4];
+  const unsigned mask = code_mask();
+  auto make = [&](int q, int buf) {
+    if (keys) {
+      f16x8 kf[2];
+      keys_of(pr.k, pr.ks, mask, kf);
+      kl[buf][page][0][lane] = kf[0];
+      kl[buf][page][1][lane] = kf[1];
+    }
+    if (values) {
+      f16x4 vf[4];
+      unsigned bad = 0;
+      if ((q + 4) * kPage <= all_see) {
+        values_of<false>(pr.v, pr.vs, mask, q + page, some_see, vf, &bad);
+      } else {
+        values_of<true>(pr.v, pr.vs, mask, q + page, some_see, vf, &bad);
+        if (r == 0) badl[buf][page][g] = bad;
       }
-      put(c0 + 16 * t + r, 16 * g + 4 * wave, std::integral_constant<int, 4>(), x, l, m);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) reinterpret_cast<f16x4*>(&vl[buf][page >> 1][j][lane])[page & 1] = vf[j];
     }
+  };
+  // Loads in flight need not land at the barrier: it orders LDS alone.
+  auto sync = [] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+  };
+  f32x4 sc[NQ][2];
+  auto scores_of = [&](int buf, int h) {
+    f16x8 kf[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      kf[i][0] = kl[buf][2 * h + i][0][lane];
+      kf[i][1] = kl[buf][2 * h + i][1][lane];
+    }
+    C.scores(kf, sc);
+  };
+  // Two pages' weights and weighted values, and the scores of the next two: the
+  // matrix products come together, so that the two waves of a SIMD can be at
+  // products and at exponentials in turn.
+  f16x8 ph[NQ], pl[NQ];
+  auto weigh = [&](int q, int buf, int h, auto masked) {
+    constexpr bool MASK = decltype(masked)::value;
+    unsigned bad = 0;
+    if constexpr (MASK) bad = badl[buf][2 * h][g] | badl[buf][2 * h + 1][g] << 4;
+    C.template weights<MASK>(sc, q, bad, ph, pl);
+  };
+  auto multiply = [&](int buf, int h, int next_buf) {
+    f16x8 vf[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vf[j] = vl[buf][h][j][lane];
+    C.values(vf, ph, pl);
+    scores_of(next_buf, h ^ 1);
+  };
+  make(p0, 0);
+  fetch(id);
+  id = page_id(p0 + 8);
+  sync();
+  // A step's operands are made while the one before is worked on, into the third
+  // of three buffers: the slowest wave may still read the one before that.
+  int p = p0, buf = 0, nxt = 1;
+  scores_of(0, 0);
+  auto tile = [&](auto masked, bool work) {
+    if (work) weigh(p, buf, 0, masked);
+    if (p + 4 < p1) make(p + 4, nxt);
+    fetch(id);
+    id = page_id(p + 12);
+    if (work) multiply(buf, 0, buf);
+    sync();
+    if (work) {
+      weigh(p + 2, buf, 1, masked);
+      multiply(buf, 1, nxt);  // (behind the last step: of what LDS holds, unused)
+    }
+    p += 4;
+    buf = nxt;
+    nxt = nxt == 2 ? 0 : nxt + 1;
+  };
+  const int full = min(all_see / kPage & ~3, p1 & ~3);  // pages below are seen by every row (p0 is a multiple of 4)
+  while (p < full) tile(std::false_type(), true);
+  while (p < p1) tile(std::true_type(), p * kPage < mine);
+
+  if (idle) return;
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[4 * i + j] = C.o[t][j][i];
+    put<16>(R, A, w, w.c0 + 16 * t + r, 16 * g, x, C.sum[t][0], C.base_of(t), joined, split, splits);
   }
 }
 
 // Splits that hold keys of column c's tile in a sequence (as the attention
 // kernel cut them); 1: the attention kernel wrote the output.
-__device__ __forceinline__ int splits_of(const Kv4Pool& P, const Seq& s, int G, int c, int tile_cols, int splits) {
+__device__ __forceinline__ int splits_of(const Kv4Pool& P, const Seq& s, int G, int c, int tile_cols, int unit,
+                                        int splits) {
   const int cols = s.n * G, c0 = c / tile_cols * tile_cols;
   const int row_b = (min(c0 + tile_cols, cols) - 1) / G;
   const int some_see = min(max(s.first + row_b + 1, 0), P.max_pages * kPage);
-  const int np = (some_see + kPage - 1) / kPage, per = split_pages(np, splits);
+  const int np = (some_see + kPage - 1) / kPage, per = split_pages(np, splits, unit);
   return per >= np ? 1 : (np + per - 1) / per;
 }
 
 // Joins the splits of few (row, head)s, a workgroup each: lane l of wave w has
 // dimensions 4 (l % 16) .. + 3 of splits 4 w + l / 16, + 16, ...: all loads are
 // in flight at once.
-__global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
+__global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int unit, int splits) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned b = blockIdx.x, row = b / (unsigned)A.hq;
   const int hd = b - row * A.hq, i = row % (unsigned)R.max_rows;
   const Seq s = load_seq(P, R, row / (unsigned)R.max_rows);
   if (i >= s.n) return;
   const int G = A.hq / P.hkv;
-  const int n = splits_of(P, s, G, i * G + hd % G, tile_cols, splits);
+  const int n = splits_of(P, s, G, i * G + hd % G, tile_cols, unit, splits);
   if (n == 1) return;
   const size_t at = (size_t)(s.row0 + i) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
   const float2* ml = reinterpret_cast<const float2*>(A.part + (size_t)splits * step * 64) + at;
@@ -870,7 +1082,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Atten
 
 // Up to 16 splits of many (row, head)s, 16 lanes each: lane l of them has
 // split l's statistics and dimensions 4 l .. + 3.
-__global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
+__global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int unit, int splits) {
   const int l16 = threadIdx.x & 15;
   const unsigned b = blockIdx.x * 16u + (threadIdx.x >> 4), row = b / (unsigned)A.hq;
   const int hd = b - row * A.hq, i = row % (unsigned)R.max_rows;
@@ -879,7 +1091,7 @@ __global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4
   const bool in = sq < (unsigned)R.n_seqs;
   const Seq s = load_seq(P, R, in ? sq : 0);
   const int G = A.hq / P.hkv;
-  const int n = in && i < s.n ? splits_of(P, s, G, i * G + hd % G, tile_cols, splits) : 1;
+  const int n = in && i < s.n ? splits_of(P, s, G, i * G + hd % G, tile_cols, unit, splits) : 1;
   const size_t at = (size_t)(s.row0 + (n > 1 ? i : 0)) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
   const float2* ml = reinterpret_cast<const float2*>(A.part + (size_t)splits * step * 64) + at;
   const float* part = A.part + at * 64 + 4 * l16;
@@ -910,24 +1122,14 @@ __global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4
   store_row<4>(A.out, (size_t)(s.row0 + i) * A.out_stride + hd * 64 + 4 * l16, A.out_type, x);
 }
 
-template <int NQ, int QT, int PT>
+template <int QT, int PT>
 void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
   const Div heads = div_by(P.hkv), splits = div_by(p.splits), tiles = div_by(p.tiles), group = div_by(A.hq / P.hkv);
-  if constexpr (NQ == 4) {
-    if (p.wk == 1) {
-      k_kv4_attend<NQ, QT, PT, 1><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
-      return;
-    }
-  }
-  k_kv4_attend<NQ, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
-}
-
-template <int QT, int PT>
-void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
-  if (p.nq == 1) launch_attend<1, QT, PT>(st, P, R, A, p);
-  else if (p.nq == 2) launch_attend<2, QT, PT>(st, P, R, A, p);
-  else launch_attend<4, QT, PT>(st, P, R, A, p);
+  if (p.rows) k_kv4_attend_rows<kRowsNq, QT, PT><<<groups, 1024 / kRowsNq, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  else if (p.nq == 1) k_kv4_attend<1, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  else if (p.nq == 2) k_kv4_attend<2, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  else k_kv4_attend<4, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
 }
 
 }  // namespace
@@ -956,11 +1158,11 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t m
   Kv4Plan p;
   const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), seqs = (int64_t)R.n_seqs * P.hkv;
   p.nq = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
-  p.wk = (cols + 255) / 256 * seqs >= 512 ? 1 : 4;
-  const int64_t tiles = p.wk == 1 ? (cols + 255) / 256 : (cols + 16 * p.nq - 1) / (16 * p.nq);
+  p.rows = cols > 128 && (cols + 255) / 256 * seqs >= 512;
+  const int width = p.rows ? kRowsTile : 16 * p.nq;
+  const int64_t tiles = (cols + width - 1) / width, outputs = (int64_t)R.n_rows * hq;
   p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-  const int64_t outputs = (int64_t)R.n_rows * hq;
-  p.splits = p.wk == 1 ? 1 : splits_for(p.nq, tiles * seqs, pages, outputs, most_bytes);
+  p.splits = p.rows ? 1 : splits_for(p.nq, tiles * seqs, pages, outputs, most_bytes);
   const int64_t join = p.splits > 1 ? (int64_t)R.n_seqs * R.max_rows * hq : 0;
   // (Columns are counted in 32 bits.)
   p.groups = cols > INT32_MAX - 1024 ? cols : std::max(seqs * tiles * p.splits, join);
@@ -977,8 +1179,9 @@ hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const 
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
     const int64_t outs = (int64_t)R.n_seqs * R.max_rows * A.hq;
-    if (p.splits > 16) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
-    else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
+    const int width = p.rows ? kRowsTile : 16 * p.nq, unit = p.rows ? 4 : 2;
+    if (p.splits > 16) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, R, A, width, unit, p.splits);
+    else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, R, A, width, unit, p.splits);
     e = hipGetLastError();
   }
   return e;
