@@ -382,8 +382,6 @@ int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
 // Operand columns are (row, query head of the kv head's group) pairs, row-major:
 // column c of a sequence is row c / G, head c % G.
 constexpr int kMaxSplits = 64;
-constexpr int kRowsTile = 256;  // columns of a workgroup of k_kv4_attend_rows
-constexpr int kRowsNq = 4;
 
 // Workspace of s splits: 64 dimensions, base and sum of weights each.
 size_t split_bytes(int s, int64_t outputs) { return (size_t)s * (size_t)outputs * (64 + 2) * sizeof(float); }
@@ -416,11 +414,10 @@ int splits_for(int nq, int64_t groups, int pages, int64_t outputs, size_t most_b
   return best;
 }
 
-// Pages of a split, given the pages that a column tile attends to, in units that
-// a workgroup takes at a time.
-__device__ __forceinline__ int split_pages(int np, int splits, int unit) {
-  const int units = (np + unit - 1) / unit;
-  return unit * ((units + splits - 1) / splits);
+// Pages of a split, given the pages that a column tile attends to: whole steps of two.
+__device__ __forceinline__ int split_pages(int np, int splits) {
+  const int pairs = (np + 1) >> 1;
+  return 2 * ((pairs + splits - 1) / splits);
 }
 
 struct PageRegs {
@@ -516,6 +513,13 @@ __device__ __forceinline__ f16x8 join8(f16x4 a, f16x4 b) {
 // leaves the step without reductions across lanes.
 constexpr float kOffset = 7.f, kSlack = 8.f;
 
+// Loads in flight need not land at this barrier: it orders LDS alone.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Where a wave stands: columns c0 .. c0 + 16 NQ - 1 of one (sequence, kv head).
 struct Place {
   Seq s;
@@ -523,32 +527,84 @@ struct Place {
   Div group;
 };
 
-// A wave's NQ tiles of 16 columns.  QT, PT: fp16 terms of queries and of weights.
-// Queries (but for fp16 ones) are scaled by a power of two that puts a row's
-// largest element into [2^13, 2^14), so that one term holds any 16-bit query
-// and two hold 22 bits of an fp32 one.
+// The query of the lane's column of a 16-column tile, 8 dimensions of each half:
+// as loaded (with its rotation), and as operands.
+struct RawQuery {
+  RawRow row;
+  f32x4 turn[4];
+};
+// QT: fp16 terms.  Queries (but for fp16 ones) are scaled by a power of two that puts a
+// row's largest element into [2^13, 2^14), so that one term holds any 16-bit
+// query and two hold 22 bits of an fp32 one.
+template <int QT>
+struct Query {
+  f16x8 h[2], l[QT == 2 ? 2 : 1];
+  float qs;  // scores to powers of two
+};
+
+// Columns behind the last one repeat it (and are not written).
+__device__ __forceinline__ int column_row(const Place& w, int c) { return (unsigned)min(c, w.cols - 1) / w.group; }
+
+__device__ __forceinline__ void load_query(RawQuery& q, const Place& w, const Kv4Attend& A, int tile) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = w.c0 + 16 * tile + (lane & 15);
+  const int rw = column_row(w, c), j = min(c, w.cols - 1) - rw * w.G;
+  const size_t at = (size_t)(w.s.row0 + rw) * A.q_stride + (w.head * w.G + j) * 64 + 8 * g;
+  load_raw(q.row, A.q, at, at + 32, A.q_type);
+  if (A.rope.at) {
+    const int pos = min(max(w.s.first + rw, 0), A.rope.len - 1);
+    const f32x4* cs = reinterpret_cast<const f32x4*>(A.rope.at + (size_t)pos * 32 + 8 * g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q.turn[i] = cs[i];
+  }
+}
+
+template <int QT>
+__device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Attend& A) {
+  Query<QT> z;
+  if (QT == 1 && A.q_type == kRowF16 && !A.rope.at) {
+    z.h[0] = __builtin_bit_cast(f16x8, q.row.w[0]);
+    z.h[1] = __builtin_bit_cast(f16x8, q.row.w[1]);
+    z.qs = fmaxf(A.scale * 1.4426950408889634f, 1e-37f);
+    return z;
+  }
+  float x[16];
+  raw_values(q.row, A.q_type, x);
+  if (A.rope.at) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float u = x[i], v = x[8 + i], co = q.turn[i >> 1][2 * (i & 1)], si = q.turn[i >> 1][2 * (i & 1) + 1];
+      x[i] = u * co - v * si;
+      x[8 + i] = v * co + u * si;
+    }
+  }
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  int e = 0;
+  if (top > 0.f && top < INFINITY) e = 14 - __builtin_amdgcn_frexp_expf(top);
+  z.qs = fmaxf(__builtin_amdgcn_ldexpf(A.scale * 1.4426950408889634f, -e), 1e-37f);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float y = __builtin_amdgcn_ldexpf(x[i], e);
+    const _Float16 h = (_Float16)y;
+    z.h[i >> 3][i & 7] = h;
+    if constexpr (QT == 2) z.l[i >> 3][i & 7] = (_Float16)(y - (float)h);
+  }
+  return z;
+}
+
+// A wave's NQ tiles of 16 columns.  PT: fp16 terms of weights.
 template <int NQ, int QT, int PT>
 struct Columns {
-  f16x8 qh[NQ][2], ql[QT == 2 ? NQ : 1][2];
-  float qs[NQ];  // scores to powers of two
-  int lim[NQ];   // keys that the column sees
+  Query<QT> q[NQ];
+  int lim[NQ];  // keys that the column sees
   f32x4 o[NQ][4], sum[NQ];
   float base[NQ];
   bool first;
 
-  // Columns behind the last one repeat it (and are not written).
-  static __device__ __forceinline__ void load(RawRow* raw, const Place& w, const Kv4Attend& A) {
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      const int c = min(w.c0 + 16 * t + r, w.cols - 1), rw = (unsigned)c / w.group, j = c - rw * w.G;
-      const size_t at = (size_t)(w.s.row0 + rw) * A.q_stride + (w.head * w.G + j) * 64 + 8 * g;
-      load_raw(raw[t], A.q, at, at + 32, A.q_type);
-    }
-  }
-
-  __device__ __forceinline__ void start(const RawRow* raw, const Place& w, const Kv4Attend& A, int most) {
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  __device__ __forceinline__ void start(const Place& w, int most) {
     first = true;
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
@@ -556,44 +612,7 @@ struct Columns {
       for (int j = 0; j < 4; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
       sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
       base[t] = 0.f;
-      const int pos = w.s.first + (int)((unsigned)min(w.c0 + 16 * t + r, w.cols - 1) / w.group);
-      lim[t] = min(max(pos + 1, 0), most);
-      if (QT == 1 && A.q_type == kRowF16 && !A.rope.at) {
-        qh[t][0] = __builtin_bit_cast(f16x8, raw[t].w[0]);
-        qh[t][1] = __builtin_bit_cast(f16x8, raw[t].w[1]);
-        qs[t] = fmaxf(A.scale * 1.4426950408889634f, 1e-37f);
-        continue;
-      }
-      float x[16];
-      raw_values(raw[t], A.q_type, x);
-      if (A.rope.at) {
-        const f32x4* cs = reinterpret_cast<const f32x4*>(A.rope.at + (size_t)min(max(pos, 0), A.rope.len - 1) * 32 + 8 * g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 cw = cs[i];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float u = x[2 * i + e], v = x[8 + 2 * i + e], co = cw[2 * e], si = cw[2 * e + 1];
-            x[2 * i + e] = u * co - v * si;
-            x[8 + 2 * i + e] = v * co + u * si;
-          }
-        }
-      }
-      float top = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      int e = 0;
-      if (top > 0.f && top < INFINITY) e = 14 - __builtin_amdgcn_frexp_expf(top);
-      qs[t] = fmaxf(__builtin_amdgcn_ldexpf(A.scale * 1.4426950408889634f, -e), 1e-37f);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float y = __builtin_amdgcn_ldexpf(x[i], e);
-        const _Float16 h = (_Float16)y;
-        qh[t][i >> 3][i & 7] = h;
-        if constexpr (QT == 2) ql[t][i >> 3][i & 7] = (_Float16)(y - (float)h);
-      }
+      lim[t] = min(max(w.s.first + column_row(w, w.c0 + 16 * t + (threadIdx.x & 15)) + 1, 0), most);
     }
   }
 
@@ -607,11 +626,11 @@ struct Columns {
       for (int i = 0; i < 2; ++i) {
         sc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         if constexpr (QT == 2) {
-          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], ql[t][0], sc[t][i], 0, 0, 0);
-          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], ql[t][1], sc[t][i], 0, 0, 0);
+          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], q[t].l[0], sc[t][i], 0, 0, 0);
+          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], q[t].l[1], sc[t][i], 0, 0, 0);
         }
-        sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], qh[t][0], sc[t][i], 0, 0, 0);
-        sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], qh[t][1], sc[t][i], 0, 0, 0);
+        sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], q[t].h[0], sc[t][i], 0, 0, 0);
+        sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], q[t].h[1], sc[t][i], 0, 0, 0);
       }
   }
 
@@ -625,7 +644,7 @@ struct Columns {
     for (int t = 0; t < NQ; ++t)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[t][i] = fmaf(sc[t][i >> 2][i & 3], qs[t], -base[t]);
+        x[t][i] = fmaf(sc[t][i >> 2][i & 3], q[t].qs, -base[t]);
         if constexpr (MASK) {
           if (bad >> i & 1u) x[t][i] = NAN;
           if ((page + (i >> 2)) * kPage + 4 * g + (i & 3) >= lim[t]) x[t][i] = -INFINITY;
@@ -732,7 +751,7 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   const int row_a = (unsigned)w.c0 / group, row_b = (unsigned)(min(w.c0 + 16 * NQ, cols) - 1) / group;
   const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
   const int np = (some_see + kPage - 1) / kPage;
-  const int per = split_pages(np, splits, 2);
+  const int per = split_pages(np, splits);
   const int p0 = split * per, p1 = min(p0 + per, np);
   const bool joined = per < np;  // several splits have keys
   if (split > 0 && p0 >= np) return;
@@ -757,15 +776,35 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
     for (int i = 0; i < 2; ++i)
       load_page(pr[i], P.pool + ((size_t)id[i] * (unsigned)P.hkv + (unsigned)w.head) * kKv4Block, (unsigned)lane);
   };
-  RawRow raw[NQ];
-  Columns<NQ, QT, PT> C;
-  C.load(raw, w, A);
+  // Of several tiles, each wave makes one's queries for all.
+  RawQuery raw;
+  if (NQ == 1 || wave < NQ) load_query(raw, w, A, NQ == 1 ? 0 : wave);
   PageRegs a[2], c[2];
   unsigned id[2];
   ids(p, id);
   fetch(a, id);
   ids(p + STEP, id);
-  C.start(raw, w, A, most);
+  Columns<NQ, QT, PT> C;
+  C.start(w, most);
+  if constexpr (NQ == 1) {
+    C.q[0] = make_query<QT>(raw, A);
+  } else {
+    __shared__ f16x8 made[NQ][2 * QT][64];
+    __shared__ float made_qs[NQ][64];
+    if (wave < NQ) {
+      const Query<QT> z = make_query<QT>(raw, A);
+#pragma unroll
+      for (int i = 0; i < 2 * QT; ++i) made[wave][i][lane] = i < 2 ? z.h[i] : z.l[i - 2];
+      made_qs[wave][lane] = z.qs;
+    }
+    lds_barrier();
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+      for (int i = 0; i < 2 * QT; ++i) (i < 2 ? C.q[t].h[i] : C.q[t].l[i - 2]) = made[t][i][lane];
+      C.q[t].qs = made_qs[t][lane];
+    }
+  }
 
   const unsigned mask = code_mask();
   auto step = [&](const PageRegs* pr, auto masked) {
@@ -842,186 +881,27 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   }
 }
 
-// Many columns: a workgroup has 256 of them, and all its waves take the same
-// keys, 4 pages a step.  Together they make the pages' operands, for all of
-// them, in LDS (two buffers: a barrier a step).
-template <int NQ, int QT, int PT>
-__global__ __launch_bounds__(4096 / NQ / 4) __attribute__((amdgpu_waves_per_eu(NQ == 4 ? 2 : 4))) void
-k_kv4_attend_rows(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
-  constexpr int WAVES = 16 / NQ;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 15, g = lane >> 4;
-  const unsigned b1 = blockIdx.x / heads, b2 = b1 / splits_, sq = b2 / tiles_;
-  const int split = b1 - b2 * splits_.d, splits = splits_.d;
-  const Seq s = load_seq(P, R, sq);
-  const int G = group.d, cols = s.n * G;
-  // The last tiles have the most keys: they go first.
-  const int t0 = (int)(tiles_.d - 1 - (b2 - sq * tiles_.d)) * kRowsTile;
-  if (t0 >= cols) return;
-  const int c0 = t0 + wave * (16 * NQ);
-  const Place w{s, (int)(blockIdx.x - b1 * heads.d), G, cols, min(c0, cols - 1), group};
-  const bool idle = c0 >= cols;  // such a wave makes operands only
-  // Keys of the workgroup's first and last row, and of the wave's last.
-  const int most = P.max_pages * kPage;
-  const int row_a = (unsigned)t0 / group, row_b = (unsigned)(min(t0 + kRowsTile, cols) - 1) / group;
-  const int row_w = (unsigned)(min(w.c0 + 16 * NQ, cols) - 1) / group;
-  const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
-  const int mine = idle ? 0 : min(max(s.first + row_w + 1, 0), most);
-  const int np = (some_see + kPage - 1) / kPage;
-  const int per = split_pages(np, splits, 4);
-  const int p0 = split * per, p1 = min(p0 + per, np);
-  const bool joined = per < np;
-  if (split > 0 && p0 >= np) return;
-
-  const int* row = P.table + (size_t)s.trow * P.max_pages;
-  // Four waves make a page each; eight, the keys or the values of one.
-  const int page = wave * 4 / WAVES;
-  const bool keys = WAVES == 4 || !(wave & 1), values = WAVES == 4 || (wave & 1);
-  auto page_id = [&](int q) {  // the wave's page of the step at q; behind the last one, any
-    const unsigned x = (unsigned)row[max(min(q + page, np - 1), 0)];
-    return x < (unsigned)P.n_pages ? x : 0u;
-  };
-  struct {
-    u32x2 k, v, vs;
-    unsigned ks;
-  } pr;
-  auto fetch = [&](unsigned id) {
-    const unsigned char* blk = P.pool + ((size_t)id * (unsigned)P.hkv + (unsigned)w.head) * kKv4Block;
-    if (keys) {
-      pr.k = *reinterpret_cast<const u32x2*>(blk + 8 * (unsigned)lane);
-      pr.ks = *reinterpret_cast<const unsigned*>(blk + (kKeyScales + 4 * (unsigned)r));
-    }
-    if (values) {
-      pr.v = *reinterpret_cast<const u32x2*>(blk + (512 + 8 * (unsigned)lane));
-      pr.vs = *reinterpret_cast<const u32x2*>(blk + (kValueScales + (lane & 8) * 4 + 8 * (unsigned)g));
-    }
-  };
-  RawRow raw[NQ];
-  Columns<NQ, QT, PT> C;
-  C.load(raw, w, A);
-  unsigned id = page_id(p0);
-  fetch(id);
-  id = page_id(p0 + 4);
-  C.start(raw, w, A, most);
-
-  // Operands of 4 pages: keys [page][half], values [pair of pages][dimension of four].
-  __shared__ f16x8 kl[3][4][2][64], vl[3][2][4][64];
-  __shared__ unsigned badl[3][4][4];
-  const unsigned mask = code_mask();
-  auto make = [&](int q, int buf) {
-    if (keys) {
-      f16x8 kf[2];
-      keys_of(pr.k, pr.ks, mask, kf);
-      kl[buf][page][0][lane] = kf[0];
-      kl[buf][page][1][lane] = kf[1];
-    }
-    if (values) {
-      f16x4 vf[4];
-      unsigned bad = 0;
-      if ((q + 4) * kPage <= all_see) {
-        values_of<false>(pr.v, pr.vs, mask, q + page, some_see, vf, &bad);
-      } else {
-        values_of<true>(pr.v, pr.vs, mask, q + page, some_see, vf, &bad);
-        if (r == 0) badl[buf][page][g] = bad;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) reinterpret_cast<f16x4*>(&vl[buf][page >> 1][j][lane])[page & 1] = vf[j];
-    }
-  };
-  // Loads in flight need not land at the barrier: it orders LDS alone.
-  auto sync = [] {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-  };
-  f32x4 sc[NQ][2];
-  auto scores_of = [&](int buf, int h) {
-    f16x8 kf[2][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      kf[i][0] = kl[buf][2 * h + i][0][lane];
-      kf[i][1] = kl[buf][2 * h + i][1][lane];
-    }
-    C.scores(kf, sc);
-  };
-  // Two pages' weights and weighted values, and the scores of the next two: the
-  // matrix products come together, so that the two waves of a SIMD can be at
-  // products and at exponentials in turn.
-  f16x8 ph[NQ], pl[NQ];
-  auto weigh = [&](int q, int buf, int h, auto masked) {
-    constexpr bool MASK = decltype(masked)::value;
-    unsigned bad = 0;
-    if constexpr (MASK) bad = badl[buf][2 * h][g] | badl[buf][2 * h + 1][g] << 4;
-    C.template weights<MASK>(sc, q, bad, ph, pl);
-  };
-  auto multiply = [&](int buf, int h, int next_buf) {
-    f16x8 vf[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) vf[j] = vl[buf][h][j][lane];
-    C.values(vf, ph, pl);
-    scores_of(next_buf, h ^ 1);
-  };
-  make(p0, 0);
-  fetch(id);
-  id = page_id(p0 + 8);
-  sync();
-  // A step's operands are made while the one before is worked on, into the third
-  // of three buffers: the slowest wave may still read the one before that.
-  int p = p0, buf = 0, nxt = 1;
-  scores_of(0, 0);
-  auto tile = [&](auto masked, bool work) {
-    if (work) weigh(p, buf, 0, masked);
-    if (p + 4 < p1) make(p + 4, nxt);
-    fetch(id);
-    id = page_id(p + 12);
-    if (work) multiply(buf, 0, buf);
-    sync();
-    if (work) {
-      weigh(p + 2, buf, 1, masked);
-      multiply(buf, 1, nxt);  // (behind the last step: of what LDS holds, unused)
-    }
-    p += 4;
-    buf = nxt;
-    nxt = nxt == 2 ? 0 : nxt + 1;
-  };
-  const int full = min(all_see / kPage & ~3, p1 & ~3);  // pages below are seen by every row (p0 is a multiple of 4)
-  while (p < full) tile(std::false_type(), true);
-  while (p < p1) tile(std::true_type(), p * kPage < mine);
-
-  if (idle) return;
-#pragma unroll
-  for (int t = 0; t < NQ; ++t) {
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * i + j] = C.o[t][j][i];
-    put<16>(R, A, w, w.c0 + 16 * t + r, 16 * g, x, C.sum[t][0], C.base_of(t), joined, split, splits);
-  }
-}
-
 // Splits that hold keys of column c's tile in a sequence (as the attention
 // kernel cut them); 1: the attention kernel wrote the output.
-__device__ __forceinline__ int splits_of(const Kv4Pool& P, const Seq& s, int G, int c, int tile_cols, int unit,
-                                        int splits) {
+__device__ __forceinline__ int splits_of(const Kv4Pool& P, const Seq& s, int G, int c, int tile_cols, int splits) {
   const int cols = s.n * G, c0 = c / tile_cols * tile_cols;
   const int row_b = (min(c0 + tile_cols, cols) - 1) / G;
   const int some_see = min(max(s.first + row_b + 1, 0), P.max_pages * kPage);
-  const int np = (some_see + kPage - 1) / kPage, per = split_pages(np, splits, unit);
+  const int np = (some_see + kPage - 1) / kPage, per = split_pages(np, splits);
   return per >= np ? 1 : (np + per - 1) / per;
 }
 
 // Joins the splits of few (row, head)s, a workgroup each: lane l of wave w has
 // dimensions 4 (l % 16) .. + 3 of splits 4 w + l / 16, + 16, ...: all loads are
 // in flight at once.
-__global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int unit, int splits) {
+__global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned b = blockIdx.x, row = b / (unsigned)A.hq;
   const int hd = b - row * A.hq, i = row % (unsigned)R.max_rows;
   const Seq s = load_seq(P, R, row / (unsigned)R.max_rows);
   if (i >= s.n) return;
   const int G = A.hq / P.hkv;
-  const int n = splits_of(P, s, G, i * G + hd % G, tile_cols, unit, splits);
+  const int n = splits_of(P, s, G, i * G + hd % G, tile_cols, splits);
   if (n == 1) return;
   const size_t at = (size_t)(s.row0 + i) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
   const float2* ml = reinterpret_cast<const float2*>(A.part + (size_t)splits * step * 64) + at;
@@ -1082,7 +962,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Atten
 
 // Up to 16 splits of many (row, head)s, 16 lanes each: lane l of them has
 // split l's statistics and dimensions 4 l .. + 3.
-__global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int unit, int splits) {
+__global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4Attend A, int tile_cols, int splits) {
   const int l16 = threadIdx.x & 15;
   const unsigned b = blockIdx.x * 16u + (threadIdx.x >> 4), row = b / (unsigned)A.hq;
   const int hd = b - row * A.hq, i = row % (unsigned)R.max_rows;
@@ -1091,7 +971,7 @@ __global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4
   const bool in = sq < (unsigned)R.n_seqs;
   const Seq s = load_seq(P, R, in ? sq : 0);
   const int G = A.hq / P.hkv;
-  const int n = in && i < s.n ? splits_of(P, s, G, i * G + hd % G, tile_cols, unit, splits) : 1;
+  const int n = in && i < s.n ? splits_of(P, s, G, i * G + hd % G, tile_cols, splits) : 1;
   const size_t at = (size_t)(s.row0 + (n > 1 ? i : 0)) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
   const float2* ml = reinterpret_cast<const float2*>(A.part + (size_t)splits * step * 64) + at;
   const float* part = A.part + at * 64 + 4 * l16;
@@ -1126,8 +1006,7 @@ template <int QT, int PT>
 void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
   const Div heads = div_by(P.hkv), splits = div_by(p.splits), tiles = div_by(p.tiles), group = div_by(A.hq / P.hkv);
-  if (p.rows) k_kv4_attend_rows<kRowsNq, QT, PT><<<groups, 1024 / kRowsNq, 0, st>>>(P, R, A, heads, splits, tiles, group);
-  else if (p.nq == 1) k_kv4_attend<1, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  if (p.nq == 1) k_kv4_attend<1, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
   else if (p.nq == 2) k_kv4_attend<2, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
   else k_kv4_attend<4, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
 }
@@ -1158,11 +1037,10 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t m
   Kv4Plan p;
   const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), seqs = (int64_t)R.n_seqs * P.hkv;
   p.nq = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
-  p.rows = cols > 128 && (cols + 255) / 256 * seqs >= 512;
-  const int width = p.rows ? kRowsTile : 16 * p.nq;
+  const int width = 16 * p.nq;
   const int64_t tiles = (cols + width - 1) / width, outputs = (int64_t)R.n_rows * hq;
   p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-  p.splits = p.rows ? 1 : splits_for(p.nq, tiles * seqs, pages, outputs, most_bytes);
+  p.splits = splits_for(p.nq, tiles * seqs, pages, outputs, most_bytes);
   const int64_t join = p.splits > 1 ? (int64_t)R.n_seqs * R.max_rows * hq : 0;
   // (Columns are counted in 32 bits.)
   p.groups = cols > INT32_MAX - 1024 ? cols : std::max(seqs * tiles * p.splits, join);
@@ -1179,9 +1057,8 @@ hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const 
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
     const int64_t outs = (int64_t)R.n_seqs * R.max_rows * A.hq;
-    const int width = p.rows ? kRowsTile : 16 * p.nq, unit = p.rows ? 4 : 2;
-    if (p.splits > 16) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, R, A, width, unit, p.splits);
-    else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, R, A, width, unit, p.splits);
+    if (p.splits > 16) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
+    else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
     e = hipGetLastError();
   }
   return e;
