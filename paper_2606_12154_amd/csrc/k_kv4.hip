@@ -383,35 +383,46 @@ int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
 // column c of a sequence is row c / G, head c % G.
 constexpr int kMaxSplits = 64;
 
+// Waves that a SIMD holds, by their registers.
+constexpr int waves_fit(int nq) { return nq == 1 ? 4 : nq == 2 ? 3 : 2; }
 // Workspace of s splits: 64 dimensions, base and sum of weights each.
 size_t split_bytes(int s, int64_t outputs) { return (size_t)s * (size_t)outputs * (64 + 2) * sizeof(float); }
 
-// Key splits of `groups` (sequence, kv head, column tile)s over up to `pages`
-// pages, by the time that they would take, in ns.  Measured (32 query heads on
-// 8): a workgroup that is alone on its CU takes 65 ns a page with one column tile, 120
-// with four; four (two) of them there, as many as fit, 150 (187) each.  What
-// comes before and after the pages is 4.5 us, and 0.5 more for each neighbour; the
-// join 2.8 us, and its reads.  So one sequence of 700 positions is not split (7.6
-// us against 8.4), 8,192 take 32 splits (8.9; 16 splits 10.7), 32 sequences of
-// 4,000 take 4 (22.4; unsplit 31.3), 64 of 1,500 none (19.0; 2 splits 19.5),
-// 256 rows behind 30,000 positions 4 (92; 2 splits 118, 8 splits 99).
-int splits_for(int nq, int64_t groups, int pages, int64_t outputs, size_t most_bytes) {
-  const double page = nq == 1 ? 65 : nq == 2 ? 90 : 120, more = nq == 1 ? 28 : nq == 2 ? 50 : 67;
-  const int fit = nq == 1 ? 4 : nq == 2 ? 3 : 2;
-  const int most = std::max(1, std::min(kMaxSplits, pages / 8));
-  int best = 1;
-  double best_ns = 0;
-  for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= most_bytes); ++s) {
-    const double k = std::ceil((double)groups * s / 256), here = std::min<double>(k, fit);
-    const double each = (page + more * (here - 1)) * std::max(1.0, k / fit);
-    double ns = 4500 * std::ceil(k / fit) + 500 * (here - 1) + each * std::ceil((double)pages / s);
-    if (s > 1) ns += 2800 + 0.066 * (double)outputs * s;
-    if (s == 1 || ns < best_ns) {
-      best = s;
-      best_ns = ns;
+// Waves of a workgroup (4, or 8 with one column tile) and key splits over
+// workgroups for `groups` (sequence, kv head, column tile)s over up to `pages`
+// pages: those of the least time by what was measured, in ns (32 query heads on
+// 8; an error of 11%).  A step (two pages) takes a wave that is alone on its SIMD 740 ns with one
+// column tile (720 with two, 960 with four), and 255 (400, 536) more for each
+// neighbour, of which a SIMD has up to three (two, one).  What comes before and
+// after is 3.6 us (4.5), and 0.9 (0.5) more for each neighbour; the join 3 us, and its
+// reads.  So one sequence of 700 positions is not split (6.2 us with eight
+// waves, 6.6 with four, 7.3 in 4 splits); 3,000 take splits of four waves (7.8; one of eight
+// 13.1), 32,768 32 splits of eight (11.7; of four 13.0); 32 sequences of 1,500 take eight
+// waves (12.2; four 16.1, in 4 splits 14.3), 128 of 1,000 four (19.8; eight
+// 22.5); 256 rows behind 30,000 positions 4 splits (87; 2 splits 118, 8 splits 99).
+void cut_keys(int nq, int64_t groups, int pages, int64_t outputs, size_t most_bytes, int* waves, int* splits) {
+  const int fit = waves_fit(nq);
+  const double alone = nq == 1 ? 740 : nq == 2 ? 720 : 960, more = nq == 1 ? 255 : nq == 2 ? 400 : 536;
+  const double ends = nq == 1 ? 3600 : 4500, near = nq == 1 ? 900 : 500;
+  const int pairs = std::max(1, (pages + 1) / 2), most = std::max(1, std::min(kMaxSplits, pairs / 4));
+  double best = 0;
+  for (int w = 4; w <= (nq == 1 ? 8 : 4); w += 4) {
+    for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= most_bytes); ++s) {
+      const int per = (pairs + s - 1) / s;
+      const double here = std::ceil((double)groups * s / 256);                    // workgroups a CU
+      const double held = std::min<double>(fit, here * w / 4) - 1;                // a wave's neighbours,
+      const double busy = std::max(1.0, here * std::min(w, per) / 4);             // and those with keys
+      const double step = (alone + more * (std::min<double>(busy, fit) - 1)) * std::max(1.0, busy / fit);
+      double ns = ends * std::ceil(here * w / (4 * fit)) + near * held + step * ((per + w - 1) / w);
+      if (w > 4) ns -= 200;  // (their waves start and end together)
+      if (s > 1) ns += 3000 + 0.09 * (double)outputs * s;
+      if (best == 0 || ns < best) {
+        best = ns;
+        *waves = w;
+        *splits = s;
+      }
     }
   }
-  return best;
 }
 
 // Pages of a split, given the pages that a column tile attends to: whole steps of two.
@@ -731,10 +742,10 @@ __device__ __forceinline__ void put(const Kv4Rows& R, const Kv4Attend& A, const 
   store_row<N>(A.out, (size_t)rw * A.out_stride + hd * 64 + d0, A.out_type, y);
 }
 
-// Few columns: a workgroup has one tile of 16 NQ of them, and its four waves
-// take the tile's keys in turn (two pages a step) and join at the end.
-template <int NQ, int QT, int PT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4 : NQ == 2 ? 3 : 2))) void
+// A workgroup has a tile of 16 NQ columns; its W waves take the tile's keys in
+// turn (two pages a step) and join at the end.
+template <int NQ, int QT, int PT, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(waves_fit(NQ)))) void
 k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
@@ -761,7 +772,7 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   // step is its last step again (no branch around loads, whose waits would then have to
   // assume that it was not taken).
   const int* row = P.table + (size_t)s.trow * P.max_pages;
-  constexpr int STEP = 8;
+  constexpr int STEP = 2 * W;
   int p = p0 + 2 * wave;
   const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
   auto ids = [&](int q, unsigned* id) {
@@ -855,9 +866,9 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
     }
   }
 
-  // Join the four waves: wave v takes dimensions 16 g + 4 v .. + 3.
-  __shared__ f32x4 lo[4][4][64];
-  __shared__ float2 ls[4][64];
+  // Join the waves: of four of them, wave v takes dimensions 16 g + 4 v .. + 3.
+  __shared__ f32x4 lo[W][4][64];
+  __shared__ float2 ls[W][64];
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
     if (t) __syncthreads();
@@ -865,11 +876,12 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
     for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{C.o[t][0][i], C.o[t][1][i], C.o[t][2][i], C.o[t][3][i]};
     ls[wave][lane] = make_float2(C.base_of(t), C.sum[t][0]);
     __syncthreads();
+    if (wave >= 4) continue;
     float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < 4; ++v) m = fmaxf(m, ls[v][lane].x);
+    for (int v = 0; v < W; ++v) m = fmaxf(m, ls[v][lane].x);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
+    for (int v = 0; v < W; ++v) {
       const float2 z = ls[v][lane];
       const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
       const f32x4 y = lo[v][wave][lane];
@@ -1006,9 +1018,10 @@ template <int QT, int PT>
 void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
   const Div heads = div_by(P.hkv), splits = div_by(p.splits), tiles = div_by(p.tiles), group = div_by(A.hq / P.hkv);
-  if (p.nq == 1) k_kv4_attend<1, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
-  else if (p.nq == 2) k_kv4_attend<2, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
-  else k_kv4_attend<4, QT, PT><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  if (p.nq == 1 && p.waves == 8) k_kv4_attend<1, QT, PT, 8><<<groups, 512, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  else if (p.nq == 1) k_kv4_attend<1, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  else if (p.nq == 2) k_kv4_attend<2, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  else k_kv4_attend<4, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
 }
 
 }  // namespace
@@ -1040,7 +1053,7 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t m
   const int width = 16 * p.nq;
   const int64_t tiles = (cols + width - 1) / width, outputs = (int64_t)R.n_rows * hq;
   p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-  p.splits = splits_for(p.nq, tiles * seqs, pages, outputs, most_bytes);
+  cut_keys(p.nq, tiles * seqs, pages, outputs, most_bytes, &p.waves, &p.splits);
   const int64_t join = p.splits > 1 ? (int64_t)R.n_seqs * R.max_rows * hq : 0;
   // (Columns are counted in 32 bits.)
   p.groups = cols > INT32_MAX - 1024 ? cols : std::max(seqs * tiles * p.splits, join);
@@ -1057,7 +1070,11 @@ hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const 
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
     const int64_t outs = (int64_t)R.n_seqs * R.max_rows * A.hq;
-    if (p.splits > 16) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
+    // Five and more splits of few rows are read at once by a workgroup each (one row of
+    // 32 heads, 16 splits: 7.5 us with the attention, 8.6 by 16 lanes each; 16 rows, 8
+    // splits: 10.7 and 10.6); fewer splits or more rows want fewer workgroups (64 rows, 2
+    // splits: 16.1 and 13.1).
+    if (p.splits > 16 || (p.splits > 4 && outs <= 512)) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
     else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
     e = hipGetLastError();
   }
