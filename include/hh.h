@@ -389,7 +389,8 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
  * they are.  Positions past max_pages * 16 - 1 are taken as that.  Sums and
  * softmax are fp32; with an fp32 `out` the products take fp16 pairs (22 bits)
  * of queries and weights, with a 16-bit one the weights are single fp16 numbers,
- * 2^-12 off at most.  Equal calls give equal bits.
+ * 2^-12 off at most (pairs with an fp16 `out` where a sequence has up to 16
+ * rows times n_heads / n_kv_heads).  Equal calls give equal bits.
  * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
  * UNSUPPORTED (more than 2^31 - 1 workgroups), HIP.
  */

@@ -1014,14 +1014,33 @@ __global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4
   store_row<4>(A.out, (size_t)(s.row0 + i) * A.out_stride + hd * 64 + 4 * l16, A.out_type, x);
 }
 
+struct Cuts {
+  unsigned groups;
+  Div heads, splits, tiles, group;
+};
+Cuts cuts_of(const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
+  return {(unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits), div_by(P.hkv), div_by(p.splits), div_by(p.tiles),
+          div_by(A.hq / P.hkv)};
+}
+
+template <int QT, int PT>
+void launch_tile(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
+  const Cuts c = cuts_of(P, R, A, p);
+  if (p.waves == 8) k_kv4_attend<1, QT, PT, 8><<<c.groups, 512, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  else k_kv4_attend<1, QT, PT, 4><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+}
+
+template <int QT, int PT>
+void launch_tiles(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
+  const Cuts c = cuts_of(P, R, A, p);
+  if (p.nq == 2) k_kv4_attend<2, QT, PT, 4><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  else k_kv4_attend<4, QT, PT, 4><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+}
+
 template <int QT, int PT>
 void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
-  const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
-  const Div heads = div_by(P.hkv), splits = div_by(p.splits), tiles = div_by(p.tiles), group = div_by(A.hq / P.hkv);
-  if (p.nq == 1 && p.waves == 8) k_kv4_attend<1, QT, PT, 8><<<groups, 512, 0, st>>>(P, R, A, heads, splits, tiles, group);
-  else if (p.nq == 1) k_kv4_attend<1, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
-  else if (p.nq == 2) k_kv4_attend<2, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
-  else k_kv4_attend<4, QT, PT, 4><<<groups, 256, 0, st>>>(P, R, A, heads, splits, tiles, group);
+  if (p.nq == 1) launch_tile<QT, PT>(st, P, R, A, p);
+  else launch_tiles<QT, PT>(st, P, R, A, p);
 }
 
 }  // namespace
@@ -1063,9 +1082,14 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t m
 
 hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers, whose
-  // rounding to 11 bits is an eighth of a bf16 output's.
-  if (A.out_type == kRowF32) launch_attend<2, 2>(st, P, R, A, p);
-  else if (A.out_type == kRowF16 && (A.q_type == kRowF32 || A.rope.at)) launch_attend<2, 1>(st, P, R, A, p);
+  // rounding to 11 bits is an eighth of a bf16 output's.  Weights of one term add
+  // what an fp16 output's own rounding adds: two terms where they cost little,
+  // with one column tile (300 positions 5.0 -> 5.2 us; 256 rows behind 30,000, with one
+  // term, would go from 87 to 119).
+  const bool f16 = A.out_type == kRowF16, long_q = A.q_type == kRowF32 || A.rope.at;
+  if (A.out_type == kRowF32 || (f16 && long_q && p.nq == 1)) launch_attend<2, 2>(st, P, R, A, p);
+  else if (f16 && p.nq == 1) launch_tile<1, 2>(st, P, R, A, p);
+  else if (f16 && long_q) launch_tiles<2, 1>(st, P, R, A, p);
   else launch_attend<1, 1>(st, P, R, A, p);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {

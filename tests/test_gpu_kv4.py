@@ -254,6 +254,13 @@ def test_long_tokens_split_over_keys():
     run_case([4111], [3], 1, 8, "f32", "f32", True, seed=6)
 
 
+@pytest.mark.parametrize("seqs,most,hkv,group,t,ot", [(1, 700, 8, 4, "f16", "f16"), (24, 640, 8, 2, "bf16", "bf16"), (40, 1300, 2, 7, "f32", "f32"), (3, 1500, 4, 4, "f32", "f16")])
+def test_tokens_of_ragged_lengths(seqs, most, hkv, group, t, ot):
+    """Lengths from one position to the longest, with wide workgroups and with splits that only the long ones reach."""
+    lens = [most] + [1 + (most - 1) * i // seqs for i in range(seqs - 1)]
+    run_case(lens, [1] * seqs, hkv, group, t, ot, seqs == 24, seed=seqs)
+
+
 def test_scales_of_scores():
     """Steep and flat softmaxes, and queries far from 1."""
     run_case([200], [2], 1, 4, "f32", "f32", False, seed=7, scale=2.0)
