@@ -51,6 +51,7 @@ int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R);  // their workgroups
 // How the attention of these sizes is cut up.
 struct Kv4Plan {
   int nq;      // 16-column tiles of a workgroup
+  bool packed; // two pages side by side in one tile
   int waves;   // of a workgroup
   int tiles;   // column tiles (workgroups) a sequence and kv head
   int splits;  // key splits over workgroups

@@ -484,6 +484,14 @@ __device__ __forceinline__ void keys_of(u32x2 k, unsigned scales, unsigned mask,
   kf[0] = key_frag(k0, mask, f16x2{s[0], s[0]});
   kf[1] = key_frag(k1, mask, f16x2{s[1], s[1]});
 }
+// In steps that mask, of two pages whose scores share an accumulator: keys that
+// would make the other page's scores NaN are zeros.  Returns the lane's four slots that held NaN.
+__device__ __forceinline__ unsigned mask_keys(unsigned& scales, int page, int seen) {
+  const int lane = threadIdx.x & 63;
+  const bool nan = (scales & 0x7c00u) == 0x7c00u || (scales & 0x7c000000u) == 0x7c000000u;
+  if (nan || page * kPage + (lane & 15) >= seen) scales = 0u;
+  return (unsigned)__builtin_amdgcn_ballot_w64(nan) >> (lane >> 4) * 4 & 15u;
+}
 template <bool MASK>
 __device__ __forceinline__ void values_of(u32x2 v, u32x2 scales, unsigned mask, int page, int seen, f16x4* vf,
                                           unsigned* bad) {
@@ -553,11 +561,15 @@ struct Query {
   float qs;  // scores to powers of two
 };
 
+// A lane's column in its tile of 16 / PACK.
+template <int PACK>
+__device__ __forceinline__ int column_of() { return threadIdx.x & (16 / PACK - 1); }
 // Columns behind the last one repeat it (and are not written).
 __device__ __forceinline__ int column_row(const Place& w, int c) { return (unsigned)min(c, w.cols - 1) / w.group; }
 
+template <int PACK>
 __device__ __forceinline__ void load_query(RawQuery& q, const Place& w, const Kv4Attend& A, int tile) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, c = w.c0 + 16 * tile + (lane & 15);
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = w.c0 + 16 * tile + column_of<PACK>();
   const int rw = column_row(w, c), j = min(c, w.cols - 1) - rw * w.G;
   const size_t at = (size_t)(w.s.row0 + rw) * A.q_stride + (w.head * w.G + j) * 64 + 8 * g;
   load_raw(q.row, A.q, at, at + 32, A.q_type);
@@ -607,9 +619,16 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
 }
 
 // A wave's NQ tiles of 16 columns.  PT: fp16 terms of weights.
-template <int NQ, int QT, int PT>
+// PACK: of up to 8 columns, two copies stand side by side, the left one for the
+// first page of a step, the right one for the second, each with zeros in the
+// other's operands.  A lane then has four scores a step, not eight of which half
+// are of no column, and the copies are joined at the end (32 sequences of 4,000
+// positions 22.6 -> 21.6 us, one of 131,072 22.9 -> 22.2; 300 5.2 -> 5.3).
+template <int NQ, int QT, int PT, int PACK>
 struct Columns {
-  Query<QT> q[NQ];
+  static_assert(PACK == 1 || NQ == 1);
+  static constexpr int N = 8 / PACK;  // scores of a lane, step and tile
+  Query<QT> q[NQ * PACK];
   int lim[NQ];  // keys that the column sees
   f32x4 o[NQ][4], sum[NQ];
   float base[NQ];
@@ -623,7 +642,21 @@ struct Columns {
       for (int j = 0; j < 4; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
       sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
       base[t] = 0.f;
-      lim[t] = min(max(w.s.first + column_row(w, w.c0 + 16 * t + (threadIdx.x & 15)) + 1, 0), most);
+      lim[t] = min(max(w.s.first + column_row(w, w.c0 + 16 * t + column_of<PACK>()) + 1, 0), most);
+    }
+  }
+
+  static __device__ __forceinline__ bool right() { return threadIdx.x & 8; }
+  __device__ __forceinline__ void pack(const Query<QT>& z) {
+    const f16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      q[k].qs = z.qs;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        q[k].h[i] = right() == k ? z.h[i] : zero;
+        if constexpr (QT == 2) q[k].l[i] = right() == k ? z.l[i] : zero;
+      }
     }
   }
 
@@ -635,30 +668,32 @@ struct Columns {
     for (int t = 0; t < NQ; ++t)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        sc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4& y = sc[t][PACK == 2 ? 0 : i];
+        const Query<QT>& z = q[PACK == 2 ? i : t];
+        if (PACK == 1 || i == 0) y = f32x4{0.f, 0.f, 0.f, 0.f};
         if constexpr (QT == 2) {
-          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], q[t].l[0], sc[t][i], 0, 0, 0);
-          sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], q[t].l[1], sc[t][i], 0, 0, 0);
+          y = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], z.l[0], y, 0, 0, 0);
+          y = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], z.l[1], y, 0, 0, 0);
         }
-        sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], q[t].h[0], sc[t][i], 0, 0, 0);
-        sc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], q[t].h[1], sc[t][i], 0, 0, 0);
+        y = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][0], z.h[0], y, 0, 0, 0);
+        y = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i][1], z.h[1], y, 0, 0, 0);
       }
   }
 
-  // MASK: slots past a column's keys, and bad (8 bits, see values_of).  The check
+  // MASK: slots past a column's keys, and bad (N bits, see values_of).  The check
   // of all columns' scores is the step's only branch.
   template <bool MASK>
   __device__ __forceinline__ void weights(const f32x4 (*sc)[2], int page, unsigned bad, f16x8* ph, f16x8* pl) {
     const int g = (threadIdx.x & 63) >> 4;
-    float x[NQ][8], high = -INFINITY;
+    float x[NQ][N], high = -INFINITY;
 #pragma unroll
     for (int t = 0; t < NQ; ++t)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < N; ++i) {
         x[t][i] = fmaf(sc[t][i >> 2][i & 3], q[t].qs, -base[t]);
         if constexpr (MASK) {
           if (bad >> i & 1u) x[t][i] = NAN;
-          if ((page + (i >> 2)) * kPage + 4 * g + (i & 3) >= lim[t]) x[t][i] = -INFINITY;
+          if ((page + (PACK == 2 ? right() : i >> 2)) * kPage + 4 * g + (i & 3) >= lim[t]) x[t][i] = -INFINITY;
         }
         high = fmaxf(high, x[t][i]);
       }
@@ -669,7 +704,7 @@ struct Columns {
       for (int t = 0; t < NQ; ++t) {
         float mx = x[t][0];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[t][i]);
+        for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[t][i]);
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
         float up = mx > -INFINITY ? mx - kOffset : 0.f;
@@ -677,7 +712,7 @@ struct Columns {
         const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
         base[t] += up;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[t][i] -= up;
+        for (int i = 0; i < N; ++i) x[t][i] -= up;
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[t][j] *= f;
         sum[t] *= f;
@@ -687,12 +722,21 @@ struct Columns {
 #pragma unroll
     for (int t = 0; t < NQ; ++t)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < N; ++i) {
         const float w = __builtin_amdgcn_exp2f(x[t][i]);
         const _Float16 h = (_Float16)w;
         ph[t][i] = h;
         if constexpr (PT == 2) pl[t][i] = (_Float16)(w - (float)h);
       }
+    if constexpr (PACK == 2) {
+      ph[0] = on_side(ph[0]);
+      if constexpr (PT == 2) pl[0] = on_side(pl[0]);
+    }
+  }
+  // A lane's four weights where its page's values are.
+  static __device__ __forceinline__ f16x8 on_side(const f16x8& w) {
+    const f16x4 zero = {0, 0, 0, 0}, x = {w[0], w[1], w[2], w[3]};
+    return join8(right() ? zero : x, right() ? x : zero);
   }
 
   // vf[dimension of four].  Weights are summed as they enter the products.
@@ -744,7 +788,7 @@ __device__ __forceinline__ void put(const Kv4Rows& R, const Kv4Attend& A, const 
 
 // A workgroup has a tile of 16 NQ columns; its W waves take the tile's keys in
 // turn (two pages a step) and join at the end.
-template <int NQ, int QT, int PT, int W>
+template <int NQ, int QT, int PT, int W, int PACK>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(waves_fit(NQ)))) void
 k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -789,15 +833,17 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   };
   // Of several tiles, each wave makes one's queries for all.
   RawQuery raw;
-  if (NQ == 1 || wave < NQ) load_query(raw, w, A, NQ == 1 ? 0 : wave);
+  if (NQ == 1 || wave < NQ) load_query<PACK>(raw, w, A, NQ == 1 ? 0 : wave);
   PageRegs a[2], c[2];
   unsigned id[2];
   ids(p, id);
   fetch(a, id);
   ids(p + STEP, id);
-  Columns<NQ, QT, PT> C;
+  Columns<NQ, QT, PT, PACK> C;
   C.start(w, most);
-  if constexpr (NQ == 1) {
+  if constexpr (PACK == 2) {
+    C.pack(make_query<QT>(raw, A));
+  } else if constexpr (NQ == 1) {
     C.q[0] = make_query<QT>(raw, A);
   } else {
     __shared__ f16x8 made[NQ][2 * QT][64];
@@ -823,8 +869,13 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
     f16x8 kf[2][2], vf[4];
     f16x4 va[4], vb[4];
     unsigned bad[2] = {0u, 0u};
-    keys_of(pr[0].k, pr[0].ks, mask, kf[0]);
-    keys_of(pr[1].k, pr[1].ks, mask, kf[1]);
+    unsigned ks[2] = {pr[0].ks, pr[1].ks}, bad_key[2] = {0u, 0u};
+    if constexpr (MASK && PACK == 2) {
+      bad_key[0] = mask_keys(ks[0], p, some_see);
+      bad_key[1] = mask_keys(ks[1], p + 1, some_see);
+    }
+    keys_of(pr[0].k, ks[0], mask, kf[0]);
+    keys_of(pr[1].k, ks[1], mask, kf[1]);
     values_of<MASK>(pr[0].v, pr[0].vs, mask, p, some_see, va, &bad[0]);
     values_of<MASK>(pr[1].v, pr[1].vs, mask, p + 1, some_see, vb, &bad[1]);
 #pragma unroll
@@ -832,7 +883,8 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
     f32x4 sc[NQ][2];
     f16x8 ph[NQ], pl[NQ];
     C.scores(kf, sc);
-    C.template weights<MASK>(sc, p, bad[0] | bad[1] << 4, ph, pl);
+    const int side = C.right();
+    C.template weights<MASK>(sc, p, PACK == 2 ? (side ? bad[1] | bad_key[1] : bad[0] | bad_key[0]) : bad[0] | bad[1] << 4, ph, pl);
     C.values(vf, ph, pl);
   };
   {
@@ -888,6 +940,14 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
       l += f * z.y;
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+    }
+    if constexpr (PACK == 2) {
+      const float m2 = fmaxf(m, __shfl_xor(m, 8, 64)), f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - m2) : 0.f;
+      m = m2;
+      l = f * l + __shfl_xor(f * l, 8, 64);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = f * x[j] + __shfl_xor(f * x[j], 8, 64);
+      if (C.right()) continue;
     }
     put<4>(R, A, w, w.c0 + 16 * t + r, 16 * g + 4 * wave, x, l, m, joined, split, splits);
   }
@@ -1023,18 +1083,24 @@ Cuts cuts_of(const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Pl
           div_by(A.hq / P.hkv)};
 }
 
+template <int QT, int PT, int PACK>
+void launch_pack(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
+  const Cuts c = cuts_of(P, R, A, p);
+  if (p.waves == 8) k_kv4_attend<1, QT, PT, 8, PACK><<<c.groups, 512, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  else k_kv4_attend<1, QT, PT, 4, PACK><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+}
+
 template <int QT, int PT>
 void launch_tile(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
-  const Cuts c = cuts_of(P, R, A, p);
-  if (p.waves == 8) k_kv4_attend<1, QT, PT, 8><<<c.groups, 512, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
-  else k_kv4_attend<1, QT, PT, 4><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  if (p.packed) launch_pack<QT, PT, 2>(st, P, R, A, p);
+  else launch_pack<QT, PT, 1>(st, P, R, A, p);
 }
 
 template <int QT, int PT>
 void launch_tiles(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   const Cuts c = cuts_of(P, R, A, p);
-  if (p.nq == 2) k_kv4_attend<2, QT, PT, 4><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
-  else k_kv4_attend<4, QT, PT, 4><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  if (p.nq == 2) k_kv4_attend<2, QT, PT, 4, 1><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  else k_kv4_attend<4, QT, PT, 4, 1><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
 }
 
 template <int QT, int PT>
@@ -1069,6 +1135,7 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t m
   Kv4Plan p;
   const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), seqs = (int64_t)R.n_seqs * P.hkv;
   p.nq = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+  p.packed = cols <= 8;
   const int width = 16 * p.nq;
   const int64_t tiles = (cols + width - 1) / width, outputs = (int64_t)R.n_rows * hq;
   p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);

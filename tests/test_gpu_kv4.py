@@ -309,6 +309,28 @@ def test_rows_that_see_nothing_are_zero():
     assert (out[:2] == 0).all()
 
 
+@pytest.mark.parametrize("rows,group", [(2, 2), (4, 2), (3, 5), (2, 1)])
+@pytest.mark.parametrize("n", [5, 16, 17, 30, 33, 50, 64, 65, 300])
+@pytest.mark.parametrize("t", ["f16", "f32"])
+def test_nan_in_the_last_position_of_few_rows(rows, group, n, t):
+    """Only the last row attends to a key (head 0) or a value (head 1) that is
+    not finite: the others, whose keys share operands with it, are exact."""
+    c = Cache(1, 2, (n + 15) // 16)
+    rng = np.random.default_rng(n)
+    k, v = (rng.standard_normal((n, 2, 64)).astype(np.float32) for _ in "kv")
+    k[n - 1, 0, 40], v[n - 1, 1, 3] = np.inf, np.nan
+    r, keep = c.rows([0, n], [0], n)
+    append(c, r, dev(k), dev(v), "f32")
+    q = torch.randn(rows, 2 * group, 64, device="cuda:0").to(TYPES[t][1])
+    out = torch.empty_like(q)
+    r, keep = c.rows([0, rows], [n - rows], rows)
+    attend(c, r, q, t, out, t)
+    got, qf = out.double().cpu().numpy(), q.double().cpu().numpy()
+    assert np.isnan(got[-1]).all()
+    kz, vz = kv4.values(np.nan_to_num(k, posinf=0)), kv4.values(np.nan_to_num(v))
+    check(got[:-1], qf[:-1], kz, vz, 0.125, n - rows, t)
+
+
 @pytest.mark.parametrize("rows", [30, 200])
 @pytest.mark.parametrize("t", ["f16", "f32"])
 def test_nan_reaches_only_rows_that_attend_to_it(rows, t):
