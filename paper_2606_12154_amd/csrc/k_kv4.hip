@@ -60,6 +60,35 @@ __device__ __forceinline__ Seq load_seq(const Kv4Pool& P, const Kv4Rows& R, int 
   return q;
 }
 
+// Exchanges without LDS.  The lane's number 8 lanes on in its row of 16:
+__device__ __forceinline__ unsigned other8(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, false); }
+__device__ __forceinline__ float other8(float x) { return __uint_as_float(other8(__float_as_uint(x))); }
+// Largest of 8 lanes, ...
+template <int CTRL>
+__device__ __forceinline__ unsigned max_dpp(unsigned x) {
+  return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ unsigned max8(unsigned x) { return max_dpp<0x141>(max_dpp<0x4E>(max_dpp<0xB1>(x))); }
+// ... and of the lanes with one number in the wave's four rows of 16 (and their sum).
+__device__ __forceinline__ unsigned rows_max(unsigned x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  const unsigned y = max((unsigned)a[0], (unsigned)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  return max((unsigned)b[0], (unsigned)b[1]);
+}
+__device__ __forceinline__ float rows_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 // x / d as a product (x < 2^31): the multiplier is 2^(31 + s) / d rounded up, s the
 // least with 2^s >= d, so it is off by less than 2^s / d of 2^-31.
 struct Div {
@@ -186,10 +215,16 @@ __device__ __forceinline__ float group_scale(float a) {
 // Reciprocal of a scale; 0, and hence code 0, for a zero scale or NaN.
 __device__ __forceinline__ float scale_rcp(float s) { return s > 0.f ? __builtin_amdgcn_rcpf(s) : 0.f; }
 
-// n = c + 8 of a finite x: r is scale_rcp(s); s is finite.
-__device__ __forceinline__ unsigned code_of(float x, float s, float r) {
-  return (unsigned)((int)fminf(fmaxf(rintf(quotient(x, s, r)), -7.f), 7.f) + 8);
+// Nibbles c + 8 of four finite elements, a's the lowest: r is scale_rcp(s); s is
+// finite.  (Their number, a sum of at most 30,583, is exact in fp32.)
+__device__ __forceinline__ unsigned codes_of(float a, float b, float c, float d, float s, float r) {
+  auto code = [&](float x) { return __builtin_amdgcn_fmed3f(rintf(quotient(x, s, r)), -7.f, 7.f); };
+  return (unsigned)((int)fmaf(fmaf(fmaf(code(d), 16.f, code(c)), 16.f, code(b)), 16.f, code(a)) + 0x8888);
 }
+
+// Magnitudes as integers have their order, and Inf and NaN above all of them.
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+constexpr unsigned kInfBits = 0x7f800000u;
 
 __device__ __forceinline__ unsigned short half_bits(float s) {
   return __builtin_bit_cast(unsigned short, (_Float16)s);
@@ -240,31 +275,20 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Pool P, Kv4Rows R, const 
         }
       }
     }
-    float top[2] = {0.f, 0.f};
-    int bad = 0;
+    unsigned top[2] = {0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      top[i >> 3] = fmaxf(top[i >> 3], fabsf(x[i]));
-      bad |= !(fabsf(x[i]) < INFINITY);
-    }
-#pragma unroll
-    for (int o = 16; o < 64; o <<= 1) {
-      top[0] = fmaxf(top[0], __shfl_xor(top[0], o, 64));
-      top[1] = fmaxf(top[1], __shfl_xor(top[1], o, 64));
-      bad |= __shfl_xor(bad, o, 64);
-    }
+    for (int i = 0; i < 16; ++i) top[i >> 3] = max(top[i >> 3], magnitude(x[i]));
+    top[0] = rows_max(top[0]);
+    top[1] = rows_max(top[1]);
+    const bool bad = max(top[0], top[1]) >= kInfBits;
     unsigned word[2], sc = 0;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
+      const float s = group_scale(__uint_as_float(top[t])), rs = scale_rcp(s);
+      const float* y = x + 8 * t;
+      const unsigned d = codes_of(y[0], y[2], y[4], y[6], s, rs) | codes_of(y[1], y[3], y[5], y[7], s, rs) << 16;
       // (A row that is not finite: codes of 0.)
-      const float s = bad ? 0.f : group_scale(top[t]), rs = scale_rcp(s);
-      unsigned d = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        d |= code_of(bad ? 0.f : x[8 * t + 2 * j], s, rs) << (4 * j);
-        d |= code_of(bad ? 0.f : x[8 * t + 2 * j + 1], s, rs) << (4 * j + 16);
-      }
-      word[t] = d;
+      word[t] = bad ? 0x88888888u : d;
       sc |= (bad ? 0x7e00u : (unsigned)half_bits(s)) << (16 * t);
     }
     if (mine) {
@@ -281,24 +305,14 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Pool P, Kv4Rows R, const 
     mine[i] = pos >= lo && pos < hi;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
     if (mine[i]) load_row<4>(v, (size_t)(q.row0 + (pos - q.first)) * vs + head * 64 + 4 * r, type, x);
-    float top = 0.f;
-    int bad = 0;
+    unsigned top = 0u;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      top = fmaxf(top, fabsf(x[j]));
-      bad |= !(fabsf(x[j]) < INFINITY);
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      top = fmaxf(top, __shfl_xor(top, o, 64));
-      bad |= __shfl_xor(bad, o, 64);
-    }
-    bad |= __shfl_xor(bad, 8, 64);
-    const float s = bad ? 0.f : group_scale(top), rs = scale_rcp(s);
-    unsigned d = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) d |= code_of(bad ? 0.f : x[j], s, rs) << (4 * j);
-    code[i] = (unsigned short)d;
+    for (int j = 0; j < 4; ++j) top = max(top, magnitude(x[j]));
+    top = max8(top);
+    const bool bad = max(top, other8(top)) >= kInfBits;
+    const float s = group_scale(__uint_as_float(top)), rs = scale_rcp(s);
+    const unsigned d = codes_of(x[0], x[1], x[2], x[3], s, rs);
+    code[i] = (unsigned short)(bad ? 0x8888u : d);
     sc[i] = bad ? 0x7e00u : half_bits(s);
   }
   unsigned short* vb = reinterpret_cast<unsigned short*>(blk + 512) + 4 * lane;
@@ -514,7 +528,7 @@ __device__ __forceinline__ void values_of(u32x2 v, u32x2 scales, unsigned mask, 
   }
   if constexpr (MASK) {
     // Either group of a value row may hold the NaN: lanes r and r ^ 8.
-    *bad = nan4 | (unsigned)__shfl_xor((int)nan4, 8, 64);
+    *bad = nan4 | other8(nan4);
   }
   vf[0] = value_frag<0>(v, mask, s, b);
   vf[1] = value_frag<1>(v, mask, s, b);
@@ -603,8 +617,7 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
   float top = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
-  top = fmaxf(top, __shfl_xor(top, 16, 64));
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  top = rows_max(top);
   int e = 0;
   if (top > 0.f && top < INFINITY) e = 14 - __builtin_amdgcn_frexp_expf(top);
   z.qs = fmaxf(__builtin_amdgcn_ldexpf(A.scale * 1.4426950408889634f, -e), 1e-37f);
@@ -705,8 +718,7 @@ struct Columns {
         float mx = x[t][0];
 #pragma unroll
         for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[t][i]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        mx = rows_max(mx);
         float up = mx > -INFINITY ? mx - kOffset : 0.f;
         if (!first) up = fmaxf(up, 0.f);
         const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
@@ -942,11 +954,11 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
       for (int j = 0; j < 4; ++j) x[j] += f * y[j];
     }
     if constexpr (PACK == 2) {
-      const float m2 = fmaxf(m, __shfl_xor(m, 8, 64)), f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - m2) : 0.f;
+      const float m2 = fmaxf(m, other8(m)), f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - m2) : 0.f;
       m = m2;
-      l = f * l + __shfl_xor(f * l, 8, 64);
+      l = f * l + other8(f * l);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = f * x[j] + __shfl_xor(f * x[j], 8, 64);
+      for (int j = 0; j < 4; ++j) x[j] = f * x[j] + other8(f * x[j]);
       if (C.right()) continue;
     }
     put<4>(R, A, w, w.c0 + 16 * t + r, 16 * g + 4 * wave, x, l, m, joined, split, splits);
@@ -994,8 +1006,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Atten
   float m = -INFINITY;
 #pragma unroll
   for (int k = 0; k < N; ++k) m = fmaxf(m, z[k].x);
-  m = fmaxf(m, __shfl_xor(m, 16, 64));
-  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  m = rows_max(m);
   float x[5] = {0.f, 0.f, 0.f, 0.f, 0.f};  // 4 dimensions and the sum of weights, against m
 #pragma unroll
   for (int k = 0; k < N; ++k) {
@@ -1005,10 +1016,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Atten
     x[4] += f * z[k].y;
   }
 #pragma unroll
-  for (int j = 0; j < 5; ++j) {
-    x[j] += __shfl_xor(x[j], 16, 64);
-    x[j] += __shfl_xor(x[j], 32, 64);
-  }
+  for (int j = 0; j < 5; ++j) x[j] = rows_sum(x[j]);
   __shared__ float xs[4][6][16];
   if (lane < 16) {
 #pragma unroll
