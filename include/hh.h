@@ -356,7 +356,7 @@ typedef struct {
  * negative, or past the page table's max_pages * 16 or rope_len, are skipped.
  * Two rows of one call must not have the same place in the cache.
  * Errors: INVALID_ARG (NULL or misaligned pointers, a size < 1, a stride, an
- * element type), UNSUPPORTED (more than 2^31 - 1 work items), HIP.
+ * element type), UNSUPPORTED (max_rows near 2^28 and above), HIP.
  */
 hh_status hh_kv4_append(const hh_kv4_pool* pool, const hh_kv4_rows* rows, const void* k, const void* v, int32_t dtype,
                         int64_t k_stride, int64_t v_stride, const float* rope, int32_t rope_len, void* hip_stream);
@@ -381,18 +381,20 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
  *            overlap q.  n_heads is a multiple of n_kv_heads.
  *  scale     finite, > 0.
  *  rope      NULL, or as above: queries are rotated at their positions first
- *            (in fp32).
+ *            (in fp32; those from rope_len on as at rope_len - 1).
  *  workspace device, 256-byte aligned, hh_kv4_attention_workspace() bytes (NULL
  *            if that is 0); its contents need not be kept or cleared, and calls
  *            that may run at the same time need one each.
  * Rows at negative positions give 0; rows of `out` in no sequence are left as
  * they are.  Positions past max_pages * 16 - 1 are taken as that.  Sums and
- * softmax are fp32; with an fp32 `out` the products take fp16 pairs (22 bits)
- * of queries and weights, with a 16-bit one the weights are single fp16 numbers,
- * 2^-12 off at most (pairs with an fp16 `out` where a sequence has up to 16
- * rows times n_heads / n_kv_heads).  Equal calls give equal bits.
+ * softmax are fp32.  In the products, with an fp32 `out` queries and weights
+ * are fp16 pairs (22 bits).  With a 16-bit one weights are single fp16 numbers, 2^-12
+ * off at most, and so are queries (scaled by a power of two; 16-bit ones that are not rotated
+ * are exact), but with an fp16 `out` fp32 and rotated queries are pairs, and so
+ * are weights where max_rows * n_heads / n_kv_heads is at most 16.  Equal calls
+ * give equal bits.
  * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
- * UNSUPPORTED (more than 2^31 - 1 workgroups), HIP.
+ * UNSUPPORTED (max_rows * n_heads near 2^30 and above), HIP.
  */
 hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, const void* q, int32_t q_dtype,
                            int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len,

@@ -24,6 +24,7 @@ struct Kv4Rows {
   const int* first_pos;
   const int* table_row;
   int n_seqs, n_rows, max_rows;
+  int seq0 = 0;  // a launch's first sequence
 };
 
 // fp32 (cos, sin) at [position][pair], or null.
@@ -42,11 +43,14 @@ struct Kv4Attend {
   float* part;  // workspace: split outputs and statistics
 };
 
-hipError_t kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
-                      int64_t k_stride, int64_t v_stride, RopeTable rope);
-hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
-                    int64_t v_stride);
-int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R);  // their workgroups: callers refuse what does not fit a grid
+// These three launch and leave the launch's status to the caller (hipGetLastError).
+// Callers refuse sequences whose grid has more than kMaxThreads.
+constexpr int64_t kMaxThreads = UINT32_MAX;
+void kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
+                int64_t k_stride, int64_t v_stride, RopeTable rope);
+void kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
+              int64_t v_stride);
+int64_t kv4_row_threads(const Kv4Pool& P, const Kv4Rows& R);  // of a sequence, append and read
 
 // How the attention of these sizes is cut up.
 struct Kv4Plan {
@@ -55,12 +59,12 @@ struct Kv4Plan {
   int waves;   // of a workgroup
   int tiles;   // column tiles (workgroups) a sequence and kv head
   int splits;  // key splits over workgroups
-  int64_t groups;    // the larger grid: callers refuse what does not fit
+  int64_t threads;   // of a sequence's larger grid
   size_t workspace;  // bytes
 };
 // pages: a bound of the pages that a sequence holds; most_bytes: of the workspace.
 Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes = SIZE_MAX);
-hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
+void kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
 
 // n_layers pools of pages of `bytes` (a multiple of 16), layer_stride bytes apart.
 struct PagePool {

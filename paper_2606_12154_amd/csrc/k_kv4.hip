@@ -243,12 +243,12 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Pool P, Kv4Rows R, const 
   if (head >= P.hkv) return;
   const unsigned sq = blockIdx.x / (unsigned)tiles;
   const int tile = blockIdx.x - sq * tiles;
-  const Seq q = load_seq(P, R, sq);
+  const Seq q = load_seq(P, R, R.seq0 + sq);
   const int lo = max(q.first, 0);
   int hi = min(q.first + q.n, P.max_pages * kPage);
   if (rope.at) hi = min(hi, rope.len);
   const int page = lo / kPage + tile;
-  if (page * kPage >= hi) return;
+  if (page >= (hi + kPage - 1) >> 4) return;  // (page * kPage may pass 31 bits)
   const int id = P.table[(size_t)q.trow * P.max_pages + page];
   if ((unsigned)id >= (unsigned)P.n_pages) return;
   unsigned char* blk = P.pool + ((size_t)id * P.hkv + head) * kKv4Block;
@@ -342,10 +342,10 @@ __global__ __launch_bounds__(256) void k_kv4_read(Kv4Pool P, Kv4Rows R, void* __
   if (head >= P.hkv) return;
   const unsigned sq = blockIdx.x / (unsigned)tiles;
   const int tile = blockIdx.x - sq * tiles;
-  const Seq q = load_seq(P, R, sq);
+  const Seq q = load_seq(P, R, R.seq0 + sq);
   const int page = (q.first >> 4) + tile;  // floor
   const int hi = q.first + q.n;
-  if (page * kPage >= hi) return;
+  if (page >= (hi + kPage - 1) >> 4) return;  // (page * kPage may pass 31 bits)
   const bool held = page >= 0 && page < P.max_pages;
   const unsigned char* blk =
       block_of(P, P.table + (size_t)q.trow * P.max_pages, held ? page : 0, head);
@@ -809,7 +809,7 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   const int split = b1 - b2 * splits_.d, splits = splits_.d;
   // The last tiles have the most keys: they go first.
   const int tile = tiles_.d - 1 - (b2 - sq * tiles_.d);
-  const Seq s = load_seq(P, R, sq);
+  const Seq s = load_seq(P, R, R.seq0 + sq);
   const int G = group.d, cols = s.n * G;  // below 2^31 with a tile to spare (kv4_plan)
   const Place w{s, (int)(blockIdx.x - b1 * heads.d), G, cols, tile * (16 * NQ), group};
   if (w.c0 >= cols) return;
@@ -982,7 +982,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(Kv4Pool P, Kv4Rows R, Kv4Atten
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned b = blockIdx.x, row = b / (unsigned)A.hq;
   const int hd = b - row * A.hq, i = row % (unsigned)R.max_rows;
-  const Seq s = load_seq(P, R, row / (unsigned)R.max_rows);
+  const Seq s = load_seq(P, R, R.seq0 + row / (unsigned)R.max_rows);
   if (i >= s.n) return;
   const int G = A.hq / P.hkv;
   const int n = splits_of(P, s, G, i * G + hd % G, tile_cols, splits);
@@ -1049,7 +1049,7 @@ __global__ __launch_bounds__(256) void k_kv4_join_rows(Kv4Pool P, Kv4Rows R, Kv4
   const unsigned sq = row / (unsigned)R.max_rows;
   // (No early return: the lanes of a wave exchange below.)
   const bool in = sq < (unsigned)R.n_seqs;
-  const Seq s = load_seq(P, R, in ? sq : 0);
+  const Seq s = load_seq(P, R, R.seq0 + (in ? sq : 0));
   const int G = A.hq / P.hkv;
   const int n = in && i < s.n ? splits_of(P, s, G, i * G + hd % G, tile_cols, splits) : 1;
   const size_t at = (size_t)(s.row0 + (n > 1 ? i : 0)) * A.hq + hd, step = (size_t)R.n_rows * A.hq;
@@ -1119,29 +1119,44 @@ void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4
 
 }  // namespace
 
-int64_t kv4_row_groups(const Kv4Pool& P, const Kv4Rows& R) { return (int64_t)R.n_seqs * row_tiles(R); }
+// A launch has fewer than 2^32 threads: as many sequences as fit (those with
+// fewer rows than the longest have workgroups that end at once).
+template <typename F>
+static void by_sequences(const Kv4Rows& R, int64_t threads_each, F launch) {
+  Kv4Rows r = R;
+  const int most = (int)std::max<int64_t>(1, std::min<int64_t>(R.n_seqs, kMaxThreads / threads_each));
+  for (int s = 0; s < R.n_seqs; s += r.n_seqs) {
+    r.seq0 = s;
+    r.n_seqs = std::min(most, R.n_seqs - s);
+    launch(r);
+  }
+}
 
 // A wave a (page, head).  Workgroups of one wave while each CU gets a few of them,
 // or else of four heads, whose rows are neighbours (append and read: 32 tokens 6.9 us
 // against 8.1, 1,024 rows 9.0 and 9.3, 2,048 rows 11.7 and 10.8, 8,192 21.6 and 20.9).
 static int row_heads(const Kv4Pool& P, const Kv4Rows& R) {
-  return kv4_row_groups(P, R) * P.hkv <= 1024 ? 1 : std::min(P.hkv, 4);
+  return (int64_t)R.n_seqs * row_tiles(R) * P.hkv <= 1024 ? 1 : std::min(P.hkv, 4);
 }
-static dim3 row_grid(const Kv4Pool& P, const Kv4Rows& R) {
+int64_t kv4_row_threads(const Kv4Pool& P, const Kv4Rows& R) { return (int64_t)row_tiles(R) * 64 * row_heads(P, R); }
+static dim3 row_grid(const Kv4Pool& P, const Kv4Rows& R, int heads) {
+  return dim3((unsigned)R.n_seqs * (unsigned)row_tiles(R), (unsigned)((P.hkv + heads - 1) / heads));
+}
+
+void kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
+                int64_t k_stride, int64_t v_stride, RopeTable rope) {
   const int h = row_heads(P, R);
-  return dim3((unsigned)kv4_row_groups(P, R), (unsigned)((P.hkv + h - 1) / h));
+  by_sequences(R, kv4_row_threads(P, R), [&](const Kv4Rows& r) {
+    k_kv4_append<<<row_grid(P, r, h), 64 * h, 0, st>>>(P, r, k, v, type, k_stride, v_stride, rope, row_tiles(r));
+  });
 }
 
-hipError_t kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
-                      int64_t k_stride, int64_t v_stride, RopeTable rope) {
-  k_kv4_append<<<row_grid(P, R), 64 * row_heads(P, R), 0, st>>>(P, R, k, v, type, k_stride, v_stride, rope, row_tiles(R));
-  return hipGetLastError();
-}
-
-hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
-                    int64_t v_stride) {
-  k_kv4_read<<<row_grid(P, R), 64 * row_heads(P, R), 0, st>>>(P, R, k, v, type, k_stride, v_stride, row_tiles(R));
-  return hipGetLastError();
+void kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
+              int64_t v_stride) {
+  const int h = row_heads(P, R);
+  by_sequences(R, kv4_row_threads(P, R), [&](const Kv4Rows& r) {
+    k_kv4_read<<<row_grid(P, r, h), 64 * h, 0, st>>>(P, r, k, v, type, k_stride, v_stride, row_tiles(r));
+  });
 }
 
 Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes) {
@@ -1153,36 +1168,34 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t m
   const int64_t tiles = (cols + width - 1) / width, outputs = (int64_t)R.n_rows * hq;
   p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
   cut_keys(p.nq, tiles * seqs, pages, outputs, most_bytes, &p.waves, &p.splits);
-  const int64_t join = p.splits > 1 ? (int64_t)R.n_seqs * R.max_rows * hq : 0;
   // (Columns are counted in 32 bits.)
-  p.groups = cols > INT32_MAX - 1024 ? cols : std::max(seqs * tiles * p.splits, join);
+  p.threads = cols > INT32_MAX - 1024 ? INT64_MAX : tiles * P.hkv * p.splits * 64 * p.waves;
+  if (p.splits > 1) p.threads = std::max(p.threads, (int64_t)R.max_rows * hq * 256);
   p.workspace = p.splits > 1 ? split_bytes(p.splits, outputs) : 0;
   return p;
 }
 
-hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
+void kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers, whose
   // rounding to 11 bits is an eighth of a bf16 output's.  Weights of one term add
   // what an fp16 output's own rounding adds: two terms where they cost little,
   // with one column tile (300 positions 5.0 -> 5.2 us; 256 rows behind 30,000, with one
   // term, would go from 87 to 119).
   const bool f16 = A.out_type == kRowF16, long_q = A.q_type == kRowF32 || A.rope.at;
-  if (A.out_type == kRowF32 || (f16 && long_q && p.nq == 1)) launch_attend<2, 2>(st, P, R, A, p);
-  else if (f16 && p.nq == 1) launch_tile<1, 2>(st, P, R, A, p);
-  else if (f16 && long_q) launch_tiles<2, 1>(st, P, R, A, p);
-  else launch_attend<1, 1>(st, P, R, A, p);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && p.splits > 1) {
-    const int64_t outs = (int64_t)R.n_seqs * R.max_rows * A.hq;
+  by_sequences(R, p.threads, [&](const Kv4Rows& r) {
+    if (A.out_type == kRowF32 || (f16 && long_q && p.nq == 1)) launch_attend<2, 2>(st, P, r, A, p);
+    else if (f16 && p.nq == 1) launch_tile<1, 2>(st, P, r, A, p);
+    else if (f16 && long_q) launch_tiles<2, 1>(st, P, r, A, p);
+    else launch_attend<1, 1>(st, P, r, A, p);
+    if (p.splits == 1) return;
+    const int64_t outs = (int64_t)r.n_seqs * r.max_rows * A.hq;
     // Five and more splits of few rows are read at once by a workgroup each (one row of
     // 32 heads, 16 splits: 7.5 us with the attention, 8.6 by 16 lanes each; 16 rows, 8
     // splits: 10.7 and 10.6); fewer splits or more rows want fewer workgroups (64 rows, 2
     // splits: 16.1 and 13.1).
-    if (p.splits > 16 || (p.splits > 4 && outs <= 512)) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
-    else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, R, A, 16 * p.nq, p.splits);
-    e = hipGetLastError();
-  }
-  return e;
+    if (p.splits > 16 || (p.splits > 4 && outs <= 512)) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, r, A, 16 * p.nq, p.splits);
+    else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, r, A, 16 * p.nq, p.splits);
+  });
 }
 
 }  // namespace hh

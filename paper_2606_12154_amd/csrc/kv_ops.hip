@@ -79,8 +79,9 @@ hh_status hh_kv4_append(const hh_kv4_pool* pool, const hh_kv4_rows* rows, const 
   if (!aligned(k, 16) || !aligned(v, 16) || !row_stride(k_stride, n, size) || !row_stride(v_stride, n, size) ||
       !rope_table(rope, rope_len, &T))
     return HH_ERR_INVALID_ARG;
-  if (kv4_row_groups(P, R) > INT32_MAX) return HH_ERR_UNSUPPORTED;
-  return from_hip(kv4_append(static_cast<hipStream_t>(hip_stream), P, R, k, v, type, k_stride, v_stride, T));
+  if (kv4_row_threads(P, R) > kMaxThreads) return HH_ERR_UNSUPPORTED;
+  kv4_append(static_cast<hipStream_t>(hip_stream), P, R, k, v, type, k_stride, v_stride, T);
+  return from_hip(hipGetLastError());
 }
 
 hh_status hh_kv4_read(const hh_kv4_pool* pool, const hh_kv4_rows* rows, void* k, void* v, int32_t dtype,
@@ -93,8 +94,9 @@ hh_status hh_kv4_read(const hh_kv4_pool* pool, const hh_kv4_rows* rows, void* k,
   const int64_t n = (int64_t)P.hkv * 64;
   if (!aligned(k, 16) || !aligned(v, 16) || !row_stride(k_stride, n, size) || !row_stride(v_stride, n, size))
     return HH_ERR_INVALID_ARG;
-  if (kv4_row_groups(P, R) > INT32_MAX) return HH_ERR_UNSUPPORTED;
-  return from_hip(kv4_read(static_cast<hipStream_t>(hip_stream), P, R, k, v, type, k_stride, v_stride));
+  if (kv4_row_threads(P, R) > kMaxThreads) return HH_ERR_UNSUPPORTED;
+  kv4_read(static_cast<hipStream_t>(hip_stream), P, R, k, v, type, k_stride, v_stride);
+  return from_hip(hipGetLastError());
 }
 
 hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows* rows, int32_t n_heads, size_t* bytes) {
@@ -102,7 +104,7 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
   Kv4Rows R;
   if (!bytes || !describe(pool, rows, &P, &R) || n_heads < 1 || n_heads % P.hkv != 0) return HH_ERR_INVALID_ARG;
   const Kv4Plan plan = kv4_plan(P, R, n_heads, P.max_pages);
-  if (plan.groups > INT32_MAX) return HH_ERR_UNSUPPORTED;
+  if (plan.threads > kMaxThreads) return HH_ERR_UNSUPPORTED;
   *bytes = plan.workspace;
   return HH_OK;
 }
@@ -124,7 +126,7 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
       !(scale > 0.f) || !std::isfinite(scale))
     return HH_ERR_INVALID_ARG;
   const Kv4Plan plan = kv4_plan(P, R, n_heads, P.max_pages);
-  if (plan.groups > INT32_MAX) return HH_ERR_UNSUPPORTED;
+  if (plan.threads > kMaxThreads) return HH_ERR_UNSUPPORTED;
   if (plan.workspace && (!aligned(workspace, 256) || workspace_bytes < plan.workspace)) return HH_ERR_INVALID_ARG;
   A.q = q;
   A.out = out;
@@ -133,7 +135,8 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
   A.hq = n_heads;
   A.scale = scale;
   A.part = static_cast<float*>(workspace);
-  return from_hip(kv4_attend(static_cast<hipStream_t>(hip_stream), P, R, A, plan));
+  kv4_attend(static_cast<hipStream_t>(hip_stream), P, R, A, plan);
+  return from_hip(hipGetLastError());
 }
 
 hh_status hh_kv_copy_pages(void* pool, int32_t n_layers, int64_t layer_stride, int64_t page_bytes, int32_t n_pages,

@@ -254,6 +254,33 @@ def test_long_tokens_split_over_keys():
     run_case([4111], [3], 1, 8, "f32", "f32", True, seed=6)
 
 
+def test_more_sequences_than_a_launch_takes():
+    """1,100 sequences of up to 2^20 rows by the description (most have none):
+    2^32 threads and more, which two launches of each call share."""
+    n_seqs, most = 1100, 1 << 20
+    lens = np.zeros(n_seqs, int)
+    lens[[0, 7, 1022, 1023, 1024, 1099]] = [3, 1, 4, 2, 1, 5]
+    start = np.concatenate([[0], np.cumsum(lens)])
+    n = int(start[-1])
+    c = Cache(n_seqs, 1, 2)
+    rng = np.random.default_rng(11)
+    k, v = (rng.standard_normal((n, 1, 64)).astype(np.float32) for _ in "kv")
+    keep = [ints(start), ints(np.zeros(n_seqs))]
+    r = hh.hh_kv4_rows(keep[0].data_ptr(), keep[1].data_ptr(), None, n_seqs, n, most)
+    append(c, r, dev(k), dev(v), "f32")
+    back = [torch.full((n, 1, 64), 9.0, device="cuda:0") for _ in "kv"]
+    hh.hh_kv4_read(c.desc, r, back[0].data_ptr(), back[1].data_ptr(), hh.HH_F32, 64, 64, stream())
+    for got, x in zip(back, (k, v)):
+        assert np.array_equal(got.double().cpu().numpy(), kv4.values(x))
+    q = torch.randn(n, 1, 64, device="cuda:0")
+    out = torch.full_like(q, 9.0)
+    attend(c, r, q, "f32", out, "f32")
+    got, qf = out.double().cpu().numpy(), q.double().cpu().numpy()
+    for i in np.flatnonzero(lens):
+        rows = slice(start[i], start[i + 1])
+        check(got[rows], qf[rows], kv4.values(k[rows]), kv4.values(v[rows]), 0.125, 0, "f32")
+
+
 @pytest.mark.parametrize("seqs,most,hkv,group,t,ot", [(1, 700, 8, 4, "f16", "f16"), (24, 640, 8, 2, "bf16", "bf16"), (40, 1300, 2, 7, "f32", "f32"), (3, 1500, 4, 4, "f32", "f16")])
 def test_tokens_of_ragged_lengths(seqs, most, hkv, group, t, ot):
     """Lengths from one position to the longest, with wide workgroups and with splits that only the long ones reach."""
