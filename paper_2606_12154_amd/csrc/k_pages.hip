@@ -212,21 +212,27 @@ int pieces_of(const PagePool& P) { return (int)((P.bytes + kPiece - 1) / kPiece)
 hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst, bool once) {
   once = once && n * P.bytes * P.n_layers > kCached;
   const int pieces = pieces_of(P);
-  // Pairs of a launch, so that its workgroups stay within a grid.
-  const int64_t each = (int64_t)pieces * P.n_layers;
-  const int most = (int)std::max<int64_t>(1, std::min<int64_t>(kPairs, ((int64_t)1 << 31) / each));
-  for (int o = 0; o < n; o += most) {
-    PairArgs a;
-    a.n = std::min(most, n - o);
-    for (int i = 0; i < a.n; ++i) {
-      a.src[i] = src[o + i];
-      a.dst[i] = dst[o + i];
+  // Layers and pairs of a launch, which has fewer than 2^32 threads.
+  constexpr int64_t kWaves = 1 << 25;
+  const int layers = (int)std::min<int64_t>(P.n_layers, kWaves / pieces);  // (a page has 2^15 pieces at most)
+  const int most = (int)std::min<int64_t>(kPairs, kWaves / pieces / layers);
+  for (int l = 0; l < P.n_layers; l += layers) {
+    PagePool Q = P;
+    Q.pool += l * P.layer_stride;
+    Q.n_layers = std::min(layers, P.n_layers - l);
+    for (int o = 0; o < n; o += most) {
+      PairArgs a;
+      a.n = std::min(most, n - o);
+      for (int i = 0; i < a.n; ++i) {
+        a.src[i] = src[o + i];
+        a.dst[i] = dst[o + i];
+      }
+      const unsigned groups = (unsigned)(((int64_t)a.n * pieces * Q.n_layers + 3) / 4);
+      if (once) k_copy_pages<true><<<groups, 256, 0, st>>>(Q, pieces, a);
+      else k_copy_pages<false><<<groups, 256, 0, st>>>(Q, pieces, a);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
     }
-    const unsigned groups = (unsigned)((a.n * each + 3) / 4);
-    if (once) k_copy_pages<true><<<groups, 256, 0, st>>>(P, pieces, a);
-    else k_copy_pages<false><<<groups, 256, 0, st>>>(P, pieces, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
