@@ -127,6 +127,22 @@ def test_append_bytes_and_read(t, rope, lens, first):
         assert np.array_equal(got.double().cpu().numpy(), ref.double().numpy(), equal_nan=True)
 
 
+@pytest.mark.parametrize("hkv", [3, 5, 8])
+def test_many_rows_of_several_heads_a_workgroup(hkv):
+    lens, first = [4000, 1, 1700, 33], [3, 40, 0, 15]
+    n = sum(lens)
+    c = Cache(4, hkv, 256)
+    k, v = (torch.randn(n, hkv, 64, device="cuda:0") for _ in "kv")
+    r, keep = c.rows(np.concatenate([[0], np.cumsum(lens)]), first, n)
+    append(c, r, k, v, "f32")
+    back = [torch.full_like(k, 9.0) for _ in "kv"]
+    hh.hh_kv4_read(c.desc, r, back[0].data_ptr(), back[1].data_ptr(), hh.HH_F32, hkv * 64, hkv * 64, stream())
+    for got, x in zip(back, (k, v)):
+        assert np.array_equal(got.double().cpu().numpy(), kv4.values(x.cpu().numpy()))
+    held = (c.pool != 255).any(-1).all(-1).sum().item()
+    assert held == sum((f + m - 1) // 16 - f // 16 + 1 for f, m in zip(first, lens))
+
+
 def test_rows_that_are_not_finite_read_as_nan():
     c = Cache(1, 2, 2)
     k, v = (torch.randn(20, 2, 64, device="cuda:0") for _ in "kv")
