@@ -391,8 +391,7 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
  * are fp16 pairs (22 bits).  With a 16-bit one weights are single fp16 numbers, 2^-12
  * off at most, and so are queries (scaled by a power of two; 16-bit ones that are not rotated
  * are exact), but with an fp16 `out` fp32 and rotated queries are pairs, and so
- * are weights where max_rows * n_heads / n_kv_heads is at most 16.  Equal calls
- * give equal bits.
+ * are weights in calls with few rows.  Equal calls give equal bits.
  * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
  * UNSUPPORTED (max_rows * n_heads near 2^30 and above), HIP.
  */

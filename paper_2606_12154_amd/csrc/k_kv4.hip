@@ -17,6 +17,12 @@
 // 4 (l / 16) + i), leave each lane with the slots of both pages that its value
 // bytes hold; with the contraction of O^T[dim][query] += V^T P^T taken in that
 // order, weights go from accumulators to operands within their lanes.
+//
+// What bounds it (counters): vector instructions.  A step of two pages takes a
+// wave about 110 of them to unpack, 3.5 (exponentials count as four) a score
+// and lane, and 9 matrix instructions a column tile; the two kinds hardly run at
+// once.  One sequence of 131,072 positions (75 MB; 32 query heads on 8) takes 22 us,
+// 3.4 TB/s; an 8,192-token prompt 345 us, 0.8 PFLOP/s.
 #include "hh_device.h"
 #include "hh_kv.h"
 
@@ -401,43 +407,6 @@ constexpr int kMaxSplits = 64;
 constexpr int waves_fit(int nq) { return nq == 1 ? 4 : nq == 2 ? 3 : 2; }
 // Workspace of s splits: 64 dimensions, base and sum of weights each.
 size_t split_bytes(int s, int64_t outputs) { return (size_t)s * (size_t)outputs * (64 + 2) * sizeof(float); }
-
-// Waves of a workgroup (4, or 8 with one column tile) and key splits over
-// workgroups for `groups` (sequence, kv head, column tile)s over up to `pages`
-// pages: those of the least time by what was measured, in ns (32 query heads on
-// 8; an error of 11%).  A step (two pages) takes a wave that is alone on its SIMD 740 ns with one
-// column tile (720 with two, 960 with four), and 255 (400, 536) more for each
-// neighbour, of which a SIMD has up to three (two, one).  What comes before and
-// after is 3.6 us (4.5), and 0.9 (0.5) more for each neighbour; the join 3 us, and its
-// reads.  So one sequence of 700 positions is not split (6.2 us with eight
-// waves, 6.6 with four, 7.3 in 4 splits); 3,000 take splits of four waves (7.8; one of eight
-// 13.1), 32,768 32 splits of eight (11.7; of four 13.0); 32 sequences of 1,500 take eight
-// waves (12.2; four 16.1, in 4 splits 14.3), 128 of 1,000 four (19.8; eight
-// 22.5); 256 rows behind 30,000 positions 4 splits (87; 2 splits 118, 8 splits 99).
-void cut_keys(int nq, int64_t groups, int pages, int64_t outputs, size_t most_bytes, int* waves, int* splits) {
-  const int fit = waves_fit(nq);
-  const double alone = nq == 1 ? 740 : nq == 2 ? 720 : 960, more = nq == 1 ? 255 : nq == 2 ? 400 : 536;
-  const double ends = nq == 1 ? 3600 : 4500, near = nq == 1 ? 900 : 500;
-  const int pairs = std::max(1, (pages + 1) / 2), most = std::max(1, std::min(kMaxSplits, pairs / 4));
-  double best = 0;
-  for (int w = 4; w <= (nq == 1 ? 8 : 4); w += 4) {
-    for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= most_bytes); ++s) {
-      const int per = (pairs + s - 1) / s;
-      const double here = std::ceil((double)groups * s / 256);                    // workgroups a CU
-      const double held = std::min<double>(fit, here * w / 4) - 1;                // a wave's neighbours,
-      const double busy = std::max(1.0, here * std::min(w, per) / 4);             // and those with keys
-      const double step = (alone + more * (std::min<double>(busy, fit) - 1)) * std::max(1.0, busy / fit);
-      double ns = ends * std::ceil(here * w / (4 * fit)) + near * held + step * ((per + w - 1) / w);
-      if (w > 4) ns -= 200;  // (their waves start and end together)
-      if (s > 1) ns += 3000 + 0.09 * (double)outputs * s;
-      if (best == 0 || ns < best) {
-        best = ns;
-        *waves = w;
-        *splits = s;
-      }
-    }
-  }
-}
 
 // Pages of a split, given the pages that a column tile attends to: whole steps of two.
 __device__ __forceinline__ int split_pages(int np, int splits) {
@@ -1159,15 +1128,81 @@ void kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void*
   });
 }
 
+// Column tiles and waves of a workgroup and key splits over workgroups: those of
+// the least time by what was measured, in ns (32 query heads on 8, every type; the
+// choices cost 1% on average against the best ones, 7% at most).  A step (two
+// pages) takes a wave that is alone on its SIMD 740 ns with one column tile, 860
+// with two and 1,250 with four, and 255, 310 and 430 more for each neighbour there, of
+// which there are up to three, two and one.  What comes before and after is 3.6,
+// 6 and 8.1 us, and 0.9, 0.3 and 0.45 more for each neighbour; the join 3 us, and its
+// reads.  So 2,000 prompt rows take four tiles (bf16: 38 us; two 43, one 56), 1,200 two
+// (22.0; four 22.8, one 27), 300 one (7.3; two 7.9, four 9.9), 8 sequences of 64 rows
+// behind 1,000 positions two (21.3; four 22.2, one 23.6).  One token at 700
+// positions is not split (6.2 with eight waves, 6.6 with four, 7.3 in 4 splits); at
+// 3,000 it takes splits of four waves (7.8; one of eight 13.1), at 32,768 32 splits
+// of eight (11.7; of four 13.0); 32 tokens at 1,500 take eight waves (12.2; four 16.1,
+// in 4 splits 14.3), 128 at 1,000 four (19.8; eight 22.5).  Eight waves are for
+// sequences of one tile.
+struct Cut {
+  int nq, waves, splits;
+};
+static Cut cut(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes) {
+  struct Cost {
+    int nq;
+    double alone, more, ends, near;
+  };
+  constexpr Cost kCosts[] = {{1, 740, 255, 3600, 900}, {2, 860, 310, 6000, 300}, {4, 1250, 430, 8100, 450}};
+  const int group = hq / P.hkv;
+  const int64_t cols = (int64_t)R.max_rows * group, outputs = (int64_t)R.n_rows * hq;
+  const double mean_cols = (double)R.n_rows * group / R.n_seqs;
+  const int pairs = std::max(1, (pages + 1) / 2), most = std::max(1, std::min(kMaxSplits, pairs / 4));
+  // Pairs that a tile attends to on average: a causal prompt's see half.
+  const double mean_pairs = std::max(pages - R.max_rows / 32.0, pages / 2.0) / 2;
+  const double even = 4 * mean_pairs / std::max(pages, 1) - 1;  // 1: all tiles alike, 0: from none to all
+  Cut best{};
+  double best_ns = 0;
+  for (const Cost& c : kCosts) {
+    if (c.nq > 1 && cols <= 8 * c.nq) break;  // half of its columns would be none
+    const double seqs = (double)R.n_seqs * P.hkv * std::max(1.0, std::ceil(mean_cols / (16 * c.nq)));
+    const int fit = waves_fit(c.nq);
+    for (int w = 4; w <= (cols <= 16 ? 8 : 4); w += 4) {
+      for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= most_bytes); ++s) {
+        const int per = (pairs + s - 1) / s, steps = (per + w - 1) / w;
+        const double here = std::max(1.0, seqs * s / 256);          // workgroups a CU gets
+        const double load = here * w / 4, held = std::min<double>(fit, std::ceil(load));  // waves a SIMD, and at once
+        const double busy = std::min<double>(fit, std::max(1.0, std::ceil(load * std::min(w, per) / w)));  // with keys
+        auto step = [&](double waves) { return c.alone + c.more * (waves - 1); };
+        // A wave's steps are the longest one's at least.  More waves than fit come in
+        // turns, which end together where all have as many keys, and even out in a prompt.
+        double each = load > held ? step(held) * load / held : step(busy);
+        if (load > fit) {
+          const double turns = std::floor(std::ceil(here) * w / 4 / fit), rest = std::ceil(here) * w / 4 - turns * fit;
+          each += even * std::max(0.0, turns * step(fit) + (rest > 0 ? step(rest) : 0) - each);
+        }
+        double ns = c.ends + c.near * (held - 1) + 0.3 * c.ends * std::max(0.0, load / fit - 1) +
+                    std::max(step(busy) * steps, each * std::max(1.0, mean_pairs / s / w));
+        if (w > 4) ns -= s == 1 ? 700 : 200;  // (their waves start and end together)
+        if (s > 1) ns += 3000 + 0.09 * (double)outputs * s;
+        if (best.nq == 0 || ns < best_ns) {
+          best = Cut{c.nq, w, s};
+          best_ns = ns;
+        }
+      }
+    }
+  }
+  return best;
+}
+
 Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes) {
   Kv4Plan p;
-  const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), seqs = (int64_t)R.n_seqs * P.hkv;
-  p.nq = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+  const Cut c = cut(P, R, hq, pages, most_bytes);
+  const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), outputs = (int64_t)R.n_rows * hq;
+  p.nq = c.nq;
+  p.waves = c.waves;
+  p.splits = c.splits;
   p.packed = cols <= 8;
-  const int width = 16 * p.nq;
-  const int64_t tiles = (cols + width - 1) / width, outputs = (int64_t)R.n_rows * hq;
+  const int64_t tiles = (cols + 16 * p.nq - 1) / (16 * p.nq);
   p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-  cut_keys(p.nq, tiles * seqs, pages, outputs, most_bytes, &p.waves, &p.splits);
   // (Columns are counted in 32 bits.)
   p.threads = cols > INT32_MAX - 1024 ? INT64_MAX : tiles * P.hkv * p.splits * 64 * p.waves;
   if (p.splits > 1) p.threads = std::max(p.threads, (int64_t)R.max_rows * hq * 256);
