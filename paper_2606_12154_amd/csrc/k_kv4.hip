@@ -1146,6 +1146,11 @@ void kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void*
 struct Cut {
   int nq, waves, splits;
 };
+// Sizes here are far below 2^63.
+static double up(double x) {
+  const double y = (double)(int64_t)x;
+  return y < x ? y + 1 : y;
+}
 static Cut cut(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes) {
   struct Cost {
     int nq;
@@ -1163,20 +1168,21 @@ static Cut cut(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t mos
   double best_ns = 0;
   for (const Cost& c : kCosts) {
     if (c.nq > 1 && cols <= 8 * c.nq) break;  // half of its columns would be none
-    const double seqs = (double)R.n_seqs * P.hkv * std::max(1.0, std::ceil(mean_cols / (16 * c.nq)));
+    const double seqs = (double)R.n_seqs * P.hkv * std::max(1.0, up(mean_cols / (16 * c.nq)));
     const int fit = waves_fit(c.nq);
     for (int w = 4; w <= (cols <= 16 ? 8 : 4); w += 4) {
-      for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= most_bytes); ++s) {
+      // (Every number up to 16, then less dense: this runs at each call.)
+      for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= most_bytes); s += s < 16 ? 1 : s < 32 ? 2 : 4) {
         const int per = (pairs + s - 1) / s, steps = (per + w - 1) / w;
         const double here = std::max(1.0, seqs * s / 256);          // workgroups a CU gets
-        const double load = here * w / 4, held = std::min<double>(fit, std::ceil(load));  // waves a SIMD, and at once
-        const double busy = std::min<double>(fit, std::max(1.0, std::ceil(load * std::min(w, per) / w)));  // with keys
+        const double load = here * w / 4, held = std::min<double>(fit, up(load));  // waves a SIMD, and at once
+        const double busy = std::min<double>(fit, std::max(1.0, up(load * std::min(w, per) / w)));  // with keys
         auto step = [&](double waves) { return c.alone + c.more * (waves - 1); };
         // A wave's steps are the longest one's at least.  More waves than fit come in
         // turns, which end together where all have as many keys, and even out in a prompt.
         double each = load > held ? step(held) * load / held : step(busy);
         if (load > fit) {
-          const double turns = std::floor(std::ceil(here) * w / 4 / fit), rest = std::ceil(here) * w / 4 - turns * fit;
+          const double turns = (double)(int64_t)(up(here) * w / 4 / fit), rest = up(here) * w / 4 - turns * fit;
           each += even * std::max(0.0, turns * step(fit) + (rest > 0 ? step(rest) : 0) - each);
         }
         double ns = c.ends + c.near * (held - 1) + 0.3 * c.ends * std::max(0.0, load / fit - 1) +
