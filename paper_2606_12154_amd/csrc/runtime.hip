@@ -473,11 +473,12 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
       const bool fold = prefill_stream < 0 && head_row == -1;
       QkvFold<TKV> qf;
       if (L.kv4) {
-        // The product's rows in fp32 (it adds, so they start at zero); keys are
-        // rotated and quantized as they go into their pages, queries rotated as
-        // the attention reads them.
-        float* rows = c->at<float>(L.qkv32);
-        zero_floats(st, rows, (size_t)n * L.nqkv);
+        // The product's rows in fp32 (it adds, so they start at zero, all layers'
+        // at once where the buffer holds them); keys are rotated and quantized as
+        // they go into their pages, queries rotated as the attention reads them.
+        const bool ahead = (size_t)n * g.n_layers <= (size_t)L.rows_cap;
+        float* rows = c->at<float>(L.qkv32) + (ahead ? (size_t)l * n * L.nqkv : 0);
+        if (!ahead || l == 0) zero_floats(st, rows, (size_t)n * L.nqkv * (ahead ? g.n_layers : 1));
         GK::resid(st, gws, h, n, c->at<TM>(L.wqkvM[l]), d, L.nqkv, ws, rows, nullptr, 0.f, nullptr, tq);
         Kv4Pool pool = pass->pool;
         pool.pool += (size_t)l * L.n_pages * L.page_bytes;
