@@ -136,13 +136,16 @@ __device__ __forceinline__ void load_row(const void* p, size_t at, int type, flo
     w[2 * i] = v[0];
     w[2 * i + 1] = v[1];
   }
+  if (type == kRowF16) {
 #pragma unroll
-  for (int i = 0; i < N / 2; ++i) {
-    if (type == kRowF16) {
+    for (int i = 0; i < N / 2; ++i) {
       const f16x2 h = __builtin_bit_cast(f16x2, w[i]);
       f[2 * i] = (float)h[0];
       f[2 * i + 1] = (float)h[1];
-    } else {
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
       f[2 * i] = __uint_as_float(w[i] << 16);
       f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
@@ -168,13 +171,28 @@ __device__ __forceinline__ void load_raw(RawRow& r, const void* p, size_t at, si
   }
 }
 __device__ __forceinline__ void raw_values(const RawRow& r, int type, float* f) {
+  // (One branch on the type, not one an element.)
+  if (type == kRowF32) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const unsigned full = r.w[i >> 2][i & 3], word = r.w[i >> 3][(i >> 1) & 3];
-    const unsigned half = i & 1 ? word >> 16 : word & 0xffffu;
-    f[i] = type == kRowF32 ? __uint_as_float(full)
-           : type == kRowF16 ? (float)__builtin_bit_cast(_Float16, (unsigned short)half)
-                             : __uint_as_float(half << 16);
+    for (int i = 0; i < 16; ++i) {
+      const unsigned w = r.w[i >> 2][i & 3];
+      f[i] = __uint_as_float(w);
+    }
+  } else if (type == kRowF16) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const unsigned w = r.w[i >> 3][(i >> 1) & 3];
+      const f16x2 h = __builtin_bit_cast(f16x2, w);
+      f[i] = (float)h[0];
+      f[i + 1] = (float)h[1];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const unsigned w = r.w[i >> 3][(i >> 1) & 3];
+      f[i] = __uint_as_float(w << 16);
+      f[i + 1] = __uint_as_float(w & 0xffff0000u);
+    }
   }
 }
 
@@ -793,33 +811,42 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   if (split > 0 && p0 >= np) return;
 
   // What the first step needs goes out before the queries are worked on.  Loads
-  // run one step ahead, page ids two; what would lie behind the wave's last
-  // step is its last step again (no branch around loads, whose waits would then have to
-  // assume that it was not taken).
+  // run one step ahead; what would lie behind the wave's last step is its last
+  // step again (no branch around loads, whose waits would then have to assume that it was
+  // not taken).  Lane i holds the page ids of the i-th of 64 steps: a load of ids
+  // in each step would be waited for there.
   const int* row = P.table + (size_t)s.trow * P.max_pages;
   constexpr int STEP = 2 * W;
   int p = p0 + 2 * wave;
   const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
-  auto ids = [&](int q, unsigned* id) {
+  unsigned ids[2];
+  auto load_ids = [&](int q) {
+    const int at = min(q + lane * STEP, last);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const unsigned x = (unsigned)row[max(min(min(q, last) + i, np - 1), 0)];
-      id[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
+      const unsigned x = (unsigned)row[max(min(at + i, np - 1), 0)];
+      ids[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
     }
   };
-  auto fetch = [&](PageRegs* pr, const unsigned* id) {
+  int ahead = 0;  // the step that is fetched next
+  auto fetch = [&](PageRegs* pr) {
+    if (ahead == 64) {
+      load_ids(p + STEP);
+      ahead = 0;
+    }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      load_page(pr[i], P.pool + ((size_t)id[i] * (unsigned)P.hkv + (unsigned)w.head) * kKv4Block, (unsigned)lane);
+    for (int i = 0; i < 2; ++i) {
+      const unsigned id = (unsigned)__builtin_amdgcn_readlane((int)ids[i], ahead);
+      load_page(pr[i], P.pool + ((size_t)id * (unsigned)P.hkv + (unsigned)w.head) * kKv4Block, (unsigned)lane);
+    }
+    ++ahead;
   };
+  load_ids(p);
   // Of several tiles, each wave makes one's queries for all.
   RawQuery raw;
   if (NQ == 1 || wave < NQ) load_query<PACK>(raw, w, A, NQ == 1 ? 0 : wave);
   PageRegs a[2], c[2];
-  unsigned id[2];
-  ids(p, id);
-  fetch(a, id);
-  ids(p + STEP, id);
+  fetch(a);
   Columns<NQ, QT, PT, PACK> C;
   C.start(w, most);
   if constexpr (PACK == 2) {
@@ -872,16 +899,14 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
     const int full = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
     bool swapped = false;
     while (p < full) {
-      fetch(c, id);
-      ids(p + 2 * STEP, id);
+      fetch(c);
       step(a, std::false_type());
       p += STEP;
       if (p >= full) {
         swapped = true;
         break;
       }
-      fetch(a, id);
-      ids(p + 2 * STEP, id);
+      fetch(a);
       step(c, std::false_type());
       p += STEP;
     }
@@ -890,8 +915,7 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
       a[1] = c[1];
     }
     while (p < p1) {
-      fetch(c, id);
-      ids(p + 2 * STEP, id);
+      fetch(c);
       step(a, std::true_type());
       a[0] = c[0];
       a[1] = c[1];
