@@ -437,11 +437,14 @@ struct PageRegs {
   unsigned ks;
 };
 
+// The block as a buffer: its base stays in scalar registers, a lane's offset in
+// one vector register (with addresses of 64 bits a lane, 2 to 5% more).
 __device__ __forceinline__ void load_page(PageRegs& r, const unsigned char* blk, unsigned lane) {
-  r.k = *reinterpret_cast<const u32x2*>(blk + 8 * lane);
-  r.v = *reinterpret_cast<const u32x2*>(blk + (512 + 8 * lane));
-  r.ks = *reinterpret_cast<const unsigned*>(blk + (kKeyScales + 4 * (lane & 15)));
-  r.vs = *reinterpret_cast<const u32x2*>(blk + (kValueScales + (lane & 8) * 4 + 8 * (lane >> 4)));
+  const auto b = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(blk), 0, kKv4Block, 0x00027000);
+  r.k = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, 8 * lane, 0, 0));
+  r.v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, 8 * lane + 512, 0, 0));
+  r.ks = __builtin_amdgcn_raw_buffer_load_b32(b, 4 * (lane & 15) + kKeyScales, 0, 0);
+  r.vs = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, (lane & 8) * 4 + 8 * (lane >> 4) + kValueScales, 0, 0));
 }
 
 // Nibble j of both halves of w as 16 + n.  The mask comes in a vector register:
