@@ -21,8 +21,9 @@
 // What bounds it (counters): vector instructions.  A step of two pages takes a
 // wave about 110 of them to unpack, 3.5 (exponentials count as four) a score
 // and lane, and 9 matrix instructions a column tile; the two kinds hardly run at
-// once.  One sequence of 131,072 positions (75 MB; 32 query heads on 8) takes 22 us,
-// 3.4 TB/s; an 8,192-token prompt 345 us, 0.8 PFLOP/s.
+// once.  With few rows what a step waits for itself comes on top: one sequence of
+// 131,072 positions (75 MB; 32 query heads on 8) takes 21 us, 3.6 TB/s, 32 of 4,000 19.5;
+// an 8,192-token prompt 340 us, 0.8 PFLOP/s.
 #include "hh_device.h"
 #include "hh_kv.h"
 
@@ -626,7 +627,7 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
 // first page of a step, the right one for the second, each with zeros in the
 // other's operands.  A lane then has four scores a step, not eight of which half
 // are of no column, and the copies are joined at the end (32 sequences of 4,000
-// positions 22.6 -> 21.6 us, one of 131,072 22.9 -> 22.2; 300 5.2 -> 5.3).
+// positions 20.8 -> 19.5 us, one of 131,072 22.3 -> 21.2, of 300 5.0 -> 4.8).
 template <int NQ, int QT, int PT, int PACK>
 struct Columns {
   static_assert(PACK == 1 || NQ == 1);
@@ -1129,8 +1130,8 @@ static void by_sequences(const Kv4Rows& R, int64_t threads_each, F launch) {
 }
 
 // A wave a (page, head).  Workgroups of one wave while each CU gets a few of them,
-// or else of four heads, whose rows are neighbours (append and read: 32 tokens 6.9 us
-// against 8.1, 1,024 rows 9.0 and 9.3, 2,048 rows 11.7 and 10.8, 8,192 21.6 and 20.9).
+// or else of four heads, whose rows are neighbours (append and read: 32 tokens 6.8 us
+// against 8.0, 1,024 rows 8.7 and 9.0, 2,048 rows 11.6 and 10.6, 8,192 21.7 and 20.9).
 static int row_heads(const Kv4Pool& P, const Kv4Rows& R) {
   return (int64_t)R.n_seqs * row_tiles(R) * P.hkv <= 1024 ? 1 : std::min(P.hkv, 4);
 }
@@ -1162,14 +1163,15 @@ void kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void*
 // with two and 1,250 with four, and 255, 310 and 430 more for each neighbour there, of
 // which there are up to three, two and one.  What comes before and after is 3.6,
 // 6 and 8.1 us, and 0.9, 0.3 and 0.45 more for each neighbour; the join 3 us, and its
-// reads.  So 2,000 prompt rows take four tiles (bf16: 38 us; two 43, one 56), 1,200 two
-// (22.0; four 22.8, one 27), 300 one (7.3; two 7.9, four 9.9), 8 sequences of 64 rows
-// behind 1,000 positions two (21.3; four 22.2, one 23.6).  One token at 700
-// positions is not split (6.2 with eight waves, 6.6 with four, 7.3 in 4 splits); at
-// 3,000 it takes splits of four waves (7.8; one of eight 13.1), at 32,768 32 splits
-// of eight (11.7; of four 13.0); 32 tokens at 1,500 take eight waves (12.2; four 16.1,
-// in 4 splits 14.3), 128 at 1,000 four (19.8; eight 22.5).  Eight waves are for
-// sequences of one tile.
+// reads.  So 2,000 prompt rows take four tiles (bf16: 33 us; two 39, one 50), 1,200 two
+// (19.7; four 20.4, one 24.7), 300 one (6.3; two 6.6, four 8.6), 8 sequences of 64 rows
+// behind 1,000 positions two (19.4; four 20.2, one 21.5).  One token at 700
+// positions is not split (6.2 with eight waves, 6.3 with four, 7.2 in 4 splits); at
+// 3,000 it takes splits of four waves (7.6; one of eight 12.6), at 32,768 32 splits
+// of eight (10.9; of four 11.2); 32 tokens at 1,500 take eight waves (10.4; four 11.9,
+// in 4 splits 13.6), 128 at 1,000 four (18.3; eight 20.8).  Eight waves are for
+// sequences of one tile; with sixteen, 64 tokens at 1,500 took 19.3 instead of 15.1, and
+// nothing less than 1% less.
 struct Cut {
   int nq, waves, splits;
 };
@@ -1247,8 +1249,8 @@ void kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Att
   // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers, whose
   // rounding to 11 bits is an eighth of a bf16 output's.  Weights of one term add
   // what an fp16 output's own rounding adds: two terms where they cost little,
-  // with one column tile (300 positions 5.0 -> 5.2 us; 256 rows behind 30,000, with one
-  // term, would go from 87 to 119).
+  // with one column tile (300 positions 4.7 -> 4.8 us; 256 rows behind 30,000, with one
+  // term, would go from 86 to 118).
   const bool f16 = A.out_type == kRowF16, long_q = A.q_type == kRowF32 || A.rope.at;
   by_sequences(R, p.threads, [&](const Kv4Rows& r) {
     if (A.out_type == kRowF32 || (f16 && long_q && p.nq == 1)) launch_attend<2, 2>(st, P, r, A, p);
@@ -1258,9 +1260,9 @@ void kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Att
     if (p.splits == 1) return;
     const int64_t outs = (int64_t)r.n_seqs * r.max_rows * A.hq;
     // Five and more splits of few rows are read at once by a workgroup each (one row of
-    // 32 heads, 16 splits: 7.5 us with the attention, 8.6 by 16 lanes each; 16 rows, 8
-    // splits: 10.7 and 10.6); fewer splits or more rows want fewer workgroups (64 rows, 2
-    // splits: 16.1 and 13.1).
+    // 32 heads, 16 splits: 7.1 us with the attention, 8.5 by 16 lanes each; 16 rows, 8
+    // splits: 10.0 and 9.9); fewer splits or more rows want fewer workgroups (64 rows, 2
+    // splits: 15.8 and 12.5).
     if (p.splits > 16 || (p.splits > 4 && outs <= 512)) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, r, A, 16 * p.nq, p.splits);
     else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, r, A, 16 * p.nq, p.splits);
   });
