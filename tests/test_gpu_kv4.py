@@ -304,6 +304,30 @@ def test_tokens_of_ragged_lengths(seqs, most, hkv, group, t, ot):
     run_case(lens, [1] * seqs, hkv, group, t, ot, seqs == 24, seed=seqs)
 
 
+@pytest.mark.parametrize("rows,seqs", [(1, 1024), (20, 512)])
+def test_long_ranges_that_are_not_split(rows, seqs):
+    """So many sequences (of one table row) that each workgroup takes its whole
+    range: up to 160 steps a wave, whose fp32 sums add 160 * 2^-24 of the weights and of
+    the products, < 2^-15.6, to check()'s bound (which counts them as 2^-17)."""
+    n = 20000
+    c, kv = filled([n], 1, 21)
+    rng = np.random.default_rng(rows)
+    first = rng.integers(8000, n - rows, seqs)
+    first[:3] = [n - rows, 8192, 8191]
+    q = dev(rng.standard_normal((seqs * rows, 2, 64)), torch.float32)
+    out = torch.full_like(q, 9.0)
+    r, keep = c.rows(np.arange(seqs + 1) * rows, first, seqs * rows, table_row=np.zeros(seqs))
+    assert hh.hh_kv4_attention_workspace(c.desc, r, 2) == 0
+    attend(c, r, q, "f32", out, "f32")
+    k, v = kv[0]
+    more = float(np.abs(v).max()) * 2.0 ** -15.6
+    for s in range(16):
+        at = slice(s * rows, s * rows + rows)
+        qs, got = q[at].double().cpu().numpy(), out[at].double().cpu().numpy()
+        ref = kv4.attend(qs, k, v, 0.125, int(first[s]))
+        check(got - np.clip(got - ref, -more, more), qs, k, v, 0.125, int(first[s]), "f32")
+
+
 def test_scales_of_scores():
     """Steep and flat softmaxes, and queries far from 1."""
     run_case([200], [2], 1, 4, "f32", "f32", False, seed=7, scale=2.0)
