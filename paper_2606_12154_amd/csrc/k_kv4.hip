@@ -21,9 +21,10 @@
 // What bounds it (counters): vector instructions.  A step of two pages takes a
 // wave about 110 of them to unpack, 3.5 (exponentials count as four) a score
 // and lane, and 9 matrix instructions a column tile; the two kinds hardly run at
-// once.  With few rows what a step waits for itself comes on top: one sequence of
-// 131,072 positions (75 MB; 32 query heads on 8) takes 21 us, 3.6 TB/s, 32 of 4,000 19.5;
-// an 8,192-token prompt 340 us, 0.8 PFLOP/s.
+// once: an 8,192-token prompt (32 query heads on 8) takes 340 us, 0.8 PFLOP/s.
+// With few rows memory does, and hides only a part of them: 32 sequences of 4,000
+// positions (74 MB) take 19.5 us, 3.8 TB/s, the same loads alone 16; one of 131,072 21,
+// and 18.
 #include "hh_device.h"
 #include "hh_kv.h"
 
