@@ -387,11 +387,10 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
  *            that may run at the same time need one each.
  * Rows at negative positions give 0; rows of `out` in no sequence are left as
  * they are.  Positions past max_pages * 16 - 1 are taken as that.  Sums and
- * softmax are fp32.  In the products, with an fp32 `out` queries and weights
- * are fp16 pairs (22 bits).  With a 16-bit one weights are single fp16 numbers, 2^-12
- * off at most, and so are queries (scaled by a power of two; 16-bit ones that are not rotated
- * are exact), but with an fp16 `out` fp32 and rotated queries are pairs, and so
- * are weights in calls with few rows.  Equal calls give equal bits.
+ * softmax are fp32.  In the products, whatever the types and sizes of a call,
+ * weights are fp16 pairs (22 bits), and so are queries, scaled by a power of two
+ * (16-bit ones that are not rotated are single fp16 numbers, exactly).  Equal
+ * calls give equal bits.
  * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
  * UNSUPPORTED (max_rows * n_heads near 2^30 and above), HIP.
  */

@@ -18,12 +18,18 @@
 // bytes hold; with the contraction of O^T[dim][query] += V^T P^T taken in that
 // order, weights go from accumulators to operands within their lanes.
 //
-// What bounds it (counters): vector instructions.  A step of two pages takes a
-// wave about 110 of them to unpack, 3.5 (exponentials count as four) a score
-// and lane, and 9 matrix instructions a column tile; the two kinds hardly run at
-// once: an 8,192-token prompt (32 query heads on 8) takes 340 us, 0.8 PFLOP/s.
+// Precision: a query and a weight are two fp16 terms each, 22 bits, with every
+// output type (one term where a 16-bit query needs no other): bf16 results differ
+// from those of fp32 products by 4e-5 of their norm, beside a rounding of 1.7e-3.
+// Single terms made that 1e-3 (and an 8,192-token prompt 338 us, 32 sequences of 4,000
+// positions 19.3).
+//
+// What bounds it: vector and matrix instructions, which hardly run at once.  A step of
+// two pages takes a wave about 110 vector ones to unpack, 7.5 issue slots (the
+// exponential four of them) a score and lane, and 18 matrix ones a column tile (14 with
+// queries of one term): an 8,192-token prompt (32 query heads on 8) takes 513 us, 0.54 PFLOP/s.
 // With few rows memory does, and hides only a part of them: 32 sequences of 4,000
-// positions (74 MB) take 19.5 us, 3.8 TB/s, the same loads alone 16; one of 131,072 21,
+// positions (74 MB) take 22 us, 3.4 TB/s, the same loads alone 16; one of 131,072 21.6,
 // and 18.
 #include "hh_device.h"
 #include "hh_kv.h"
@@ -528,6 +534,18 @@ __device__ __forceinline__ void values_of(u32x2 v, u32x2 scales, unsigned mask, 
   vf[3] = value_frag<3>(v, mask, s, b);
 }
 
+// A weight as two fp16 terms: what its nearest fp16 number leaves goes into the second
+// (two at once: two conversions of pairs and two mixed FMAs, where single
+// conversions there and back take twice as many instructions).
+__device__ __forceinline__ void split_weights(float a, float b, f16x2& h, f16x2& l) {
+  h = f16x2{(_Float16)a, (_Float16)b};
+  const unsigned w = __builtin_bit_cast(unsigned, h);
+  float x, y;
+  asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel_hi:[1,0,0]" : "=v"(x) : "v"(w), "v"(a));
+  asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(y) : "v"(w), "v"(b));
+  l = f16x2{(_Float16)x, (_Float16)y};
+}
+
 __device__ __forceinline__ f16x8 join8(f16x4 a, f16x4 b) {
   return f16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
@@ -558,8 +576,9 @@ struct RawQuery {
   RawRow row;
   f32x4 turn[4];
 };
-// QT: fp16 terms.  Queries (but for fp16 ones) are scaled by a power of two that puts a
-// row's largest element into [2^13, 2^14), so that one term holds any 16-bit
+// QT: fp16 terms, two of fp32 and rotated queries, one of 16-bit ones that are not
+// rotated.  Queries (but for fp16 ones of one term) are scaled by a power of two that puts
+// a row's largest element into [2^13, 2^14), so that one term holds any 16-bit
 // query and two hold 22 bits of an fp32 one.
 template <int QT>
 struct Query {
@@ -573,13 +592,13 @@ __device__ __forceinline__ int column_of() { return threadIdx.x & (16 / PACK - 1
 // Columns behind the last one repeat it (and are not written).
 __device__ __forceinline__ int column_row(const Place& w, int c) { return (unsigned)min(c, w.cols - 1) / w.group; }
 
-template <int PACK>
+template <int QT, int PACK>
 __device__ __forceinline__ void load_query(RawQuery& q, const Place& w, const Kv4Attend& A, int tile) {
   const int lane = threadIdx.x & 63, g = lane >> 4, c = w.c0 + 16 * tile + column_of<PACK>();
   const int rw = column_row(w, c), j = min(c, w.cols - 1) - rw * w.G;
   const size_t at = (size_t)(w.s.row0 + rw) * A.q_stride + (w.head * w.G + j) * 64 + 8 * g;
   load_raw(q.row, A.q, at, at + 32, A.q_type);
-  if (A.rope.at) {
+  if (QT == 2 && A.rope.at) {
     const int pos = min(max(w.s.first + rw, 0), A.rope.len - 1);
     const f32x4* cs = reinterpret_cast<const f32x4*>(A.rope.at + (size_t)pos * 32 + 8 * g);
 #pragma unroll
@@ -590,7 +609,7 @@ __device__ __forceinline__ void load_query(RawQuery& q, const Place& w, const Kv
 template <int QT>
 __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Attend& A) {
   Query<QT> z;
-  if (QT == 1 && A.q_type == kRowF16 && !A.rope.at) {
+  if (QT == 1 && A.q_type == kRowF16) {
     z.h[0] = __builtin_bit_cast(f16x8, q.row.w[0]);
     z.h[1] = __builtin_bit_cast(f16x8, q.row.w[1]);
     z.qs = fmaxf(A.scale * 1.4426950408889634f, 1e-37f);
@@ -598,7 +617,7 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
   }
   float x[16];
   raw_values(q.row, A.q_type, x);
-  if (A.rope.at) {
+  if (QT == 2 && A.rope.at) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float u = x[i], v = x[8 + i], co = q.turn[i >> 1][2 * (i & 1)], si = q.turn[i >> 1][2 * (i & 1) + 1];
@@ -623,13 +642,13 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
   return z;
 }
 
-// A wave's NQ tiles of 16 columns.  PT: fp16 terms of weights.
+// A wave's NQ tiles of 16 columns.
 // PACK: of up to 8 columns, two copies stand side by side, the left one for the
 // first page of a step, the right one for the second, each with zeros in the
 // other's operands.  A lane then has four scores a step, not eight of which half
 // are of no column, and the copies are joined at the end (32 sequences of 4,000
 // positions 20.8 -> 19.5 us, one of 131,072 22.3 -> 21.2, of 300 5.0 -> 4.8).
-template <int NQ, int QT, int PT, int PACK>
+template <int NQ, int QT, int PACK>
 struct Columns {
   static_assert(PACK == 1 || NQ == 1);
   static constexpr int N = 8 / PACK;  // scores of a lane, step and tile
@@ -726,15 +745,17 @@ struct Columns {
 #pragma unroll
     for (int t = 0; t < NQ; ++t)
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float w = __builtin_amdgcn_exp2f(x[t][i]);
-        const _Float16 h = (_Float16)w;
-        ph[t][i] = h;
-        if constexpr (PT == 2) pl[t][i] = (_Float16)(w - (float)h);
+      for (int i = 0; i < N; i += 2) {
+        f16x2 h, l;
+        split_weights(__builtin_amdgcn_exp2f(x[t][i]), __builtin_amdgcn_exp2f(x[t][i + 1]), h, l);
+        ph[t][i] = h[0];
+        ph[t][i + 1] = h[1];
+        pl[t][i] = l[0];
+        pl[t][i + 1] = l[1];
       }
     if constexpr (PACK == 2) {
       ph[0] = on_side(ph[0]);
-      if constexpr (PT == 2) pl[0] = on_side(pl[0]);
+      pl[0] = on_side(pl[0]);
     }
   }
   // A lane's four weights where its page's values are.
@@ -748,11 +769,9 @@ struct Columns {
     const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
-      if constexpr (PT == 2) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], pl[t], o[t][j], 0, 0, 0);
-        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl[t], sum[t], 0, 0, 0);
-      }
+      for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], pl[t], o[t][j], 0, 0, 0);
+      sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl[t], sum[t], 0, 0, 0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], ph[t], o[t][j], 0, 0, 0);
       sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph[t], sum[t], 0, 0, 0);
@@ -792,7 +811,7 @@ __device__ __forceinline__ void put(const Kv4Rows& R, const Kv4Attend& A, const 
 
 // A workgroup has a tile of 16 NQ columns; its W waves take the tile's keys in
 // turn (two pages a step) and join at the end.
-template <int NQ, int QT, int PT, int W, int PACK>
+template <int NQ, int QT, int W, int PACK>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(waves_fit(NQ)))) void
 k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -849,10 +868,10 @@ k_kv4_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   load_ids(p);
   // Of several tiles, each wave makes one's queries for all.
   RawQuery raw;
-  if (NQ == 1 || wave < NQ) load_query<PACK>(raw, w, A, NQ == 1 ? 0 : wave);
+  if (NQ == 1 || wave < NQ) load_query<QT, PACK>(raw, w, A, NQ == 1 ? 0 : wave);
   PageRegs a[2], c[2];
   fetch(a);
-  Columns<NQ, QT, PT, PACK> C;
+  Columns<NQ, QT, PACK> C;
   C.start(w, most);
   if constexpr (PACK == 2) {
     C.pack(make_query<QT>(raw, A));
@@ -1089,30 +1108,20 @@ Cuts cuts_of(const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Pl
           div_by(A.hq / P.hkv)};
 }
 
-template <int QT, int PT, int PACK>
+template <int QT, int PACK>
 void launch_pack(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   const Cuts c = cuts_of(P, R, A, p);
-  if (p.waves == 8) k_kv4_attend<1, QT, PT, 8, PACK><<<c.groups, 512, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
-  else k_kv4_attend<1, QT, PT, 4, PACK><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  if (p.waves == 8) k_kv4_attend<1, QT, 8, PACK><<<c.groups, 512, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  else k_kv4_attend<1, QT, 4, PACK><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
 }
 
-template <int QT, int PT>
-void launch_tile(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
-  if (p.packed) launch_pack<QT, PT, 2>(st, P, R, A, p);
-  else launch_pack<QT, PT, 1>(st, P, R, A, p);
-}
-
-template <int QT, int PT>
-void launch_tiles(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
-  const Cuts c = cuts_of(P, R, A, p);
-  if (p.nq == 2) k_kv4_attend<2, QT, PT, 4, 1><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
-  else k_kv4_attend<4, QT, PT, 4, 1><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
-}
-
-template <int QT, int PT>
+template <int QT>
 void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
-  if (p.nq == 1) launch_tile<QT, PT>(st, P, R, A, p);
-  else launch_tiles<QT, PT>(st, P, R, A, p);
+  const Cuts c = cuts_of(P, R, A, p);
+  if (p.nq == 1 && p.packed) launch_pack<QT, 2>(st, P, R, A, p);
+  else if (p.nq == 1) launch_pack<QT, 1>(st, P, R, A, p);
+  else if (p.nq == 2) k_kv4_attend<2, QT, 4, 1><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  else k_kv4_attend<4, QT, 4, 1><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
 }
 
 }  // namespace
@@ -1247,17 +1256,11 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t m
 }
 
 void kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
-  // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers, whose
-  // rounding to 11 bits is an eighth of a bf16 output's.  Weights of one term add
-  // what an fp16 output's own rounding adds: two terms where they cost little,
-  // with one column tile (300 positions 4.7 -> 4.8 us; 256 rows behind 30,000, with one
-  // term, would go from 86 to 118).
-  const bool f16 = A.out_type == kRowF16, long_q = A.q_type == kRowF32 || A.rope.at;
+  // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers.
+  const bool one = A.q_type != kRowF32 && !A.rope.at;
   by_sequences(R, p.threads, [&](const Kv4Rows& r) {
-    if (A.out_type == kRowF32 || (f16 && long_q && p.nq == 1)) launch_attend<2, 2>(st, P, r, A, p);
-    else if (f16 && p.nq == 1) launch_tile<1, 2>(st, P, r, A, p);
-    else if (f16 && long_q) launch_tiles<2, 1>(st, P, r, A, p);
-    else launch_attend<1, 1>(st, P, r, A, p);
+    if (one) launch_attend<1>(st, P, r, A, p);
+    else launch_attend<2>(st, P, r, A, p);
     if (p.splits == 1) return;
     const int64_t outs = (int64_t)r.n_seqs * r.max_rows * A.hq;
     // Five and more splits of few rows are read at once by a workgroup each (one row of

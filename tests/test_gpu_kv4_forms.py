@@ -1,0 +1,114 @@
+"""Attention over the 4-bit paged cache: its error in every pairing of element
+types, element by element, against fp64 attention over the values that the pages hold.
+
+Bound of an element, whatever kernel a call takes, with s = sum of w |v| over the attended
+keys, a = scale * sum of |q_i k_i| of the row's key where that is largest (|q_i| of a rotated
+query: the length of the pair it is rotated in, which no rotation changes), n keys:
+  - scores: queries hold 22 bits (2^-22 of each product); the sums of 64 products take 64 fp32
+    roundings (2^-18 of a), a rotation 3 * 2^-24, scaling and base 4 * 2^-24 and one 2^-24
+    more for each time the base is raised (24 of them counted): 2^-17.5 a in all;
+  - a weight: the exponential's 2^-23 and its argument's rounding, 2^-24 of less than 2^5, and
+    22 bits: 2^-18.5; the smallest weights, down to 0, are 2^-32 of the largest off: 2^-32 n;
+  - so each weight is off by e = 2^-17.5 a + 2^-18.5 + 2^-32 n, numerator and denominator both: 2 e s;
+    sums over the keys, 32 at a time, n / 32 roundings each and 16 for joins: 2 (n / 32 + 16) 2^-24 s;
+  - then half a step of the output's type.
+One fp16 number for a weight or a rotated query is up to 2^-12 of it off, 2^-12 a for the query, and
+passes this bound in rows of few keys.
+"""
+import numpy as np
+import pytest
+
+from oracle import kv4
+from test_gpu_kv4 import TYPES, Cache, append, attend, dev, rope_table
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+HALF_STEP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+def reference(q, k, v, scale, pos, length):
+    """fp64 rows [n, heads, 64] at positions pos [n] over k and v [keys, kv heads, 64];
+    length: |q| for a. Returns the results and s and a."""
+    n, hq, _ = q.shape
+    keys, hkv, _ = k.shape
+    g = hq // hkv
+    out, s, a = torch.empty_like(q), torch.empty_like(q), torch.empty(n, hq, 1, dtype=torch.float64, device=q.device)
+    hidden = torch.arange(keys, device=q.device)[None] > pos[:, None]
+    for h in range(hq):
+        kh, vh = k[:, h // g].contiguous(), v[:, h // g].contiguous()
+        x = (q[:, h].contiguous() @ kh.T.contiguous() * scale).masked_fill(hidden, -np.inf)
+        w = torch.softmax(x, -1)
+        out[:, h], s[:, h] = w @ vh, w @ vh.abs()
+        a[:, h, 0] = (length[:, h].contiguous() @ kh.abs().T.contiguous() * scale).masked_fill(hidden, 0).amax(-1)
+    return out, s, a
+
+
+def check(got, q, k, v, scale, pos, ot, rope=None):
+    """The docstring's bound for rows `got` (fp64) of queries q (before their rotation)."""
+    length = q.abs()
+    if rope is not None:
+        c, s = rope[pos.long()].double().unbind(-1)
+        c, s, x, y = c[:, None], s[:, None], q[..., :32], q[..., 32:]
+        length = torch.sqrt(x * x + y * y).repeat(1, 1, 2)
+        q = torch.cat([x * c - y * s, y * c + x * s], -1)
+    ref, s, a = reference(q, k, v, scale, pos, length)
+    n = (pos + 1).double()[:, None, None]
+    e = 2.0 ** -17.5 * a + 2.0 ** -18.5 + 2.0 ** -32 * n
+    e = (2 * e + 2 * (n / 32 + 16) * 2.0 ** -24) * s
+    tol = e + HALF_STEP[ot] * (ref.abs() + e) + 2.0 ** -25
+    assert torch.isfinite(got).all()
+    over = ((got - ref).abs() - tol).amax().item()
+    worst = ((got - ref).abs() / tol).amax().item()
+    assert over <= 0, f"an element is {worst:.3g} times the bound off ({over:.3g} over it)"
+    return worst
+
+
+def run(rows, first, hkv, group, t, ot, rope, seed, max_pages=None, scale=0.125, sample=None):
+    """rows[i] rows of sequence i from position first[i] on; sample: rows compared of each."""
+    torch.manual_seed(seed)
+    lens = [r + f for r, f in zip(rows, first)]
+    c = Cache(len(lens), hkv, max_pages or (max(lens) + 15) // 16, seed)
+    n, hq = sum(lens), hkv * group
+    at = np.concatenate([[0], np.cumsum(lens)])
+    x = [torch.randn(n, hkv, 64, device="cuda:0") for _ in "kv"]
+    r, keep = c.rows(at, [0] * len(lens), n)
+    append(c, r, *x, "f32")
+    held = [torch.empty_like(a) for a in x]
+    from paper_2606_12154_amd import hh
+    hh.hh_kv4_read(c.desc, r, held[0].data_ptr(), held[1].data_ptr(), hh.HH_F32, hkv * 64, hkv * 64,
+                   torch.cuda.current_stream().cuda_stream)
+    k, v = (a.double() for a in held)
+    start = np.concatenate([[0], np.cumsum(rows)])
+    q = torch.randn(int(start[-1]), hq, 64, device="cuda:0").to(TYPES[t][1])
+    out = torch.full(q.shape, 3.0, dtype=TYPES[ot][1], device="cuda:0")
+    tab = dev(rope_table(max(lens))) if rope else None
+    r, keep = c.rows(start, first, int(start[-1]))
+    attend(c, r, q, t, out, ot, scale, tab)
+    worst = 0.0
+    for i in range(len(rows)):
+        which = torch.arange(rows[i], device="cuda:0")
+        if sample and rows[i] > sample:  # the first, the last, and others between them
+            some = torch.randperm(rows[i] - 1, device="cuda:0")[:sample - sample // 2 - 1]
+            which = torch.cat([torch.arange(sample // 2, device="cuda:0"), some, which[-1:]])
+        at_row = which + int(start[i])
+        worst = max(worst, check(out[at_row].double(), q[at_row].double(), k[at[i]:at[i + 1]], v[at[i]:at[i + 1]], scale,
+                                 which + first[i], ot, tab))
+    return worst
+
+
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("ot", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+def test_single_tokens_of_few_keys(t, ot, rope):
+    """Rows of 1 to 6 keys, where one rounded weight or query shows."""
+    n = 600
+    run([1] * n, [i % 6 for i in range(n)], 2, 4, t, ot, rope, seed=1)
+
+
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("ot", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+def test_prompts_of_many_rows(t, ot, rope):
+    """The first rows of prompts have few keys, and their tiles many columns."""
+    run([1400, 9, 700], [0, 2, 0], 4, 4, t, ot, rope, seed=2, sample=64)
+    run([40] * 24, [i % 3 for i in range(24)], 8, 4, t, ot, rope, seed=3)
