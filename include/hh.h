@@ -389,8 +389,9 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
  * they are.  Positions past max_pages * 16 - 1 are taken as that.  Sums and
  * softmax are fp32.  In the products, whatever the types and sizes of a call,
  * weights are fp16 pairs (22 bits), and so are queries, scaled by a power of two
- * (16-bit ones that are not rotated are single fp16 numbers, exactly).  Equal
- * calls give equal bits.
+ * (16-bit ones that are not rotated are single fp16 numbers, exactly); a weight
+ * is 2^-37 of its row's largest off at most, so that smaller ones may count as 0.
+ * Equal calls give equal bits.
  * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
  * UNSUPPORTED (max_rows * n_heads near 2^30 and above), HIP.
  */

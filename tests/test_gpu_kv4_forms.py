@@ -3,14 +3,16 @@ types, element by element, against fp64 attention over the values that the pages
 
 Bound of an element, whatever kernel a call takes, with s = sum of w |v| over the attended
 keys, a = scale * sum of |q_i k_i| of the row's key where that is largest (|q_i| of a rotated
-query: the length of the pair it is rotated in, which no rotation changes), n keys:
+query: the length of the pair it is rotated in, which no rotation changes), n keys, m = max |v|:
   - scores: queries hold 22 bits (2^-22 of each product); the sums of 64 products take 64 fp32
     roundings (2^-18 of a), a rotation 3 * 2^-24, scaling and base 4 * 2^-24 and one 2^-24
     more for each time the base is raised (24 of them counted): 2^-17.5 a in all;
   - a weight: the exponential's 2^-23 and its argument's rounding, 2^-24 of less than 2^5, and
-    22 bits: 2^-18.5; the smallest weights, down to 0, are 2^-32 of the largest off: 2^-32 n;
-  - so each weight is off by e = 2^-17.5 a + 2^-18.5 + 2^-32 n, numerator and denominator both: 2 e s;
+    22 bits: 2^-18.5;
+  - so each weight is off by e = 2^-17.5 a + 2^-18.5, numerator and denominator both: 2 e s;
     sums over the keys, 32 at a time, n / 32 roundings each and 16 for joins: 2 (n / 32 + 16) 2^-24 s;
+  - the smallest weights are off by half the lowest step of fp16, 2^-25, where the largest
+    is 2^12 or more: 2^-37 of the largest, and so of the sum, n times, in both: 2^-36 n m;
   - then half a step of the output's type.
 One fp16 number for a weight or a rotated query is up to 2^-12 of it off, 2^-12 a for the query, and
 passes this bound in rows of few keys.
@@ -53,8 +55,8 @@ def check(got, q, k, v, scale, pos, ot, rope=None):
         q = torch.cat([x * c - y * s, y * c + x * s], -1)
     ref, s, a = reference(q, k, v, scale, pos, length)
     n = (pos + 1).double()[:, None, None]
-    e = 2.0 ** -17.5 * a + 2.0 ** -18.5 + 2.0 ** -32 * n
-    e = (2 * e + 2 * (n / 32 + 16) * 2.0 ** -24) * s
+    e = 2.0 ** -17.5 * a + 2.0 ** -18.5
+    e = (2 * e + 2 * (n / 32 + 16) * 2.0 ** -24) * s + 2.0 ** -36 * n * v.abs().max()
     tol = e + HALF_STEP[ot] * (ref.abs() + e) + 2.0 ** -25
     assert torch.isfinite(got).all()
     over = ((got - ref).abs() - tol).amax().item()
@@ -112,3 +114,36 @@ def test_prompts_of_many_rows(t, ot, rope):
     """The first rows of prompts have few keys, and their tiles many columns."""
     run([1400, 9, 700], [0, 2, 0], 4, 4, t, ot, rope, seed=2, sample=64)
     run([40] * 24, [i % 3 for i in range(24)], 8, 4, t, ot, rope, seed=3)
+
+
+@pytest.mark.parametrize("rows,seqs", [(1, 1024), (20, 512)])
+@pytest.mark.parametrize("ot", ["f32", "bf16"])
+def test_many_small_weights(rows, seqs, ot):
+    """20,000 flat keys behind steep ones, one in each wave's first pages (so many sequences of one
+    table row that no range is split). Steep keys have the value 0, the others 7, and weights
+    2^-x of the steep ones': the result is 7 n 2^-x over the steep keys' number and that sum. Beside
+    2 (n / 32 + 16 + 64) 2^-24 of it (sums as in check(), and a score of 7 b log2 e < 2^6 whose
+    two roundings the exponent takes as they are), 2^-37 of the largest weight may be lost n times."""
+    n, steep = 20000, torch.arange(8) * 32
+    k, v = torch.zeros(n, 1, 64, device="cuda:0"), torch.full((n, 1, 64), 7.0, device="cuda:0")
+    k[steep, 0, 0], v[steep] = 7.0, 0.0
+    c = Cache(1, 1, n // 16)
+    r, keep = c.rows([0, n], [0], n)
+    append(c, r, k, v, "f32")
+    x = torch.arange(30, 42, dtype=torch.float64)
+    b = (x * np.log(2.0) / 7).float()
+    q = torch.zeros(seqs * rows, 12, 64, device="cuda:0")
+    q[..., 0] = dev(b)
+    out = torch.full(q.shape, 9.0, dtype=TYPES[ot][1], device="cuda:0")
+    first = n - rows
+    r, keep = c.rows(np.arange(seqs + 1) * rows, [first] * seqs, seqs * rows, table_row=np.zeros(seqs))
+    attend(c, r, q, "f32", out, ot, 1.0)
+    w = torch.exp(-7 * b.double())
+    for i in {0, rows - 1}:
+        flat = first + i + 1 - len(steep)
+        ref = 7 * flat * w / (len(steep) + flat * w)
+        tol = 2 * (n / 32 + 80) * 2.0 ** -24 * ref + 2.0 ** -37 * 7 * flat / len(steep)
+        tol += HALF_STEP[ot] * (ref + tol)
+        got = out.view(seqs, rows, 12, 64)[:, i].double().cpu()
+        err = (got - ref[:, None]).abs() / tol[:, None]
+        assert err.max() <= 1, [f"2^-{int(a)}: {e:.3g}" for a, e in zip(x, err.amax((0, 2)))]
