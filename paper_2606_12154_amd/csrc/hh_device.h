@@ -17,6 +17,18 @@ constexpr int kHeadDim = 64;   // head dimension the kernels are written for
 constexpr int kPage = 16;      // tokens per KV page
 constexpr int kWave = 64;      // CDNA wavefront width
 
+// Launches a kernel and returns the launch's own status: the thread's last error, which
+// <<< >>> leaves it to, may be another library's.
+template <typename T>
+struct Same {
+  typedef T type;
+};
+template <typename... P>
+hipError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t st, typename Same<P>::type... args) {
+  void* at[] = {static_cast<void*>(&args)...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, at, lds, st);
+}
+
 // Elements of T in one 16-byte load.
 template <typename T> struct Vec16 { static constexpr int n = 16 / sizeof(T); };
 

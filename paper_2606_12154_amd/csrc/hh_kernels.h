@@ -46,9 +46,10 @@ struct DecodeKernels {
 void finalize(hipStream_t st, int r0, int n, const int* row_stream, const int* row_pos, unsigned long long* slot,
               int* pending, int* hist, int* pos, int max_ctx);
 
-// dst[0 .. n) = src[0 .. n) (host ints) through kernel arguments, kPutInts per launch.
+// dst[0 .. n) = src[0 .. n) (host ints) through kernel arguments, kPutInts per launch;
+// returns the launches' own status.
 constexpr int kPutInts = 62;
-void put_ints(hipStream_t st, int* dst, const int* src, int n);
+hipError_t put_ints(hipStream_t st, int* dst, const int* src, int n);
 // Position, pending token and argmax slot of streams [s0, s0 + n) to zero,
 // and the decode-step error word (when given).  Returns the launch's own
 // status: the thread's last error may be another library's.

@@ -72,7 +72,7 @@ struct PagePool {
   int64_t layer_stride, bytes;
   int n_layers, n_pages;
 };
-// once: no page is the source of two copies.
+// These return their launches' own status. once: no page is the source of two copies.
 hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, const int* dst, bool once);
 constexpr int kMaxCompactPages = 1 << 20;  // one bit each in LDS: 128 KiB
 size_t compact_workspace(int n_pages);

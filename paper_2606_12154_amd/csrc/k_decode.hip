@@ -891,13 +891,15 @@ __global__ void k_put_ints(int* __restrict__ dst, IntArgs a) {
   if ((int)threadIdx.x < a.n) dst[threadIdx.x] = a.v[threadIdx.x];
 }
 
-void put_ints(hipStream_t st, int* dst, const int* src, int n) {
+hipError_t put_ints(hipStream_t st, int* dst, const int* src, int n) {
   for (int o = 0; o < n; o += kPutInts) {
     IntArgs a;
     a.n = n - o < kPutInts ? n - o : kPutInts;
     for (int i = 0; i < a.n; ++i) a.v[i] = src[o + i];
-    k_put_ints<<<1, 64, 0, st>>>(dst + o, a);
+    const hipError_t e = launch(k_put_ints, 1, 64, 0, st, dst + o, a);
+    if (e != hipSuccess) return e;
   }
+  return hipSuccess;
 }
 
 __global__ void k_reset_streams(int s0, int n, int* __restrict__ pos, int* __restrict__ pending,
@@ -912,8 +914,7 @@ __global__ void k_reset_streams(int s0, int n, int* __restrict__ pos, int* __res
 }
 
 hipError_t reset_streams(hipStream_t st, int s0, int n, int* pos, int* pending, unsigned long long* slot, int* err) {
-  void* args[] = {&s0, &n, &pos, &pending, &slot, &err};
-  return hipLaunchKernel(reinterpret_cast<const void*>(k_reset_streams), dim3((n + 63) / 64), dim3(64), args, 0, st);
+  return launch(k_reset_streams, (n + 63) / 64, 64, 0, st, s0, n, pos, pending, slot, err);
 }
 
 void finalize(hipStream_t st, int r0, int n, const int* row_stream, const int* row_pos, unsigned long long* slot,

@@ -228,9 +228,7 @@ hipError_t copy_pages(hipStream_t st, const PagePool& P, int n, const int* src, 
         a.dst[i] = dst[o + i];
       }
       const unsigned groups = (unsigned)(((int64_t)a.n * pieces * Q.n_layers + 3) / 4);
-      if (once) k_copy_pages<true><<<groups, 256, 0, st>>>(Q, pieces, a);
-      else k_copy_pages<false><<<groups, 256, 0, st>>>(Q, pieces, a);
-      const hipError_t e = hipGetLastError();
+      const hipError_t e = launch(once ? k_copy_pages<true> : k_copy_pages<false>, groups, 256, 0, st, Q, pieces, a);
       if (e != hipSuccess) return e;
     }
   }
@@ -249,8 +247,8 @@ hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int tabl
                                              hipFuncAttributeMaxDynamicSharedMemorySize, kMaxCompactPages / 8);
     if (e != hipSuccess) return e;
   }
-  k_compact_plan<<<1, kPlanThreads, lds, st>>>(P.n_pages, table, table_rows, max_pages, lengths, live, moves);
-  hipError_t e = hipGetLastError();
+  const hipError_t e =
+      launch(k_compact_plan, 1, kPlanThreads, lds, st, P.n_pages, table, table_rows, max_pages, lengths, live, moves);
   if (e != hipSuccess) return e;
   const int pieces = pieces_of(P);
   // At most half the pool moves; the loop takes what is left beyond 2,048 workgroups.
@@ -259,11 +257,9 @@ hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int tabl
   const int table_groups = std::min(table_rows, 256);
   const unsigned all = move_groups + table_groups;
   // (Their number is known to the device alone: half of the pool at most.)
-  if (P.n_pages / 2 * P.bytes * P.n_layers > kCached)
-    k_compact_move<true><<<all, 256, 0, st>>>(P, pieces, moves, move_groups, table, table_rows, max_pages, lengths, live);
-  else
-    k_compact_move<false><<<all, 256, 0, st>>>(P, pieces, moves, move_groups, table, table_rows, max_pages, lengths, live);
-  return hipGetLastError();
+  const bool once = P.n_pages / 2 * P.bytes * P.n_layers > kCached;
+  return launch(once ? k_compact_move<true> : k_compact_move<false>, all, 256, 0, st, P, pieces, moves, move_groups, table,
+                table_rows, max_pages, lengths, live);
 }
 
 hipError_t fork_streams(hipStream_t st, int src, int n, const int* ids, const int* last, int len, int max_ctx,
@@ -277,16 +273,15 @@ hipError_t fork_streams(hipStream_t st, int src, int n, const int* ids, const in
       a.last[i] = last ? last[o + i] : 0;
     }
     const dim3 grid((unsigned)std::max(1, (len + 255) / 256), (unsigned)a.n);
-    k_fork_streams<<<grid, 256, 0, st>>>(src, len, max_ctx, max_pages, a, table, pos, pending, slot, hist);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e =
+        launch(k_fork_streams, grid, 256, 0, st, src, len, max_ctx, max_pages, a, table, pos, pending, slot, hist);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
 hipError_t truncate_stream(hipStream_t st, int s, int len, int max_ctx, int* pos, int* pending, const int* hist) {
-  k_truncate_stream<<<1, 1, 0, st>>>(s, len, max_ctx, pos, pending, hist);
-  return hipGetLastError();
+  return launch(k_truncate_stream, 1, 1, 0, st, s, len, max_ctx, pos, pending, hist);
 }
 
 void zero_floats(hipStream_t st, float* p, size_t n) {

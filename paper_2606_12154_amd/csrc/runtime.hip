@@ -1571,8 +1571,7 @@ hh_status hh_truncate(hh_ctx* c, int32_t s, int32_t length) {
     drop_page(c, from);
     pg.back() = to;
     if (c->cfg.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, 1, &from, &to, false));
-    put_ints(c->stream, c->at<int>(L.page_table) + (size_t)s * L.max_pages + keep - 1, &to, 1);
-    HIPCHK(c, hipGetLastError());
+    HIPCHK(c, put_ints(c->stream, c->at<int>(L.page_table) + (size_t)s * L.max_pages + keep - 1, &to, 1));
   }
   HIPCHK(c, truncate_stream(c->stream, s, length, c->cfg.max_context, c->at<int>(L.pos), c->at<int>(L.pending),
                             c->at<int>(L.hist)));
@@ -1608,8 +1607,7 @@ hh_status hh_compact(hh_ctx* c, int32_t* pages_in_use) {
     for (int p = L.n_pages - 1; p >= live; --p) spare.push_back(p);
     const PagePool pool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes, g.n_layers,
                         L.n_pages};
-    put_ints(c->stream, c->at<int>(L.lengths), c->len.data(), g.max_streams);
-    HIPCHK(c, hipGetLastError());
+    HIPCHK(c, put_ints(c->stream, c->at<int>(L.lengths), c->len.data(), g.max_streams));
     HIPCHK(c, compact_pages(c->stream, pool, c->at<int>(L.page_table), g.max_streams, L.max_pages, c->at<int>(L.lengths),
                             c->at<int>(L.scratch_u32), c->at<int>(L.compact)));
     for (int p = 0; p < L.n_pages; ++p) refs[to[p]] += c->refs[p];

@@ -1,0 +1,78 @@
+"""A HIP call of the program's own that failed leaves its error on the thread. The calls on
+a cache's pages and on streams report their own launches, do their work, and leave that error to the
+program."""
+import ctypes
+from contextlib import contextmanager, nullcontext
+
+import numpy as np
+import pytest
+
+import synth
+from paper_2606_12154_amd import hh
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@contextmanager
+def pending_error():
+    """An error of another call's on this thread, still there at the end."""
+    torch.cuda.synchronize()
+    hh.load_library()
+    with open("/proc/self/maps") as f:
+        path = next(line.split()[-1] for line in f if "libamdhip64" in line)
+    hip = ctypes.CDLL(path)
+    hip.hipGetLastError.restype = ctypes.c_int
+    try:
+        assert hip.hipSetDevice(1 << 20) != 0
+        yield
+        assert hip.hipGetLastError() != 0
+    finally:
+        hip.hipGetLastError()
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def test_page_copies_and_compaction():
+    pool = torch.randint(0, 256, (2, 12, 1152), dtype=torch.uint8, device="cuda:0")
+    want = pool.clone()
+    with pending_error():
+        hh.hh_kv_copy_pages(pool.data_ptr(), 2, pool.stride(0), 1152, 12, [10, 3], [1, 2], stream())
+    want[:, [1, 2]] = want[:, [10, 3]]
+    assert torch.equal(pool, want)
+    table = torch.tensor([[11, 4]], dtype=torch.int32, device="cuda:0")
+    lens = torch.tensor([32], dtype=torch.int32, device="cuda:0")
+    live = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    ws = torch.zeros(hh.hh_kv_compact_workspace(12), dtype=torch.uint8, device="cuda:0")
+    with pending_error():
+        hh.hh_kv_compact(pool.data_ptr(), 2, pool.stride(0), 1152, 12, table.data_ptr(), 1, 2, lens.data_ptr(), live.data_ptr(),
+                         ws.data_ptr(), ws.numel(), stream())
+    want[:, [0, 1]] = want[:, [4, 11]]
+    assert torch.equal(pool, want) and table.tolist() == [[1, 0]] and live.item() == 2
+
+
+@pytest.mark.parametrize("kv", [0, hh.HH_KV_Q4])
+def test_forks_cuts_and_compaction_of_streams(kv):
+    shape = synth.TINY
+    ctx = hh.Context(hh.make_config(shape, 3, 128, weight_format=kv))
+    ctx.load_weights(synth.make_weights(shape, 3, gain_std=0.1))
+    p = synth.make_tokens(shape.vocab, 40, 7)
+
+    def run(around):
+        ctx.reset()
+        ctx.prefill(1, p[:20])
+        ctx.prefill(0, p)
+        with around():
+            ctx.fork(0, [1, 2])
+        with around():
+            ctx.truncate(1, 37)      # copies the shared third page
+        ctx.reset(0)
+        with around():
+            assert ctx.compact() == 4
+        return ctx.decode_step([1, 2], [5, 6], logits=True)[1].copy()
+
+    want = run(nullcontext)
+    assert np.array_equal(run(pending_error), want)
+    ctx.close()
