@@ -43,13 +43,13 @@ struct Kv4Attend {
   float* part;  // workspace: split outputs and statistics
 };
 
-// These three launch and leave the launch's status to the caller (hipGetLastError).
-// Callers refuse sequences whose grid has more than kMaxThreads.
+// These three return their launches' own status.  Callers refuse sequences whose grid
+// has more than kMaxThreads.
 constexpr int64_t kMaxThreads = UINT32_MAX;
-void kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
-                int64_t k_stride, int64_t v_stride, RopeTable rope);
-void kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
-              int64_t v_stride);
+hipError_t kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
+                      int64_t k_stride, int64_t v_stride, RopeTable rope);
+hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
+                    int64_t v_stride);
 int64_t kv4_row_threads(const Kv4Pool& P, const Kv4Rows& R);  // of a sequence, append and read
 
 // How the attention of these sizes is cut up.
@@ -64,7 +64,7 @@ struct Kv4Plan {
 };
 // pages: a bound of the pages that a sequence holds; most_bytes: of the workspace.
 Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes = SIZE_MAX);
-void kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
+hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
 
 // n_layers pools of pages of `bytes` (a multiple of 16), layer_stride bytes apart.
 struct PagePool {

@@ -1111,20 +1111,14 @@ Cuts cuts_of(const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Pl
           div_by(A.hq / P.hkv)};
 }
 
-template <int QT, int PACK>
-void launch_pack(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
-  const Cuts c = cuts_of(P, R, A, p);
-  if (p.waves == 8) k_kv4_attend<1, QT, 8, PACK><<<c.groups, 512, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
-  else k_kv4_attend<1, QT, 4, PACK><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
-}
-
 template <int QT>
-void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
+hipError_t launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
+  const auto kernel = p.nq == 2     ? k_kv4_attend<2, QT, 4, 1>
+                      : p.nq == 4   ? k_kv4_attend<4, QT, 4, 1>
+                      : p.waves == 4 ? (p.packed ? k_kv4_attend<1, QT, 4, 2> : k_kv4_attend<1, QT, 4, 1>)
+                                     : (p.packed ? k_kv4_attend<1, QT, 8, 2> : k_kv4_attend<1, QT, 8, 1>);
   const Cuts c = cuts_of(P, R, A, p);
-  if (p.nq == 1 && p.packed) launch_pack<QT, 2>(st, P, R, A, p);
-  else if (p.nq == 1) launch_pack<QT, 1>(st, P, R, A, p);
-  else if (p.nq == 2) k_kv4_attend<2, QT, 4, 1><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
-  else k_kv4_attend<4, QT, 4, 1><<<c.groups, 256, 0, st>>>(P, R, A, c.heads, c.splits, c.tiles, c.group);
+  return launch(kernel, c.groups, 64 * p.waves, 0, st, P, R, A, c.heads, c.splits, c.tiles, c.group);
 }
 
 }  // namespace
@@ -1132,14 +1126,16 @@ void launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4
 // A launch has fewer than 2^32 threads: as many sequences as fit (those with
 // fewer rows than the longest have workgroups that end at once).
 template <typename F>
-static void by_sequences(const Kv4Rows& R, int64_t threads_each, F launch) {
+static hipError_t by_sequences(const Kv4Rows& R, int64_t threads_each, F some) {
   Kv4Rows r = R;
   const int most = (int)std::max<int64_t>(1, std::min<int64_t>(R.n_seqs, kMaxThreads / threads_each));
   for (int s = 0; s < R.n_seqs; s += r.n_seqs) {
     r.seq0 = s;
     r.n_seqs = std::min(most, R.n_seqs - s);
-    launch(r);
+    const hipError_t e = some(r);
+    if (e != hipSuccess) return e;
   }
+  return hipSuccess;
 }
 
 // A wave a (page, head).  Workgroups of one wave while each CU gets a few of them,
@@ -1153,19 +1149,19 @@ static dim3 row_grid(const Kv4Pool& P, const Kv4Rows& R, int heads) {
   return dim3((unsigned)R.n_seqs * (unsigned)row_tiles(R), (unsigned)((P.hkv + heads - 1) / heads));
 }
 
-void kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
-                int64_t k_stride, int64_t v_stride, RopeTable rope) {
+hipError_t kv4_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
+                      int64_t k_stride, int64_t v_stride, RopeTable rope) {
   const int h = row_heads(P, R);
-  by_sequences(R, kv4_row_threads(P, R), [&](const Kv4Rows& r) {
-    k_kv4_append<<<row_grid(P, r, h), 64 * h, 0, st>>>(P, r, k, v, type, k_stride, v_stride, rope, row_tiles(r));
+  return by_sequences(R, kv4_row_threads(P, R), [&](const Kv4Rows& r) {
+    return launch(k_kv4_append, row_grid(P, r, h), 64 * h, 0, st, P, r, k, v, type, k_stride, v_stride, rope, row_tiles(r));
   });
 }
 
-void kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
-              int64_t v_stride) {
+hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
+                    int64_t v_stride) {
   const int h = row_heads(P, R);
-  by_sequences(R, kv4_row_threads(P, R), [&](const Kv4Rows& r) {
-    k_kv4_read<<<row_grid(P, r, h), 64 * h, 0, st>>>(P, r, k, v, type, k_stride, v_stride, row_tiles(r));
+  return by_sequences(R, kv4_row_threads(P, R), [&](const Kv4Rows& r) {
+    return launch(k_kv4_read, row_grid(P, r, h), 64 * h, 0, st, P, r, k, v, type, k_stride, v_stride, row_tiles(r));
   });
 }
 
@@ -1258,20 +1254,20 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t m
   return p;
 }
 
-void kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
+hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
   // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers.
   const bool one = A.q_type != kRowF32 && !A.rope.at;
-  by_sequences(R, p.threads, [&](const Kv4Rows& r) {
-    if (one) launch_attend<1>(st, P, r, A, p);
-    else launch_attend<2>(st, P, r, A, p);
-    if (p.splits == 1) return;
+  return by_sequences(R, p.threads, [&](const Kv4Rows& r) {
+    const hipError_t e = one ? launch_attend<1>(st, P, r, A, p) : launch_attend<2>(st, P, r, A, p);
+    if (e != hipSuccess || p.splits == 1) return e;
     const int64_t outs = (int64_t)r.n_seqs * r.max_rows * A.hq;
     // Five and more splits of few rows are read at once by a workgroup each (one row of
     // 32 heads, 16 splits: 7.1 us with the attention, 8.5 by 16 lanes each; 16 rows, 8
     // splits: 10.0 and 9.9); fewer splits or more rows want fewer workgroups (64 rows, 2
     // splits: 15.8 and 12.5).
-    if (p.splits > 16 || (p.splits > 4 && outs <= 512)) k_kv4_join<<<(unsigned)outs, 256, 0, st>>>(P, r, A, 16 * p.nq, p.splits);
-    else k_kv4_join_rows<<<(unsigned)((outs + 15) / 16), 256, 0, st>>>(P, r, A, 16 * p.nq, p.splits);
+    if (p.splits > 16 || (p.splits > 4 && outs <= 512))
+      return launch(k_kv4_join, (unsigned)outs, 256, 0, st, P, r, A, 16 * p.nq, p.splits);
+    return launch(k_kv4_join_rows, (unsigned)((outs + 15) / 16), 256, 0, st, P, r, A, 16 * p.nq, p.splits);
   });
 }
 

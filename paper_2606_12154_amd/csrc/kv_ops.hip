@@ -80,8 +80,7 @@ hh_status hh_kv4_append(const hh_kv4_pool* pool, const hh_kv4_rows* rows, const 
       !rope_table(rope, rope_len, &T))
     return HH_ERR_INVALID_ARG;
   if (kv4_row_threads(P, R) > kMaxThreads) return HH_ERR_UNSUPPORTED;
-  kv4_append(static_cast<hipStream_t>(hip_stream), P, R, k, v, type, k_stride, v_stride, T);
-  return from_hip(hipGetLastError());
+  return from_hip(kv4_append(static_cast<hipStream_t>(hip_stream), P, R, k, v, type, k_stride, v_stride, T));
 }
 
 hh_status hh_kv4_read(const hh_kv4_pool* pool, const hh_kv4_rows* rows, void* k, void* v, int32_t dtype,
@@ -95,8 +94,7 @@ hh_status hh_kv4_read(const hh_kv4_pool* pool, const hh_kv4_rows* rows, void* k,
   if (!aligned(k, 16) || !aligned(v, 16) || !row_stride(k_stride, n, size) || !row_stride(v_stride, n, size))
     return HH_ERR_INVALID_ARG;
   if (kv4_row_threads(P, R) > kMaxThreads) return HH_ERR_UNSUPPORTED;
-  kv4_read(static_cast<hipStream_t>(hip_stream), P, R, k, v, type, k_stride, v_stride);
-  return from_hip(hipGetLastError());
+  return from_hip(kv4_read(static_cast<hipStream_t>(hip_stream), P, R, k, v, type, k_stride, v_stride));
 }
 
 hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows* rows, int32_t n_heads, size_t* bytes) {
@@ -135,8 +133,7 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
   A.hq = n_heads;
   A.scale = scale;
   A.part = static_cast<float*>(workspace);
-  kv4_attend(static_cast<hipStream_t>(hip_stream), P, R, A, plan);
-  return from_hip(hipGetLastError());
+  return from_hip(kv4_attend(static_cast<hipStream_t>(hip_stream), P, R, A, plan));
 }
 
 hh_status hh_kv_copy_pages(void* pool, int32_t n_layers, int64_t layer_stride, int64_t page_bytes, int32_t n_pages,

@@ -483,7 +483,8 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
         Kv4Pool pool = pass->pool;
         pool.pool += (size_t)l * L.n_pages * L.page_bytes;
         const RopeTable rt{rope, g.max_context};
-        kv4_append(st, pool, pass->rows, rows + hq * 64, rows + (hq + hkv) * 64, kRowF32, L.nqkv, L.nqkv, rt);
+        // (Launch errors here are found as the other kernels' are, at the end of the call.)
+        (void)kv4_append(st, pool, pass->rows, rows + hq * 64, rows + (hq + hkv) * 64, kRowF32, L.nqkv, L.nqkv, rt);
         Kv4Attend a{};
         a.q = rows;
         a.out = oM;
@@ -495,7 +496,7 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
         a.scale = 0.125f;
         a.rope = rt;
         a.part = c->at<float>(L.kv4_work);
-        kv4_attend(st, pool, pass->rows, a, pass->plan);
+        (void)kv4_attend(st, pool, pass->rows, a, pass->plan);
       } else if (fold) {
         const int sp = GK::qkv_deferred(st, gws, h, n, c->at<TM>(L.wqkvM[l]), d, hq, hkv, ws, rs, rp, rope, q, kv, kl, l,
                                         pt, tq,

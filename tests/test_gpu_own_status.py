@@ -76,3 +76,32 @@ def test_forks_cuts_and_compaction_of_streams(kv):
     want = run(nullcontext)
     assert np.array_equal(run(pending_error), want)
     ctx.close()
+
+
+def test_calls_of_a_4_bit_cache():
+    n, hkv, hq, pages = 600, 2, 8, 40
+    pool = torch.zeros((pages, hkv, 1152), dtype=torch.uint8, device="cuda:0")
+    table = torch.arange(pages, dtype=torch.int32, device="cuda:0")
+    start, first = (torch.tensor(a, dtype=torch.int32, device="cuda:0") for a in ([0, n], [0]))
+    desc = hh.hh_kv4_pool(pool.data_ptr(), table.data_ptr(), pages, hkv, pages, 1)
+    rows = hh.hh_kv4_rows(start.data_ptr(), first.data_ptr(), None, 1, n, n)
+    last = torch.tensor([n - 1], dtype=torch.int32, device="cuda:0")
+    one = hh.hh_kv4_rows(None, last.data_ptr(), None, 1, 1, 1)
+    k, v = (torch.randn(n, hkv, 64, device="cuda:0") for _ in "kv")
+    q = torch.randn(1, hq, 64, device="cuda:0")
+    ws = torch.zeros(hh.hh_kv4_attention_workspace(desc, one, hq), dtype=torch.uint8, device="cuda:0")
+
+    def run(around):
+        pool.zero_()
+        back, out = [torch.full_like(k, 9.0) for _ in "kv"], torch.full_like(q, 9.0)
+        with around():
+            hh.hh_kv4_append(desc, rows, k.data_ptr(), v.data_ptr(), hh.HH_F32, 128, 128, None, 0, stream())
+        with around():
+            hh.hh_kv4_read(desc, rows, back[0].data_ptr(), back[1].data_ptr(), hh.HH_F32, 128, 128, stream())
+        with around():
+            hh.hh_kv4_attention(desc, one, q.data_ptr(), hh.HH_F32, hq * 64, hq, 0.125, None, 0, out.data_ptr(), hh.HH_F32,
+                                hq * 64, ws.data_ptr() or None, ws.numel(), stream())
+        return [pool.clone(), *back, out]
+
+    for a, b in zip(run(nullcontext), run(pending_error)):
+        assert torch.equal(a, b)
