@@ -224,7 +224,8 @@ hh_status hh_reset(hh_ctx* ctx, int32_t stream_id);
  * prompt evaluation of it.
  *  dst  host, n distinct stream ids other than src.
  * Only enqueues.  Errors: INVALID_ARG (an id out of range, repeated or src, n
- * outside 1..max_streams - 1), OOM (host memory), HIP.
+ * outside 1..max_streams - 1), OOM (host memory), HIP; after HIP each listed stream is
+ * forked, or as it was, or empty.
  */
 hh_status hh_fork(hh_ctx* ctx, int32_t src, int32_t n, const int32_t* dst);
 
@@ -236,7 +237,7 @@ hh_status hh_fork(hh_ctx* ctx, int32_t src, int32_t n, const int32_t* dst);
  * decode step of the stream must be given its token.  length 0 is as
  * hh_reset of the stream, but for the record of a failed step.
  * Only enqueues.  Errors: INVALID_ARG (an id out of range, length < 0 or past
- * the stream's), HIP.
+ * the stream's), HIP; the stream is then as it was.
  */
 hh_status hh_truncate(hh_ctx* ctx, int32_t stream_id, int32_t length);
 

@@ -82,11 +82,14 @@ hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int tabl
 // ---- a context's streams (hh_fork, hh_truncate)
 // Streams ids[0 .. n) become the first len positions of stream src: page-table
 // entries of its full pages, then last[i] (where given) for the partly filled one;
-// position, pending token and argmax history.
+// position, pending token and argmax history.  One launch, n at most kForks.
+constexpr int kForks = 62;
 hipError_t fork_streams(hipStream_t st, int src, int n, const int* ids, const int* last, int len, int max_ctx,
                         int max_pages, int* table, int* pos, int* pending, unsigned long long* slot, int* hist);
-// Stream s ends at len > 0: its pending token is the argmax of position len - 1.
-hipError_t truncate_stream(hipStream_t st, int s, int len, int max_ctx, int* pos, int* pending, const int* hist);
+// Stream s ends at len > 0: its pending token is the argmax of position len - 1, and
+// `entry` (where given) of its page table is `page`.
+hipError_t truncate_stream(hipStream_t st, int s, int len, int max_ctx, int* pos, int* pending, const int* hist,
+                           int* entry, int page);
 // p[0 .. n) = 0, as a kernel (a graph's replays may clear memory only so).
 void zero_floats(hipStream_t st, float* p, size_t n);
 

@@ -167,7 +167,6 @@ __global__ __launch_bounds__(256) void k_compact_move(PagePool P, int pieces, co
 
 // ------------------------------------------------------------------ streams
 
-constexpr int kForks = 62;
 struct ForkArgs {
   int n, has_last;
   int ids[kForks], last[kForks];
@@ -191,7 +190,8 @@ __global__ __launch_bounds__(256) void k_fork_streams(int src, int len, int max_
 }
 
 __global__ void k_truncate_stream(int s, int len, int max_ctx, int* __restrict__ pos, int* __restrict__ pending,
-                                  const int* __restrict__ hist) {
+                                  const int* __restrict__ hist, int* __restrict__ entry, int page) {
+  if (entry) *entry = page;
   pos[s] = len;
   pending[s] = hist[(size_t)s * max_ctx + len - 1];
 }
@@ -264,24 +264,20 @@ hipError_t compact_pages(hipStream_t st, const PagePool& P, int* table, int tabl
 
 hipError_t fork_streams(hipStream_t st, int src, int n, const int* ids, const int* last, int len, int max_ctx,
                         int max_pages, int* table, int* pos, int* pending, unsigned long long* slot, int* hist) {
-  for (int o = 0; o < n; o += kForks) {
-    ForkArgs a{};
-    a.n = std::min(kForks, n - o);
-    a.has_last = last != nullptr;
-    for (int i = 0; i < a.n; ++i) {
-      a.ids[i] = ids[o + i];
-      a.last[i] = last ? last[o + i] : 0;
-    }
-    const dim3 grid((unsigned)std::max(1, (len + 255) / 256), (unsigned)a.n);
-    const hipError_t e =
-        launch(k_fork_streams, grid, 256, 0, st, src, len, max_ctx, max_pages, a, table, pos, pending, slot, hist);
-    if (e != hipSuccess) return e;
+  ForkArgs a{};
+  a.n = n;
+  a.has_last = last != nullptr;
+  for (int i = 0; i < n; ++i) {
+    a.ids[i] = ids[i];
+    a.last[i] = last ? last[i] : 0;
   }
-  return hipSuccess;
+  const dim3 grid((unsigned)std::max(1, (len + 255) / 256), (unsigned)n);
+  return launch(k_fork_streams, grid, 256, 0, st, src, len, max_ctx, max_pages, a, table, pos, pending, slot, hist);
 }
 
-hipError_t truncate_stream(hipStream_t st, int s, int len, int max_ctx, int* pos, int* pending, const int* hist) {
-  return launch(k_truncate_stream, 1, 1, 0, st, s, len, max_ctx, pos, pending, hist);
+hipError_t truncate_stream(hipStream_t st, int s, int len, int max_ctx, int* pos, int* pending, const int* hist,
+                           int* entry, int page) {
+  return launch(k_truncate_stream, 1, 1, 0, st, s, len, max_ctx, pos, pending, hist, entry, page);
 }
 
 void zero_floats(hipStream_t st, float* p, size_t n) {

@@ -1091,9 +1091,20 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
   return HH_OK;
 }
 
+// The context's KV pages, every layer's.
+PagePool page_pool(const hh_ctx* c) {
+  const Layout& L = c->L;
+  return PagePool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes,
+                  c->cfg.n_layers, L.n_pages};
+}
+
 // Streams [s0, s0 + n): pages back to the pool, lengths and device words to
-// zero in one launch (the decode-step kernel's error word with clear_error).
+// zero in one launch (the decode-step kernel's error word with clear_error); if
+// that fails, nothing has changed.
 hh_status reset_range(hh_ctx* c, int s0, int n, bool clear_error) {
+  int* err = clear_error && c->step_wg > 0 ? reinterpret_cast<int*>(c->at<unsigned long long>(c->L.ll) + c->L.ll_words - 8) : nullptr;
+  HIPCHK(c, reset_streams(c->stream, s0, n, c->at<int>(c->L.pos), c->at<int>(c->L.pending),
+                          c->at<unsigned long long>(c->L.slot), err));
   for (int s = s0; s < s0 + n; ++s) {
     for (int p : c->pages[s]) drop_page(c, p);
     c->pages[s].clear();
@@ -1101,9 +1112,6 @@ hh_status reset_range(hh_ctx* c, int s0, int n, bool clear_error) {
     c->recorded[s].clear();
     c->pending_known[s] = 0;
   }
-  int* err = clear_error && c->step_wg > 0 ? reinterpret_cast<int*>(c->at<unsigned long long>(c->L.ll) + c->L.ll_words - 8) : nullptr;
-  HIPCHK(c, reset_streams(c->stream, s0, n, c->at<int>(c->L.pos), c->at<int>(c->L.pending),
-                          c->at<unsigned long long>(c->L.slot), err));
   return HH_OK;
 }
 
@@ -1509,8 +1517,8 @@ hh_status hh_fork(hh_ctx* c, int32_t src, int32_t n, const int32_t* dst) {
       seen[dst[i]] = 1;
     }
     // Full pages are shared; a partly filled last page is copied, since its
-    // stream goes on writing to it.  (There is a free page for each copy: a
-    // stream never has more than its share of the pool.)
+    // stream goes on writing to it.  The host's lists follow launches that were
+    // accepted: copies go to free pages, and a fork is one kernel's work.
     const int len = c->len[src], full = len / kPage;
     const bool part = len % kPage != 0;
     const std::vector<int> shared(c->pages[src].begin(), c->pages[src].begin() + full);
@@ -1521,26 +1529,50 @@ hh_status hh_fork(hh_ctx* c, int32_t src, int32_t n, const int32_t* dst) {
       c->pages[dst[i]].reserve(full + 1);
       c->recorded[dst[i]].reserve(len);
     }
-    for (int i = 0; i < n; ++i) {
-      const int s = dst[i];
-      for (int p : c->pages[s]) drop_page(c, p);
-      c->pages[s].assign(shared.begin(), shared.end());
-      for (int p : shared) ++c->refs[p];
-      c->recorded[s] = c->recorded[src];
-      c->pending_known[s] = c->pending_known[src];
-      c->len[s] = len;
+    auto give_back = [&](int first) {
+      for (int i = (int)to.size() - 1; i >= first; --i) c->free_pages.push_back(to[i]);
+    };
+    if (part) {
+      // Where too few pages are free, listed streams give theirs back first.  (That
+      // is enough: a stream never has more than its share of the pool.)
+      for (int i = 0; i < n && (int)c->free_pages.size() < n; ++i) {
+        const hh_status rc = reset_range(c, dst[i], 1, false);
+        if (rc != HH_OK) return rc;
+      }
+      for (int i = 0; i < n; ++i) {
+        from.push_back(c->pages[src][full]);
+        to.push_back(c->free_pages.back());
+        c->free_pages.pop_back();
+      }
+      const hipError_t e = g.n_layers > 0 ? copy_pages(c->stream, page_pool(c), n, from.data(), to.data(), false) : hipSuccess;
+      if (e != hipSuccess) {
+        give_back(0);
+        return c->hip_fail(e, "page copies of a fork");
+      }
     }
-    for (int i = 0; i < n && part; ++i) {
-      from.push_back(c->pages[src][full]);
-      to.push_back(take_page(c));
-      c->pages[dst[i]].push_back(to.back());
+    for (int o = 0; o < n; o += kForks) {
+      const int m = std::min(kForks, n - o);
+      const hipError_t e = fork_streams(c->stream, src, m, ids.data() + o, part ? to.data() + o : nullptr, len,
+                                        g.max_context, L.max_pages, c->at<int>(L.page_table), c->at<int>(L.pos),
+                                        c->at<int>(L.pending), c->at<unsigned long long>(L.slot), c->at<int>(L.hist));
+      if (e != hipSuccess) {
+        give_back(o);
+        return c->hip_fail(e, "fork of a stream");
+      }
+      for (int i = o; i < o + m; ++i) {
+        const int s = dst[i];
+        for (int p : c->pages[s]) drop_page(c, p);
+        c->pages[s].assign(shared.begin(), shared.end());
+        for (int p : shared) ++c->refs[p];
+        if (part) {
+          c->pages[s].push_back(to[i]);
+          c->refs[to[i]] = 1;
+        }
+        c->recorded[s] = c->recorded[src];
+        c->pending_known[s] = c->pending_known[src];
+        c->len[s] = len;
+      }
     }
-    const PagePool pool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes, g.n_layers,
-                        L.n_pages};
-    if (part && g.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, n, from.data(), to.data(), false));
-    HIPCHK(c, fork_streams(c->stream, src, n, ids.data(), part ? to.data() : nullptr, len, g.max_context, L.max_pages,
-                           c->at<int>(L.page_table), c->at<int>(L.pos), c->at<int>(L.pending),
-                           c->at<unsigned long long>(L.slot), c->at<int>(L.hist)));
   } catch (const std::bad_alloc&) {
     return HH_ERR_OOM;
   }
@@ -1555,7 +1587,21 @@ hh_status hh_truncate(hh_ctx* c, int32_t s, int32_t length) {
   if (length == 0) return reset_range(c, s, 1, false);
   if (length == c->len[s]) return HH_OK;
   std::vector<int>& pg = c->pages[s];
-  const int keep = (length + kPage - 1) / kPage;
+  const int keep = (length + kPage - 1) / kPage, last = pg[keep - 1];
+  // The page that the stream writes next must be its own.  (Another stream
+  // holds it too, so a page is free.)  It gets a copy of it in the launch that
+  // cuts the stream; the host's lists follow.
+  const bool copy = length % kPage != 0 && c->refs[last] > 1;
+  const int to = copy ? c->free_pages.back() : -1;
+  if (copy && c->cfg.n_layers > 0) HIPCHK(c, copy_pages(c->stream, page_pool(c), 1, &last, &to, false));
+  HIPCHK(c, truncate_stream(c->stream, s, length, c->cfg.max_context, c->at<int>(L.pos), c->at<int>(L.pending),
+                            c->at<int>(L.hist),
+                            copy ? c->at<int>(L.page_table) + (size_t)s * L.max_pages + keep - 1 : nullptr, to));
+  if (copy) {
+    take_page(c);
+    drop_page(c, last);
+    pg[keep - 1] = to;
+  }
   while ((int)pg.size() > keep) {
     drop_page(c, pg.back());
     pg.pop_back();
@@ -1563,19 +1609,6 @@ hh_status hh_truncate(hh_ctx* c, int32_t s, int32_t length) {
   c->len[s] = length;
   c->recorded[s].resize(length);
   c->pending_known[s] = c->recorded[s].back();
-  // The page that the stream writes next must be its own.  (Another stream
-  // holds it too, so a page is free.)
-  if (length % kPage != 0 && c->refs[pg.back()] > 1) {
-    const int from = pg.back(), to = take_page(c);
-    const PagePool pool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes,
-                        c->cfg.n_layers, L.n_pages};
-    drop_page(c, from);
-    pg.back() = to;
-    if (c->cfg.n_layers > 0) HIPCHK(c, copy_pages(c->stream, pool, 1, &from, &to, false));
-    HIPCHK(c, put_ints(c->stream, c->at<int>(L.page_table) + (size_t)s * L.max_pages + keep - 1, &to, 1));
-  }
-  HIPCHK(c, truncate_stream(c->stream, s, length, c->cfg.max_context, c->at<int>(L.pos), c->at<int>(L.pending),
-                            c->at<int>(L.hist)));
   return HH_OK;
 }
 
@@ -1606,10 +1639,8 @@ hh_status hh_compact(hh_ctx* c, int32_t* pages_in_use) {
       to[p] = hole++;
     }
     for (int p = L.n_pages - 1; p >= live; --p) spare.push_back(p);
-    const PagePool pool{c->at<unsigned char>(L.kv), (int64_t)(L.n_pages * L.page_bytes), (int64_t)L.page_bytes, g.n_layers,
-                        L.n_pages};
     HIPCHK(c, put_ints(c->stream, c->at<int>(L.lengths), c->len.data(), g.max_streams));
-    HIPCHK(c, compact_pages(c->stream, pool, c->at<int>(L.page_table), g.max_streams, L.max_pages, c->at<int>(L.lengths),
+    HIPCHK(c, compact_pages(c->stream, page_pool(c), c->at<int>(L.page_table), g.max_streams, L.max_pages, c->at<int>(L.lengths),
                             c->at<int>(L.scratch_u32), c->at<int>(L.compact)));
     for (int p = 0; p < L.n_pages; ++p) refs[to[p]] += c->refs[p];
     for (auto& pg : c->pages)

@@ -1,0 +1,450 @@
+// A context's streams on the CPU, built with AddressSanitizer and
+// UndefinedBehaviorSanitizer by tests/test_host_streams.py: forks, cuts, compaction, resets,
+// prompts and steps in any order, with launches that fail.  HIP's calls are those below: a
+// launch of a kernel that keeps the streams' books does on host memory what the kernel does,
+// any other launch nothing, and the launch that `fail_in` names fails.  Every position of a stream is
+// stamped with its token in its KV page as the device's page table gives it, so that
+// a page that is lost, shared by mistake or moved without its entry shows.
+#include <hip/hip_runtime_api.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <map>
+#include <random>
+#include <string>
+#include <vector>
+
+#include "hh.h"
+
+static int failures = 0;
+static const char* at_op = "";
+#define CHECK(cond)                                                                       \
+  do {                                                                                    \
+    if (!(cond)) {                                                                        \
+      if (failures < 20) std::fprintf(stderr, "check failed at line %d (%s): %s\n", __LINE__, at_op, #cond); \
+      ++failures;                                                                         \
+    }                                                                                     \
+  } while (0)
+
+// ------------------------------------------------------------------ HIP
+
+static std::map<const void*, std::string> kernels;
+static int fail_in = -1;  // launches before the one that fails; < 0: none does
+static hipError_t last_error = hipSuccess;
+static int launches = 0;
+
+struct IntArgs { int n; int v[62]; };
+struct PairArgs { int n; int src[480], dst[480]; };
+struct ForkArgs { int n, has_last; int ids[62], last[62]; };
+struct PagePool { unsigned char* pool; int64_t layer_stride, bytes; int n_layers, n_pages; };
+
+// What the launches tell: where the books are.
+static struct Books {
+  int *table = nullptr, *pos = nullptr, *pending = nullptr, *hist = nullptr;
+  int max_pages = 0, max_ctx = 0;
+  PagePool pool{};
+  const int* feed = nullptr;
+} dev;
+
+template <typename T>
+static T arg(void** a, int i) { return *static_cast<T*>(a[i]); }
+
+static void move_page(const PagePool& p, int from, int to) {
+  for (int l = 0; l < p.n_layers; ++l)
+    std::memcpy(p.pool + l * p.layer_stride + to * p.bytes, p.pool + l * p.layer_stride + from * p.bytes, (size_t)p.bytes);
+}
+
+static void run(const std::string& k, dim3 grid, void** a) {
+  auto is = [&](const char* name) { return k.find(name) != std::string::npos; };
+  if (is("k_put_ints")) {
+    const IntArgs& v = *static_cast<IntArgs*>(a[1]);
+    std::memcpy(arg<int*>(a, 0), v.v, (size_t)v.n * sizeof(int));
+  } else if (is("k_reset_streams")) {
+    dev.pos = arg<int*>(a, 2);
+    dev.pending = arg<int*>(a, 3);
+    for (int s = arg<int>(a, 0); s < arg<int>(a, 0) + arg<int>(a, 1); ++s) dev.pos[s] = dev.pending[s] = 0;
+  } else if (is("k_prep_embed")) {
+    const int s = arg<int>(a, 0);
+    dev.feed = arg<const int*>(a, 1);
+    int *rs = arg<int*>(a, 2), *rp = arg<int*>(a, 3), *pos = arg<int*>(a, 4);
+    for (int r = 0; s != -2 && r < (int)grid.x; ++r) {
+      rp[r] = s >= 0 ? pos[s] + r : pos[rs[r]];
+      if (s >= 0) rs[r] = s;
+    }
+  } else if (is("10k_finalize")) {
+    const int r0 = arg<int>(a, 0), n = arg<int>(a, 1);
+    dev.hist = arg<int*>(a, 6);
+    dev.max_ctx = arg<int>(a, 8);
+    for (int r = r0; r < r0 + n; ++r) {
+      const int s = arg<int*>(a, 2)[r], p = arg<int*>(a, 3)[r];
+      if (arg<void*>(a, 4)) arg<int*>(a, 5)[s] = dev.hist[(size_t)s * dev.max_ctx + p] = dev.feed[r];
+      arg<int*>(a, 7)[s] = p + 1;
+    }
+  } else if (is("k_copy_pages")) {
+    dev.pool = arg<PagePool>(a, 0);
+    const PairArgs& v = *static_cast<PairArgs*>(a[2]);
+    for (int i = 0; i < v.n; ++i) move_page(dev.pool, v.src[i], v.dst[i]);
+  } else if (is("k_fork_streams")) {
+    const int src = arg<int>(a, 0), len = arg<int>(a, 1), ctx = arg<int>(a, 2), mp = arg<int>(a, 3), full = len / 16;
+    const ForkArgs& v = *static_cast<ForkArgs*>(a[4]);
+    int *table = arg<int*>(a, 5), *pos = arg<int*>(a, 6), *pending = arg<int*>(a, 7), *hist = arg<int*>(a, 9);
+    dev.table = table;
+    dev.max_pages = mp;
+    for (int i = 0; i < v.n; ++i) {
+      const int s = v.ids[i];
+      std::copy(hist + (size_t)src * ctx, hist + (size_t)src * ctx + len, hist + (size_t)s * ctx);
+      std::copy(table + (size_t)src * mp, table + (size_t)src * mp + full, table + (size_t)s * mp);
+      if (v.has_last) table[(size_t)s * mp + full] = v.last[i];
+      pos[s] = len;
+      pending[s] = pending[src];
+    }
+  } else if (is("k_truncate_stream")) {
+    const int s = arg<int>(a, 0), len = arg<int>(a, 1), ctx = arg<int>(a, 2);
+    arg<int*>(a, 3)[s] = len;
+    arg<int*>(a, 4)[s] = arg<int*>(a, 5)[(size_t)s * ctx + len - 1];
+#ifndef TWO_LAUNCHES
+    if (int* entry = arg<int*>(a, 6)) *entry = arg<int>(a, 7);
+#endif
+  } else if (is("k_compact_move")) {
+    const PagePool p = arg<PagePool>(a, 0);
+    int* table = arg<int*>(a, 4);
+    const int rows = arg<int>(a, 5), mp = arg<int>(a, 6);
+    const int* lens = arg<int*>(a, 7);
+    std::vector<int> used(p.n_pages, 0), to(p.n_pages);
+    for (int r = 0; r < rows; ++r)
+      for (int i = 0; i < (lens[r] + 15) / 16; ++i) used[table[(size_t)r * mp + i]] = 1;
+    const int live = (int)std::count(used.begin(), used.end(), 1);
+    int hole = 0;
+    for (int i = 0; i < p.n_pages; ++i) {
+      to[i] = i;
+      if (i < live || !used[i]) continue;
+      while (used[hole]) ++hole;
+      move_page(p, i, hole);
+      to[i] = hole++;
+    }
+    for (int r = 0; r < rows; ++r)
+      for (int i = 0; i < (lens[r] + 15) / 16; ++i) table[(size_t)r * mp + i] = to[table[(size_t)r * mp + i]];
+  }
+}
+
+extern "C" {
+
+void** __hipRegisterFatBinary(const void*) { static void* none = nullptr; return &none; }
+void __hipUnregisterFatBinary(void**) {}
+void __hipRegisterFunction(void**, const void* host, char*, const char* name, unsigned, void*, void*, void*, void*, int*) {
+  kernels[host] = name;
+}
+void __hipRegisterVar(void**, void*, char*, char*, int, size_t, int, int) {}
+static struct { dim3 grid, block; size_t lds; hipStream_t st; } config;
+hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t lds, hipStream_t st) {
+  config = {grid, block, lds, st};
+  return hipSuccess;
+}
+hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* lds, hipStream_t* st) {
+  *grid = config.grid;
+  *block = config.block;
+  *lds = config.lds;
+  *st = config.st;
+  return hipSuccess;
+}
+hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, hipStream_t) {
+  ++launches;
+  if (fail_in == 0) {
+    fail_in = -1;
+    return last_error = hipErrorLaunchFailure;
+  }
+  if (fail_in > 0) --fail_in;
+  run(kernels.at(f), grid, args);
+  return hipSuccess;
+}
+hipError_t hipGetLastError() {
+  const hipError_t e = last_error;
+  last_error = hipSuccess;
+  return e;
+}
+const char* hipGetErrorString(hipError_t) { return "an error"; }
+hipError_t hipMemcpyAsync(void* to, const void* from, size_t n, hipMemcpyKind, hipStream_t) {
+  std::memmove(to, from, n);
+  return hipSuccess;
+}
+hipError_t hipMemsetAsync(void* to, int v, size_t n, hipStream_t) {
+  std::memset(to, v, n);
+  return hipSuccess;
+}
+hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
+hipError_t hipGetDevice(int* d) {
+  *d = 0;
+  return hipSuccess;
+}
+hipError_t hipDeviceGetAttribute(int* v, hipDeviceAttribute_t, int) {
+  *v = 256;
+  return hipSuccess;
+}
+hipError_t hipPointerGetAttributes(hipPointerAttribute_t*, const void*) { return hipErrorInvalidValue; }
+hipError_t hipFuncSetAttribute(const void*, hipFuncAttribute, int) { return hipSuccess; }
+hipError_t hipGetSymbolAddress(void**, const void*) { return hipErrorInvalidSymbol; }
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ streams
+
+constexpr int kStreams = 5, kContext = 128;
+
+struct Streams {
+  hh_ctx* ctx = nullptr;
+  void* arena = nullptr;
+  std::vector<int> held[kStreams];      // each stream's tokens
+  std::vector<char> recorded[kStreams];  // positions whose argmax was recorded
+  std::mt19937 rng;
+  int rand(int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(rng); }
+
+  explicit Streams(unsigned seed) : rng(seed) {
+    dev = Books();
+    hh_config c{};
+    c.n_layers = 2; c.d_model = 64; c.n_heads = 2; c.n_kv_heads = 1; c.head_dim = 64; c.ffn_dim = 64; c.vocab = 4096;
+    c.rms_eps = 1e-5f; c.rope_theta = 10000.f; c.tied_embeddings = 1; c.dtype = HH_F32;
+    c.max_streams = kStreams; c.max_context = kContext; c.page_size = 16; c.weight_format = HH_WF_DTYPE;
+    size_t bytes = 0;
+    CHECK(hh_workspace_size(&c, &bytes) == HH_OK);
+    arena = std::aligned_alloc(256, (bytes + 255) / 256 * 256);
+    std::memset(arena, 0, bytes);
+    CHECK(hh_create(&c, arena, bytes, reinterpret_cast<void*>(256), &ctx) == HH_OK);
+    const std::vector<float> w((size_t)4096 * 64, 0.f);
+    const std::vector<const void*> tensors(1 + 9 * 2 + 1, w.data());
+    CHECK(hh_load_weights(ctx, tensors.data(), (int)tensors.size()) == HH_OK);
+    // Launches that tell where the books are.
+    CHECK(feed(0, 17) == HH_OK);
+    const int one = 1;
+    CHECK(hh_fork(ctx, 0, 1, &one) == HH_OK);
+    CHECK(hh_reset(ctx, -1) == HH_OK);
+    held[0].clear();
+    recorded[0].clear();
+  }
+  ~Streams() {
+    hh_destroy(ctx);
+    std::free(arena);
+  }
+
+  int* stamp(int s, int p, int layer) {
+    const int page = dev.table[(size_t)s * dev.max_pages + p / 16];
+    return reinterpret_cast<int*>(dev.pool.pool + layer * dev.pool.layer_stride + page * dev.pool.bytes) + p % 16;
+  }
+  // What the layers' kernels do: the rows' keys and values go into their pages.
+  void added(int s, const std::vector<int>& t) {
+    for (int x : t) {
+      held[s].push_back(x);
+      recorded[s].push_back(0);
+      if (dev.table)
+        for (int l = 0; l < 2; ++l) *stamp(s, (int)held[s].size() - 1, l) = x;
+    }
+    recorded[s].back() = 1;
+  }
+  std::vector<int> tokens(int n) {
+    std::vector<int> t(n);
+    for (int& x : t) x = rand(0, 4095);
+    return t;
+  }
+  hh_status feed(int s, int n) {
+    const std::vector<int> t = tokens(n);
+    const hh_status rc = hh_prefill(ctx, s, t.data(), n, HH_LOGITS_NONE, nullptr, nullptr);
+    if (rc == HH_OK) added(s, t);
+    return rc;
+  }
+  hh_status step(int s) {
+    const std::vector<int> t = tokens(1);
+    const hh_status rc = hh_decode_step(ctx, 1, &s, t.data(), nullptr, nullptr);
+    if (rc == HH_OK) added(s, t);
+    return rc;
+  }
+  hh_status fork(int s, const std::vector<int>& dst) {
+    const hh_status rc = hh_fork(ctx, s, (int)dst.size(), dst.data());
+    for (int d : dst) {
+      // After an error a listed stream is a fork, or as it was, or empty.
+      int32_t n = -1;
+      CHECK(hh_stream_length(ctx, d, &n) == HH_OK);
+      if (rc == HH_OK || same(d, held[s])) {
+        held[d] = held[s];
+        recorded[d] = recorded[s];
+      } else if (!same(d, held[d]) || n != (int)held[d].size()) {
+        CHECK(n == 0);
+        held[d].clear();
+        recorded[d].clear();
+      }
+    }
+    return rc;
+  }
+  hh_status cut(int s, int n) {
+    const hh_status rc = hh_truncate(ctx, s, n);
+    if (rc == HH_OK) {
+      held[s].resize(n);
+      recorded[s].resize(n);
+    }
+    return rc;
+  }
+  hh_status reset(int s) {
+    const hh_status rc = hh_reset(ctx, s);
+    if (rc == HH_OK) {
+      held[s].clear();
+      recorded[s].clear();
+    }
+    return rc;
+  }
+  bool same(int s, const std::vector<int>& t) {
+    int32_t n = -1;
+    if (hh_stream_length(ctx, s, &n) != HH_OK || n != (int)t.size() || dev.pos[s] != n) return false;
+    for (int p = 0; p < n; ++p)
+      for (int l = 0; l < 2; ++l)
+        if (*stamp(s, p, l) != t[p]) return false;
+    return true;
+  }
+  // Host, device and content agree.
+  void check() {
+    for (int s = 0; s < kStreams; ++s) {
+      int32_t n = -1;
+      CHECK(hh_stream_length(ctx, s, &n) == HH_OK && n == (int)held[s].size());
+      CHECK(dev.pos[s] == n);
+      CHECK(same(s, held[s]));
+      if (n > 0 && recorded[s][n - 1]) {
+        int32_t x = -1;
+        CHECK(dev.pending[s] == held[s].back());
+        CHECK(hh_read_argmax(ctx, s, n - 1, 1, &x) == HH_OK && x == held[s].back());
+      }
+    }
+  }
+  // No page is lost or held twice: the pool can be filled to its last page.
+  void refill() {
+    CHECK(hh_reset(ctx, -1) == HH_OK);
+    for (int s = 0; s < kStreams; ++s) {
+      held[s].clear();
+      recorded[s].clear();
+    }
+    int32_t n = -1;
+    CHECK(hh_compact(ctx, &n) == HH_OK && n == 0);
+    for (int s = 0; s < kStreams; ++s) CHECK(feed(s, kContext) == HH_OK);
+    check();
+    CHECK(hh_compact(ctx, &n) == HH_OK && n == kStreams * kContext / 16);
+    check();
+  }
+};
+
+// One call whose k-th launch fails, for every k: nothing has happened, and the same call works then.
+static void check_errors() {
+  for (int what = 0; what < 4; ++what)
+    for (int k = 0; k < 8; ++k) {
+      Streams t(100 + what);
+      at_op = what == 0 ? "cut" : what == 1 ? "fork" : what == 2 ? "compact" : "reset";
+      CHECK(t.feed(2, 50) == HH_OK && t.feed(0, 45) == HH_OK && t.fork(0, {1, 3}) == HH_OK && t.reset(2) == HH_OK);
+      t.check();
+      auto call = [&] {
+        int32_t n = 0;
+        return what == 0 ? t.cut(1, 20) : what == 1 ? t.fork(0, {4, 3}) : what == 2 ? hh_compact(t.ctx, &n) : t.reset(3);
+      };
+      fail_in = k;
+      const hh_status rc = call();
+      const bool failed = fail_in < 0;
+      fail_in = -1;
+      CHECK(rc == (failed ? HH_ERR_HIP : HH_OK));
+      (void)hipGetLastError();
+      t.check();
+      // Other streams take free pages; what the call left must not be among them.
+      CHECK(t.feed(2, 30) == HH_OK);
+      t.check();
+      CHECK(call() == HH_OK);
+      t.check();
+      for (int s = 0; s < kStreams; ++s) CHECK(t.step(s) == HH_OK);
+      t.check();
+      t.refill();
+    }
+}
+
+// A full pool: the forks' copies take pages that their streams held.
+static void check_full_pool() {
+  for (int k = -1; k < 8; ++k) {
+    at_op = "fork in a full pool";
+    Streams t(7);
+    CHECK(t.feed(0, kContext - 5) == HH_OK);
+    for (int s = 1; s < kStreams; ++s) CHECK(t.feed(s, kContext) == HH_OK);
+    fail_in = k;
+    const hh_status rc = t.fork(0, {1, 2, 3, 4});
+    CHECK(rc == (k >= 0 && fail_in < 0 ? HH_ERR_HIP : HH_OK));
+    fail_in = -1;
+    (void)hipGetLastError();
+    t.check();
+    CHECK(t.fork(0, {4, 3, 2, 1}) == HH_OK);
+    t.check();
+    for (int s = 0; s < kStreams; ++s) CHECK(t.feed(s, 5) == HH_OK);
+    t.check();
+    t.refill();
+  }
+}
+
+// An error that another call left is neither taken nor reported.
+static void check_pending_error() {
+  Streams t(9);
+  at_op = "pending error";
+  CHECK(t.feed(0, 45) == HH_OK);
+  last_error = hipErrorInvalidDevice;
+  CHECK(t.fork(0, {1, 2}) == HH_OK && t.cut(1, 20) == HH_OK && t.cut(2, 40) == HH_OK && t.reset(0) == HH_OK);
+  int32_t n = 0;
+  CHECK(hh_compact(t.ctx, &n) == HH_OK && n == 4);
+  CHECK(last_error == hipErrorInvalidDevice);
+  (void)hipGetLastError();
+  t.check();
+}
+
+static void check_any_order() {
+  for (unsigned seed = 0; seed < 60; ++seed) {
+    Streams t(seed);
+    for (int i = 0; i < 150; ++i) {
+      const int s = t.rand(0, kStreams - 1), what = t.rand(0, 9), len = (int)t.held[s].size();
+      if (what >= 4 && t.rand(0, 3) == 0) fail_in = t.rand(0, 3);
+      if (what <= 2 && len < kContext) {
+        at_op = "prompt";
+        CHECK(t.feed(s, t.rand(1, std::min(40, kContext - len))) == HH_OK);
+      } else if (what == 3 && len < kContext) {
+        at_op = "step";
+        CHECK(t.step(s) == HH_OK);
+      } else if (what <= 6) {
+        at_op = "fork";
+        std::vector<int> all = {0, 1, 2, 3, 4};
+        all.erase(all.begin() + s);
+        std::shuffle(all.begin(), all.end(), t.rng);
+        all.resize(t.rand(1, kStreams - 1));
+        t.fork(s, all);
+      } else if (what <= 7) {
+        at_op = "cut";
+        t.cut(s, t.rand(0, len));
+      } else if (what == 8) {
+        at_op = "compact";
+        hh_compact(t.ctx, nullptr);
+      } else {
+        at_op = "reset";
+        t.reset(s);
+      }
+      fail_in = -1;
+      (void)hipGetLastError();
+      t.check();
+      if (failures) {
+        std::fprintf(stderr, "(seed %u, call %d)\n", seed, i);
+        return;
+      }
+    }
+    t.refill();
+  }
+}
+
+int main() {
+  check_pending_error();
+  check_errors();
+  check_full_pool();
+  check_any_order();
+  if (failures) {
+    std::fprintf(stderr, "%d stream checks failed\n", failures);
+    return 1;
+  }
+  std::printf("stream checks passed (%d launches)\n", launches);
+  return 0;
+}
