@@ -726,9 +726,14 @@ hh_status ensure_pages(hh_ctx* c, int s, int new_len) {
   if ((int)c->free_pages.size() < need - first_new) return c->fail(HH_ERR_CONTEXT_FULL, "KV page pool exhausted");
   for (int i = first_new; i < need; ++i) pg.push_back(take_page(c));
   int* dst = c->at<int>(c->L.page_table) + (size_t)s * c->L.max_pages + first_new;
-  put_ints(c->stream, dst, pg.data() + first_new, need - first_new);
-  HIPCHK(c, hipGetLastError());
-  return HH_OK;
+  const hipError_t e = put_ints(c->stream, dst, pg.data() + first_new, need - first_new);
+  if (e == hipSuccess) return HH_OK;
+  // (The device does not know them: another call must not take them for uploaded.)
+  while ((int)pg.size() > first_new) {
+    drop_page(c, pg.back());
+    pg.pop_back();
+  }
+  return c->hip_fail(e, "upload of page-table entries");
 }
 
 // n more positions of stream s, the last one's argmax recorded and pending.

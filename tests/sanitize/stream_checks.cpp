@@ -360,6 +360,41 @@ static void check_errors() {
     }
 }
 
+// The launch that uploads a prompt's or a step's new page-table entries fails: the stream is as it
+// was, and the same call works then.
+static void check_new_pages() {
+  for (int what = 0; what < 3; ++what) {
+    at_op = what == 0 ? "prompt" : what == 1 ? "batch of prompts" : "step";
+    Streams t(20);
+    CHECK(t.feed(0, 32) == HH_OK && t.fork(0, {2}) == HH_OK);
+    const std::vector<int> a = t.tokens(20);
+    const int ids[2] = {0, 1}, lens[2] = {20, 20};
+    std::vector<int> both = a;
+    both.insert(both.end(), a.begin(), a.end());
+    auto call = [&] {
+      if (what == 0) return hh_prefill(t.ctx, 0, a.data(), 20, HH_LOGITS_NONE, nullptr, nullptr);
+      if (what == 1) return hh_prefill_batch(t.ctx, 2, ids, lens, both.data(), nullptr);
+      return hh_decode_step(t.ctx, 1, ids, a.data(), nullptr, nullptr);
+    };
+    fail_in = 0;
+    CHECK(call() == HH_ERR_HIP);
+    CHECK(fail_in == -1);
+    fail_in = -1;
+    (void)hipGetLastError();
+    t.check();
+    CHECK(t.feed(3, 40) == HH_OK);
+    t.check();
+    CHECK(call() == HH_OK);
+    t.added(0, what == 2 ? std::vector<int>(a.begin(), a.begin() + 1) : a);
+    if (what == 1) t.added(1, a);
+    if (what == 1) t.recorded[0].back() = t.recorded[1].back() = 0;  // (their argmaxes are not played here)
+    t.check();
+    for (int s : {2, 4}) CHECK(t.feed(s, 30) == HH_OK);
+    t.check();
+    t.refill();
+  }
+}
+
 // A full pool: the forks' copies take pages that their streams held.
 static void check_full_pool() {
   for (int k = -1; k < 8; ++k) {
@@ -439,6 +474,7 @@ static void check_any_order() {
 int main() {
   check_pending_error();
   check_errors();
+  check_new_pages();
   check_full_pool();
   check_any_order();
   if (failures) {
