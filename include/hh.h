@@ -15,6 +15,9 @@
  *  - Every function returns an hh_status; HH_OK is 0, errors are negative.
  *    On any error the context's state (stream lengths, KV contents, pending
  *    tokens, loaded weights) is unchanged and hh_last_error() describes it.
+ *    An error that an earlier HIP call left on the thread is not theirs, and
+ *    stays; prompts, hh_load_weights (and steps without graphs) report and take
+ *    it, with nothing done.
  *  - A context is not thread-safe: use it from one host thread at a time.
  *  - All GPU work of a context is enqueued on the HIP stream given to
  *    hh_create.  Calls whose outputs are host memory synchronize that stream

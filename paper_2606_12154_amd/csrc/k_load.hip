@@ -184,14 +184,13 @@ __global__ __launch_bounds__(256) void k_q4g32(const __bf16* src, size_t n_group
   }
 }
 
-void q4g32(hipStream_t st, const __bf16* src, size_t rows, int K, unsigned char* q4, _Float16* deq, float scale) {
+hipError_t q4g32(hipStream_t st, const __bf16* src, size_t rows, int K, unsigned char* q4, _Float16* deq, float scale) {
   const int gpr = K / 32;
   const size_t n = rows * (size_t)gpr;
   const unsigned grid = (unsigned)((n + 64 * kQ4Groups - 1) / (64 * kQ4Groups));
   const int rs = 64 / gpr, gs = 64 % gpr;
-  if (q4 && deq) k_q4g32<true, true><<<grid, 256, 0, st>>>(src, n, K, rs, gs, q4, deq, scale);
-  else if (q4) k_q4g32<true, false><<<grid, 256, 0, st>>>(src, n, K, rs, gs, q4, deq, scale);
-  else k_q4g32<false, true><<<grid, 256, 0, st>>>(src, n, K, rs, gs, q4, deq, scale);
+  return launch(q4 && deq ? k_q4g32<true, true> : q4 ? k_q4g32<true, false> : k_q4g32<false, true>, grid, 256, 0, st, src, n,
+                K, rs, gs, q4, deq, scale);
 }
 
 __global__ void k_tile_q4(const unsigned char* __restrict__ src, unsigned char* __restrict__ codes,
@@ -286,9 +285,9 @@ __global__ __launch_bounds__(256) void k_read_probe(const u32x4* __restrict__ p,
   if (acc == 0x9E3779B9u) g_probe_sink = acc;
 }
 
-void read_probe(hipStream_t st, const void* src, size_t bytes) {
+hipError_t read_probe(hipStream_t st, const void* src, size_t bytes) {
   const size_t n = bytes / 16;
-  k_read_probe<<<32768, 256, 0, st>>>(reinterpret_cast<const u32x4*>(src), n);
+  return launch(k_read_probe, 32768, 256, 0, st, reinterpret_cast<const u32x4*>(src), n);
 }
 
 }  // namespace hh

@@ -1649,8 +1649,7 @@ static hipError_t launch_step(const StepParams<TW, TKV>& P, int nwg, hipStream_t
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  kern<<<nwg, kStepThreads, lds, st>>>(P);
-  return hipGetLastError();
+  return launch(kern, nwg, kStepThreads, lds, st, P);
 }
 
 // Instantiated row shapes (every streamed row has d elements): bf16 rows of

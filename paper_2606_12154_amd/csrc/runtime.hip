@@ -715,6 +715,11 @@ void drop_page(hh_ctx* c, int p) {
   if (--c->refs[p] == 0) c->free_pages.push_back(p);
 }
 
+// What the thread's last error is before kernels are launched whose errors it is
+// to tell: an earlier call's, of the program or another library, is reported (and
+// taken) while the context is as it was.
+hipError_t earlier_error() { return hipGetLastError(); }
+
 // Make sure stream s owns pages for positions [0, new_len); upload new entries.
 // (The page that holds the stream's last position, if it is not full, is the
 // stream's alone: hh_fork and hh_truncate copy such a page.)
@@ -820,6 +825,7 @@ hh_status do_prefill(hh_ctx* c, int s, const int32_t* tokens, int n, int mode, f
   using DK = DecodeKernels<TW, TKV, TM>;
   hipStream_t st = c->stream;
   const int V = c->cfg.vocab;
+  HIPCHK(c, earlier_error());
   hh_status rc = ensure_pages(c, s, c->len[s] + n);
   if (rc != HH_OK) return rc;
   const int chunk = L.rows_cap;
@@ -885,6 +891,7 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
   hipStream_t st = c->stream;
   const hh_config& g = c->cfg;
   const int d = g.d_model;
+  HIPCHK(c, earlier_error());
   for (int i = 0; i < n; ++i) {
     hh_status rc = ensure_pages(c, ids[i], c->len[ids[i]] + lens[i]);
     if (rc != HH_OK) return rc;
@@ -1021,14 +1028,10 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
     if (rc != HH_OK) return rc;
   }
   if (c->uploaded_streams != ids) {
-    put_ints(st, c->at<int>(L.row_stream), ids.data(), n);
-    HIPCHK(c, hipGetLastError());
+    HIPCHK(c, put_ints(st, c->at<int>(L.row_stream), ids.data(), n));
     c->uploaded_streams = ids;
   }
-  if (tokens) {
-    put_ints(st, c->at<int>(L.feed), tokens, n);
-    HIPCHK(c, hipGetLastError());
-  }
+  if (tokens) HIPCHK(c, put_ints(st, c->at<int>(L.feed), tokens, n));
   const bool want_logits = logits != nullptr;
   // A 4-bit cache's attention is cut up for the longest stream's pages, in
   // powers of two (a graph for each).
@@ -1072,6 +1075,7 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
     }
     HIPCHK(c, hipGraphLaunch(it->second, st));
   } else {
+    HIPCHK(c, earlier_error());
     enqueue_decode<TW, TKV, TM>(c, n, tokens != nullptr, want_logits, pages);
     HIPCHK(c, hipGetLastError());
   }
@@ -1245,6 +1249,7 @@ hh_status hh_load_weights(hh_ctx* c, const void* const* tensors, int32_t n_tenso
     return c->fail(HH_ERR_INVALID_ARG, "expected " + std::to_string(expect) + " weight tensors");
   for (int i = 0; i < n_tensors; ++i)
     if (!tensors[i]) return c->fail(HH_ERR_INVALID_ARG, "NULL weight tensor " + std::to_string(i));
+  HIPCHK(c, earlier_error());
   const Layout& L = c->L;
   hipStream_t st = c->stream;
   const size_t d = g.d_model, F = g.ffn_dim, V = g.vocab, hq = g.n_heads, hkv = g.n_kv_heads;
@@ -1306,7 +1311,7 @@ hh_status hh_load_weights(hh_ctx* c, const void* const* tensors, int32_t n_tenso
       // 4-bit rows for the streaming decode kernel; the fp16 copies hold their
       // values q * s (times 2^s, exactly), so every path computes with them.
       auto quant = [&](size_t src, size_t rows, size_t K, size_t q4, size_t dst) {
-        q4g32(st, c->at<__bf16>(src), rows, (int)K, c->at<unsigned char>(q4), c->at<_Float16>(dst), c->wscale);
+        (void)q4g32(st, c->at<__bf16>(src), rows, (int)K, c->at<unsigned char>(q4), c->at<_Float16>(dst), c->wscale);
       };
       if (g.tied_embeddings) {
         quant(L.embed, V, d, L.lm_headQ, L.embedM);
@@ -1490,8 +1495,7 @@ hh_status hh_decode_step_noalloc(hh_ctx* c, int32_t s, const int32_t* token, flo
   }
   // The error word must start at zero (a fill kernel: capture-safe).
   const int n_err = 8;
-  k_zero_words<<<1, 64, 0, c->stream>>>(w.base + need - n_err, n_err);
-  HIPCHK(c, hipGetLastError());
+  HIPCHK(c, launch(k_zero_words, 1, 64, 0, c->stream, w.base + need - n_err, n_err));
   const std::vector<int> ids{s};
   hh_status rc = g.dtype == HH_BF16 ? do_decode<__bf16, _Float16, _Float16>(c, 1, ids, token, logits, next, &w)
                                     : do_decode<float, float, float>(c, 1, ids, token, logits, next, &w);
@@ -1699,15 +1703,15 @@ const char* hh_last_error(const hh_ctx* c) { return c ? c->err.c_str() : "NULL c
 
 hh_status hh_q4g32_quantize(const uint16_t* src, int64_t rows, int32_t K, uint8_t* dst, void* hip_stream) {
   if (!src || !dst || rows < 1 || K < 32 || K % 32 != 0) return HH_ERR_INVALID_ARG;
-  q4g32(static_cast<hipStream_t>(hip_stream), reinterpret_cast<const __bf16*>(src), (size_t)rows, K,
-        reinterpret_cast<unsigned char*>(dst), nullptr, 1.f);
-  return hipGetLastError() == hipSuccess ? HH_OK : HH_ERR_HIP;
+  const hipError_t e = q4g32(static_cast<hipStream_t>(hip_stream), reinterpret_cast<const __bf16*>(src), (size_t)rows, K,
+                             reinterpret_cast<unsigned char*>(dst), nullptr, 1.f);
+  return e == hipSuccess ? HH_OK : HH_ERR_HIP;
 }
 
 }  // extern "C"
 
 namespace hh {
-void read_probe(hipStream_t st, const void* src, size_t bytes);  // k_load.hip
+hipError_t read_probe(hipStream_t st, const void* src, size_t bytes);  // k_load.hip
 }
 
 extern "C" {
@@ -1715,8 +1719,7 @@ extern "C" {
 hh_status hh_read_probe(const void* src, size_t bytes, void* hip_stream) {
   if (!src || bytes < 16 || bytes % 16 != 0 || reinterpret_cast<uintptr_t>(src) % 16 != 0) return HH_ERR_INVALID_ARG;
   if (!is_device_ptr(src)) return HH_ERR_INVALID_ARG;
-  read_probe(static_cast<hipStream_t>(hip_stream), src, bytes);
-  return hipGetLastError() == hipSuccess ? HH_OK : HH_ERR_HIP;
+  return read_probe(static_cast<hipStream_t>(hip_stream), src, bytes) == hipSuccess ? HH_OK : HH_ERR_HIP;
 }
 
 }  // extern "C"

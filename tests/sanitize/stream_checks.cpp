@@ -428,6 +428,26 @@ static void check_pending_error() {
   CHECK(last_error == hipErrorInvalidDevice);
   (void)hipGetLastError();
   t.check();
+  // Prompts and steps (no new page, and with one) report it and do nothing.
+  CHECK(t.cut(2, 31) == HH_OK);
+  for (int i = 0; i < 6; ++i) {
+    at_op = i % 3 == 0 ? "prompt after an error" : i % 3 == 1 ? "step after an error" : "batch after an error";
+    const std::vector<int> a = t.tokens(1);
+    const int id = 2, one = 1;
+    auto call = [&] {
+      if (i % 3 == 2) return hh_prefill_batch(t.ctx, 1, &id, &one, a.data(), nullptr);
+      return i % 3 == 1 ? hh_decode_step(t.ctx, 1, &id, a.data(), nullptr, nullptr)
+                        : hh_prefill(t.ctx, id, a.data(), 1, HH_LOGITS_NONE, nullptr, nullptr);
+    };
+    last_error = hipErrorInvalidDevice;
+    CHECK(call() == HH_ERR_HIP);
+    CHECK(last_error == hipSuccess);
+    t.check();
+    CHECK(call() == HH_OK);
+    t.added(id, a);
+    if (i % 3 == 2) t.recorded[id].back() = 0;
+    t.check();
+  }
 }
 
 static void check_any_order() {

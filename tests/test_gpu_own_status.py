@@ -105,3 +105,56 @@ def test_calls_of_a_4_bit_cache():
 
     for a, b in zip(run(nullcontext), run(pending_error)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("wf", [0, hh.HH_KV_Q4])
+def test_steps_and_prompts(wf):
+    """Steps work beside the error; a prompt reports it with nothing done."""
+    shape = synth.TINY
+    ctx = hh.Context(hh.make_config(shape, 3, 128, weight_format=wf))
+    ctx.load_weights(synth.make_weights(shape, 3, gain_std=0.1))
+    p = synth.make_tokens(shape.vocab, 24, 7)
+
+    def run(around):
+        ctx.reset()
+        for s in range(3):
+            ctx.prefill(s, p[s:])
+        out = []
+        for i in range(10):  # across a page's end
+            with around():
+                out.append(ctx.decode_step([0], [int(p[i])], logits=True)[1].copy())
+            with around():
+                out.append(ctx.decode_step([1, 2], [int(p[i])] * 2, logits=True)[1].copy())
+            with around():
+                out.append(ctx.decode_step([1, 2], None, logits=True)[1].copy())
+        return out
+
+    for a, b in zip(run(nullcontext), run(pending_error)):
+        assert np.array_equal(a, b)
+    ctx.reset()
+    _, want = ctx.prefill(0, p, logits="all")
+    for n in (24, 3):  # with new pages, and without
+        ctx.reset()
+        if n == 3:
+            ctx.prefill(0, p[:21])
+        hip_error = pytest.raises(hh.HHError)
+        with pytest.raises(AssertionError), pending_error():  # (it is taken)
+            with hip_error as e:
+                ctx.prefill(0, p[24 - n:])
+        assert e.value.status == hh.HH_ERR_HIP and ctx.length(0) == 24 - n
+        _, got = ctx.prefill(0, p[24 - n:], logits="all")
+        if n == 24:
+            assert np.array_equal(got, want)
+        assert ctx.length(0) == 24
+    ctx.close()
+
+
+def test_probe_and_quantizer():
+    x = torch.randn(8, 64, device="cuda:0").bfloat16()
+    got, want = (torch.zeros(8, 36, dtype=torch.uint8, device="cuda:0") for _ in range(2))
+    hh.hh_q4g32_quantize(x.data_ptr(), 8, 64, want.data_ptr(), stream())
+    with pending_error():
+        hh.hh_q4g32_quantize(x.data_ptr(), 8, 64, got.data_ptr(), stream())
+    assert torch.equal(got, want)
+    with pending_error():
+        hh.hh_read_probe(x.data_ptr(), x.numel() * 2, stream())
