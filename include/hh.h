@@ -372,7 +372,10 @@ hh_status hh_kv4_read(const hh_kv4_pool* pool, const hh_kv4_rows* rows, void* k,
                       int64_t k_stride, int64_t v_stride, void* hip_stream);
 
 /* Bytes of device memory that hh_kv4_attention needs for these sizes (their
- * pointers are not read): 0 or more. */
+ * pointers are not read; row_start counts as given or NULL): 0 to
+ * HH_KV4_WORKSPACE_MOST.  Fewer sequences or rows may need more, so a caller of
+ * calls of several sizes takes the largest or the bound. */
+enum { HH_KV4_WORKSPACE_MOST = 16 << 20 };
 hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows* rows, int32_t n_heads, size_t* bytes);
 
 /*

@@ -62,8 +62,11 @@ struct Kv4Plan {
   int64_t threads;   // of a sequence's larger grid
   size_t workspace;  // bytes
 };
-// pages: a bound of the pages that a sequence holds; most_bytes: of the workspace.
-Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes = SIZE_MAX);
+// Split outputs: as many splits as fit.  (300 rows of 32 heads over 8,192 pages would take
+// ten splits, 25 MB, without a bound; where rows are many, there are workgroups enough.)
+constexpr size_t kKv4Workspace = (size_t)16 << 20;
+// pages: a bound of the pages that a sequence holds.
+Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages);
 hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
 
 // n_layers pools of pages of `bytes` (a multiple of 16), layer_stride bytes apart.

@@ -1189,7 +1189,7 @@ static double up(double x) {
   const double y = (double)(int64_t)x;
   return y < x ? y + 1 : y;
 }
-static Cut cut(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes) {
+static Cut cut(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
   struct Cost {
     int nq;
     double alone, more, ends, near;
@@ -1210,7 +1210,7 @@ static Cut cut(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t mos
     const int fit = waves_fit(c.nq);
     for (int w = 4; w <= (cols <= 16 ? 8 : 4); w += 4) {
       // (Every number up to 16, then less dense: this runs at each call.)
-      for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= most_bytes); s += s < 16 ? 1 : s < 32 ? 2 : 4) {
+      for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= kKv4Workspace); s += s < 16 ? 1 : s < 32 ? 2 : 4) {
         const int per = (pairs + s - 1) / s, steps = (per + w - 1) / w;
         const double here = std::max(1.0, seqs * s / 256);          // workgroups a CU gets
         const double load = here * w / 4, held = std::min<double>(fit, up(load));  // waves a SIMD, and at once
@@ -1237,9 +1237,9 @@ static Cut cut(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t mos
   return best;
 }
 
-Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages, size_t most_bytes) {
+Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
   Kv4Plan p;
-  const Cut c = cut(P, R, hq, pages, most_bytes);
+  const Cut c = cut(P, R, hq, pages);
   const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), outputs = (int64_t)R.n_rows * hq;
   p.nq = c.nq;
   p.waves = c.waves;

@@ -13,6 +13,8 @@ using namespace hh;
 
 namespace {
 
+static_assert(kKv4Workspace == HH_KV4_WORKSPACE_MOST, "the header's bound");
+
 bool aligned(const void* p, size_t a) { return p && reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 hh_status from_hip(hipError_t e) { return e == hipSuccess ? HH_OK : HH_ERR_HIP; }

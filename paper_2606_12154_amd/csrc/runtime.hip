@@ -30,7 +30,6 @@ constexpr int kSplitMax = 64;   // attention splits per (row, kv head) in decode
 constexpr int kLogitRows = 64;  // rows of the logits staging buffer (prefill ALL)
 constexpr int kSplitRows = 1024;  // rows of one many-row LM head launch
 constexpr int kMaxStepWG = 1024; // upper bound on persistent decode-step workgroups
-constexpr size_t kKv4Work = (size_t)16 << 20;  // split outputs of the 4-bit cache's attention (it takes as many splits as fit)
 
 size_t al(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -270,7 +269,7 @@ Layout make_layout(const hh_config& asked) {
   if (L.kv4) {
     L.qkv32 = take(R * L.nqkv * 4);
     L.seqs = take((3 * (size_t)c.max_streams + 1) * 4);
-    L.kv4_work = take(kKv4Work);
+    L.kv4_work = take(kKv4Workspace);
   }
   L.total = off;
   return L;
@@ -389,7 +388,7 @@ Kv4Pass kv4_pass(const hh_ctx* c, int n_seqs, int n_rows, int max_rows, const in
   p.pool = Kv4Pool{c->at<unsigned char>(L.kv), c->at<int>(L.page_table), L.n_pages, c->cfg.n_kv_heads, L.max_pages,
                    c->cfg.max_streams};
   p.rows = Kv4Rows{starts, first_pos, streams, n_seqs, n_rows, max_rows};
-  p.plan = kv4_plan(p.pool, p.rows, c->cfg.n_heads, std::min(pages, L.max_pages), kKv4Work);
+  p.plan = kv4_plan(p.pool, p.rows, c->cfg.n_heads, std::min(pages, L.max_pages));
   return p;
 }
 

@@ -23,6 +23,7 @@ HH_F32, HH_BF16, HH_F16 = 0, 1, 2
 HH_LOGITS_NONE, HH_LOGITS_LAST, HH_LOGITS_ALL = 0, 1, 2
 HH_WF_DTYPE, HH_WF_Q4G32 = 0, 1
 HH_KV_Q4 = 0x100  # added to a weight format: 4-bit KV cache
+HH_KV4_WORKSPACE_MOST = 16 << 20  # bound of hh_kv4_attention_workspace
 
 EXPORTED = ["hh_workspace_size", "hh_create", "hh_load_weights", "hh_prefill", "hh_prefill_batch", "hh_decode_step",
             "hh_decode_step_noalloc", "hh_reset", "hh_stream_length", "hh_read_argmax", "hh_destroy", "hh_last_error",
