@@ -359,7 +359,8 @@ typedef struct {
  * Only the slots of the given positions are written.  Rows whose position is
  * negative, or past the page table's max_pages * 16 or rope_len, are skipped.
  * Two rows of one call must not have the same place in the cache.
- * Errors: INVALID_ARG (NULL or misaligned pointers, a size < 1, a stride, an
+ * Errors: INVALID_ARG (NULL or misaligned pointers, a size < 1, n_kv_heads over
+ * 1,024, max_pages over 2^26, n_rows or max_rows from 2^30 on, a stride, an
  * element type), UNSUPPORTED (max_rows near 2^28 and above), HIP.
  */
 hh_status hh_kv4_append(const hh_kv4_pool* pool, const hh_kv4_rows* rows, const void* k, const void* v, int32_t dtype,
@@ -400,7 +401,7 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
  * is 2^-37 of its row's largest off at most, so that smaller ones may count as 0.
  * Equal calls give equal bits.
  * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
- * UNSUPPORTED (max_rows * n_heads near 2^30 and above), HIP.
+ * UNSUPPORTED (max_rows * n_heads near 2^30 and above, n_heads from 2^25 on), HIP.
  */
 hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, const void* q, int32_t q_dtype,
                            int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len,
@@ -411,8 +412,8 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
  * Pages of any paged cache: n_layers pools of n_pages pages of page_bytes, a
  * pool every layer_stride bytes from `pool` (device, 16-byte aligned;
  * page_bytes and layer_stride multiples of 16, page_bytes at most 64 MiB;
- * layer_stride at least n_pages * page_bytes where there are several layers).  Streams, devices and
- * captures as above.
+ * layer_stride at least n_pages * page_bytes where there are several layers).
+ * Streams, devices and captures as above.
  * ------------------------------------------------------------------------ */
 
 /*

@@ -1247,8 +1247,8 @@ Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
   p.packed = cols <= 8;
   const int64_t tiles = (cols + 16 * p.nq - 1) / (16 * p.nq);
   p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-  // (Columns are counted in 32 bits.)
-  p.threads = cols > INT32_MAX - 1024 ? INT64_MAX : tiles * P.hkv * p.splits * 64 * p.waves;
+  // (Columns, and the elements of a row, are counted in 32 bits.)
+  p.threads = cols > INT32_MAX - 1024 || hq >= 1 << 25 ? INT64_MAX : tiles * P.hkv * p.splits * 64 * p.waves;
   if (p.splits > 1) p.threads = std::max(p.threads, (int64_t)R.max_rows * hq * 256);
   p.workspace = p.splits > 1 ? split_bytes(p.splits, outputs) : 0;
   return p;

@@ -22,3 +22,16 @@ def test_workspace_has_a_bound():
         for heads, kv in ((32, 8), (4, 2), (8, 1), (64, 8), (128, 128), (7, 7)):
             most = max(most, need(seqs, rows, pages, heads, kv))
     assert (8 << 20) < most <= hh.HH_KV4_WORKSPACE_MOST
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1 << 25, 1), ((1 << 25) + 1024, 1024), (1 << 30, 2)])
+def test_heads_past_32_bit_offsets_are_refused(heads, kv_heads):
+    """A row's elements are counted in 32 bits."""
+    with pytest.raises(hh.HHError) as e:
+        need(1, 1, 1, heads, kv_heads)
+    assert e.value.status == hh.HH_ERR_UNSUPPORTED
+    pool = hh.hh_kv4_pool(A, A, 1, kv_heads, 1, 1)
+    with pytest.raises(hh.HHError) as e:
+        hh.hh_kv4_attention(pool, hh.hh_kv4_rows(None, A, None, 1, 1, 1), A, hh.HH_F16, heads * 64, heads, 1.0, None, 0, A,
+                            hh.HH_F16, heads * 64, A, 1 << 30, None)
+    assert e.value.status == hh.HH_ERR_UNSUPPORTED
