@@ -413,7 +413,8 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
  * pool every layer_stride bytes from `pool` (device, 16-byte aligned;
  * page_bytes and layer_stride multiples of 16, page_bytes at most 64 MiB;
  * layer_stride at least n_pages * page_bytes where there are several layers).
- * Streams, devices and captures as above.
+ * Streams, devices and captures as above; hh_kv_copy_pages takes n_pages bytes
+ * of host memory for its checks while it runs.
  * ------------------------------------------------------------------------ */
 
 /*
