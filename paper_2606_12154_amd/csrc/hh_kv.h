@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "kv4_plan.h"
+
 namespace hh {
 
 constexpr int kKv4Block = 1152;  // bytes of one (page, kv head): codes 512 + 512, scales 64 + 64
@@ -52,21 +54,10 @@ hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k,
                     int64_t v_stride);
 int64_t kv4_row_threads(const Kv4Pool& P, const Kv4Rows& R);  // of a sequence, append and read
 
-// How the attention of these sizes is cut up.
-struct Kv4Plan {
-  int nq;      // 16-column tiles of a workgroup
-  bool packed; // two pages side by side in one tile
-  int waves;   // of a workgroup
-  int tiles;   // column tiles (workgroups) a sequence and kv head
-  int splits;  // key splits over workgroups
-  int64_t threads;   // of a sequence's larger grid
-  size_t workspace;  // bytes
-};
-// Split outputs: as many splits as fit.  (300 rows of 32 heads over 8,192 pages would take
-// ten splits, 25 MB, without a bound; where rows are many, there are workgroups enough.)
-constexpr size_t kKv4Workspace = (size_t)16 << 20;
 // pages: a bound of the pages that a sequence holds.
-Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages);
+inline Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
+  return kv4_plan(Kv4Sizes{R.n_seqs, R.n_rows, R.max_rows, hq, P.hkv, pages});
+}
 hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
 
 // n_layers pools of pages of `bytes` (a multiple of 16), layer_stride bytes apart.

@@ -427,13 +427,6 @@ int row_tiles(const Kv4Rows& R) { return (R.max_rows + kPage - 2) / kPage + 1; }
 
 // Operand columns are (row, query head of the kv head's group) pairs, row-major:
 // column c of a sequence is row c / G, head c % G.
-constexpr int kMaxSplits = 64;
-
-// Waves that a SIMD holds, by their registers.
-constexpr int waves_fit(int nq) { return nq == 1 ? 4 : nq == 2 ? 3 : 2; }
-// Workspace of s splits: 64 dimensions, base and sum of weights each.
-size_t split_bytes(int s, int64_t outputs) { return (size_t)s * (size_t)outputs * (64 + 2) * sizeof(float); }
-
 // Pages of a split, given the pages that a column tile attends to: whole steps of two.
 __device__ __forceinline__ int split_pages(int np, int splits) {
   const int pairs = (np + 1) >> 1;
@@ -1163,95 +1156,6 @@ hipError_t kv4_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k,
   return by_sequences(R, kv4_row_threads(P, R), [&](const Kv4Rows& r) {
     return launch(k_kv4_read, row_grid(P, r, h), 64 * h, 0, st, P, r, k, v, type, k_stride, v_stride, row_tiles(r));
   });
-}
-
-// Column tiles and waves of a workgroup and key splits over workgroups: those of
-// the least time by what was measured, in ns (32 query heads on 8, every type; the
-// choices cost 1% on average against the best ones, 7% at most).  A step (two
-// pages) takes a wave that is alone on its SIMD 740 ns with one column tile, 860
-// with two and 1,250 with four, and 255, 310 and 430 more for each neighbour there, of
-// which there are up to three, two and one.  What comes before and after is 3.6,
-// 6 and 8.1 us, and 0.9, 0.3 and 0.45 more for each neighbour; the join 3 us, and its
-// reads.  So 2,000 prompt rows take four tiles (bf16: 33 us; two 39, one 50), 1,200 two
-// (19.7; four 20.4, one 24.7), 300 one (6.3; two 6.6, four 8.6), 8 sequences of 64 rows
-// behind 1,000 positions two (19.4; four 20.2, one 21.5).  One token at 700
-// positions is not split (6.2 with eight waves, 6.3 with four, 7.2 in 4 splits); at
-// 3,000 it takes splits of four waves (7.6; one of eight 12.6), at 32,768 32 splits
-// of eight (10.9; of four 11.2); 32 tokens at 1,500 take eight waves (10.4; four 11.9,
-// in 4 splits 13.6), 128 at 1,000 four (18.3; eight 20.8).  Eight waves are for
-// sequences of one tile; with sixteen, 64 tokens at 1,500 took 19.3 instead of 15.1, and
-// nothing less than 1% less.
-struct Cut {
-  int nq, waves, splits;
-};
-// Sizes here are far below 2^63.
-static double up(double x) {
-  const double y = (double)(int64_t)x;
-  return y < x ? y + 1 : y;
-}
-static Cut cut(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
-  struct Cost {
-    int nq;
-    double alone, more, ends, near;
-  };
-  constexpr Cost kCosts[] = {{1, 740, 255, 3600, 900}, {2, 860, 310, 6000, 300}, {4, 1250, 430, 8100, 450}};
-  const int group = hq / P.hkv;
-  const int64_t cols = (int64_t)R.max_rows * group, outputs = (int64_t)R.n_rows * hq;
-  const double mean_cols = (double)R.n_rows * group / R.n_seqs;
-  const int pairs = std::max(1, (pages + 1) / 2), most = std::max(1, std::min(kMaxSplits, pairs / 4));
-  // Pairs that a tile attends to on average: a causal prompt's see half.
-  const double mean_pairs = std::max(pages - R.max_rows / 32.0, pages / 2.0) / 2;
-  const double even = 4 * mean_pairs / std::max(pages, 1) - 1;  // 1: all tiles alike, 0: from none to all
-  Cut best{};
-  double best_ns = 0;
-  for (const Cost& c : kCosts) {
-    if (c.nq > 1 && cols <= 8 * c.nq) break;  // half of its columns would be none
-    const double seqs = (double)R.n_seqs * P.hkv * std::max(1.0, up(mean_cols / (16 * c.nq)));
-    const int fit = waves_fit(c.nq);
-    for (int w = 4; w <= (cols <= 16 ? 8 : 4); w += 4) {
-      // (Every number up to 16, then less dense: this runs at each call.)
-      for (int s = 1; s <= most && (s == 1 || split_bytes(s, outputs) <= kKv4Workspace); s += s < 16 ? 1 : s < 32 ? 2 : 4) {
-        const int per = (pairs + s - 1) / s, steps = (per + w - 1) / w;
-        const double here = std::max(1.0, seqs * s / 256);          // workgroups a CU gets
-        const double load = here * w / 4, held = std::min<double>(fit, up(load));  // waves a SIMD, and at once
-        const double busy = std::min<double>(fit, std::max(1.0, up(load * std::min(w, per) / w)));  // with keys
-        auto step = [&](double waves) { return c.alone + c.more * (waves - 1); };
-        // A wave's steps are the longest one's at least.  More waves than fit come in
-        // turns, which end together where all have as many keys, and even out in a prompt.
-        double each = load > held ? step(held) * load / held : step(busy);
-        if (load > fit) {
-          const double turns = (double)(int64_t)(up(here) * w / 4 / fit), rest = up(here) * w / 4 - turns * fit;
-          each += even * std::max(0.0, turns * step(fit) + (rest > 0 ? step(rest) : 0) - each);
-        }
-        double ns = c.ends + c.near * (held - 1) + 0.3 * c.ends * std::max(0.0, load / fit - 1) +
-                    std::max(step(busy) * steps, each * std::max(1.0, mean_pairs / s / w));
-        if (w > 4) ns -= s == 1 ? 700 : 200;  // (their waves start and end together)
-        if (s > 1) ns += 3000 + 0.09 * (double)outputs * s;
-        if (best.nq == 0 || ns < best_ns) {
-          best = Cut{c.nq, w, s};
-          best_ns = ns;
-        }
-      }
-    }
-  }
-  return best;
-}
-
-Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
-  Kv4Plan p;
-  const Cut c = cut(P, R, hq, pages);
-  const int64_t cols = (int64_t)R.max_rows * (hq / P.hkv), outputs = (int64_t)R.n_rows * hq;
-  p.nq = c.nq;
-  p.waves = c.waves;
-  p.splits = c.splits;
-  p.packed = cols <= 8;
-  const int64_t tiles = (cols + 16 * p.nq - 1) / (16 * p.nq);
-  p.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-  // (Columns, and the elements of a row, are counted in 32 bits.)
-  p.threads = cols > INT32_MAX - 1024 || hq >= 1 << 25 ? INT64_MAX : tiles * P.hkv * p.splits * 64 * p.waves;
-  if (p.splits > 1) p.threads = std::max(p.threads, (int64_t)R.max_rows * hq * 256);
-  p.workspace = p.splits > 1 ? split_bytes(p.splits, outputs) : 0;
-  return p;
 }
 
 hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p) {
