@@ -21,6 +21,7 @@ import numpy as np
 import pytest
 
 from oracle import kv4
+from kv4_cases import CASES
 from test_gpu_kv4 import TYPES, Cache, append, attend, dev, rope_table
 
 pytestmark = pytest.mark.gpu
@@ -147,3 +148,12 @@ def test_many_small_weights(rows, seqs, ot):
         got = out.view(seqs, rows, 12, 64)[:, i].double().cpu()
         err = (got - ref[:, None]).abs() / tol[:, None]
         assert err.max() <= 1, [f"2^-{int(a)}: {e:.3g}" for a, e in zip(x, err.amax((0, 2)))]
+
+
+@pytest.mark.parametrize("t,ot,rope", [("f16", "f16", False), ("bf16", "bf16", False), ("f32", "f32", False),
+                                       ("f32", "bf16", False), ("bf16", "bf16", True), ("f32", "f16", True)])
+@pytest.mark.parametrize("case", list(CASES))
+def test_every_kernel(case, t, ot, rope):
+    """Queries of one and of two terms through every kernel and way of cutting a call up."""
+    rows, first, hkv, group, pages = CASES[case]
+    run(rows, first, hkv, group, t, ot, rope, seed=7, max_pages=pages, sample=40)

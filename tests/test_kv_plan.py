@@ -1,9 +1,15 @@
 """How the attention over a 4-bit cache is cut up, without a GPU."""
 import itertools
+import os
+import shutil
+import subprocess
 
 import pytest
 
+from kv4_cases import CASES, sizes
 from paper_2606_12154_amd import hh
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 A = 1 << 20  # an aligned address that no call here may read
 
@@ -35,3 +41,39 @@ def test_heads_past_32_bit_offsets_are_refused(heads, kv_heads):
         hh.hh_kv4_attention(pool, hh.hh_kv4_rows(None, A, None, 1, 1, 1), A, hh.HH_F16, heads * 64, heads, 1.0, None, 0, A,
                             hh.HH_F16, heads * 64, A, 1 << 30, None)
     assert e.value.status == hh.HH_ERR_UNSUPPORTED
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("no g++")
+    exe = str(tmp_path_factory.mktemp("plan") / "plan")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I" + os.path.join(ROOT, "paper_2606_12154_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "kv4_plan_tool.cpp"), "-o", exe], check=True)
+
+    def ask(sizes):
+        text = "".join(" ".join(map(str, s)) + "\n" for s in sizes)
+        out = subprocess.run([exe], input=text, capture_output=True, text=True, check=True).stdout
+        return [tuple(map(int, line.split())) for line in out.splitlines()]
+    return ask
+
+
+def test_cases_reach_every_kernel(plan):
+    """Column tiles, pages side by side and waves, each with one split and with several, and both
+    kernels that join splits: what kv4_cases.py lists, and the GPU tests compare, takes them all."""
+    names = list(CASES)
+    got = dict(zip(names, plan([sizes(n) for n in names])))
+    reached = {(*p[:3], p[3] > 1) for p in got.values()}
+    shapes = [(1, 1, 4), (1, 1, 8), (1, 0, 4), (1, 0, 8), (2, 0, 4), (4, 0, 4)]
+    assert reached == {(*s, several) for s in shapes for several in (False, True)}, got
+    outs = {n: sizes(n)[1] * sizes(n)[3] for n in names}
+    joins = {p[3] > 16 or (p[3] > 4 and outs[n] <= 512) for n, p in got.items() if p[3] > 1}
+    assert joins == {False, True}
+
+
+def test_no_other_kernel_is_chosen(plan):
+    """Over the sizes of a server: nothing but the kernels of the cases."""
+    ask = [(q, q * r, r, hkv * g, hkv, p) for q, r, p, (hkv, g) in
+           itertools.product((1, 4, 32, 200), (1, 2, 4, 9, 40, 300, 5000), (1, 20, 300, 8192), ((8, 4), (1, 8), (2, 2), (40, 1)))]
+    for nq, packed, waves, splits in plan(ask):
+        assert (nq, packed, waves) in {(1, 1, 4), (1, 1, 8), (1, 0, 4), (1, 0, 8), (2, 0, 4), (4, 0, 4)} and 1 <= splits <= 64
