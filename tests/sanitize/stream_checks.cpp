@@ -1,12 +1,10 @@
 // A context's streams on the CPU, built with AddressSanitizer and
 // UndefinedBehaviorSanitizer by tests/test_host_streams.py: forks, cuts, compaction, resets,
-// prompts and steps in any order, with launches that fail.  HIP's calls are those below: a
-// launch of a kernel that keeps the streams' books does on host memory what the kernel does,
-// any other launch nothing, and the launch that `fail_in` names fails.  Every position of a stream is
+// prompts and steps in any order, with launches that fail.  HIP's calls are fake_hip.h's: a
+// launch of a kernel that keeps the streams' books does on host memory what the kernel
+// does, any other launch nothing.  Every position of a stream is
 // stamped with its token in its KV page as the device's page table gives it, so that
 // a page that is lost, shared by mistake or moved without its entry shows.
-#include <hip/hip_runtime_api.h>
-
 #include <algorithm>
 #include <cstdint>
 #include <cstdio>
@@ -17,6 +15,7 @@
 #include <string>
 #include <vector>
 
+#include "fake_hip.h"
 #include "hh.h"
 
 static int failures = 0;
@@ -29,12 +28,7 @@ static const char* at_op = "";
     }                                                                                     \
   } while (0)
 
-// ------------------------------------------------------------------ HIP
-
-static std::map<const void*, std::string> kernels;
-static int fail_in = -1;  // launches before the one that fails; < 0: none does
-static hipError_t last_error = hipSuccess;
-static int launches = 0;
+// ------------------------------------------------------------------ launches
 
 struct IntArgs { int n; int v[62]; };
 struct PairArgs { int n; int src[480], dst[480]; };
@@ -49,15 +43,12 @@ static struct Books {
   const int* feed = nullptr;
 } dev;
 
-template <typename T>
-static T arg(void** a, int i) { return *static_cast<T*>(a[i]); }
-
 static void move_page(const PagePool& p, int from, int to) {
   for (int l = 0; l < p.n_layers; ++l)
     std::memcpy(p.pool + l * p.layer_stride + to * p.bytes, p.pool + l * p.layer_stride + from * p.bytes, (size_t)p.bytes);
 }
 
-static void run(const std::string& k, dim3 grid, void** a) {
+static void run_kernel(const std::string& k, dim3 grid, dim3, void** a) {
   auto is = [&](const char* name) { return k.find(name) != std::string::npos; };
   if (is("k_put_ints")) {
     const IntArgs& v = *static_cast<IntArgs*>(a[1]);
@@ -129,65 +120,6 @@ static void run(const std::string& k, dim3 grid, void** a) {
       for (int i = 0; i < (lens[r] + 15) / 16; ++i) table[(size_t)r * mp + i] = to[table[(size_t)r * mp + i]];
   }
 }
-
-extern "C" {
-
-void** __hipRegisterFatBinary(const void*) { static void* none = nullptr; return &none; }
-void __hipUnregisterFatBinary(void**) {}
-void __hipRegisterFunction(void**, const void* host, char*, const char* name, unsigned, void*, void*, void*, void*, int*) {
-  kernels[host] = name;
-}
-void __hipRegisterVar(void**, void*, char*, char*, int, size_t, int, int) {}
-static struct { dim3 grid, block; size_t lds; hipStream_t st; } config;
-hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t lds, hipStream_t st) {
-  config = {grid, block, lds, st};
-  return hipSuccess;
-}
-hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* lds, hipStream_t* st) {
-  *grid = config.grid;
-  *block = config.block;
-  *lds = config.lds;
-  *st = config.st;
-  return hipSuccess;
-}
-hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, hipStream_t) {
-  ++launches;
-  if (fail_in == 0) {
-    fail_in = -1;
-    return last_error = hipErrorLaunchFailure;
-  }
-  if (fail_in > 0) --fail_in;
-  run(kernels.at(f), grid, args);
-  return hipSuccess;
-}
-hipError_t hipGetLastError() {
-  const hipError_t e = last_error;
-  last_error = hipSuccess;
-  return e;
-}
-const char* hipGetErrorString(hipError_t) { return "an error"; }
-hipError_t hipMemcpyAsync(void* to, const void* from, size_t n, hipMemcpyKind, hipStream_t) {
-  std::memmove(to, from, n);
-  return hipSuccess;
-}
-hipError_t hipMemsetAsync(void* to, int v, size_t n, hipStream_t) {
-  std::memset(to, v, n);
-  return hipSuccess;
-}
-hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
-hipError_t hipGetDevice(int* d) {
-  *d = 0;
-  return hipSuccess;
-}
-hipError_t hipDeviceGetAttribute(int* v, hipDeviceAttribute_t, int) {
-  *v = 256;
-  return hipSuccess;
-}
-hipError_t hipPointerGetAttributes(hipPointerAttribute_t*, const void*) { return hipErrorInvalidValue; }
-hipError_t hipFuncSetAttribute(const void*, hipFuncAttribute, int) { return hipSuccess; }
-hipError_t hipGetSymbolAddress(void**, const void*) { return hipErrorInvalidSymbol; }
-
-}  // extern "C"
 
 // ------------------------------------------------------------------ streams
 
