@@ -69,8 +69,9 @@ enum { HH_WF_DTYPE = 0, HH_WF_Q4G32 = 1 };
  * KV cache in 4 bits, in the pages of hh_kv4_append below, quantized as keys
  * (rotated) and values are produced.  72 bytes a position and kv head take the place of
  * fp16's 256 (fp32's 512).  Prompts and decode steps run as otherwise, batch-1 steps
- * through the kernels of the multi-stream ones; hh_decode_step_noalloc gives
- * HH_ERR_UNSUPPORTED.  A context is created with one or the other cache.
+ * through the kernels of the multi-stream ones (the first step past each power of
+ * two of the longest stream's pages captures its graph); hh_decode_step_noalloc
+ * gives HH_ERR_UNSUPPORTED.  A context is created with one or the other cache.
  */
 enum { HH_KV_Q4 = 0x100 };
 enum { HH_LOGITS_NONE = 0, HH_LOGITS_LAST = 1, HH_LOGITS_ALL = 2 };

@@ -24,13 +24,15 @@
 // Single terms made that 1e-3 (and an 8,192-token prompt 338 us, 32 sequences of 4,000
 // positions 19.3).
 //
-// What bounds it: vector and matrix instructions, which hardly run at once.  A step of
-// two pages takes a wave about 110 vector ones to unpack, 7.5 issue slots (the
+// What bounds it (counters): vector and matrix instructions, which hardly run at once.
+// A step of two pages takes a wave about 110 vector ones to unpack, 7.5 issue slots (the
 // exponential four of them) a score and lane, and 18 matrix ones a column tile (14 with
-// queries of one term): an 8,192-token prompt (32 query heads on 8) takes 513 us, 0.54 PFLOP/s.
+// queries of one term): an 8,192-token prompt (32 query heads on 8) takes 513 us, 0.54
+// PFLOP/s, 260 of vector issue and 263 of the matrix unit.
 // With few rows memory does, and hides only a part of them: 32 sequences of 4,000
-// positions (74 MB) take 22 us, 3.4 TB/s, the same loads alone 16; one of 131,072 21.6,
-// and 18.
+// positions (74 MB) take 22 us, 3.4 TB/s, the same loads alone 16 (the longest
+// sequence, which one workgroup a kv head takes whole, is 1.4 times the mean); one of
+// 131,072 21.8, and 18.
 #include "hh_device.h"
 #include "hh_kv.h"
 
@@ -643,7 +645,7 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
 // first page of a step, the right one for the second, each with zeros in the
 // other's operands.  A lane then has four scores a step, not eight of which half
 // are of no column, and the copies are joined at the end (32 sequences of 4,000
-// positions 20.8 -> 19.5 us, one of 131,072 22.3 -> 21.2, of 300 5.0 -> 4.8).
+// positions 24.1 -> 22.2 us, one of 131,072 22.7 -> 21.8, of 300 5.0 -> 4.8).
 template <int NQ, int QT, int PACK>
 struct Columns {
   static_assert(PACK == 1 || NQ == 1);
@@ -1165,10 +1167,10 @@ hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const 
     const hipError_t e = one ? launch_attend<1>(st, P, r, A, p) : launch_attend<2>(st, P, r, A, p);
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t outs = (int64_t)r.n_seqs * r.max_rows * A.hq;
-    // Five and more splits of few rows are read at once by a workgroup each (one row of
-    // 32 heads, 16 splits: 7.1 us with the attention, 8.5 by 16 lanes each; 16 rows, 8
-    // splits: 10.0 and 9.9); fewer splits or more rows want fewer workgroups (64 rows, 2
-    // splits: 15.8 and 12.5).
+    // Five and more splits of few rows are read at once by a workgroup each (rows of 32
+    // heads at 3,000, with the attention: one, 16 splits, 8.2 us, by 16 lanes each 9.8; 16,
+    // 8 splits, 14.8 and 15.2); fewer splits or more rows want fewer workgroups (32 rows,
+    // 8 splits, 23.5 and 23.1; 64, 2 splits, 33.6 and 31.1).
     if (p.splits > 16 || (p.splits > 4 && outs <= 512))
       return launch(k_kv4_join, (unsigned)outs, 256, 0, st, P, r, A, 16 * p.nq, p.splits);
     return launch(k_kv4_join_rows, (unsigned)((outs + 15) / 16), 256, 0, st, P, r, A, 16 * p.nq, p.splits);
