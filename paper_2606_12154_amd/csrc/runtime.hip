@@ -11,6 +11,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <map>
+#include <memory>
 #include <mutex>
 #include <new>
 #include <string>
@@ -908,9 +909,17 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
     base[i] = c->len[ids[i]];
     offset[i + 1] = offset[i] + lens[i];
   }
+  // What a pass lists, at its most (nothing is allocated once kernels are enqueued).
+  const size_t most = std::min((size_t)offset[n], (size_t)L.rows_cap);
+  std::vector<int> rs, rp, tk, last_s, last_p, last_r, starts, first, streams;
+  std::vector<FlashItem> items;
+  for (auto* v : {&rs, &rp, &tk}) v->reserve(most);
+  for (auto* v : {&last_s, &last_p, &last_r, &starts, &first, &streams}) v->reserve(n + 1);
+  items.reserve(most / 64 + n + 1);
   int cur = 0;  // first stream with rows left
   while (cur < n) {
-    std::vector<int> rs, rp, tk, last_s, last_p, last_r;
+    for (auto* v : {&rs, &rp, &tk, &last_s, &last_p, &last_r, &starts, &first, &streams}) v->clear();
+    items.clear();
     while (cur < n && (int)rs.size() < L.rows_cap) {
       const int take = std::min(lens[cur] - done[cur], L.rows_cap - (int)rs.size());
       for (int j = 0; j < take; ++j) {
@@ -929,7 +938,6 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
     const int R = (int)rs.size(), ne = (int)last_r.size();
     // fp16 caches: MFMA attention over each stream's rows where it is the
     // faster one (flash_packed_wins).
-    std::vector<FlashItem> items;
     if (sizeof(TKV) == 2 && !L.kv4 &&
         flash_prefill_supported(g.n_heads / g.n_kv_heads, g.max_context,
                                 (size_t)L.n_pages * 2 * g.n_kv_heads * kPage * kHeadDim)) {
@@ -959,15 +967,14 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
                    slot, c->at<TW>(L.embed), x, d);
     Kv4Pass pass{};
     if (L.kv4) {
-      std::vector<int> starts, first, streams;
-      int most = 1, keys = 1;
+      int longest = 1, keys = 1;
       for (int r = 0; r < R; ++r) {
         if (r == 0 || rs[r] != rs[r - 1]) {
           starts.push_back(r);
           first.push_back(rp[r]);
           streams.push_back(rs[r]);
         }
-        most = std::max(most, r + 1 - starts.back());
+        longest = std::max(longest, r + 1 - starts.back());
         keys = std::max(keys, rp[r] + 1);
       }
       const int ns = (int)starts.size();
@@ -976,7 +983,7 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
       put_ints(st, seqs, starts.data(), ns + 1);
       put_ints(st, seqs + ns + 1, first.data(), ns);
       put_ints(st, seqs + 2 * ns + 1, streams.data(), ns);
-      pass = kv4_pass(c, ns, R, most, seqs, seqs + ns + 1, seqs + 2 * ns + 1, (keys + kPage - 1) / kPage);
+      pass = kv4_pass(c, ns, R, longest, seqs, seqs + ns + 1, seqs + 2 * ns + 1, (keys + kPage - 1) / kPage);
     }
     enqueue_layers<TW, TKV, TM>(c, R, false, 1, -2, nullptr, -1, 0, (int)items.size(), &pass);
     if (ne > 0) {
@@ -1181,21 +1188,24 @@ __global__ void k_zero_words(unsigned long long* p, int n) {
 
 extern "C" {
 
-hh_status hh_workspace_size(const hh_config* cfg, size_t* bytes) {
+hh_status hh_workspace_size(const hh_config* cfg, size_t* bytes) try {
   if (!cfg || !bytes) return HH_ERR_INVALID_ARG;
   std::string why;
   if (!config_supported(*cfg, why)) return HH_ERR_UNSUPPORTED;
   *bytes = make_layout(*cfg).total;
   return HH_OK;
+} catch (const std::bad_alloc&) {
+  return HH_ERR_OOM;
 }
 
-hh_status hh_create(const hh_config* cfg, void* arena, size_t arena_bytes, void* hip_stream, hh_ctx** out) {
+hh_status hh_create(const hh_config* cfg, void* arena, size_t arena_bytes, void* hip_stream, hh_ctx** out) try {
   if (!cfg || !out || !arena || !hip_stream || (reinterpret_cast<uintptr_t>(arena) & 255)) return HH_ERR_INVALID_ARG;
   std::string why;
   if (!config_supported(*cfg, why)) return HH_ERR_UNSUPPORTED;
   Layout L = make_layout(*cfg);
   if (arena_bytes < L.total) return HH_ERR_OOM;
-  hh_ctx* c = new hh_ctx();
+  std::unique_ptr<hh_ctx> owned(new hh_ctx());
+  hh_ctx* c = owned.get();
   c->cfg = without_kv(*cfg);
   c->L = L;
   c->arena = static_cast<char*>(arena);
@@ -1218,6 +1228,9 @@ hh_status hh_create(const hh_config* cfg, void* arena, size_t arena_bytes, void*
   c->pages.assign(cfg->max_streams, {});
   c->refs.assign(L.n_pages, 0);
   c->recorded.assign(cfg->max_streams, {});
+  // (No later call needs host memory for a stream's books once its kernels are enqueued.)
+  for (auto& p : c->pages) p.reserve(L.max_pages);
+  for (auto& r : c->recorded) r.reserve(cfg->max_context);
   c->pending_known.assign(cfg->max_streams, 0);
   for (int p = L.n_pages - 1; p >= 0; --p) c->free_pages.push_back(p);
   // RoPE table: angle p * theta^(-2i/64) in fp64, cos/sin rounded to fp32.
@@ -1232,15 +1245,14 @@ hh_status hh_create(const hh_config* cfg, void* arena, size_t arena_bytes, void*
   if (e == hipSuccess) e = hipMemsetAsync(c->arena + L.page_table, 0, L.row_stream - L.page_table, c->stream);
   if (e == hipSuccess) e = setup_step_kernel(c);
   if (e == hipSuccess) e = hipStreamSynchronize(c->stream);
-  if (e != hipSuccess) {
-    delete c;
-    return HH_ERR_HIP;
-  }
-  *out = c;
+  if (e != hipSuccess) return HH_ERR_HIP;
+  *out = owned.release();
   return HH_OK;
+} catch (const std::bad_alloc&) {
+  return HH_ERR_OOM;
 }
 
-hh_status hh_load_weights(hh_ctx* c, const void* const* tensors, int32_t n_tensors) {
+hh_status hh_load_weights(hh_ctx* c, const void* const* tensors, int32_t n_tensors) try {
   if (!c) return HH_ERR_INVALID_ARG;
   const hh_config& g = c->cfg;
   const int expect = 1 + 9 * g.n_layers + 1 + (g.tied_embeddings ? 0 : 1);
@@ -1374,10 +1386,12 @@ hh_status hh_load_weights(hh_ctx* c, const void* const* tensors, int32_t n_tenso
   c->loaded = true;
   c->err.clear();
   return HH_OK;
+} catch (const std::bad_alloc&) {
+  return HH_ERR_OOM;
 }
 
 hh_status hh_prefill(hh_ctx* c, int32_t s, const int32_t* tokens, int32_t n, int32_t mode, float* logits,
-                     int32_t* next) {
+                     int32_t* next) try {
   if (!c) return HH_ERR_INVALID_ARG;
   if (!c->loaded) return c->fail(HH_ERR_NOT_LOADED, "weights not loaded");
   const hh_config& g = c->cfg;
@@ -1392,10 +1406,12 @@ hh_status hh_prefill(hh_ctx* c, int32_t s, const int32_t* tokens, int32_t n, int
                                     : do_prefill<float, float, float>(c, s, tokens, n, mode, logits, next);
   if (rc != HH_OK) return rc;
   return finish(c, (logits && !is_device_ptr(logits)) || (next && !is_device_ptr(next)));
+} catch (const std::bad_alloc&) {
+  return HH_ERR_OOM;
 }
 
 hh_status hh_prefill_batch(hh_ctx* c, int32_t n, const int32_t* stream_ids, const int32_t* lengths,
-                           const int32_t* tokens, int32_t* next_tokens) {
+                           const int32_t* tokens, int32_t* next_tokens) try {
   if (!c) return HH_ERR_INVALID_ARG;
   if (!c->loaded) return c->fail(HH_ERR_NOT_LOADED, "weights not loaded");
   const hh_config& g = c->cfg;
@@ -1420,10 +1436,12 @@ hh_status hh_prefill_batch(hh_ctx* c, int32_t n, const int32_t* stream_ids, cons
                      : do_prefill_batch<float, float, float>(c, n, stream_ids, lengths, tokens, next_tokens);
   if (rc != HH_OK) return rc;
   return finish(c, next_tokens && !is_device_ptr(next_tokens));
+} catch (const std::bad_alloc&) {
+  return HH_ERR_OOM;
 }
 
 hh_status hh_decode_step(hh_ctx* c, int32_t n, const int32_t* stream_ids, const int32_t* tokens, float* logits,
-                         int32_t* next) {
+                         int32_t* next) try {
   if (!c) return HH_ERR_INVALID_ARG;
   if (!c->loaded) return c->fail(HH_ERR_NOT_LOADED, "weights not loaded");
   const hh_config& g = c->cfg;
@@ -1453,9 +1471,11 @@ hh_status hh_decode_step(hh_ctx* c, int32_t n, const int32_t* stream_ids, const 
                                     : do_decode<float, float, float>(c, n, ids, tokens, logits, next);
   if (rc != HH_OK) return rc;
   return finish(c, (logits && !is_device_ptr(logits)) || (next && !is_device_ptr(next)));
+} catch (const std::bad_alloc&) {
+  return HH_ERR_OOM;
 }
 
-hh_status hh_decode_step_noalloc(hh_ctx* c, int32_t s, const int32_t* token, float* logits, int32_t* next) {
+hh_status hh_decode_step_noalloc(hh_ctx* c, int32_t s, const int32_t* token, float* logits, int32_t* next) try {
   if (!c) return HH_ERR_INVALID_ARG;
   if (!c->loaded) return c->fail(HH_ERR_NOT_LOADED, "weights not loaded");
   const hh_config& g = c->cfg;
@@ -1500,6 +1520,8 @@ hh_status hh_decode_step_noalloc(hh_ctx* c, int32_t s, const int32_t* token, flo
                                     : do_decode<float, float, float>(c, 1, ids, token, logits, next, &w);
   if (rc != HH_OK) return rc;
   return finish(c, (logits && !is_device_ptr(logits)) || (next && !is_device_ptr(next)), step_err_word(g, w));
+} catch (const std::bad_alloc&) {
+  return HH_ERR_OOM;
 }
 
 hh_status hh_reset(hh_ctx* c, int32_t s) {

@@ -11,6 +11,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <map>
+#include <new>
 #include <random>
 #include <string>
 #include <vector>
@@ -121,6 +122,20 @@ static void run_kernel(const std::string& k, dim3 grid, dim3, void** a) {
   }
 }
 
+// ------------------------------------------------------------------ host memory
+
+static int no_memory_in = -1;  // allocations before the one that fails; < 0: none does
+static int asked = 0;
+void* operator new(size_t n) {
+  ++asked;
+  if (no_memory_in == 0) throw std::bad_alloc();
+  if (no_memory_in > 0) --no_memory_in;
+  if (void* p = std::malloc(n ? n : 1)) return p;
+  throw std::bad_alloc();
+}
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, size_t) noexcept { std::free(p); }
+
 // ------------------------------------------------------------------ streams
 
 constexpr int kStreams = 5, kContext = 128;
@@ -133,13 +148,16 @@ struct Streams {
   std::mt19937 rng;
   int rand(int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(rng); }
 
-  explicit Streams(unsigned seed) : rng(seed) {
+  hh_config config{};
+  size_t bytes = 0;
+
+  explicit Streams(unsigned seed, int max_prefill = 0) : rng(seed) {
     dev = Books();
-    hh_config c{};
+    hh_config& c = config;
     c.n_layers = 2; c.d_model = 64; c.n_heads = 2; c.n_kv_heads = 1; c.head_dim = 64; c.ffn_dim = 64; c.vocab = 4096;
     c.rms_eps = 1e-5f; c.rope_theta = 10000.f; c.tied_embeddings = 1; c.dtype = HH_F32;
     c.max_streams = kStreams; c.max_context = kContext; c.page_size = 16; c.weight_format = HH_WF_DTYPE;
-    size_t bytes = 0;
+    c.max_prefill = max_prefill;
     CHECK(hh_workspace_size(&c, &bytes) == HH_OK);
     arena = std::aligned_alloc(256, (bytes + 255) / 256 * 256);
     std::memset(arena, 0, bytes);
@@ -327,6 +345,74 @@ static void check_new_pages() {
   }
 }
 
+// Host memory runs out at the k-th allocation of a call (and stays out): HH_ERR_OOM, nothing thrown and
+// nothing changed, or the call needed no more.
+static void check_no_memory() {
+  static const char* const names[] = {"prompt", "step", "steps", "batch", "fork", "cut", "compact", "reset", "create"};
+  for (int what = 0; what < 9; ++what) {
+    at_op = names[what];
+    bool done = false;
+    for (int k = 0; k < 200 && !done; ++k) {
+      Streams t(30, 24);
+      CHECK(t.feed(0, 30) == HH_OK && t.feed(1, 40) == HH_OK && t.fork(1, {2}) == HH_OK);
+      const std::vector<int> a = t.tokens(60);
+      const int ids[2] = {0, 1}, lens[2] = {30, 30}, dst[2] = {3, 4};
+      int32_t n = 0;
+      hh_ctx* made = nullptr;
+      auto call = [&]() -> hh_status {
+        switch (what) {
+          case 0: return hh_prefill(t.ctx, 0, a.data(), 30, HH_LOGITS_NONE, nullptr, nullptr);
+          case 1: return hh_decode_step(t.ctx, 1, ids, a.data(), nullptr, nullptr);
+          case 2: return hh_decode_step(t.ctx, 2, ids, a.data(), nullptr, nullptr);
+          case 3: return hh_prefill_batch(t.ctx, 2, ids, lens, a.data(), nullptr);
+          case 4: return hh_fork(t.ctx, 1, 2, dst);
+          case 5: return hh_truncate(t.ctx, 2, 35);
+          case 6: return hh_compact(t.ctx, &n);
+          case 7: return hh_reset(t.ctx, 2);
+          default: return hh_create(&t.config, t.arena, t.bytes, reinterpret_cast<void*>(256), &made);
+        }
+      };
+      asked = 0;
+      no_memory_in = k;
+      hh_status rc = HH_OK;
+      bool thrown = false;
+      try {
+        rc = call();
+      } catch (...) {
+        thrown = true;
+      }
+      done = asked <= k;
+      no_memory_in = -1;
+      CHECK(!thrown);
+      if (thrown) return;
+      CHECK(rc == (done ? HH_OK : HH_ERR_OOM));
+      if (what == 8) {
+        if (made) hh_destroy(made);
+        continue;
+      }
+      if (rc == HH_OK) {
+        if (what == 0) t.added(0, {a.begin(), a.begin() + 30});
+        if (what == 1 || what == 2) t.added(0, {a[0]});
+        if (what == 2) t.added(1, {a[1]});
+        if (what == 3) {
+          t.added(0, {a.begin(), a.begin() + 30});
+          t.added(1, {a.begin() + 30, a.end()});
+          t.recorded[0].back() = t.recorded[1].back() = 0;
+        }
+        for (int d : dst)
+          if (what == 4) t.held[d] = t.held[1], t.recorded[d] = t.recorded[1];
+        if (what == 5) t.held[2].resize(35), t.recorded[2].resize(35);
+        if (what == 7) t.held[2].clear(), t.recorded[2].clear();
+      }
+      t.check();
+      CHECK(t.step(1) == HH_OK);
+      t.check();
+      t.refill();
+    }
+    CHECK(done);
+  }
+}
+
 // A full pool: the forks' copies take pages that their streams held.
 static void check_full_pool() {
   for (int k = -1; k < 8; ++k) {
@@ -427,6 +513,7 @@ int main() {
   check_pending_error();
   check_errors();
   check_new_pages();
+  check_no_memory();
   check_full_pool();
   check_any_order();
   if (failures) {
