@@ -36,8 +36,8 @@ struct Kv4Plan {
 
 // Column tiles and waves of a workgroup and key splits over workgroups: those of
 // the least time by what was measured, in ns (48 sizes, 32 query heads on 8, queries of
-// one and of two terms: profiles/kv4_choices.md; the choices cost 1.4% on average
-// against the best ones, 16% at most).  A step (two pages) takes a wave that is alone on
+// one and of two terms; the choices cost 1.4% on average against the best ones, 16% at
+// most).  A step (two pages) takes a wave that is alone on
 // its SIMD 610 ns with one column tile, 700 with two and 1,250 with four, and 205, 285
 // and 390 more for each neighbour there, of which there are up to three, two and one.
 // What comes before and after is 3.5, 5.2 and 6.4 us, and 0.7, 0.25 and 0.4 more for each
