@@ -410,6 +410,128 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
                            void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * A paged cache in 8 bits, and attention over selected blocks of it, on the
+ * caller's own device memory.
+ *
+ * 136 bytes a position and kv head (fp16 takes 256, the 4-bit cache 72), at a
+ * twentieth of the 4-bit cache's error.  A block (the 16 positions of a page of one kv head)
+ * has one scale for its keys and one for its values, and a summary of its keys, by
+ * which a step over a long stream can choose the blocks that it reads.
+ *
+ * Values.  A scale is 2^e, e the least integer from -20 to 9 with max|x| <=
+ * 127 * 2^e over the block's keys (or values); a code is
+ * c = clamp(rint(x / 2^e), -127, 127) (ties to even), the value c * 2^e.
+ * Magnitudes above 65,024 saturate.  A key or value row (64 dimensions of a position)
+ * with an infinity or NaN is marked, counts for no scale, and is NaN: what attends it
+ * is NaN, as it would be unquantized.
+ * While a page fills, its scales grow and never shrink: where rows come behind kept ones
+ * whose scale is 2^d, e is at least d, and kept codes become rint(c * 2^(d - e)).
+ * The summary of a block is m = rint(S / 2^j), S the sum of the key codes over the
+ * slots and j the least of 0 .. 4 with max|S| <= 127 * 2^j; m * 2^(e + j - 4) is its
+ * mean key.
+ *
+ * Pages.  One page of one kv head is a block of HH_KV8_BLOCK bytes; a page is
+ * n_kv_heads blocks in head order, a pool n_pages pages.  Codes are bytes c + 128:
+ *   keys    bytes 0 .. 1023: the code of (slot, dimension 32 h + 8 g + j) is
+ *           byte 256 g + 16 slot + 8 h + j;
+ *   values  bytes 1024 .. 2047: the code of (slot 4 g + i, dimension 4 r + j)
+ *           is byte 1024 + 256 g + 16 r + 4 j + i;
+ *   summary bytes 2048 .. 2111: m, int8, by dimension;
+ *   scales  fp16 at byte 2112 (keys), 2114 (values), 2120 (summary);
+ *   marks   16-bit sets of slots at 2116 (keys), 2118 (values);
+ *   bytes 2122 .. 2127 are 0, those from 2128 on neither read nor written.
+ *
+ * The descriptions are those of the 4-bit cache, with these blocks, and so is what
+ * is said there of streams, devices, captures and pointers.
+ * ------------------------------------------------------------------------ */
+
+enum { HH_KV8_BLOCK = 2176 };
+typedef hh_kv4_pool hh_kv8_pool;  /* pool: n_pages * n_kv_heads * 2176 bytes */
+typedef hh_kv4_rows hh_kv8_rows;
+
+/*
+ * Quantize key and value rows into their pages: arguments, rotation and skipped
+ * rows as in hh_kv4_append.
+ * A page that rows go to is written whole: its slots in front of the call's first
+ * row of that sequence stay (requantized where the scale grows), those behind
+ * its last are dropped and hold zeros.  So a sequence ends with its last
+ * row, and one that was cut is appended to at its new end.  Sequences of one call must
+ * not have rows in the same page, nor may a page be shared that rows go to.
+ * Errors as hh_kv4_append's.
+ */
+hh_status hh_kv8_append(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const void* k, const void* v, int32_t dtype,
+                        int64_t k_stride, int64_t v_stride, const float* rope, int32_t rope_len, void* hip_stream);
+
+/* The values that the pages hold for the given rows, into k and v (c * 2^e
+ * rounded to nearest even to `dtype`, NaN for marked rows).  Rows at positions that
+ * have no page are set to 0.  Errors as hh_kv4_append's. */
+hh_status hh_kv8_read(const hh_kv8_pool* pool, const hh_kv8_rows* rows, void* k, void* v, int32_t dtype,
+                      int64_t k_stride, int64_t v_stride, void* hip_stream);
+
+/* Bytes of device memory that hh_kv8_attention needs for these sizes: as
+ * hh_kv4_attention_workspace. */
+enum { HH_KV8_WORKSPACE_MOST = 16 << 20 };
+hh_status hh_kv8_attention_workspace(const hh_kv8_pool* pool, const hh_kv8_rows* rows, int32_t n_heads, size_t* bytes);
+
+/*
+ * Causal grouped-query attention over the pages: arguments, masks, precision and
+ * errors as in hh_kv4_attention (scale at most 2^100).
+ */
+hh_status hh_kv8_attention(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const void* q, int32_t q_dtype,
+                           int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len,
+                           void* out, int32_t out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                           void* hip_stream);
+
+/* Bytes of device memory that hh_kv8_select needs for these sizes: 0 to
+ * HH_KV8_WORKSPACE_MOST, as above. */
+enum { HH_KV8_MOST_BLOCKS = 1 << 16 };
+hh_status hh_kv8_select_workspace(const hh_kv8_pool* pool, const hh_kv8_rows* rows, int32_t n_heads, int32_t n_blocks,
+                                  size_t* bytes);
+
+/*
+ * For each row and kv head, the n_blocks blocks that score highest.  A row at position
+ * p has the blocks 0 .. p / 16 of its sequence (at most max_pages).  The first keep_first
+ * and the last keep_last of them are selected, and then those between with the largest
+ *   score(b) = (sum_d a_d m_b,d) * 2^(e + j - 4),
+ * the block's mean key against the queries of the kv head's group: a_d = rint(Q_d / 2^f),
+ * f the least integer with max|Q| <= 127 * 2^f, Q the sum of the group's queries
+ * (rotated), in 64 bits.  Scores are exact; among equal ones the lowest block wins.
+ * Queries with an element that is not finite score 0 everywhere.
+ *  q, rope   as in hh_kv4_attention (rotated in 64 bits).
+ *  blocks    device int32 [n_rows][n_kv_heads][n_blocks]: in ascending order, -1
+ *            behind the last where a row has fewer; rows at negative positions
+ *            get -1 alone, and rows in no sequence are left as they are.
+ * Every block but a row's last ones must be full, as appending leaves them
+ * (keep_last >= 1 covers its own).
+ * Errors: INVALID_ARG (as above; keep_first < 0, keep_last < 1, their sum over
+ * n_blocks), UNSUPPORTED (n_blocks or max_pages over 65,536; max_rows * n_kv_heads from
+ * 2^22 on), HIP.
+ */
+hh_status hh_kv8_select(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const void* q, int32_t q_dtype,
+                        int64_t q_stride, int32_t n_heads, const float* rope, int32_t rope_len, int32_t n_blocks,
+                        int32_t keep_first, int32_t keep_last, int32_t* blocks, void* workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
+/* Bytes of device memory that hh_kv8_attention_blocks needs for these sizes: 0 to
+ * HH_KV8_WORKSPACE_MOST, as above. */
+hh_status hh_kv8_attention_blocks_workspace(const hh_kv8_pool* pool, const hh_kv8_rows* rows, int32_t n_heads,
+                                            int32_t n_blocks, size_t* bytes);
+
+/*
+ * Attention over listed blocks: a row at position p attends, for each kv head, to the
+ * positions 0 .. p that lie in the blocks it lists.
+ *  blocks  device int32 [n_rows][n_kv_heads][n_blocks], in any order; entries that
+ *          are no block of the row (negative, or past p / 16) are skipped, and one
+ *          that is listed twice counts twice.  A row without any gives 0.
+ * Otherwise as hh_kv8_attention.  Errors: as there, INVALID_ARG (blocks NULL or
+ * misaligned, n_blocks < 1), UNSUPPORTED (n_blocks over 65,536).
+ */
+hh_status hh_kv8_attention_blocks(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const int32_t* blocks,
+                                  int32_t n_blocks, const void* q, int32_t q_dtype, int64_t q_stride, int32_t n_heads,
+                                  float scale, const float* rope, int32_t rope_len, void* out, int32_t out_dtype,
+                                  int64_t out_stride, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * Pages of any paged cache: n_layers pools of n_pages pages of page_bytes, a
  * pool every layer_stride bytes from `pool` (device, 16-byte aligned;
  * page_bytes and layer_stride multiples of 16, page_bytes at most 64 MiB;

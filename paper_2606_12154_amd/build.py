@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libhh.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["k_decode.hip", "k_gemm.hip", "k_attn_prefill.hip", "k_load.hip", "k_step.hip", "k_kv4.hip",
-           "k_pages.hip", "kv_ops.hip", "runtime.hip", "router.cpp"]
+           "k_kv8.hip", "k_kv8_select.hip", "k_pages.hip", "kv_ops.hip", "kv8_ops.hip", "runtime.hip", "router.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,5 +1,6 @@
-// Launchers of the 4-bit paged cache's kernels (k_kv4.hip) and of the page
-// kernels (k_pages.hip); arguments have been checked by the callers.
+// Launchers of the quantized paged caches' kernels (4 bits: k_kv4.hip; 8 bits:
+// k_kv8.hip, k_kv8_select.hip) and of the page kernels (k_pages.hip); arguments have
+// been checked by the callers.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -7,6 +8,7 @@
 #include <stdint.h>
 
 #include "kv4_plan.h"
+#include "kv8_plan.h"
 
 namespace hh {
 
@@ -59,6 +61,47 @@ inline Kv4Plan kv4_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
   return kv4_plan(Kv4Sizes{R.n_seqs, R.n_rows, R.max_rows, hq, P.hkv, pages});
 }
 hipError_t kv4_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv4Plan& p);
+
+// ---- the 8-bit cache: blocks of another size, descriptions alike
+constexpr int kKv8Block = 2176;  // codes 1024 + 1024, summary 64, scales and marks 16 (of 64)
+constexpr int kKv8Values = 1024, kKv8Sums = 2048, kKv8Scales = 2112;  // byte offsets
+constexpr int kKv8Low = -20, kKv8High = 9;                            // exponents of scales
+
+hipError_t kv8_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
+                      int64_t k_stride, int64_t v_stride, RopeTable rope);
+hipError_t kv8_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
+                    int64_t v_stride);
+int64_t kv8_row_threads(const Kv4Pool& P, const Kv4Rows& R);
+
+inline Kv8Plan kv8_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
+  return kv8_plan(Kv4Sizes{R.n_seqs, R.n_rows, R.max_rows, hq, P.hkv, pages});
+}
+hipError_t kv8_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8Plan& p);
+
+// Listed blocks: device [n_rows][hkv][n].
+struct Kv8List {
+  const int* blocks;
+  int n;
+};
+inline Kv8ListPlan kv8_list_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int n) {
+  return kv8_list_plan(Kv4Sizes{R.n_seqs, R.n_rows, R.max_rows, hq, P.hkv, P.max_pages}, n);
+}
+hipError_t kv8_attend_list(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8List& list,
+                           const Kv8ListPlan& p);
+
+struct Kv8Select {
+  const void* q;
+  int64_t q_stride;
+  int q_type, hq;
+  RopeTable rope;
+  int n, first, last;  // blocks a row, forced ones at both ends
+  int* out;            // [n_rows][hkv][n]
+  float* scores;       // workspace, see Kv8SelectPlan
+};
+inline Kv8SelectPlan kv8_select_plan(const Kv4Pool& P, const Kv4Rows& R) {
+  return kv8_select_plan(Kv4Sizes{R.n_seqs, R.n_rows, R.max_rows, P.hkv, P.hkv, P.max_pages});
+}
+hipError_t kv8_select(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv8Select& S, const Kv8SelectPlan& p);
 
 // n_layers pools of pages of `bytes` (a multiple of 16), layer_stride bytes apart.
 struct PagePool {

@@ -1,0 +1,597 @@
+// A paged KV cache in 8 bits: quantizing rows into pages, reading them back, and
+// causal grouped-query attention over the pages or over listed ones (gfx950).
+//
+// Values are c * s: c an integer in -127 .. 127, s a power of two of the page's and head's
+// keys, or of its values.  So a code's byte n = c + 128 behind the byte 0x64 (1024 + n as
+// fp16) becomes c * s / 16 by one packed fp16 FMA, (1024 + n) t - 1152 t with t = s / 16,
+// without a rounding (1152 s itself would pass fp16's range): a byte permutation
+// and an FMA for two elements.  The sixteens go into the scale of the scores and out of the sums.
+//
+// The block of a (page, head) is laid out so that a lane's 16 bytes are what it needs
+// as operands of mfma_f32_16x16x32_f16 (lane l: row or column l % 16, contraction elements
+// 8 (l / 16) .. + 7), with no transposition:
+//   keys    lane l holds slot l % 16, dimensions 8 (l / 16) .. + 7 of each half;
+//   values  lane l holds dimensions 4 (l % 16) .. + 3, of each its slots 4 (l / 16) .. + 3.
+// The scores of two pages, S^T[slot][query], leave each lane with the slots of both pages
+// that its value bytes hold (see kv_attend.h for what follows).
+#include "kv_attend.h"
+
+#include <type_traits>
+
+namespace hh {
+namespace {
+
+// ------------------------------------------------------------------ append and read
+
+// The least e with a <= 127 * 2^e, within the format's; a is finite and not negative.
+__device__ __forceinline__ int scale_exponent(float a) {
+  const int e = __builtin_amdgcn_frexp_expf(a) - (__builtin_amdgcn_frexp_mantf(a) <= 127.f / 128.f ? 7 : 6);
+  return a > 0.f ? min(max(e, kKv8Low), kKv8High) : kKv8Low;
+}
+__device__ __forceinline__ float power2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+__device__ __forceinline__ float from_half(unsigned bits) { return (float)__builtin_bit_cast(_Float16, (unsigned short)bits); }
+__device__ __forceinline__ unsigned half_bits(float s) { return __builtin_bit_cast(unsigned short, (_Float16)s); }
+// A held scale's exponent, whatever the bytes say.
+__device__ __forceinline__ int held_exponent(unsigned bits) {
+  return min(max((int)(__float_as_uint(from_half(bits & 0x7fffu)) >> 23) - 127, kKv8Low), kKv8High);
+}
+
+// Four codes as bytes c + 128, a's the lowest.
+__device__ __forceinline__ unsigned bytes_of(float a, float b, float c, float d) {
+  const unsigned lo = (unsigned)((int)fmaf(b, 256.f, a) + 0x8080), hi = (unsigned)((int)fmaf(d, 256.f, c) + 0x8080);
+  return lo | hi << 16;
+}
+__device__ __forceinline__ float code_at(unsigned w, int i) { return (float)((int)(w >> (8 * i) & 255u) - 128); }
+__device__ __forceinline__ float clamp127(float c) { return __builtin_amdgcn_fmed3f(c, -127.f, 127.f); }
+
+__device__ __forceinline__ unsigned max16(unsigned x) { return max_dpp<0x128>(max_dpp<0x124>(max_dpp<0x4E>(max_dpp<0xB1>(x)))); }
+
+// One wave has one (page, head) of one sequence: the rows of the call that lie in that
+// page, and what the page held in front of them.  Its scales become those that the largest
+// of the new rows need, and never less than the kept ones' own: codes that stay are
+// divided by the power of two between, to nearest even, so that a value that was
+// held through several such steps is off by less than one step of the last scale.
+// The page is written whole: slots behind the rows hold zeros.
+__global__ __launch_bounds__(256) void k_kv8_append(Kv4Pool P, Kv4Rows R, const void* __restrict__ k,
+                                                    const void* __restrict__ v, int type, int64_t ks, int64_t vs,
+                                                    RopeTable rope, int tiles) {
+  const int lane = threadIdx.x & 63;
+  const int head = blockIdx.y * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (head >= P.hkv) return;
+  const unsigned sq = blockIdx.x / (unsigned)tiles;
+  const int tile = blockIdx.x - sq * tiles;
+  const Seq q = load_seq(P, R, R.seq0 + sq);
+  const int lo = max(q.first, 0);
+  int hi = min(q.first + q.n, P.max_pages * kPage);
+  if (rope.at) hi = min(hi, rope.len);
+  const int page = lo / kPage + tile;
+  // (page * kPage may pass 31 bits.)  Without rows the page stays as it is.
+  if (lo >= hi || page >= (hi + kPage - 1) >> 4) return;
+  const int id = P.table[(size_t)q.trow * P.max_pages + page];
+  if ((unsigned)id >= (unsigned)P.n_pages) return;
+  unsigned char* blk = P.pool + ((size_t)id * P.hkv + head) * kKv8Block;
+  const int r = lane & 15, g = lane >> 4;
+  const int from = max(lo - page * kPage, 0), to = min(hi - page * kPage, kPage);  // the page's new slots
+
+  // What the page holds in front of them.
+  u32x4 old_k = {0u, 0u, 0u, 0u}, old_v = old_k;
+  unsigned old_s = 0, old_bad = 0;
+  if (from > 0) {
+    old_k = *reinterpret_cast<const u32x4*>(blk + 16 * lane);
+    old_v = *reinterpret_cast<const u32x4*>(blk + kKv8Values + 16 * lane);
+    old_s = *reinterpret_cast<const unsigned*>(blk + kKv8Scales);
+    old_bad = *reinterpret_cast<const unsigned*>(blk + kKv8Scales + 4);
+    const unsigned kept = (1u << from) - 1u;
+    old_bad &= kept | kept << 16;
+  }
+
+  // Keys: lane (slot r, quarter g) has whole rotation pairs (i, i + 32).
+  float x[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = 0.f;
+  const bool mine = r >= from && r < to;
+  if (mine) {
+    const int pos = page * kPage + r;
+    const size_t at = (size_t)(q.row0 + (pos - q.first)) * ks + head * 64 + 8 * g;
+    load_row<8>(k, at, type, x);
+    load_row<8>(k, at + 32, type, x + 8);
+    if (rope.at) {
+      const float2* cs = rope.at + (size_t)pos * 32 + 8 * g;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 t = cs[i];
+        const double a = x[i], b = x[8 + i], c = t.x, s = t.y;
+        x[i] = (float)(a * c - b * s);
+        x[8 + i] = (float)(b * c + a * s);
+      }
+    }
+  }
+  // Values: lane (r, g) has slots 4 g .. + 3, dimensions 4 r .. + 3.
+  float y[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int slot = 4 * g + i;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[i][j] = 0.f;
+    if (slot >= from && slot < to)
+      load_row<4>(v, (size_t)(q.row0 + (page * kPage + slot - q.first)) * vs + head * 64 + 4 * r, type, y[i]);
+  }
+
+  // Rows that are not finite: marked, codes of 0.
+  unsigned bad_k, bad_v;
+  {
+    unsigned top = 0u;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, magnitude(x[i]));
+    top = rows_max(top);
+    const bool bad = top >= kInfBits;
+    bad_k = (unsigned)__builtin_amdgcn_ballot_w64(bad) & 0xffffu;
+    if (bad) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+      top = 0u;
+    }
+    top = max16(top);
+    const int need = scale_exponent(__uint_as_float(top)), before = held_exponent(old_s & 0xffffu);
+    const int e = from > 0 ? max(need, before) : need;
+    const float down = power2(-e), shrink = power2(before - e);
+    float c[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      c[i] = r < from ? clamp127(rintf(code_at(old_k[i >> 2], i & 3) * (from > 0 ? shrink : 0.f))) : clamp127(rintf(x[i] * down));
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = bytes_of(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]);
+    *reinterpret_cast<u32x4*>(blk + 16 * lane) = w;
+
+    // The summary: sums of codes over the slots, a lane's 16 dimensions in pairs
+    // a + 4096 b (both at most 2,032, so the pair is exact), in 8 bits.
+    float high = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = row_sum16(fmaf(c[8 + i], 4096.f, c[i]));
+      c[8 + i] = rintf(t * (1.f / 4096.f));
+      c[i] = fmaf(c[8 + i], -4096.f, t);
+      high = fmaxf(high, fmaxf(fabsf(c[i]), fabsf(c[8 + i])));
+    }
+    high = rows_max(high);
+    const int less = (high > 127.f) + (high > 254.f) + (high > 508.f) + (high > 1016.f);
+    const float part = power2(-less);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c[i] = rintf(c[i] * part);
+    if (r == 0) {
+      unsigned* m = reinterpret_cast<unsigned*>(blk + kKv8Sums + 8 * g);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float* z = c + 8 * h;
+        *reinterpret_cast<u32x2*>(m + 8 * h) = u32x2{bytes_of(z[0], z[1], z[2], z[3]) ^ 0x80808080u,
+                                                     bytes_of(z[4], z[5], z[6], z[7]) ^ 0x80808080u};
+      }
+    }
+    // The last of these is the summary's scale, for means.
+    old_s = (old_s & 0xffff0000u) | half_bits(power2(e));
+    old_k[0] = half_bits(power2(e + less - 4));
+  }
+  {
+    unsigned top[4], all = 0u, marks = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      top[i] = 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top[i] = max(top[i], magnitude(y[i][j]));
+      top[i] = max16(top[i]);
+      if (top[i] >= kInfBits) {
+        marks |= 1u << (4 * g + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[i][j] = 0.f;
+        top[i] = 0u;
+      }
+      all = max(all, top[i]);
+    }
+    bad_v = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad_v |= (unsigned)__builtin_amdgcn_readlane((int)marks, 16 * i);
+    all = rows_max(all);
+    const int need = scale_exponent(__uint_as_float(all)), before = held_exponent(old_s >> 16);
+    const int e = from > 0 ? max(need, before) : need;
+    const float down = power2(-e), shrink = power2(before - e);
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float c[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        c[i] = 4 * g + i < from ? clamp127(rintf(code_at(old_v[j], i) * shrink)) : clamp127(rintf(y[i][j] * down));
+      w[j] = bytes_of(c[0], c[1], c[2], c[3]);
+    }
+    *reinterpret_cast<u32x4*>(blk + kKv8Values + 16 * lane) = w;
+    old_s = (old_s & 0xffffu) | half_bits(power2(e)) << 16;
+  }
+  if (lane == 0)
+    *reinterpret_cast<u32x4*>(blk + kKv8Scales) = u32x4{old_s, old_bad | bad_k | bad_v << 16, old_k[0], 0u};
+}
+
+// The same lanes the other way round.  Tiles are counted from the page of the
+// first position, which may be negative: such rows, and those past the page
+// table, are set to zero.
+__global__ __launch_bounds__(256) void k_kv8_read(Kv4Pool P, Kv4Rows R, void* __restrict__ k, void* __restrict__ v,
+                                                  int type, int64_t ks, int64_t vs, int tiles) {
+  const int lane = threadIdx.x & 63;
+  const int head = blockIdx.y * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (head >= P.hkv) return;
+  const unsigned sq = blockIdx.x / (unsigned)tiles;
+  const int tile = blockIdx.x - sq * tiles;
+  const Seq q = load_seq(P, R, R.seq0 + sq);
+  const int page = (q.first >> 4) + tile;  // floor
+  const int hi = q.first + q.n;
+  if (page >= (hi + kPage - 1) >> 4) return;  // (page * kPage may pass 31 bits)
+  const bool held = page >= 0 && page < P.max_pages;
+  const unsigned id = (unsigned)P.table[(size_t)q.trow * P.max_pages + (held ? page : 0)];
+  // An id outside the pool reads its first page.
+  const unsigned char* blk = P.pool + ((size_t)(id < (unsigned)P.n_pages ? id : 0u) * P.hkv + head) * kKv8Block;
+  const int r = lane & 15, g = lane >> 4;
+  const u32x4 kw = *reinterpret_cast<const u32x4*>(blk + 16 * lane);
+  const u32x4 vw = *reinterpret_cast<const u32x4*>(blk + kKv8Values + 16 * lane);
+  const u32x2 sc = *reinterpret_cast<const u32x2*>(blk + kKv8Scales);
+  const unsigned bad = sc[1];
+  const float k_scale = from_half(sc[0] & 0xffffu), v_scale = from_half(sc[0] >> 16);
+
+  {
+    const int pos = page * kPage + r;
+    if (pos >= q.first && pos < hi) {
+      const float s = bad >> r & 1u ? NAN : k_scale;
+      const size_t at = (size_t)(q.row0 + (pos - q.first)) * ks + head * 64 + 8 * g;
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = held ? code_at(kw[i >> 2], i & 3) * s : 0.f;
+      store_row<8>(k, at, type, x);
+      store_row<8>(k, at + 32, type, x + 8);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int slot = 4 * g + i, pos = page * kPage + slot;
+    if (pos < q.first || pos >= hi) continue;
+    const float s = bad >> (16 + slot) & 1u ? NAN : v_scale;
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = held ? code_at(vw[j], i) * s : 0.f;
+    store_row<4>(v, (size_t)(q.row0 + (pos - q.first)) * vs + head * 64 + 4 * r, type, x);
+  }
+}
+
+// ------------------------------------------------------------------ attention
+
+struct PageRegs {
+  u32x4 k, v;
+  u32x2 s;  // scales, marks
+};
+
+// The block as a buffer: its base stays in scalar registers, a lane's offset in one
+// vector register.
+__device__ __forceinline__ void load_page(PageRegs& r, const unsigned char* blk, unsigned lane) {
+  const auto b = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(blk), 0, kKv8Block, 0x00027000);
+  r.k = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, 16 * lane, 0, 0));
+  r.v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, 16 * lane + kKv8Values, 0, 0));
+  r.s = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, 0, kKv8Scales, 0));
+}
+
+// Bytes 2 J and 2 J + 1 of w as 1024 + n.
+template <int J>
+__device__ __forceinline__ f16x2 codes16(unsigned w) {
+  return __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, J ? 0x04030402u : 0x04010400u));
+}
+// A scale's sixteenth and -1152 times that, each twice.
+struct Scale {
+  f16x2 s, b;
+};
+__device__ __forceinline__ Scale scale_of(unsigned both) {
+  Scale z;
+  z.s = __builtin_bit_cast(f16x2, both) * f16x2{(_Float16)0.0625f, (_Float16)0.0625f};
+  z.b = z.s * f16x2{(_Float16)-1152, (_Float16)-1152};
+  return z;
+}
+__device__ __forceinline__ f16x4 four(unsigned w, Scale z) {
+  const f16x2 lo = __builtin_elementwise_fma(codes16<0>(w), z.s, z.b), hi = __builtin_elementwise_fma(codes16<1>(w), z.s, z.b);
+  return f16x4{lo[0], lo[1], hi[0], hi[1]};
+}
+
+// A page's operands: keys of each half, and the values of each dimension of four.
+// Without MASK every column sees every slot, so that a page with a marked one makes all
+// of them NaN; with it the marks go through the scores, to the rows that see them.
+template <bool MASK>
+__device__ __forceinline__ void operands(const PageRegs& p, f16x8* kf, f16x4* vf) {
+  unsigned sk = __builtin_amdgcn_perm(p.s[0], p.s[0], 0x01000100u), sv = __builtin_amdgcn_perm(p.s[0], p.s[0], 0x03020302u);
+  if constexpr (!MASK)
+    if (p.s[1]) sk = 0x7e007e00u;
+  const Scale a = scale_of(sk), b = scale_of(sv);
+  kf[0] = join8(four(p.k[0], a), four(p.k[1], a));
+  kf[1] = join8(four(p.k[2], a), four(p.k[3], a));
+#pragma unroll
+  for (int j = 0; j < 4; ++j) vf[j] = four(p.v[j], b);
+}
+
+constexpr int kNowhere = 1 << 30;  // a listed block that is none: behind every column's keys
+
+// A workgroup has a tile of 16 NQ columns; its W waves take the tile's pages (LIST: the
+// blocks that the columns' one row lists) in turn, two a step, and join at the end.
+template <int NQ, int QT, int W, int PACK, bool LIST>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(waves_fit(NQ)))) void
+k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits_, Div tiles_, Div group, Div row_tiles_) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const unsigned b1 = blockIdx.x / heads, b2 = b1 / splits_, sq = b2 / tiles_;
+  const int split = b1 - b2 * splits_.d, splits = splits_.d;
+  // The last tiles have the most keys: they go first.
+  const int tile = tiles_.d - 1 - (b2 - sq * tiles_.d);
+  const Seq s = load_seq(P, R, R.seq0 + sq);
+  const int G = group.d, own = LIST ? (unsigned)tile / row_tiles_ : 0;  // LIST: the row
+  if (LIST && own >= s.n) return;
+  const int cols = LIST ? (own + 1) * G : s.n * G;  // below 2^31 with a tile to spare (kv8_plan)
+  const Place w{s, (int)(blockIdx.x - b1 * heads.d), G, cols,
+                LIST ? own * G + 16 * (tile - own * (int)row_tiles_.d) : tile * (16 * NQ), group};
+  if (w.c0 >= cols) return;
+  // Keys of the tile's first and last row.
+  const int most = P.max_pages * kPage;
+  const int row_a = (unsigned)w.c0 / group, row_b = (unsigned)(min(w.c0 + 16 * NQ, cols) - 1) / group;
+  const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
+  const int np = LIST ? B.n : (some_see + kPage - 1) / kPage;
+  const int per = split_pages(np, splits);
+  const int p0 = split * per, p1 = min(p0 + per, np);
+  const bool joined = per < np;  // several splits have keys
+  if (split > 0 && p0 >= np) return;
+
+  // What the first step needs goes out before the queries are worked on.  Loads
+  // run one step ahead; what would lie behind the wave's last step is its last
+  // step again (no branch around loads, whose waits would then have to assume that it was
+  // not taken).  Lane i holds the page ids of the i-th of 64 steps.
+  const int* row = P.table + (size_t)s.trow * P.max_pages;
+  const int* list = LIST ? B.blocks + ((size_t)(s.row0 + own) * P.hkv + w.head) * B.n : nullptr;
+  constexpr int STEP = 2 * W;
+  int p = p0 + 2 * wave;
+  const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
+  unsigned ids[2];
+  int at[2];                 // LIST: the blocks' first positions
+  uint64_t todo = 0, full = 0;  // LIST: steps with a block, steps that every column sees whole
+  auto load_ids = [&](int q) {
+    const int from = LIST ? q + lane * STEP : min(q + lane * STEP, last);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int page = max(min(from + i, np - 1), 0);
+      if constexpr (LIST) {
+        const int b = list[page];
+        const bool in = from + i < p1 && b >= 0 && b <= (some_see - 1) >> 4;
+        at[i] = in ? b * kPage : kNowhere;
+        page = in ? b : 0;
+      }
+      const unsigned x = (unsigned)row[page];
+      ids[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
+    }
+    if constexpr (LIST) {
+      todo = __builtin_amdgcn_ballot_w64(min(at[0], at[1]) < kNowhere);
+      full = __builtin_amdgcn_ballot_w64(max(at[0], at[1]) + kPage <= some_see);
+    }
+  };
+  auto fetch_step = [&](PageRegs* pr, int i) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const unsigned id = (unsigned)__builtin_amdgcn_readlane((int)ids[j], i);
+      load_page(pr[j], P.pool + ((size_t)id * (unsigned)P.hkv + (unsigned)w.head) * kKv8Block, (unsigned)lane);
+    }
+  };
+  int ahead = 0;  // the step that is fetched next
+  auto fetch = [&](PageRegs* pr) {
+    if constexpr (LIST) {
+      // The next step with a block (or any other, once there is none).
+      ahead = todo ? __builtin_ctzll(todo) : 0;
+      fetch_step(pr, ahead);
+    } else {
+      if (ahead == 64) {
+        load_ids(p + STEP);
+        ahead = 0;
+      }
+      fetch_step(pr, ahead);
+      ++ahead;
+    }
+  };
+  load_ids(p);
+  // Of several tiles, each wave makes one's queries for all.
+  RawQuery raw;
+  if (NQ == 1 || wave < NQ) load_query<QT, PACK>(raw, w, A, NQ == 1 ? 0 : wave);
+  PageRegs a[2], c[2];
+  fetch(a);
+  Columns<NQ, QT, PACK> C;
+  C.start(w, most);
+  if constexpr (PACK == 2) {
+    C.pack(make_query<QT>(raw, A));
+  } else if constexpr (NQ == 1) {
+    C.q[0] = make_query<QT>(raw, A);
+  } else {
+    __shared__ f16x8 made[NQ][2 * QT][64];
+    __shared__ float made_qs[NQ][64];
+    if (wave < NQ) {
+      const Query<QT> z = make_query<QT>(raw, A);
+#pragma unroll
+      for (int i = 0; i < 2 * QT; ++i) made[wave][i][lane] = i < 2 ? z.h[i] : z.l[i - 2];
+      made_qs[wave][lane] = z.qs;
+    }
+    lds_barrier();
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+      for (int i = 0; i < 2 * QT; ++i) (i < 2 ? C.q[t].h[i] : C.q[t].l[i - 2]) = made[t][i][lane];
+      C.q[t].qs = made_qs[t][lane];
+    }
+  }
+
+  auto step = [&](const PageRegs* pr, int at0, int at1, auto masked) {
+    constexpr bool MASK = decltype(masked)::value;
+    f16x8 kf[2][2], vf[4];
+    f16x4 va[4], vb[4];
+    operands<MASK>(pr[0], kf[0], va);
+    operands<MASK>(pr[1], kf[1], vb);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vf[j] = join8(va[j], vb[j]);
+    unsigned bad[2] = {0u, 0u};
+    if constexpr (MASK) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) bad[i] = (pr[i].s[1] | pr[i].s[1] >> 16) >> (4 * g) & 15u;
+    }
+    f32x4 sc[NQ][2];
+    f16x8 ph[NQ], pl[NQ];
+    C.scores(kf, sc);
+    C.template weights<MASK>(sc, at0, at1, PACK == 2 ? (C.right() ? bad[1] : bad[0]) : bad[0] | bad[1] << 4, ph, pl);
+    C.values(vf, ph, pl);
+  };
+  if constexpr (LIST) {
+    while (true) {
+      while (todo) {
+        const int now = ahead;
+        todo &= todo - 1;
+        fetch(c);
+        if (full >> now & 1)
+          step(a, 0, 0, std::false_type());
+        else
+          step(a, __builtin_amdgcn_readlane(at[0], now), __builtin_amdgcn_readlane(at[1], now), std::true_type());
+        a[0] = c[0];
+        a[1] = c[1];
+      }
+      p += 64 * STEP;
+      if (p >= p1) break;
+      load_ids(p);
+      fetch(a);
+    }
+  } else {
+    const int whole = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
+    bool swapped = false;
+    while (p < whole) {
+      fetch(c);
+      step(a, 0, 0, std::false_type());
+      p += STEP;
+      if (p >= whole) {
+        swapped = true;
+        break;
+      }
+      fetch(a);
+      step(c, 0, 0, std::false_type());
+      p += STEP;
+    }
+    if (swapped) {
+      a[0] = c[0];
+      a[1] = c[1];
+    }
+    while (p < p1) {
+      fetch(c);
+      step(a, p * kPage, (p + 1) * kPage, std::true_type());
+      a[0] = c[0];
+      a[1] = c[1];
+      p += STEP;
+    }
+  }
+
+  // Join the waves: of four of them, wave v takes dimensions 16 g + 4 v .. + 3.
+  __shared__ f32x4 lo[W][4][64];
+  __shared__ float2 ls[W][64];
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    if (t) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{C.o[t][0][i], C.o[t][1][i], C.o[t][2][i], C.o[t][3][i]};
+    ls[wave][lane] = make_float2(C.base_of(t), C.sum[t][0]);
+    __syncthreads();
+    if (wave >= 4) continue;
+    float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < W; ++v) m = fmaxf(m, ls[v][lane].x);
+#pragma unroll
+    for (int v = 0; v < W; ++v) {
+      const float2 z = ls[v][lane];
+      const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
+      const f32x4 y = lo[v][wave][lane];
+      l += f * z.y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+    }
+    if constexpr (PACK == 2) {
+      const float m2 = fmaxf(m, other8(m)), f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - m2) : 0.f;
+      m = m2;
+      l = f * l + other8(f * l);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = f * x[j] + other8(f * x[j]);
+      if (C.right()) continue;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] *= 16.f;  // of the values' scale
+    put<4>(R, A, w, w.c0 + 16 * t + r, 16 * g + 4 * wave, x, l, m, joined, split, splits);
+  }
+}
+
+template <int QT>
+hipError_t launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8Plan& p) {
+  const auto kernel = p.nq == 2     ? k_kv8_attend<2, QT, 4, 1, false>
+                      : p.nq == 4   ? k_kv8_attend<4, QT, 4, 1, false>
+                      : p.waves == 4 ? (p.packed ? k_kv8_attend<1, QT, 4, 2, false> : k_kv8_attend<1, QT, 4, 1, false>)
+                                     : (p.packed ? k_kv8_attend<1, QT, 8, 2, false> : k_kv8_attend<1, QT, 8, 1, false>);
+  const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
+  return launch(kernel, groups, 64 * p.waves, 0, st, P, R, A, Kv8List{nullptr, 0}, div_by(P.hkv), div_by(p.splits),
+                div_by(p.tiles), div_by(A.hq / P.hkv), div_by(1));
+}
+
+template <int QT>
+hipError_t launch_list(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8List& B,
+                       const Kv8ListPlan& p) {
+  const auto kernel = p.packed ? k_kv8_attend<1, QT, 4, 2, true> : k_kv8_attend<1, QT, 4, 1, true>;
+  const int tiles = R.max_rows * p.tiles;
+  const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * tiles * p.splits);
+  return launch(kernel, groups, 64 * p.waves, 0, st, P, R, A, B, div_by(P.hkv), div_by(p.splits), div_by(tiles),
+                div_by(A.hq / P.hkv), div_by(p.tiles));
+}
+
+// A wave a (page, head), as in the 4-bit cache's calls.
+int row_heads(const Kv4Pool& P, const Kv4Rows& R) {
+  return (int64_t)R.n_seqs * row_tiles(R) * P.hkv <= 1024 ? 1 : std::min(P.hkv, 4);
+}
+dim3 row_grid(const Kv4Pool& P, const Kv4Rows& R, int heads) {
+  return dim3((unsigned)R.n_seqs * (unsigned)row_tiles(R), (unsigned)((P.hkv + heads - 1) / heads));
+}
+
+}  // namespace
+
+int64_t kv8_row_threads(const Kv4Pool& P, const Kv4Rows& R) { return (int64_t)row_tiles(R) * 64 * row_heads(P, R); }
+
+hipError_t kv8_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const void* k, const void* v, int type,
+                      int64_t k_stride, int64_t v_stride, RopeTable rope) {
+  const int h = row_heads(P, R);
+  return by_sequences(R, kv8_row_threads(P, R), [&](const Kv4Rows& r) {
+    return launch(k_kv8_append, row_grid(P, r, h), 64 * h, 0, st, P, r, k, v, type, k_stride, v_stride, rope, row_tiles(r));
+  });
+}
+
+hipError_t kv8_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k, void* v, int type, int64_t k_stride,
+                    int64_t v_stride) {
+  const int h = row_heads(P, R);
+  return by_sequences(R, kv8_row_threads(P, R), [&](const Kv4Rows& r) {
+    return launch(k_kv8_read, row_grid(P, r, h), 64 * h, 0, st, P, r, k, v, type, k_stride, v_stride, row_tiles(r));
+  });
+}
+
+hipError_t kv8_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8Plan& p) {
+  // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers.
+  const bool one = A.q_type != kRowF32 && !A.rope.at;
+  return by_sequences(R, p.threads, [&](const Kv4Rows& r) {
+    const hipError_t e = one ? launch_attend<1>(st, P, r, A, p) : launch_attend<2>(st, P, r, A, p);
+    return e != hipSuccess || p.splits == 1 ? e : launch_join(st, P, r, A, 16 * p.nq, p.splits, 0);
+  });
+}
+
+hipError_t kv8_attend_list(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8List& B,
+                           const Kv8ListPlan& p) {
+  const bool one = A.q_type != kRowF32 && !A.rope.at;
+  const int per = 2 * (((B.n + 1) / 2 + p.splits - 1) / p.splits), used = (B.n + per - 1) / per;
+  return by_sequences(R, p.threads, [&](const Kv4Rows& r) {
+    const hipError_t e = one ? launch_list<1>(st, P, r, A, B, p) : launch_list<2>(st, P, r, A, B, p);
+    return e != hipSuccess || used == 1 ? e : launch_join(st, P, r, A, 16, p.splits, used);
+  });
+}
+
+}  // namespace hh

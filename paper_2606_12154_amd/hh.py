@@ -24,13 +24,19 @@ HH_LOGITS_NONE, HH_LOGITS_LAST, HH_LOGITS_ALL = 0, 1, 2
 HH_WF_DTYPE, HH_WF_Q4G32 = 0, 1
 HH_KV_Q4 = 0x100  # added to a weight format: 4-bit KV cache
 HH_KV4_WORKSPACE_MOST = 16 << 20  # bound of hh_kv4_attention_workspace
+HH_KV8_BLOCK = 2176  # bytes of one page of one kv head
+HH_KV8_WORKSPACE_MOST = 16 << 20  # bound of the hh_kv8 calls' workspaces
+HH_KV8_MOST_BLOCKS = 1 << 16
 
 EXPORTED = ["hh_workspace_size", "hh_create", "hh_load_weights", "hh_prefill", "hh_prefill_batch", "hh_decode_step",
             "hh_decode_step_noalloc", "hh_reset", "hh_stream_length", "hh_read_argmax", "hh_destroy", "hh_last_error",
             "hh_q4g32_quantize", "hh_router_create", "hh_router_query", "hh_router_route",
             "hh_router_size", "hh_router_destroy", "hh_render_marker", "hh_read_probe",
             "hh_kv4_append", "hh_kv4_read", "hh_kv4_attention_workspace", "hh_kv4_attention", "hh_kv_copy_pages",
-            "hh_kv_compact_workspace", "hh_kv_compact", "hh_fork", "hh_truncate", "hh_compact"]
+            "hh_kv_compact_workspace", "hh_kv_compact", "hh_fork", "hh_truncate", "hh_compact",
+            "hh_kv8_append", "hh_kv8_read", "hh_kv8_attention_workspace", "hh_kv8_attention",
+            "hh_kv8_select_workspace", "hh_kv8_select", "hh_kv8_attention_blocks_workspace",
+            "hh_kv8_attention_blocks"]
 
 
 class hh_config(ctypes.Structure):
@@ -50,6 +56,11 @@ class hh_kv4_pool(ctypes.Structure):
 class hh_kv4_rows(ctypes.Structure):
     _fields_ = [("row_start", c_void_p), ("first_pos", c_void_p), ("table_row", c_void_p), ("n_seqs", c_int32),
                 ("n_rows", c_int32), ("max_rows", c_int32)]
+
+
+# The 8-bit cache's descriptions have the same fields (blocks of HH_KV8_BLOCK bytes).
+hh_kv8_pool = hh_kv4_pool
+hh_kv8_rows = hh_kv4_rows
 
 
 class HHError(RuntimeError):
@@ -105,6 +116,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "hh_kv_compact_workspace": ([c_int32, POINTER(c_size_t)], c_int32),
         "hh_kv_compact": ([c_void_p, c_int32, c_int64, c_int64, c_int32, c_void_p, c_int32, c_int32, c_void_p, c_void_p,
                            c_void_p, c_size_t, c_void_p], c_int32),
+        "hh_kv8_append": ([poolp, rowsp, c_void_p, c_void_p, c_int32, c_int64, c_int64, c_void_p, c_int32, c_void_p],
+                          c_int32),
+        "hh_kv8_read": ([poolp, rowsp, c_void_p, c_void_p, c_int32, c_int64, c_int64, c_void_p], c_int32),
+        "hh_kv8_attention_workspace": ([poolp, rowsp, c_int32, POINTER(c_size_t)], c_int32),
+        "hh_kv8_attention": ([poolp, rowsp, c_void_p, c_int32, c_int64, c_int32, c_float, c_void_p, c_int32, c_void_p,
+                              c_int32, c_int64, c_void_p, c_size_t, c_void_p], c_int32),
+        "hh_kv8_select_workspace": ([poolp, rowsp, c_int32, c_int32, POINTER(c_size_t)], c_int32),
+        "hh_kv8_select": ([poolp, rowsp, c_void_p, c_int32, c_int64, c_int32, c_void_p, c_int32, c_int32, c_int32,
+                           c_int32, c_void_p, c_void_p, c_size_t, c_void_p], c_int32),
+        "hh_kv8_attention_blocks_workspace": ([poolp, rowsp, c_int32, c_int32, POINTER(c_size_t)], c_int32),
+        "hh_kv8_attention_blocks": ([poolp, rowsp, c_void_p, c_int32, c_void_p, c_int32, c_int64, c_int32, c_float,
+                                     c_void_p, c_int32, c_void_p, c_int32, c_int64, c_void_p, c_size_t, c_void_p], c_int32),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -259,6 +282,60 @@ def hh_kv_compact(pool_ptr, n_layers: int, layer_stride: int, page_bytes: int, n
     _check(None, load_library().hh_kv_compact(pool_ptr, n_layers, layer_stride, page_bytes, n_pages, table_ptr,
                                               table_rows, max_pages, lengths_ptr, live_ptr, workspace_ptr,
                                               workspace_bytes, hip_stream))
+
+
+def hh_kv8_append(pool: hh_kv8_pool, rows: hh_kv8_rows, k_ptr, v_ptr, dtype: int, k_stride: int, v_stride: int,
+                  rope_ptr, rope_len: int, hip_stream) -> None:
+    _check(None, load_library().hh_kv8_append(byref(pool), byref(rows), k_ptr, v_ptr, dtype, k_stride, v_stride,
+                                              rope_ptr, rope_len, hip_stream))
+
+
+def hh_kv8_read(pool: hh_kv8_pool, rows: hh_kv8_rows, k_ptr, v_ptr, dtype: int, k_stride: int, v_stride: int,
+                hip_stream) -> None:
+    _check(None, load_library().hh_kv8_read(byref(pool), byref(rows), k_ptr, v_ptr, dtype, k_stride, v_stride,
+                                            hip_stream))
+
+
+def hh_kv8_attention_workspace(pool: hh_kv8_pool, rows: hh_kv8_rows, n_heads: int) -> int:
+    n = c_size_t()
+    _check(None, load_library().hh_kv8_attention_workspace(byref(pool), byref(rows), n_heads, byref(n)))
+    return n.value
+
+
+def hh_kv8_attention(pool: hh_kv8_pool, rows: hh_kv8_rows, q_ptr, q_dtype: int, q_stride: int, n_heads: int,
+                     scale: float, rope_ptr, rope_len: int, out_ptr, out_dtype: int, out_stride: int, workspace_ptr,
+                     workspace_bytes: int, hip_stream) -> None:
+    _check(None, load_library().hh_kv8_attention(byref(pool), byref(rows), q_ptr, q_dtype, q_stride, n_heads, scale,
+                                                 rope_ptr, rope_len, out_ptr, out_dtype, out_stride, workspace_ptr,
+                                                 workspace_bytes, hip_stream))
+
+
+def hh_kv8_select_workspace(pool: hh_kv8_pool, rows: hh_kv8_rows, n_heads: int, n_blocks: int) -> int:
+    n = c_size_t()
+    _check(None, load_library().hh_kv8_select_workspace(byref(pool), byref(rows), n_heads, n_blocks, byref(n)))
+    return n.value
+
+
+def hh_kv8_select(pool: hh_kv8_pool, rows: hh_kv8_rows, q_ptr, q_dtype: int, q_stride: int, n_heads: int, rope_ptr,
+                  rope_len: int, n_blocks: int, keep_first: int, keep_last: int, blocks_ptr, workspace_ptr,
+                  workspace_bytes: int, hip_stream) -> None:
+    _check(None, load_library().hh_kv8_select(byref(pool), byref(rows), q_ptr, q_dtype, q_stride, n_heads, rope_ptr,
+                                              rope_len, n_blocks, keep_first, keep_last, blocks_ptr, workspace_ptr,
+                                              workspace_bytes, hip_stream))
+
+
+def hh_kv8_attention_blocks_workspace(pool: hh_kv8_pool, rows: hh_kv8_rows, n_heads: int, n_blocks: int) -> int:
+    n = c_size_t()
+    _check(None, load_library().hh_kv8_attention_blocks_workspace(byref(pool), byref(rows), n_heads, n_blocks, byref(n)))
+    return n.value
+
+
+def hh_kv8_attention_blocks(pool: hh_kv8_pool, rows: hh_kv8_rows, blocks_ptr, n_blocks: int, q_ptr, q_dtype: int,
+                            q_stride: int, n_heads: int, scale: float, rope_ptr, rope_len: int, out_ptr, out_dtype: int,
+                            out_stride: int, workspace_ptr, workspace_bytes: int, hip_stream) -> None:
+    _check(None, load_library().hh_kv8_attention_blocks(byref(pool), byref(rows), blocks_ptr, n_blocks, q_ptr, q_dtype,
+                                                        q_stride, n_heads, scale, rope_ptr, rope_len, out_ptr, out_dtype,
+                                                        out_stride, workspace_ptr, workspace_bytes, hip_stream))
 
 
 def _text(s) -> bytes:
