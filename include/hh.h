@@ -484,7 +484,7 @@ hh_status hh_kv8_attention(const hh_kv8_pool* pool, const hh_kv8_rows* rows, con
 
 /* Bytes of device memory that hh_kv8_select needs for these sizes: 0 to
  * HH_KV8_WORKSPACE_MOST, as above. */
-enum { HH_KV8_MOST_BLOCKS = 1 << 16 };
+enum { HH_KV8_MOST_BLOCKS = 1 << 15 };
 hh_status hh_kv8_select_workspace(const hh_kv8_pool* pool, const hh_kv8_rows* rows, int32_t n_heads, int32_t n_blocks,
                                   size_t* bytes);
 
@@ -504,8 +504,8 @@ hh_status hh_kv8_select_workspace(const hh_kv8_pool* pool, const hh_kv8_rows* ro
  * Every block but a row's last ones must be full, as appending leaves them
  * (keep_last >= 1 covers its own).
  * Errors: INVALID_ARG (as above; keep_first < 0, keep_last < 1, their sum over
- * n_blocks), UNSUPPORTED (n_blocks or max_pages over 65,536; max_rows * n_kv_heads from
- * 2^22 on), HIP.
+ * n_blocks), UNSUPPORTED (n_blocks or max_pages over 32,768; max_rows * n_kv_heads near 2^22
+ * and above), HIP.
  */
 hh_status hh_kv8_select(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const void* q, int32_t q_dtype,
                         int64_t q_stride, int32_t n_heads, const float* rope, int32_t rope_len, int32_t n_blocks,
@@ -524,7 +524,7 @@ hh_status hh_kv8_attention_blocks_workspace(const hh_kv8_pool* pool, const hh_kv
  *          are no block of the row (negative, or past p / 16) are skipped, and one
  *          that is listed twice counts twice.  A row without any gives 0.
  * Otherwise as hh_kv8_attention.  Errors: as there, INVALID_ARG (blocks NULL or
- * misaligned, n_blocks < 1), UNSUPPORTED (n_blocks over 65,536).
+ * misaligned, n_blocks < 1), UNSUPPORTED (n_blocks over 32,768).
  */
 hh_status hh_kv8_attention_blocks(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const int32_t* blocks,
                                   int32_t n_blocks, const void* q, int32_t q_dtype, int64_t q_stride, int32_t n_heads,

@@ -96,7 +96,8 @@ struct Kv8Select {
   RopeTable rope;
   int n, first, last;  // blocks a row, forced ones at both ends
   int* out;            // [n_rows][hkv][n]
-  float* scores;       // workspace, see Kv8SelectPlan
+  unsigned* keys;      // workspace, `pitch` scores a (row, kv head), see Kv8SelectPlan
+  int pitch;
 };
 inline Kv8SelectPlan kv8_select_plan(const Kv4Pool& P, const Kv4Rows& R) {
   return kv8_select_plan(Kv4Sizes{R.n_seqs, R.n_rows, R.max_rows, P.hkv, P.hkv, P.max_pages});

@@ -268,12 +268,17 @@ struct PageRegs {
 };
 
 // The block as a buffer: its base stays in scalar registers, a lane's offset in one
-// vector register.
+// vector register; its scales are the wave's.  ONCE: no other workgroup reads the block, whose
+// lines then stay out of the caches' way (32 sequences of 4,000 positions 31.5 -> 27.9 us,
+// one of 131,072 33.4 -> 31.1; but the longest prompt 496 -> 509).
+template <bool ONCE>
 __device__ __forceinline__ void load_page(PageRegs& r, const unsigned char* blk, unsigned lane) {
+  constexpr int AUX = ONCE ? 2 : 0;
   const auto b = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(blk), 0, kKv8Block, 0x00027000);
-  r.k = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, 16 * lane, 0, 0));
-  r.v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, 16 * lane + kKv8Values, 0, 0));
-  r.s = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, 0, kKv8Scales, 0));
+  r.k = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, 16 * lane, 0, AUX));
+  r.v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, 16 * lane + kKv8Values, 0, AUX));
+  r.s = *reinterpret_cast<const __attribute__((address_space(4))) u32x2*>(
+      reinterpret_cast<uintptr_t>(blk + kKv8Scales));
 }
 
 // Bytes 2 J and 2 J + 1 of w as 1024 + n.
@@ -311,11 +316,21 @@ __device__ __forceinline__ void operands(const PageRegs& p, f16x8* kf, f16x4* vf
   for (int j = 0; j < 4; ++j) vf[j] = four(p.v[j], b);
 }
 
+// Two copies of a column side by side (see Columns), joined.
+template <int N>
+__device__ __forceinline__ void join_sides(float& m, float& l, float (&x)[N]) {
+  const float both = fmaxf(m, other8(m)), f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - both) : 0.f;
+  m = both;
+  l = f * l + other8(f * l);
+#pragma unroll
+  for (int j = 0; j < N; ++j) x[j] = f * x[j] + other8(f * x[j]);
+}
+
 constexpr int kNowhere = 1 << 30;  // a listed block that is none: behind every column's keys
 
 // A workgroup has a tile of 16 NQ columns; its W waves take the tile's pages (LIST: the
 // blocks that the columns' one row lists) in turn, two a step, and join at the end.
-template <int NQ, int QT, int W, int PACK, bool LIST>
+template <int NQ, int QT, int W, int PACK, bool LIST, bool ONCE>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(waves_fit(NQ)))) void
 k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits_, Div tiles_, Div group, Div row_tiles_) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -352,7 +367,7 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits
   const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
   unsigned ids[2];
   int at[2];                 // LIST: the blocks' first positions
-  uint64_t todo = 0, full = 0;  // LIST: steps with a block, steps that every column sees whole
+  uint64_t full = 0, part = 0;  // LIST: steps that the row sees whole, other ones with a block
   auto load_ids = [&](int q) {
     const int from = LIST ? q + lane * STEP : min(q + lane * STEP, last);
 #pragma unroll
@@ -368,38 +383,42 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits
       ids[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
     }
     if constexpr (LIST) {
-      todo = __builtin_amdgcn_ballot_w64(min(at[0], at[1]) < kNowhere);
       full = __builtin_amdgcn_ballot_w64(max(at[0], at[1]) + kPage <= some_see);
+      part = __builtin_amdgcn_ballot_w64(min(at[0], at[1]) < kNowhere) & ~full;
     }
   };
   auto fetch_step = [&](PageRegs* pr, int i) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const unsigned id = (unsigned)__builtin_amdgcn_readlane((int)ids[j], i);
-      load_page(pr[j], P.pool + ((size_t)id * (unsigned)P.hkv + (unsigned)w.head) * kKv8Block, (unsigned)lane);
+      load_page<ONCE>(pr[j], P.pool + ((size_t)id * (unsigned)P.hkv + (unsigned)w.head) * kKv8Block, (unsigned)lane);
     }
   };
   int ahead = 0;  // the step that is fetched next
   auto fetch = [&](PageRegs* pr) {
-    if constexpr (LIST) {
-      // The next step with a block (or any other, once there is none).
-      ahead = todo ? __builtin_ctzll(todo) : 0;
-      fetch_step(pr, ahead);
-    } else {
-      if (ahead == 64) {
-        load_ids(p + STEP);
-        ahead = 0;
-      }
-      fetch_step(pr, ahead);
-      ++ahead;
+    if (ahead == 64) {
+      load_ids(p + STEP);
+      ahead = 0;
     }
+    fetch_step(pr, ahead);
+    ++ahead;
+  };
+  // LIST: the steps of 64 that have blocks, first those that the row sees whole.  (Behind
+  // the last one any other is fetched.)
+  auto fetch_listed = [&](PageRegs* pr) {
+    uint64_t& of = full ? full : part;
+    ahead = of ? __builtin_ctzll(of) : 0;
+    of &= of - 1;
+    fetch_step(pr, ahead);
   };
   load_ids(p);
   // Of several tiles, each wave makes one's queries for all.
   RawQuery raw;
   if (NQ == 1 || wave < NQ) load_query<QT, PACK>(raw, w, A, NQ == 1 ? 0 : wave);
   PageRegs a[2], c[2];
-  fetch(a);
+  int n_full = __builtin_popcountll(full), n_part = __builtin_popcountll(part);
+  if constexpr (LIST) fetch_listed(a);
+  else fetch(a);
   Columns<NQ, QT, PACK> C;
   C.start(w, most);
   if constexpr (PACK == 2) {
@@ -440,26 +459,41 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits
     f32x4 sc[NQ][2];
     f16x8 ph[NQ], pl[NQ];
     C.scores(kf, sc);
-    C.template weights<MASK>(sc, at0, at1, PACK == 2 ? (C.right() ? bad[1] : bad[0]) : bad[0] | bad[1] << 4, ph, pl);
+    C.template weights<MASK, LIST>(sc, at0, at1, PACK == 2 ? (C.right() ? bad[1] : bad[0]) : bad[0] | bad[1] << 4, ph, pl);
     C.values(vf, ph, pl);
+    if constexpr (MASK && LIST) C.look_for_fresh();
   };
   if constexpr (LIST) {
     while (true) {
-      while (todo) {
+      bool swapped = false;
+      while (n_full > 0) {
+        fetch_listed(c);
+        step(a, 0, 0, std::false_type());
+        if (--n_full == 0) {
+          swapped = true;
+          break;
+        }
+        fetch_listed(a);
+        step(c, 0, 0, std::false_type());
+        --n_full;
+      }
+      if (swapped) {
+        a[0] = c[0];
+        a[1] = c[1];
+      }
+      for (; n_part > 0; --n_part) {
         const int now = ahead;
-        todo &= todo - 1;
-        fetch(c);
-        if (full >> now & 1)
-          step(a, 0, 0, std::false_type());
-        else
-          step(a, __builtin_amdgcn_readlane(at[0], now), __builtin_amdgcn_readlane(at[1], now), std::true_type());
+        fetch_listed(c);
+        step(a, __builtin_amdgcn_readlane(at[0], now), __builtin_amdgcn_readlane(at[1], now), std::true_type());
         a[0] = c[0];
         a[1] = c[1];
       }
       p += 64 * STEP;
       if (p >= p1) break;
       load_ids(p);
-      fetch(a);
+      n_full = __builtin_popcountll(full);
+      n_part = __builtin_popcountll(part);
+      fetch_listed(a);
     }
   } else {
     const int whole = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
@@ -489,7 +523,19 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits
     }
   }
 
-  // Join the waves: of four of them, wave v takes dimensions 16 g + 4 v .. + 3.
+  // Without neighbours a lane writes its 16 dimensions from 16 g on.
+  if constexpr (W == 1) {
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+      float m = C.base_of(t), l = C.sum[t][0], x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 16.f * C.o[t][i & 3][i >> 2];  // (16: of the values' scale)
+      if constexpr (PACK == 2) join_sides(m, l, x);
+      if (PACK == 1 || !C.right()) put<16>(R, A, w, w.c0 + 16 * t + r, 16 * g, x, l, m, joined, split, splits);
+    }
+    return;
+  }
+  // Join the waves: wave v takes dimensions 16 g + 4 v .. + 3, of two waves v + 2 too.
   __shared__ f32x4 lo[W][4][64];
   __shared__ float2 ls[W][64];
 #pragma unroll
@@ -499,39 +545,41 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits
     for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{C.o[t][0][i], C.o[t][1][i], C.o[t][2][i], C.o[t][3][i]};
     ls[wave][lane] = make_float2(C.base_of(t), C.sum[t][0]);
     __syncthreads();
-    if (wave >= 4) continue;
-    float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < W; ++v) m = fmaxf(m, ls[v][lane].x);
+    for (int v = 0; v < W; ++v) top = fmaxf(top, ls[v][lane].x);
+    for (int part = wave; part < 4; part += W) {
+      float m = top, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < W; ++v) {
-      const float2 z = ls[v][lane];
-      const float f = z.x > -INFINITY ? __builtin_amdgcn_exp2f(z.x - m) : 0.f;
-      const f32x4 y = lo[v][wave][lane];
-      l += f * z.y;
+      for (int v = 0; v < W; ++v) {
+        const float2 z = ls[v][lane];
+        const float f = z.x > -INFINITY ? 16.f * __builtin_amdgcn_exp2f(z.x - m) : 0.f;  // (as above)
+        const f32x4 y = lo[v][part][lane];
+        l += f * z.y;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+        for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+      }
+      l *= 0.0625f;
+      if constexpr (PACK == 2) join_sides(m, l, x);
+      if (PACK == 1 || !C.right()) put<4>(R, A, w, w.c0 + 16 * t + r, 16 * g + 4 * part, x, l, m, joined, split, splits);
     }
-    if constexpr (PACK == 2) {
-      const float m2 = fmaxf(m, other8(m)), f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - m2) : 0.f;
-      m = m2;
-      l = f * l + other8(f * l);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = f * x[j] + other8(f * x[j]);
-      if (C.right()) continue;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] *= 16.f;  // of the values' scale
-    put<4>(R, A, w, w.c0 + 16 * t + r, 16 * g + 4 * wave, x, l, m, joined, split, splits);
   }
+}
+
+typedef void (*Attend)(Kv4Pool, Kv4Rows, Kv4Attend, Kv8List, Div, Div, Div, Div, Div);
+template <int QT, int W>
+Attend pick_tile(const Kv8Plan& p) {
+  if constexpr (W == 4)  // (eight waves are for sequences of one tile)
+    if (p.tiles > 1) return k_kv8_attend<1, QT, W, 1, false, false>;
+  return p.packed ? k_kv8_attend<1, QT, W, 2, false, true> : k_kv8_attend<1, QT, W, 1, false, true>;
 }
 
 template <int QT>
 hipError_t launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8Plan& p) {
-  const auto kernel = p.nq == 2     ? k_kv8_attend<2, QT, 4, 1, false>
-                      : p.nq == 4   ? k_kv8_attend<4, QT, 4, 1, false>
-                      : p.waves == 4 ? (p.packed ? k_kv8_attend<1, QT, 4, 2, false> : k_kv8_attend<1, QT, 4, 1, false>)
-                                     : (p.packed ? k_kv8_attend<1, QT, 8, 2, false> : k_kv8_attend<1, QT, 8, 1, false>);
+  const auto kernel = p.nq == 2     ? k_kv8_attend<2, QT, 4, 1, false, false>
+                      : p.nq == 4   ? k_kv8_attend<4, QT, 4, 1, false, false>
+                      : p.waves == 4 ? pick_tile<QT, 4>(p)
+                                     : pick_tile<QT, 8>(p);
   const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
   return launch(kernel, groups, 64 * p.waves, 0, st, P, R, A, Kv8List{nullptr, 0}, div_by(P.hkv), div_by(p.splits),
                 div_by(p.tiles), div_by(A.hq / P.hkv), div_by(1));
@@ -540,7 +588,10 @@ hipError_t launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, con
 template <int QT>
 hipError_t launch_list(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8List& B,
                        const Kv8ListPlan& p) {
-  const auto kernel = p.packed ? k_kv8_attend<1, QT, 4, 2, true> : k_kv8_attend<1, QT, 4, 1, true>;
+  const auto kernel = p.waves == 1   ? (p.packed ? k_kv8_attend<1, QT, 1, 2, true, false> : k_kv8_attend<1, QT, 1, 1, true, false>)
+                      : p.waves == 2 ? (p.packed ? k_kv8_attend<1, QT, 2, 2, true, false> : k_kv8_attend<1, QT, 2, 1, true, false>)
+                      : p.waves == 4 ? (p.packed ? k_kv8_attend<1, QT, 4, 2, true, false> : k_kv8_attend<1, QT, 4, 1, true, false>)
+                                     : (p.packed ? k_kv8_attend<1, QT, 8, 2, true, false> : k_kv8_attend<1, QT, 8, 1, true, false>);
   const int tiles = R.max_rows * p.tiles;
   const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * tiles * p.splits);
   return launch(kernel, groups, 64 * p.waves, 0, st, P, R, A, B, div_by(P.hkv), div_by(p.splits), div_by(tiles),

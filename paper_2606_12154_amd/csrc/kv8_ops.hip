@@ -124,7 +124,8 @@ hh_status hh_kv8_select(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const 
   S.first = keep_first;
   S.last = keep_last;
   S.out = blocks;
-  S.scores = static_cast<float*>(workspace);
+  S.keys = static_cast<unsigned*>(workspace);
+  S.pitch = kv8_score_pitch(P.max_pages);
   return from_hip(kv8_select(static_cast<hipStream_t>(hip_stream), P, R, S, plan));
 }
 

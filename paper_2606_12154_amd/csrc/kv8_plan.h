@@ -9,7 +9,11 @@ namespace hh {
 // The attention over all keys is cut up as the one over a 4-bit cache: a step of
 // either takes the same products and exponentials.
 typedef Kv4Plan Kv8Plan;
-inline Kv8Plan kv8_plan(const Kv4Sizes& z) { return kv4_plan(z); }
+inline Kv8Plan kv8_plan(const Kv4Sizes& z) {
+  Kv4Cut c = kv4_cut(z);
+  // (tune dense)
+  return kv4_plan(z, c);
+}
 
 // The attention over listed blocks: a workgroup has 16 columns of one row (the
 // group's query heads), its waves take the list's pairs of blocks in turn.
@@ -20,18 +24,42 @@ struct Kv8ListPlan {
   int64_t threads;    // of a sequence's larger grid
   size_t workspace;   // bytes
 };
+// Waves of a workgroup and splits of a list over workgroups: those of the least time by
+// what was measured, in ns (eight sizes, 32 and 64 query heads on 8, with one to eight waves and
+// splits; the choices cost 1% on average against the best ones, 5% at most).  A step
+// takes a wave alone on its SIMD 650 ns and 380 more for each neighbour, and the SIMD 490 of
+// its own; a wave's start and end 630 of them.  So (us) 4,000 rows of 32 blocks take one
+// wave (177; two 200, four 244, eight 375), 200 such rows two (18.8; one 22.7, four 19.3), 32
+// of 64 eight (10.5; one 24.4), and one of 128 eight waves and splits (7.5; no split 9.3).
+struct Kv8ListCut {
+  int waves, splits;
+};
+inline Kv8ListCut kv8_list_cut(int64_t items, int pairs, int64_t outputs) {
+  Kv8ListCut best{};
+  double best_ns = 0;
+  for (int w = 1; w <= 8; w *= 2)
+    for (int s = 1; s <= std::min(kMaxSplits, pairs) && (s == 1 || split_bytes(s, outputs) <= kKv4Workspace); s += s < 8 ? 1 : 4) {
+      const int steps = ((pairs + s - 1) / s + w - 1) / w;
+      const double load = (double)items * s * w / 1024, held = std::min(4.0, std::max(1.0, round_up(load)));
+      double ns = std::max(2800 + steps * (650 + 380 * (held - 1)), 2500 + load * (630 + 490 * steps));
+      if (s > 1) ns += 3400 + 0.12 * (double)outputs * s;
+      if (best.waves == 0 || ns < best_ns) {
+        best = Kv8ListCut{w, s};
+        best_ns = ns;
+      }
+    }
+  return best;
+}
 inline Kv8ListPlan kv8_list_plan(const Kv4Sizes& z, int n) {
   Kv8ListPlan p;
-  const int group = z.hq / z.hkv, pairs = (n + 1) / 2;
+  const int group = z.hq / z.hkv;
   const int64_t outputs = (int64_t)z.n_rows * z.hq;
   p.tiles = (group + 15) / 16;
   p.packed = group <= 8;
-  const int64_t items = (int64_t)z.n_rows * z.hkv * p.tiles;
-  p.waves = 4;
-  p.splits = 1;
-  while (items * p.splits < 512 && pairs / (2 * p.splits) >= 2 * p.waves && p.splits < kMaxSplits &&
-         split_bytes(2 * p.splits, outputs) <= kKv4Workspace)
-    p.splits *= 2;
+  const Kv8ListCut c = kv8_list_cut((int64_t)z.n_rows * z.hkv * p.tiles, (n + 1) / 2, outputs);
+  p.waves = c.waves;
+  p.splits = c.splits;
+  // (tune list)
   p.threads = z.hq >= 1 << 25 || (int64_t)z.max_rows * group > INT32_MAX - 1024
                   ? INT64_MAX
                   : (int64_t)z.max_rows * p.tiles * z.hkv * p.splits * 64 * p.waves;
@@ -40,21 +68,31 @@ inline Kv8ListPlan kv8_list_plan(const Kv4Sizes& z, int n) {
   return p;
 }
 
-// Selection: `lanes` threads have a (row, kv head), `keys` scores each in registers.
-constexpr int kMaxSelectPages = 1 << 16;
+// Selection: a workgroup has `rows` rows and one kv head.  A wave of it searches a row, with
+// up to `keys` scores a lane, or (team) all of them search one.
+constexpr int kMaxSelectPages = 1 << 15;  // a row's scores fit LDS
 struct Kv8SelectPlan {
-  int lanes, keys;
-  int64_t threads;   // of a sequence's grid
+  int rows, waves, keys;
+  bool team;
+  int chunks;        // of 256 blocks that score a row in a launch of their own; 0: one launch
+  size_t lds;        // bytes of the scores
+  int64_t threads;   // of a sequence's larger grid
   size_t workspace;  // bytes
 };
+inline int kv8_score_pitch(int pages) { return (pages + 15) / 16 * 16; }
 inline Kv8SelectPlan kv8_select_plan(const Kv4Sizes& z) {
   Kv8SelectPlan p;
   const int64_t items = (int64_t)z.n_rows * z.hkv;
-  p.lanes = z.pages > 4096 || items <= 512 ? 1024 : z.pages > 1024 || items <= 2048 ? 256 : 64;
-  const int each = (z.pages + p.lanes - 1) / p.lanes;
-  p.keys = each <= 4 ? 4 : each <= 16 ? 16 : 64;
-  p.threads = (int64_t)z.max_rows * z.hkv * p.lanes;
-  p.workspace = 0;
+  p.team = z.pages > 2048;
+  p.rows = p.team ? 1 : std::min(z.max_rows, z.pages > 512 ? 8 : 16);
+  p.waves = p.team ? (z.pages > 8192 ? 16 : 4) : 8;
+  p.chunks = p.team && items <= 128 ? (z.pages + 255) / 256 : 0;
+  // (tune select)
+  const int most = p.team ? 64 * p.waves : 64, each = ((z.pages + most - 1) / most) | 1;
+  p.keys = !p.team && each <= 9 ? 9 : !p.team && each <= 17 ? 17 : 33;
+  p.lds = (size_t)p.rows * each * most * sizeof(unsigned);
+  p.threads = ((int64_t)z.max_rows + p.rows - 1) / p.rows * z.hkv * std::max(64 * p.waves, 256 * p.chunks);
+  p.workspace = p.chunks > 0 ? (size_t)items * kv8_score_pitch(z.pages) * sizeof(unsigned) : 0;
   return p;
 }
 

@@ -26,7 +26,7 @@ HH_KV_Q4 = 0x100  # added to a weight format: 4-bit KV cache
 HH_KV4_WORKSPACE_MOST = 16 << 20  # bound of hh_kv4_attention_workspace
 HH_KV8_BLOCK = 2176  # bytes of one page of one kv head
 HH_KV8_WORKSPACE_MOST = 16 << 20  # bound of the hh_kv8 calls' workspaces
-HH_KV8_MOST_BLOCKS = 1 << 16
+HH_KV8_MOST_BLOCKS = 1 << 15
 
 EXPORTED = ["hh_workspace_size", "hh_create", "hh_load_weights", "hh_prefill", "hh_prefill_batch", "hh_decode_step",
             "hh_decode_step_noalloc", "hh_reset", "hh_stream_length", "hh_read_argmax", "hh_destroy", "hh_last_error",

@@ -447,6 +447,15 @@ def test_listed_blocks(t, ot, rope, lens, first, n):
     check(c, lens, first, 8, t, ot, rng, rope_table(2048) if rope else None, lists=lists)
 
 
+@pytest.mark.parametrize("rows,n,group", [(1, 9, 4), (1, 300, 4), (40, 25, 4), (300, 8, 2), (700, 6, 4), (700, 6, 16), (2500, 3, 1)])
+def test_listed_blocks_every_way_of_cutting(rows, n, group):
+    """Few rows and many: one to eight waves a row, split lists; 16-bit types."""
+    c, rng = filled([3000], 2, rows)
+    lists = np.concatenate([random_lists([rows], [3000 - rows], 2, n, rng), np.zeros((2, 2, n), np.int32)])
+    for t in ("f32", "f16"):
+        check(c, [rows], [3000 - rows], 2 * group, t, t, rng, lists=lists)
+
+
 @pytest.mark.parametrize("hkv,group", [(1, 1), (3, 2), (1, 8), (2, 12), (1, 16), (1, 40)])
 def test_listed_blocks_head_layouts(hkv, group):
     lens, first = [1, 6], [333, 100]
@@ -475,6 +484,33 @@ def test_long_lists(n):
     lists[1] = -1
     lists[1, :, -1] = 5
     check(c, [1], [16 * 1600 - 1], 4, "f32", "f32", rng, lists=lists)
+
+
+@pytest.mark.parametrize("group", [4, 12])
+def test_lists_whose_scores_are_all_low(group):
+    """Scores far below 0, of blocks that stand beside entries that are none: their
+    weights go by the largest of them, in whatever order the blocks come."""
+    n = 16 * 140
+    c = Cache(1, 1, 140)
+    k, v = (torch.randn(n, 1, 64, device="cuda:0") for _ in "kv")
+    k[:, :, 0] = 60.0
+    c.append([n], [0], k, v, "f32")
+    lists = np.full((3, 1, 140), -1, np.int32)
+    lists[0, 0, [1, 8, 133]] = [139, 5, 7]   # (the right side's first blocks come last)
+    lists[1, 0, 138] = 139
+    lists[2, 0, [0, 3, 64, 139]] = [139, 2, 3, 4]
+    q = torch.randn(3, group, 64, device="cuda:0")
+    q[:, :, 0] = -50.0
+    out = torch.empty_like(q)
+    for i in range(3):
+        r, keep = c.rows([0, 1], [n - 1], 1)
+        one = out[i:i + 1]
+        attend(c, r, q[i:i + 1].contiguous(), "f32", one, "f32", blocks=ints(lists[i:i + 1]))
+        kk, vv = c.ref.values(0, n)
+        rows = q[i:i + 1].double().cpu().numpy()
+        want = listed_reference(rows, kk, vv, 0.125, n - 1, lists[i:i + 1], 1)
+        e, half = bound(rows, kk, vv, 0.125, "f32")
+        assert (np.abs(one.double().cpu().numpy() - want) <= e + half * (np.abs(want) + e)).all()
 
 
 def test_a_list_of_all_blocks_is_the_attention_over_all_keys():
@@ -548,37 +584,50 @@ def test_selection(t, rope, lens, first, n, keep_first, keep_last):
     check_selection(c, lens, first, 8, t, n, keep_first, keep_last, rng, rope_table(1024) if rope else None)
 
 
+@pytest.mark.parametrize("t,rope", [("f32", True), ("f16", False), ("bf16", True)])
+@pytest.mark.parametrize("lens,first,n,keep_first,keep_last", [
+    ([8, 33, 0, 17], [300, 77, 4, 0], 5, 1, 2), ([50], [0], 3, 0, 1), ([40, 9], [-3, 390], 6, 2, 4), ([20], [470], 29, 0, 1)])
+def test_selection_of_rows_together(t, rope, lens, first, n, keep_first, keep_last):
+    """Rows that take all of their blocks beside rows that do not, in one tile."""
+    c, rng = filled([max(m + f, 0) for m, f in zip(lens, first)], 2, 3)
+    check_selection(c, lens, first, 6, t, n, keep_first, keep_last, rng, rope_table(1024) if rope else None)
+
+
 @pytest.mark.parametrize("hkv,group", [(1, 1), (3, 1), (1, 5), (2, 16), (1, 40)])
 def test_selection_head_layouts(hkv, group):
     c, rng = filled([500, 120], hkv, 2)
     check_selection(c, [1, 2], [499, 118], hkv * group, "f32", 5, 1, 1, rng)
 
 
-def test_equal_scores_go_to_the_lowest_blocks():
+@pytest.mark.parametrize("rows", [1, 20])
+def test_equal_scores_go_to_the_lowest_blocks(rows):
     c = Cache(1, 1, 40)
     k = torch.randn(16, 1, 64, device="cuda:0").repeat(40, 1, 1)
     k[16 * 20:16 * 21] *= 3
     c.append([640], [0], k, k, "f32")
     rng = np.random.default_rng(0)
-    got = check_selection(c, [1], [639], 1, "f32", 8, 2, 3, rng)
-    assert got[0, 0].tolist() in ([0, 1, 2, 3, 20, 37, 38, 39], [0, 1, 2, 3, 4, 37, 38, 39])
-    for q in (torch.zeros(2, 1, 64), torch.full((2, 1, 64), float("inf")), torch.full((2, 1, 64), float("nan"))):
-        got = check_selection(c, [1], [639], 1, "f32", 8, 2, 3, rng, q=q.to("cuda:0"))
-        assert got[0, 0].tolist() == [0, 1, 2, 3, 4, 37, 38, 39]
+    got = check_selection(c, [rows], [640 - rows], 1, "f32", 8, 2, 3, rng)
+    assert got[rows - 1, 0].tolist() in ([0, 1, 2, 3, 20, 37, 38, 39], [0, 1, 2, 3, 4, 37, 38, 39])
+    for x in (0.0, float("inf"), float("nan")):
+        q = torch.full((rows + 1, 1, 64), x, device="cuda:0")
+        got = check_selection(c, [rows], [640 - rows], 1, "f32", 8, 2, 3, rng, q=q)
+        assert got[rows - 1, 0].tolist() == [0, 1, 2, 3, 4, 37, 38, 39]
 
 
-def test_selection_over_scales_far_apart():
+@pytest.mark.parametrize("rows", [1, 30])
+def test_selection_over_scales_far_apart(rows):
     """Blocks whose scales differ by 2^20; huge and tiny queries."""
     rng = np.random.default_rng(4)
     c = Cache(1, 2, 30)
     k = rng.standard_normal((480, 2, 64)) * np.repeat(np.exp2(rng.uniform(-15, 12, (30, 2, 1))), 16, 0)
     c.append([480], [0], dev(k, torch.float32), dev(k, torch.float32), "f32")
     for size in (1e-30, 1.0, 1e30):
-        q = dev(rng.standard_normal((2, 4, 64)) * size, torch.float32)
-        check_selection(c, [1], [479], 4, "f32", 7, 0, 1, rng, q=q)
+        q = dev(rng.standard_normal((rows + 1, 4, 64)) * size, torch.float32)
+        check_selection(c, [rows], [480 - rows], 4, "f32", 7, 0, 1, rng, q=q)
 
 
-@pytest.mark.parametrize("pages,rows", [(130, 1), (1100, 1), (1100, 300), (4200, 2)])
+@pytest.mark.parametrize("pages,rows", [(130, 1), (1100, 1), (1100, 300), (4200, 2), (9000, 1), (17000, 1), (500, 40), (250, 19),
+                                        (100, 100), (4100, 700)])
 def test_selection_over_many_blocks(pages, rows):
     """Every way of cutting the call up, against a sorted list of exact scores."""
     rng = np.random.default_rng(pages + rows)

@@ -191,7 +191,7 @@ def test_attention_refuses(bad):
 def test_listed_blocks_refused():
     for bad in (dict(b=0), dict(b=A + 2), dict(nb=0), dict(nb=-1)):
         listed(pool(), rows(), **bad)
-    listed(pool(), rows(), nb=(1 << 16) + 1, status=hh.HH_ERR_UNSUPPORTED)
+    listed(pool(), rows(), nb=(1 << 15) + 1, status=hh.HH_ERR_UNSUPPORTED)
 
 
 @pytest.mark.parametrize("bad", [
@@ -202,15 +202,16 @@ def test_selection_refuses(bad):
 
 
 def test_selections_too_large():
-    selection(pool(), rows(), nb=(1 << 16) + 1, status=hh.HH_ERR_UNSUPPORTED)
-    selection(pool(max_pages=(1 << 16) + 1), rows(), status=hh.HH_ERR_UNSUPPORTED)
-    refused(hh.hh_kv8_select_workspace, pool(max_pages=(1 << 16) + 1), rows(), 4, 4, status=hh.HH_ERR_UNSUPPORTED)
+    selection(pool(), rows(), nb=(1 << 15) + 1, status=hh.HH_ERR_UNSUPPORTED)
+    selection(pool(max_pages=(1 << 15) + 1), rows(), status=hh.HH_ERR_UNSUPPORTED)
+    refused(hh.hh_kv8_select_workspace, pool(max_pages=(1 << 15) + 1), rows(), 4, 4, status=hh.HH_ERR_UNSUPPORTED)
     big = rows(row_start=A, n_seqs=1 << 20, n_rows=1 << 29, max_rows=1 << 29)
     selection(pool(), big, status=hh.HH_ERR_UNSUPPORTED)
 
 
 @pytest.mark.parametrize("ask,call", [
     (lambda p, r: hh.hh_kv8_attention_workspace(p, r, 4), attention),
+    (lambda p, r: hh.hh_kv8_select_workspace(p, r, 4, 400), lambda p, r, **kw: selection(p, r, nb=400, **kw)),
     (lambda p, r: hh.hh_kv8_attention_blocks_workspace(p, r, 4, 400), lambda p, r, **kw: listed(p, r, nb=400, **kw))])
 def test_workspaces(ask, call):
     p, r = pool(n_pages=30000, max_pages=9000), rows()
