@@ -21,6 +21,8 @@
 namespace hh {
 namespace {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 // ------------------------------------------------------------------ append and read
 
 // The least e with a <= 127 * 2^e, within the format's; a is finite and not negative.
@@ -316,23 +318,381 @@ __device__ __forceinline__ void operands(const PageRegs& p, f16x8* kf, f16x4* vf
   for (int j = 0; j < 4; ++j) vf[j] = four(p.v[j], b);
 }
 
-// Two copies of a column side by side (see Columns), joined.
-template <int N>
-__device__ __forceinline__ void join_sides(float& m, float& l, float (&x)[N]) {
-  const float both = fmaxf(m, other8(m)), f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - both) : 0.f;
-  m = both;
+constexpr int kNowhere = 1 << 30;  // a listed block that is none: behind every column's keys
+
+// ---- few columns: a token's query heads, or a row's that lists its blocks
+//
+// A tile of 16 columns holds 16 / P query heads P times, side by side (P: 2 for up to 8 heads
+// a kv head).  Copy i has its queries in page i's product and zeros in the other's, so that a lane's
+// four scores of a step of two pages are of both, not of one and half of them of no column.
+//
+// Scores are products of whole numbers: a query in three signed digits of 8 bits (23 bits of
+// its largest element) times the page's codes as they lie, mfma_i32_16x16x64_i8; three
+// conversions and two FMAs a score take the place of unpacking the keys (4,000 prompt rows of 32
+// listed blocks 177 -> 164 us, 64 sequences of 1,500 positions 22.7 -> 21.7; 16-bit queries
+// that need one term and no scaling lose 0.4 us at the start).  P = 4 takes fewer exponentials
+// a page, but 165 to 195 registers (170 and 25.6).
+template <int P>
+__device__ __forceinline__ int copy_of() { return (threadIdx.x & 15) / (16 / P); }
+
+struct Digits {
+  i32x4 d[3];
+};
+__device__ __forceinline__ i32x4 no_digits() { return i32x4{0, 0, 0, 0}; }
+// The lane's 16 dimensions as digits, and the factor of scores to powers of two.
+__device__ __forceinline__ float make_digits(const RawQuery& q, const Kv4Attend& A, Digits& z) {
+  float x[16];
+  raw_values(q.row, A.q_type, x);
+  if (A.rope.at) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float u = x[i], v = x[8 + i], co = q.turn[i >> 1][2 * (i & 1)], si = q.turn[i >> 1][2 * (i & 1) + 1];
+      x[i] = u * co - v * si;
+      x[8 + i] = v * co + u * si;
+    }
+  }
+  unsigned top = 0u;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, magnitude(x[i]));
+  top = rows_max(top);
+  // The largest becomes a number from 2^21 to 2^22.
+  const int e = top > 0u && top < kInfBits ? 22 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    unsigned y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      y[i] = ((unsigned)(int)rintf(__builtin_amdgcn_ldexpf(top < kInfBits ? x[4 * w + i] : 0.f, e)) + 0x808080u) ^ 0x808080u;
+    const unsigned a = __builtin_amdgcn_perm(y[1], y[0], 0x05010400u), b = __builtin_amdgcn_perm(y[3], y[2], 0x05010400u);
+    const unsigned c = __builtin_amdgcn_perm(y[1], y[0], 0x0c0c0602u), d = __builtin_amdgcn_perm(y[3], y[2], 0x0c0c0602u);
+    z.d[0][w] = (int)__builtin_amdgcn_perm(b, a, 0x05040100u);
+    z.d[1][w] = (int)__builtin_amdgcn_perm(b, a, 0x07060302u);
+    z.d[2][w] = (int)__builtin_amdgcn_perm(d, c, 0x05040100u);
+  }
+  // (A query that is not finite makes every score NaN.)
+  return top < kInfBits ? fmaxf(__builtin_amdgcn_ldexpf(A.scale * (1.4426950408889634f / 16.f), -e), 1e-37f) : NAN;
+}
+
+// A wave's columns: their queries, bases, sums (of a lane's own slots) and outputs.
+template <int P>
+struct Few {
+  static constexpr int N = 8 / P;  // scores of a lane and step of two pages
+  struct Places {
+    int v[2];
+  };
+  Digits q[P];
+  float qs, base, sum;
+  int lim;  // keys that the column sees
+  f32x4 o[4];
+  bool fresh;      // the column has seen no key yet
+  bool any_fresh;  // one of the wave's may not have
+
+  __device__ __forceinline__ void start(const Place& w, int most, const RawQuery& raw, const Kv4Attend& A) {
+    Digits z;
+    qs = make_digits(raw, A, z);
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+      for (int j = 0; j < 3; ++j) q[i].d[j] = P == 1 || copy_of<P>() == i ? z.d[j] : no_digits();
+    base = sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    lim = min(max(w.s.first + column_row(w, w.c0 + column_of<P>()) + 1, 0), most);
+    fresh = any_fresh = true;
+  }
+
+  // Two pages, from positions `at` on.  MASK: slots past a column's keys, and marked ones.
+  template <bool MASK>
+  __device__ __forceinline__ void step(const PageRegs (&x)[2], const Places& at) {
+    const int g = (threadIdx.x & 63) >> 4, side = copy_of<P>();
+    float sc[N];
+    float scale[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned s = !MASK && x[i].s[1] ? 0x7e00u : x[i].s[0] & 0xffffu;  // (as in operands)
+      scale[i] = qs * from_half(s);
+    }
+    i32x4 acc[P == 1 ? 2 : 1][3];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 codes = x[i].k ^ 0x80808080u;
+      const i32x4 a = __builtin_bit_cast(i32x4, codes);
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        i32x4& y = acc[P == 1 ? i : 0][j];
+        y = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, q[P == 1 ? 0 : i].d[j], P == 1 || i == 0 ? no_digits() : y, 0, 0, 0);
+      }
+    }
+    const float mine = P == 2 && side ? scale[1] : scale[0];
+    float high = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const i32x4* y = acc[P == 1 ? i >> 2 : 0];
+      const float s = fmaf((float)y[2][i & 3], 65536.f, fmaf((float)y[1][i & 3], 256.f, (float)y[0][i & 3]));
+      sc[i] = fmaf(s, P == 1 ? scale[i >> 2] : mine, -base);
+    }
+    if constexpr (MASK) {
+      unsigned bad[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) bad[i] = x[i].s[1] | x[i].s[1] >> 16;
+      const unsigned of = P == 2 && side ? bad[1] : bad[0];
+      const int from = P == 2 && side ? at.v[1] : at.v[0];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if ((P == 1 ? bad[i >> 2] : of) >> (4 * g + (i & 3)) & 1u) sc[i] = NAN;
+        if ((P == 1 ? at.v[i >> 2] : from) + 4 * g + (i & 3) >= lim) sc[i] = -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) high = fmaxf(high, sc[i]);
+    if (any_fresh || __builtin_amdgcn_ballot_w64(high > kOffset + kSlack)) {
+      const float mx = rows_max(high);
+      float up = mx > -INFINITY ? mx - kOffset : 0.f;
+      if (!fresh) up = fmaxf(up, 0.f);
+      const float f = fresh ? 1.f : __builtin_amdgcn_exp2f(-up);
+      base += up;
+      sum *= f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) sc[i] -= up;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] *= f;
+      fresh = fresh && !(mx > -INFINITY);
+      any_fresh = __builtin_amdgcn_ballot_w64(fresh);
+    }
+    f16x2 h[N / 2], l[N / 2];
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float a = __builtin_amdgcn_exp2f(sc[i]), b = __builtin_amdgcn_exp2f(sc[i + 1]);
+      sum += a + b;
+      split_weights(a, b, h[i / 2], l[i / 2]);
+    }
+    // A lane's weights where their page's values are.
+    auto weights = [&](const f16x2* y) {
+      const f16x4 z = {y[0][0], y[0][1], y[1][0], y[1][1]}, none = {0, 0, 0, 0};
+      if constexpr (P == 1) return join8(z, f16x4{y[2][0], y[2][1], y[3][0], y[3][1]});
+      return join8(side ? none : z, side ? z : none);
+    };
+    const f16x8 ph = weights(h), pl = weights(l);
+    Scale vs[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      // (A block that is none has no values: what is read in its place may have any scale.)
+      const unsigned s = MASK && at.v[i] == kNowhere ? 0u : x[i].s[0];
+      vs[i] = scale_of(__builtin_amdgcn_perm(s, s, 0x03020302u));
+    }
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const f16x8 v = join8(four(x[0].v[d], vs[0]), four(x[1].v[d], vs[1]));
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl, o[d], 0, 0, 0);
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph, o[d], 0, 0, 0);
+    }
+  }
+};
+
+// Copies of a column side by side (16 / P lanes apart), joined.
+template <int P, int N>
+__device__ __forceinline__ void join_copies(float& m, float& l, float (&x)[N]) {
+  if constexpr (P == 1) return;
+  const float top = fmaxf(m, other8(m)), f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+  m = top;
   l = f * l + other8(f * l);
 #pragma unroll
   for (int j = 0; j < N; ++j) x[j] = f * x[j] + other8(f * x[j]);
 }
 
-constexpr int kNowhere = 1 << 30;  // a listed block that is none: behind every column's keys
+// A workgroup has a sequence's columns of one kv head (LIST: a row's, or 16 of them); its W
+// waves take the pages (the listed blocks) in turn, NP a step, and join at the end.
+template <int P, int W, bool LIST, bool ONCE>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) void
+k_kv8_few(Kv4Pool Q, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits_, Div tiles_, Div group, Div row_tiles_) {
+  constexpr int NP = 2, STEP = NP * W;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const unsigned b1 = blockIdx.x / heads, b2 = b1 / splits_, sq = b2 / tiles_;
+  const int split = b1 - b2 * splits_.d, splits = splits_.d;
+  const int tile = b2 - sq * tiles_.d;
+  const Seq s = load_seq(Q, R, R.seq0 + sq);
+  const int G = group.d, own = LIST ? (unsigned)tile / row_tiles_ : 0;  // LIST: the row
+  if (LIST && own >= s.n) return;
+  const int cols = LIST ? (own + 1) * G : s.n * G;
+  const Place w{s, (int)(blockIdx.x - b1 * heads.d), G, cols, LIST ? own * G + 16 * (tile - own * (int)row_tiles_.d) : 0, group};
+  if (w.c0 >= cols) return;
+  // Keys of the first and last row.
+  const int most = Q.max_pages * kPage;
+  const int row_b = (unsigned)(min(w.c0 + 16, cols) - 1) / group;
+  const int all_see = min(max(s.first + (LIST ? row_b : 0) + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
+  const int np = LIST ? B.n : (some_see + kPage - 1) / kPage;
+  const int per = split_pages(np, splits);
+  const int p0 = split * per, p1 = min(p0 + per, np);
+  const bool joined = per < np;  // several splits have keys
+  if (split > 0 && p0 >= np) return;
 
-// A workgroup has a tile of 16 NQ columns; its W waves take the tile's pages (LIST: the
-// blocks that the columns' one row lists) in turn, two a step, and join at the end.
-template <int NQ, int QT, int W, int PACK, bool LIST, bool ONCE>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(waves_fit(NQ)))) void
-k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits_, Div tiles_, Div group, Div row_tiles_) {
+  // What the first step needs goes out before the queries are worked on.  Loads run one
+  // step ahead; what would lie behind the wave's last step is its last step again (no branch
+  // around loads, whose waits would then have to assume that it was not taken).  Lane i holds
+  // the page ids of the i-th of 64 steps.
+  const int* row = Q.table + (size_t)s.trow * Q.max_pages;
+  const int* list = LIST ? B.blocks + ((size_t)(s.row0 + own) * Q.hkv + w.head) * B.n : nullptr;
+  int p = p0 + NP * wave;
+  const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
+  unsigned ids[NP];
+  int at[NP];                   // LIST: the blocks' first positions
+  uint64_t full = 0, part = 0;  // LIST: steps that the row sees whole, other ones with a block
+  auto load_ids = [&](int q) {
+    const int from = LIST ? q + lane * STEP : min(q + lane * STEP, last);
+    int low = kNowhere, high = 0;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      int page = max(min(from + i, np - 1), 0);
+      if constexpr (LIST) {
+        const int b = list[page];
+        const bool in = from + i < p1 && b >= 0 && b <= (some_see - 1) >> 4;
+        at[i] = in ? b * kPage : kNowhere;
+        page = in ? b : 0;
+        low = min(low, at[i]);
+        high = max(high, at[i]);
+      }
+      const unsigned x = (unsigned)row[page];
+      ids[i] = x < (unsigned)Q.n_pages ? x : 0u;  // an id outside the pool reads its first page
+    }
+    if constexpr (LIST) {
+      full = __builtin_amdgcn_ballot_w64(high + kPage <= some_see);
+      part = __builtin_amdgcn_ballot_w64(low < kNowhere) & ~full;
+    }
+  };
+  int ahead = 0;  // the step that is fetched next
+  auto fetch = [&](PageRegs* x) {
+    if constexpr (LIST) {
+      // First the steps that the row sees whole.  (Behind the last one any other is fetched.)
+      uint64_t& of = full ? full : part;
+      ahead = of ? __builtin_ctzll(of) : 0;
+      of &= of - 1;
+    } else if (ahead == 64) {
+      load_ids(p + STEP);
+      ahead = 0;
+    }
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      const unsigned id = (unsigned)__builtin_amdgcn_readlane((int)ids[j], ahead);
+      load_page<ONCE>(x[j], Q.pool + ((size_t)id * (unsigned)Q.hkv + (unsigned)w.head) * kKv8Block, (unsigned)lane);
+    }
+    if constexpr (!LIST) ++ahead;
+  };
+  load_ids(p);
+  RawQuery raw;
+  load_query<2, P>(raw, w, A, 0);
+  PageRegs a[NP], c[NP];
+  int n_full = __builtin_popcountll(full), n_part = __builtin_popcountll(part);
+  fetch(a);
+  Few<P> C;
+  C.start(w, most, raw, A);
+  auto to_a = [&] {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) a[i] = c[i];
+  };
+  if constexpr (LIST) {
+    while (true) {
+      bool swapped = false;
+      while (n_full > 0) {
+        fetch(c);
+        C.template step<false>(a, {});
+        if (--n_full == 0) {
+          swapped = true;
+          break;
+        }
+        fetch(a);
+        C.template step<false>(c, {});
+        --n_full;
+      }
+      if (swapped) to_a();
+      for (; n_part > 0; --n_part) {
+        typename Few<P>::Places from;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) from.v[i] = __builtin_amdgcn_readlane(at[i], ahead);
+        fetch(c);
+        C.template step<true>(a, from);
+        to_a();
+      }
+      p += 64 * STEP;
+      if (p >= p1) break;
+      load_ids(p);
+      n_full = __builtin_popcountll(full);
+      n_part = __builtin_popcountll(part);
+      fetch(a);
+    }
+  } else {
+    const int whole = min(all_see / kPage, p1);  // pages below are seen by every row
+    bool swapped = false;
+    while (p + NP <= whole) {
+      fetch(c);
+      C.template step<false>(a, {});
+      p += STEP;
+      if (p + NP > whole) {
+        swapped = true;
+        break;
+      }
+      fetch(a);
+      C.template step<false>(c, {});
+      p += STEP;
+    }
+    if (swapped) to_a();
+    while (p < p1) {
+      typename Few<P>::Places from;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) from.v[i] = p + i < p1 ? (p + i) * kPage : kNowhere;
+      fetch(c);
+      C.template step<true>(a, from);
+      to_a();
+      p += STEP;
+    }
+  }
+
+  const float total = rows_sum(C.sum), base = total == 0.f ? -INFINITY : C.base;  // (no key, no base)
+  const bool writes = P == 1 || copy_of<P>() == 0;
+  // Without neighbours a lane writes its 16 dimensions from 16 g on.
+  if constexpr (W == 1) {
+    float m = base, l = total, x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 16.f * C.o[i & 3][i >> 2];  // (16: of the values' scale)
+    join_copies<P>(m, l, x);
+    if (writes) put<16>(R, A, w, w.c0 + r, 16 * g, x, l, m, joined, split, splits);
+    return;
+  }
+  // Join the waves: wave v takes dimensions 16 g + 4 v .. + 3, of two waves v + 2 too.
+  __shared__ f32x4 lo[W][4][64];
+  __shared__ float2 ls[W][64];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{C.o[0][i], C.o[1][i], C.o[2][i], C.o[3][i]};
+  ls[wave][lane] = make_float2(base, total);
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int v = 0; v < W; ++v) top = fmaxf(top, ls[v][lane].x);
+  for (int part4 = wave; part4 < 4; part4 += W) {
+    float m = top, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < W; ++v) {
+      const float2 z = ls[v][lane];
+      const float f = z.x > -INFINITY ? 16.f * __builtin_amdgcn_exp2f(z.x - m) : 0.f;  // (as above)
+      const f32x4 y = lo[v][part4][lane];
+      l += f * z.y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+    }
+    l *= 0.0625f;
+    join_copies<P>(m, l, x);
+    if (writes) put<4>(R, A, w, w.c0 + r, 16 * g + 4 * part4, x, l, m, joined, split, splits);
+  }
+}
+
+// ---- many columns: prompts
+//
+// A workgroup has a tile of 16 NQ columns; its four waves take the tile's pages in turn, two a
+// step, and join at the end.
+template <int NQ, int QT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_fit(NQ)))) void
+k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tiles_, Div group) {
+  constexpr int W = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   const unsigned b1 = blockIdx.x / heads, b2 = b1 / splits_, sq = b2 / tiles_;
@@ -340,90 +700,55 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits
   // The last tiles have the most keys: they go first.
   const int tile = tiles_.d - 1 - (b2 - sq * tiles_.d);
   const Seq s = load_seq(P, R, R.seq0 + sq);
-  const int G = group.d, own = LIST ? (unsigned)tile / row_tiles_ : 0;  // LIST: the row
-  if (LIST && own >= s.n) return;
-  const int cols = LIST ? (own + 1) * G : s.n * G;  // below 2^31 with a tile to spare (kv8_plan)
-  const Place w{s, (int)(blockIdx.x - b1 * heads.d), G, cols,
-                LIST ? own * G + 16 * (tile - own * (int)row_tiles_.d) : tile * (16 * NQ), group};
+  const int G = group.d, cols = s.n * G;  // below 2^31 with a tile to spare (kv8_plan)
+  const Place w{s, (int)(blockIdx.x - b1 * heads.d), G, cols, tile * (16 * NQ), group};
   if (w.c0 >= cols) return;
   // Keys of the tile's first and last row.
   const int most = P.max_pages * kPage;
   const int row_a = (unsigned)w.c0 / group, row_b = (unsigned)(min(w.c0 + 16 * NQ, cols) - 1) / group;
   const int all_see = min(max(s.first + row_a + 1, 0), most), some_see = min(max(s.first + row_b + 1, 0), most);
-  const int np = LIST ? B.n : (some_see + kPage - 1) / kPage;
+  const int np = (some_see + kPage - 1) / kPage;
   const int per = split_pages(np, splits);
   const int p0 = split * per, p1 = min(p0 + per, np);
   const bool joined = per < np;  // several splits have keys
   if (split > 0 && p0 >= np) return;
 
-  // What the first step needs goes out before the queries are worked on.  Loads
-  // run one step ahead; what would lie behind the wave's last step is its last
-  // step again (no branch around loads, whose waits would then have to assume that it was
-  // not taken).  Lane i holds the page ids of the i-th of 64 steps.
+  // (Loads and page ids as above.)
   const int* row = P.table + (size_t)s.trow * P.max_pages;
-  const int* list = LIST ? B.blocks + ((size_t)(s.row0 + own) * P.hkv + w.head) * B.n : nullptr;
   constexpr int STEP = 2 * W;
   int p = p0 + 2 * wave;
   const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
   unsigned ids[2];
-  int at[2];                 // LIST: the blocks' first positions
-  uint64_t full = 0, part = 0;  // LIST: steps that the row sees whole, other ones with a block
   auto load_ids = [&](int q) {
-    const int from = LIST ? q + lane * STEP : min(q + lane * STEP, last);
+    const int from = min(q + lane * STEP, last);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      int page = max(min(from + i, np - 1), 0);
-      if constexpr (LIST) {
-        const int b = list[page];
-        const bool in = from + i < p1 && b >= 0 && b <= (some_see - 1) >> 4;
-        at[i] = in ? b * kPage : kNowhere;
-        page = in ? b : 0;
-      }
-      const unsigned x = (unsigned)row[page];
+      const unsigned x = (unsigned)row[max(min(from + i, np - 1), 0)];
       ids[i] = x < (unsigned)P.n_pages ? x : 0u;  // an id outside the pool reads its first page
-    }
-    if constexpr (LIST) {
-      full = __builtin_amdgcn_ballot_w64(max(at[0], at[1]) + kPage <= some_see);
-      part = __builtin_amdgcn_ballot_w64(min(at[0], at[1]) < kNowhere) & ~full;
-    }
-  };
-  auto fetch_step = [&](PageRegs* pr, int i) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const unsigned id = (unsigned)__builtin_amdgcn_readlane((int)ids[j], i);
-      load_page<ONCE>(pr[j], P.pool + ((size_t)id * (unsigned)P.hkv + (unsigned)w.head) * kKv8Block, (unsigned)lane);
     }
   };
   int ahead = 0;  // the step that is fetched next
-  auto fetch = [&](PageRegs* pr) {
+  auto fetch = [&](PageRegs* x) {
     if (ahead == 64) {
       load_ids(p + STEP);
       ahead = 0;
     }
-    fetch_step(pr, ahead);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned id = (unsigned)__builtin_amdgcn_readlane((int)ids[i], ahead);
+      load_page<false>(x[i], P.pool + ((size_t)id * (unsigned)P.hkv + (unsigned)w.head) * kKv8Block, (unsigned)lane);
+    }
     ++ahead;
-  };
-  // LIST: the steps of 64 that have blocks, first those that the row sees whole.  (Behind
-  // the last one any other is fetched.)
-  auto fetch_listed = [&](PageRegs* pr) {
-    uint64_t& of = full ? full : part;
-    ahead = of ? __builtin_ctzll(of) : 0;
-    of &= of - 1;
-    fetch_step(pr, ahead);
   };
   load_ids(p);
   // Of several tiles, each wave makes one's queries for all.
   RawQuery raw;
-  if (NQ == 1 || wave < NQ) load_query<QT, PACK>(raw, w, A, NQ == 1 ? 0 : wave);
+  if (NQ == 1 || wave < NQ) load_query<QT, 1>(raw, w, A, NQ == 1 ? 0 : wave);
   PageRegs a[2], c[2];
-  int n_full = __builtin_popcountll(full), n_part = __builtin_popcountll(part);
-  if constexpr (LIST) fetch_listed(a);
-  else fetch(a);
-  Columns<NQ, QT, PACK> C;
+  fetch(a);
+  Columns<NQ, QT, 1> C;
   C.start(w, most);
-  if constexpr (PACK == 2) {
-    C.pack(make_query<QT>(raw, A));
-  } else if constexpr (NQ == 1) {
+  if constexpr (NQ == 1) {
     C.q[0] = make_query<QT>(raw, A);
   } else {
     __shared__ f16x8 made[NQ][2 * QT][64];
@@ -443,99 +768,52 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits
     }
   }
 
-  auto step = [&](const PageRegs* pr, int at0, int at1, auto masked) {
+  auto step = [&](const PageRegs* x, auto masked) {
     constexpr bool MASK = decltype(masked)::value;
     f16x8 kf[2][2], vf[4];
     f16x4 va[4], vb[4];
-    operands<MASK>(pr[0], kf[0], va);
-    operands<MASK>(pr[1], kf[1], vb);
+    operands<MASK>(x[0], kf[0], va);
+    operands<MASK>(x[1], kf[1], vb);
 #pragma unroll
     for (int j = 0; j < 4; ++j) vf[j] = join8(va[j], vb[j]);
     unsigned bad[2] = {0u, 0u};
     if constexpr (MASK) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) bad[i] = (pr[i].s[1] | pr[i].s[1] >> 16) >> (4 * g) & 15u;
+      for (int i = 0; i < 2; ++i) bad[i] = (x[i].s[1] | x[i].s[1] >> 16) >> (4 * g) & 15u;
     }
     f32x4 sc[NQ][2];
     f16x8 ph[NQ], pl[NQ];
     C.scores(kf, sc);
-    C.template weights<MASK, LIST>(sc, at0, at1, PACK == 2 ? (C.right() ? bad[1] : bad[0]) : bad[0] | bad[1] << 4, ph, pl);
+    C.template weights<MASK>(sc, p * kPage, (p + 1) * kPage, bad[0] | bad[1] << 4, ph, pl);
     C.values(vf, ph, pl);
-    if constexpr (MASK && LIST) C.look_for_fresh();
   };
-  if constexpr (LIST) {
-    while (true) {
-      bool swapped = false;
-      while (n_full > 0) {
-        fetch_listed(c);
-        step(a, 0, 0, std::false_type());
-        if (--n_full == 0) {
-          swapped = true;
-          break;
-        }
-        fetch_listed(a);
-        step(c, 0, 0, std::false_type());
-        --n_full;
-      }
-      if (swapped) {
-        a[0] = c[0];
-        a[1] = c[1];
-      }
-      for (; n_part > 0; --n_part) {
-        const int now = ahead;
-        fetch_listed(c);
-        step(a, __builtin_amdgcn_readlane(at[0], now), __builtin_amdgcn_readlane(at[1], now), std::true_type());
-        a[0] = c[0];
-        a[1] = c[1];
-      }
-      p += 64 * STEP;
-      if (p >= p1) break;
-      load_ids(p);
-      n_full = __builtin_popcountll(full);
-      n_part = __builtin_popcountll(part);
-      fetch_listed(a);
+  const int whole = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
+  bool swapped = false;
+  while (p < whole) {
+    fetch(c);
+    step(a, std::false_type());
+    p += STEP;
+    if (p >= whole) {
+      swapped = true;
+      break;
     }
-  } else {
-    const int whole = min(all_see / kPage & ~1, p1 & ~1);  // pages below are seen by every row
-    bool swapped = false;
-    while (p < whole) {
-      fetch(c);
-      step(a, 0, 0, std::false_type());
-      p += STEP;
-      if (p >= whole) {
-        swapped = true;
-        break;
-      }
-      fetch(a);
-      step(c, 0, 0, std::false_type());
-      p += STEP;
-    }
-    if (swapped) {
-      a[0] = c[0];
-      a[1] = c[1];
-    }
-    while (p < p1) {
-      fetch(c);
-      step(a, p * kPage, (p + 1) * kPage, std::true_type());
-      a[0] = c[0];
-      a[1] = c[1];
-      p += STEP;
-    }
+    fetch(a);
+    step(c, std::false_type());
+    p += STEP;
+  }
+  if (swapped) {
+    a[0] = c[0];
+    a[1] = c[1];
+  }
+  while (p < p1) {
+    fetch(c);
+    step(a, std::true_type());
+    a[0] = c[0];
+    a[1] = c[1];
+    p += STEP;
   }
 
-  // Without neighbours a lane writes its 16 dimensions from 16 g on.
-  if constexpr (W == 1) {
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-      float m = C.base_of(t), l = C.sum[t][0], x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 16.f * C.o[t][i & 3][i >> 2];  // (16: of the values' scale)
-      if constexpr (PACK == 2) join_sides(m, l, x);
-      if (PACK == 1 || !C.right()) put<16>(R, A, w, w.c0 + 16 * t + r, 16 * g, x, l, m, joined, split, splits);
-    }
-    return;
-  }
-  // Join the waves: wave v takes dimensions 16 g + 4 v .. + 3, of two waves v + 2 too.
+  // Join the waves: wave v takes dimensions 16 g + 4 v .. + 3.
   __shared__ f32x4 lo[W][4][64];
   __shared__ float2 ls[W][64];
 #pragma unroll
@@ -545,57 +823,31 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Kv8List B, Div heads, Div splits
     for (int i = 0; i < 4; ++i) lo[wave][i][lane] = f32x4{C.o[t][0][i], C.o[t][1][i], C.o[t][2][i], C.o[t][3][i]};
     ls[wave][lane] = make_float2(C.base_of(t), C.sum[t][0]);
     __syncthreads();
-    float top = -INFINITY;
+    float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < W; ++v) top = fmaxf(top, ls[v][lane].x);
-    for (int part = wave; part < 4; part += W) {
-      float m = top, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int v = 0; v < W; ++v) m = fmaxf(m, ls[v][lane].x);
 #pragma unroll
-      for (int v = 0; v < W; ++v) {
-        const float2 z = ls[v][lane];
-        const float f = z.x > -INFINITY ? 16.f * __builtin_amdgcn_exp2f(z.x - m) : 0.f;  // (as above)
-        const f32x4 y = lo[v][part][lane];
-        l += f * z.y;
+    for (int v = 0; v < W; ++v) {
+      const float2 z = ls[v][lane];
+      const float f = z.x > -INFINITY ? 16.f * __builtin_amdgcn_exp2f(z.x - m) : 0.f;  // (16: of the values' scale)
+      const f32x4 y = lo[v][wave][lane];
+      l += f * z.y;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] += f * y[j];
-      }
-      l *= 0.0625f;
-      if constexpr (PACK == 2) join_sides(m, l, x);
-      if (PACK == 1 || !C.right()) put<4>(R, A, w, w.c0 + 16 * t + r, 16 * g + 4 * part, x, l, m, joined, split, splits);
+      for (int j = 0; j < 4; ++j) x[j] += f * y[j];
     }
+    put<4>(R, A, w, w.c0 + 16 * t + r, 16 * g + 4 * wave, x, l * 0.0625f, m, joined, split, splits);
   }
 }
 
-typedef void (*Attend)(Kv4Pool, Kv4Rows, Kv4Attend, Kv8List, Div, Div, Div, Div, Div);
-template <int QT, int W>
-Attend pick_tile(const Kv8Plan& p) {
-  if constexpr (W == 4)  // (eight waves are for sequences of one tile)
-    if (p.tiles > 1) return k_kv8_attend<1, QT, W, 1, false, false>;
-  return p.packed ? k_kv8_attend<1, QT, W, 2, false, true> : k_kv8_attend<1, QT, W, 1, false, true>;
+typedef void (*FewKernel)(Kv4Pool, Kv4Rows, Kv4Attend, Kv8List, Div, Div, Div, Div, Div);
+template <int W, bool LIST>
+FewKernel pick_few(int columns) {
+  return columns <= 8 ? k_kv8_few<2, W, LIST, !LIST> : k_kv8_few<1, W, LIST, !LIST>;
 }
-
 template <int QT>
-hipError_t launch_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8Plan& p) {
-  const auto kernel = p.nq == 2     ? k_kv8_attend<2, QT, 4, 1, false, false>
-                      : p.nq == 4   ? k_kv8_attend<4, QT, 4, 1, false, false>
-                      : p.waves == 4 ? pick_tile<QT, 4>(p)
-                                     : pick_tile<QT, 8>(p);
-  const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * p.tiles * p.splits);
-  return launch(kernel, groups, 64 * p.waves, 0, st, P, R, A, Kv8List{nullptr, 0}, div_by(P.hkv), div_by(p.splits),
-                div_by(p.tiles), div_by(A.hq / P.hkv), div_by(1));
-}
-
-template <int QT>
-hipError_t launch_list(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8List& B,
-                       const Kv8ListPlan& p) {
-  const auto kernel = p.waves == 1   ? (p.packed ? k_kv8_attend<1, QT, 1, 2, true, false> : k_kv8_attend<1, QT, 1, 1, true, false>)
-                      : p.waves == 2 ? (p.packed ? k_kv8_attend<1, QT, 2, 2, true, false> : k_kv8_attend<1, QT, 2, 1, true, false>)
-                      : p.waves == 4 ? (p.packed ? k_kv8_attend<1, QT, 4, 2, true, false> : k_kv8_attend<1, QT, 4, 1, true, false>)
-                                     : (p.packed ? k_kv8_attend<1, QT, 8, 2, true, false> : k_kv8_attend<1, QT, 8, 1, true, false>);
-  const int tiles = R.max_rows * p.tiles;
-  const unsigned groups = (unsigned)((int64_t)R.n_seqs * P.hkv * tiles * p.splits);
-  return launch(kernel, groups, 64 * p.waves, 0, st, P, R, A, B, div_by(P.hkv), div_by(p.splits), div_by(tiles),
-                div_by(A.hq / P.hkv), div_by(p.tiles));
+hipError_t launch_prompt(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8Plan& p, unsigned groups) {
+  const auto kernel = p.nq == 1 ? k_kv8_attend<1, QT> : p.nq == 2 ? k_kv8_attend<2, QT> : k_kv8_attend<4, QT>;
+  return launch(kernel, groups, 256, 0, st, P, R, A, div_by(P.hkv), div_by(p.splits), div_by(p.tiles), div_by(A.hq / P.hkv));
 }
 
 // A wave a (page, head), as in the 4-bit cache's calls.
@@ -629,18 +881,31 @@ hipError_t kv8_read(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, void* k,
 hipError_t kv8_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8Plan& p) {
   // 16-bit queries fit one fp16 term; rotated ones are fp32 numbers.
   const bool one = A.q_type != kRowF32 && !A.rope.at;
+  const int group = A.hq / P.hkv;
   return by_sequences(R, p.threads, [&](const Kv4Rows& r) {
-    const hipError_t e = one ? launch_attend<1>(st, P, r, A, p) : launch_attend<2>(st, P, r, A, p);
+    const unsigned groups = (unsigned)((int64_t)r.n_seqs * P.hkv * p.tiles * p.splits);
+    hipError_t e;
+    if (p.tiles == 1 && p.nq == 1)
+      e = launch(p.waves == 4 ? pick_few<4, false>(r.max_rows * group) : pick_few<8, false>(r.max_rows * group), groups,
+                 64 * p.waves, 0, st, P, r, A, Kv8List{nullptr, 0}, div_by(P.hkv), div_by(p.splits), div_by(1), div_by(group), div_by(1));
+    else
+      e = one ? launch_prompt<1>(st, P, r, A, p, groups) : launch_prompt<2>(st, P, r, A, p, groups);
     return e != hipSuccess || p.splits == 1 ? e : launch_join(st, P, r, A, 16 * p.nq, p.splits, 0);
   });
 }
 
 hipError_t kv8_attend_list(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8List& B,
                            const Kv8ListPlan& p) {
-  const bool one = A.q_type != kRowF32 && !A.rope.at;
+  const int group = A.hq / P.hkv, tiles = R.max_rows * p.tiles;
   const int per = 2 * (((B.n + 1) / 2 + p.splits - 1) / p.splits), used = (B.n + per - 1) / per;
+  const auto kernel = p.waves == 1   ? pick_few<1, true>(group)
+                      : p.waves == 2 ? pick_few<2, true>(group)
+                      : p.waves == 4 ? pick_few<4, true>(group)
+                                     : pick_few<8, true>(group);
   return by_sequences(R, p.threads, [&](const Kv4Rows& r) {
-    const hipError_t e = one ? launch_list<1>(st, P, r, A, B, p) : launch_list<2>(st, P, r, A, B, p);
+    const unsigned groups = (unsigned)((int64_t)r.n_seqs * P.hkv * tiles * p.splits);
+    const hipError_t e = launch(kernel, groups, 64 * p.waves, 0, st, P, r, A, B, div_by(P.hkv), div_by(p.splits), div_by(tiles),
+                                div_by(group), div_by(p.tiles));
     return e != hipSuccess || used == 1 ? e : launch_join(st, P, r, A, 16, p.splits, used);
   });
 }

@@ -20,17 +20,16 @@ inline Kv8Plan kv8_plan(const Kv4Sizes& z) {
 struct Kv8ListPlan {
   int waves, splits;
   int tiles;          // workgroups a row and kv head
-  bool packed;        // two blocks side by side in one tile
   int64_t threads;    // of a sequence's larger grid
   size_t workspace;   // bytes
 };
 // Waves of a workgroup and splits of a list over workgroups: those of the least time by
 // what was measured, in ns (eight sizes, 32 and 64 query heads on 8, with one to eight waves and
-// splits; the choices cost 1% on average against the best ones, 5% at most).  A step
-// takes a wave alone on its SIMD 650 ns and 380 more for each neighbour, and the SIMD 490 of
-// its own; a wave's start and end 630 of them.  So (us) 4,000 rows of 32 blocks take one
-// wave (177; two 200, four 244, eight 375), 200 such rows two (18.8; one 22.7, four 19.3), 32
-// of 64 eight (10.5; one 24.4), and one of 128 eight waves and splits (7.5; no split 9.3).
+// splits; the choices cost 2% on average against the best ones, 7% at most).  A step
+// takes a wave alone on its SIMD 500 ns and 100 more for each neighbour, and the SIMD 455 of
+// its own; a wave's start and end 730 of them.  So (us) 4,000 rows of 32 blocks take one
+// wave (163; two 188, four 232, eight 371), 200 such rows one (16.7; two 17.3, eight 24.9), 32
+// of 64 eight (10.3; one 19.6), and one of 128 eight waves and splits (8.0; no split 9.5).
 struct Kv8ListCut {
   int waves, splits;
 };
@@ -41,8 +40,8 @@ inline Kv8ListCut kv8_list_cut(int64_t items, int pairs, int64_t outputs) {
     for (int s = 1; s <= std::min(kMaxSplits, pairs) && (s == 1 || split_bytes(s, outputs) <= kKv4Workspace); s += s < 8 ? 1 : 4) {
       const int steps = ((pairs + s - 1) / s + w - 1) / w;
       const double load = (double)items * s * w / 1024, held = std::min(4.0, std::max(1.0, round_up(load)));
-      double ns = std::max(2800 + steps * (650 + 380 * (held - 1)), 2500 + load * (630 + 490 * steps));
-      if (s > 1) ns += 3400 + 0.12 * (double)outputs * s;
+      double ns = std::max(3700 + steps * (500 + 100 * (held - 1)), 2500 + load * (730 + 455 * steps));
+      if (s > 1) ns += 3340 + 0.093 * (double)outputs * s;
       if (best.waves == 0 || ns < best_ns) {
         best = Kv8ListCut{w, s};
         best_ns = ns;
@@ -55,7 +54,6 @@ inline Kv8ListPlan kv8_list_plan(const Kv4Sizes& z, int n) {
   const int group = z.hq / z.hkv;
   const int64_t outputs = (int64_t)z.n_rows * z.hq;
   p.tiles = (group + 15) / 16;
-  p.packed = group <= 8;
   const Kv8ListCut c = kv8_list_cut((int64_t)z.n_rows * z.hkv * p.tiles, (n + 1) / 2, outputs);
   p.waves = c.waves;
   p.splits = c.splits;

@@ -193,9 +193,8 @@ struct Columns {
 
   // MASK: slots past a column's keys (the pages' first positions are at0 and at1), and
   // bad ones (N bits), whose keys or values are NaN.  The check of all columns' scores is
-  // the step's only branch.  ANY: pages come in any order, so that a column may see none of
-  // the first ones; such a column's sum is 0, and its base is set by the first that it sees.
-  template <bool MASK, bool ANY = false>
+  // the step's only branch.
+  template <bool MASK>
   __device__ __forceinline__ void weights(const f32x4 (*sc)[2], int at0, int at1, unsigned bad, f16x8* ph, f16x8* pl) {
     const int g = (threadIdx.x & 63) >> 4;
     float x[NQ][N], high = -INFINITY;
@@ -219,10 +218,9 @@ struct Columns {
 #pragma unroll
         for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[t][i]);
         mx = rows_max(mx);
-        const bool fresh = ANY ? sum[t][0] == 0.f : first;
         float up = mx > -INFINITY ? mx - kOffset : 0.f;
-        if (!fresh) up = fmaxf(up, 0.f);
-        const float f = fresh ? 1.f : __builtin_amdgcn_exp2f(-up);
+        if (!first) up = fmaxf(up, 0.f);
+        const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
         base[t] += up;
 #pragma unroll
         for (int i = 0; i < N; ++i) x[t][i] -= up;
@@ -266,14 +264,6 @@ struct Columns {
       for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], ph[t], o[t][j], 0, 0, 0);
       sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph[t], sum[t], 0, 0, 0);
     }
-  }
-
-  // ANY: whether a column may have no base yet, after a step that masks.
-  __device__ __forceinline__ void look_for_fresh() {
-    bool none = false;
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) none = none || sum[t][0] == 0.f;
-    first = __builtin_amdgcn_ballot_w64(none);
   }
 
   // A column that saw no key has no base.

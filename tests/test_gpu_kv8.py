@@ -7,7 +7,9 @@
   Its bound, for every element (a = max over the attended keys of
   scale * sum |q_i k_i|, m = max |v|):
     - scores: queries as two fp16 terms, 2^-22 of each product, and 64 fp32 sums,
-      2^-18 of sum |q k|; a rotation in fp32, 3 * 2^-24 more; the power's argument
+      2^-18 of sum |q k| (or, of few columns, as whole numbers, 2^-22 of the largest
+      element at most, in random directions: 8 * 2^-22 of its products' 64 rather than sums of
+      fp32); a rotation in fp32, 3 * 2^-24 more; the power's argument
       and the exponential, 2^-20 and 2^-21 of a weight (|argument| < 2^7):
       e = 2^-17.5 a + 2^-19;
     - weights relative to their sum: 2 e, and two fp16 terms each, 2 * 2^-22; sums of
@@ -484,6 +486,19 @@ def test_long_lists(n):
     lists[1] = -1
     lists[1, :, -1] = 5
     check(c, [1], [16 * 1600 - 1], 4, "f32", "f32", rng, lists=lists)
+
+
+@pytest.mark.parametrize("group", [4, 12])
+def test_entries_that_are_none_read_no_page(group):
+    """A sequence whose first pages were never written (bytes that make NaN scales), and
+    lists of its others with entries that are none beside them."""
+    rng = np.random.default_rng(0)
+    c = Cache(1, 1, 6)
+    k, v = (torch.randn(64, 1, 64, device="cuda:0") for _ in "kv")
+    c.append([64], [32], k, v, "f32")
+    lists = np.array([[2, -1, -1, 3, 5, -1, -1, -1], [-1, -1, 4, -1, -1, 99, 2, -1]], np.int32)[:, None]
+    lists = np.concatenate([lists, np.zeros((2, 1, 8), np.int32)])
+    check(c, [2], [93], group, "f32", "f32", rng, lists=lists)
 
 
 @pytest.mark.parametrize("group", [4, 12])
