@@ -48,57 +48,39 @@ __device__ __forceinline__ float clamp127(float c) { return __builtin_amdgcn_fme
 
 __device__ __forceinline__ unsigned max16(unsigned x) { return max_dpp<0x128>(max_dpp<0x124>(max_dpp<0x4E>(max_dpp<0xB1>(x)))); }
 
-// One wave has one (page, head) of one sequence: the rows of the call that lie in that
-// page, and what the page held in front of them.  Its scales become those that the largest
-// of the new rows need, and never less than the kept ones' own: codes that stay are
-// divided by the power of two between, to nearest even, so that a value that was
+// One wave has the keys, or the values, of one (page, head) of one sequence: the rows of the
+// call that lie in that page, and what the page held in front of them.  The scale becomes the
+// one that the largest of the new rows needs, and never less than the kept ones' own: codes that
+// stay are divided by the power of two between, to nearest even, so that a value that was
 // held through several such steps is off by less than one step of the last scale.
 // The page is written whole: slots behind the rows hold zeros.
-__global__ __launch_bounds__(256) void k_kv8_append(Kv4Pool P, Kv4Rows R, const void* __restrict__ k,
-                                                    const void* __restrict__ v, int type, int64_t ks, int64_t vs,
-                                                    RopeTable rope, int tiles) {
-  const int lane = threadIdx.x & 63;
-  const int head = blockIdx.y * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (head >= P.hkv) return;
-  const unsigned sq = blockIdx.x / (unsigned)tiles;
-  const int tile = blockIdx.x - sq * tiles;
-  const Seq q = load_seq(P, R, R.seq0 + sq);
-  const int lo = max(q.first, 0);
-  int hi = min(q.first + q.n, P.max_pages * kPage);
-  if (rope.at) hi = min(hi, rope.len);
-  const int page = lo / kPage + tile;
-  // (page * kPage may pass 31 bits.)  Without rows the page stays as it is.
-  if (lo >= hi || page >= (hi + kPage - 1) >> 4) return;
-  const int id = P.table[(size_t)q.trow * P.max_pages + page];
-  if ((unsigned)id >= (unsigned)P.n_pages) return;
-  unsigned char* blk = P.pool + ((size_t)id * P.hkv + head) * kKv8Block;
-  const int r = lane & 15, g = lane >> 4;
-  const int from = max(lo - page * kPage, 0), to = min(hi - page * kPage, kPage);  // the page's new slots
+struct PageRows {
+  Seq q;
+  int page, from, to;  // the page's new slots
+  unsigned char* blk;
+  size_t row;  // the buffer's, of slot 0
+};
 
-  // What the page holds in front of them.
-  u32x4 old_k = {0u, 0u, 0u, 0u}, old_v = old_k;
-  unsigned old_s = 0, old_bad = 0;
+__device__ __forceinline__ void put_keys(const PageRows& z, int head, const void* __restrict__ k, int type, int64_t stride, RopeTable rope) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, from = z.from;
+  unsigned char* blk = z.blk;
+  u32x4 old = {0u, 0u, 0u, 0u};
+  unsigned old_s = 0u, old_bad = 0u;
   if (from > 0) {
-    old_k = *reinterpret_cast<const u32x4*>(blk + 16 * lane);
-    old_v = *reinterpret_cast<const u32x4*>(blk + kKv8Values + 16 * lane);
-    old_s = *reinterpret_cast<const unsigned*>(blk + kKv8Scales);
-    old_bad = *reinterpret_cast<const unsigned*>(blk + kKv8Scales + 4);
-    const unsigned kept = (1u << from) - 1u;
-    old_bad &= kept | kept << 16;
+    old = *reinterpret_cast<const u32x4*>(blk + 16 * lane);
+    old_s = *reinterpret_cast<const unsigned short*>(blk + kKv8Scales);
+    old_bad = *reinterpret_cast<const unsigned short*>(blk + kKv8Scales + 4) & ((1u << from) - 1u);
   }
-
-  // Keys: lane (slot r, quarter g) has whole rotation pairs (i, i + 32).
+  // Lane (slot r, quarter g) has whole rotation pairs (i, i + 32).
   float x[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = 0.f;
-  const bool mine = r >= from && r < to;
-  if (mine) {
-    const int pos = page * kPage + r;
-    const size_t at = (size_t)(q.row0 + (pos - q.first)) * ks + head * 64 + 8 * g;
+  if (r >= from && r < z.to) {
+    const size_t at = (z.row + r) * stride + head * 64 + 8 * g;
     load_row<8>(k, at, type, x);
     load_row<8>(k, at + 32, type, x + 8);
     if (rope.at) {
-      const float2* cs = rope.at + (size_t)pos * 32 + 8 * g;
+      const float2* cs = rope.at + (size_t)(z.page * kPage + r) * 32 + 8 * g;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float2 t = cs[i];
@@ -108,109 +90,151 @@ __global__ __launch_bounds__(256) void k_kv8_append(Kv4Pool P, Kv4Rows R, const 
       }
     }
   }
-  // Values: lane (r, g) has slots 4 g .. + 3, dimensions 4 r .. + 3.
+  // Rows that are not finite: marked, codes of 0.
+  unsigned top = 0u;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, magnitude(x[i]));
+  top = rows_max(top);
+  const bool bad = top >= kInfBits;
+  const unsigned marks = ((unsigned)__builtin_amdgcn_ballot_w64(bad) & 0xffffu) | old_bad;
+  if (bad) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    top = 0u;
+  }
+  int e = scale_exponent(__uint_as_float(max16(top)));
+  const int before = held_exponent(old_s);
+  if (from > 0) e = max(e, before);
+  const float down = power2(-e);
+  float c[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) c[i] = clamp127(rintf(x[i] * down));
+  if (from > 0) {
+    const float shrink = power2(before - e);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c[i] = r < from ? clamp127(rintf(code_at(old[i >> 2], i & 3) * shrink)) : c[i];
+  }
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = bytes_of(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]);
+  *reinterpret_cast<u32x4*>(blk + 16 * lane) = w;
+
+  // The summary: sums of codes over the slots, a lane's 16 dimensions in pairs
+  // a + 4096 b (both at most 2,032, so the pair is exact), in 8 bits.
+  float high = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = row_sum16(fmaf(c[8 + i], 4096.f, c[i]));
+    c[8 + i] = rintf(t * (1.f / 4096.f));
+    c[i] = fmaf(c[8 + i], -4096.f, t);
+    high = fmaxf(high, fmaxf(fabsf(c[i]), fabsf(c[8 + i])));
+  }
+  high = rows_max(high);
+  const int less = (high > 127.f) + (high > 254.f) + (high > 508.f) + (high > 1016.f);
+  const float part = power2(-less);
+  if (r == 0) {
+    unsigned* m = reinterpret_cast<unsigned*>(blk + kKv8Sums + 8 * g);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = rintf(c[8 * h + i] * part);
+      *reinterpret_cast<u32x2*>(m + 8 * h) = u32x2{bytes_of(y[0], y[1], y[2], y[3]) ^ 0x80808080u,
+                                                   bytes_of(y[4], y[5], y[6], y[7]) ^ 0x80808080u};
+    }
+  }
+  if (lane == 0) {
+    *reinterpret_cast<unsigned short*>(blk + kKv8Scales) = (unsigned short)half_bits(power2(e));
+    *reinterpret_cast<unsigned short*>(blk + kKv8Scales + 4) = (unsigned short)marks;
+    // The summary's scale, for means, and nothing behind it.
+    *reinterpret_cast<u32x2*>(blk + kKv8Scales + 8) = u32x2{half_bits(power2(e + less - 4)), 0u};
+  }
+}
+
+__device__ __forceinline__ void put_values(const PageRows& z, int head, const void* __restrict__ v, int type, int64_t stride) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, from = z.from;
+  unsigned char* blk = z.blk;
+  u32x4 old = {0u, 0u, 0u, 0u};
+  unsigned old_s = 0u, old_bad = 0u;
+  if (from > 0) {
+    old = *reinterpret_cast<const u32x4*>(blk + kKv8Values + 16 * lane);
+    old_s = *reinterpret_cast<const unsigned short*>(blk + kKv8Scales + 2);
+    old_bad = *reinterpret_cast<const unsigned short*>(blk + kKv8Scales + 6) & ((1u << from) - 1u);
+  }
+  // Lane (r, g) has slots 4 g .. + 3, dimensions 4 r .. + 3.
   float y[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int slot = 4 * g + i;
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[i][j] = 0.f;
-    if (slot >= from && slot < to)
-      load_row<4>(v, (size_t)(q.row0 + (page * kPage + slot - q.first)) * vs + head * 64 + 4 * r, type, y[i]);
+    if (slot >= from && slot < z.to) load_row<4>(v, (z.row + slot) * stride + head * 64 + 4 * r, type, y[i]);
   }
-
-  // Rows that are not finite: marked, codes of 0.
-  unsigned bad_k, bad_v;
-  {
+  unsigned all = 0u, marks = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
     unsigned top = 0u;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, magnitude(x[i]));
-    top = rows_max(top);
-    const bool bad = top >= kInfBits;
-    bad_k = (unsigned)__builtin_amdgcn_ballot_w64(bad) & 0xffffu;
-    if (bad) {
+    for (int j = 0; j < 4; ++j) top = max(top, magnitude(y[i][j]));
+    top = max16(top);
+    if (top >= kInfBits) {
+      marks |= 1u << (4 * g + i);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+      for (int j = 0; j < 4; ++j) y[i][j] = 0.f;
       top = 0u;
     }
-    top = max16(top);
-    const int need = scale_exponent(__uint_as_float(top)), before = held_exponent(old_s & 0xffffu);
-    const int e = from > 0 ? max(need, before) : need;
-    const float down = power2(-e), shrink = power2(before - e);
-    float c[16];
+    all = max(all, top);
+  }
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      c[i] = r < from ? clamp127(rintf(code_at(old_k[i >> 2], i & 3) * (from > 0 ? shrink : 0.f))) : clamp127(rintf(x[i] * down));
-    u32x4 w;
+  for (int i = 0; i < 4; ++i) old_bad |= (unsigned)__builtin_amdgcn_readlane((int)marks, 16 * i);
+  int e = scale_exponent(__uint_as_float(rows_max(all)));
+  const int before = held_exponent(old_s);
+  if (from > 0) e = max(e, before);
+  const float down = power2(-e), shrink = power2(before - e);
+  u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = bytes_of(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]);
-    *reinterpret_cast<u32x4*>(blk + 16 * lane) = w;
+  for (int j = 0; j < 4; ++j) {
+    float c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = clamp127(rintf(y[i][j] * down));
+    if (from > 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = 4 * g + i < from ? clamp127(rintf(code_at(old[j], i) * shrink)) : c[i];
+    }
+    w[j] = bytes_of(c[0], c[1], c[2], c[3]);
+  }
+  *reinterpret_cast<u32x4*>(blk + kKv8Values + 16 * lane) = w;
+  if (lane == 0) {
+    *reinterpret_cast<unsigned short*>(blk + kKv8Scales + 2) = (unsigned short)half_bits(power2(e));
+    *reinterpret_cast<unsigned short*>(blk + kKv8Scales + 6) = (unsigned short)old_bad;
+  }
+}
 
-    // The summary: sums of codes over the slots, a lane's 16 dimensions in pairs
-    // a + 4096 b (both at most 2,032, so the pair is exact), in 8 bits.
-    float high = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = row_sum16(fmaf(c[8 + i], 4096.f, c[i]));
-      c[8 + i] = rintf(t * (1.f / 4096.f));
-      c[i] = fmaf(c[8 + i], -4096.f, t);
-      high = fmaxf(high, fmaxf(fabsf(c[i]), fabsf(c[8 + i])));
-    }
-    high = rows_max(high);
-    const int less = (high > 127.f) + (high > 254.f) + (high > 508.f) + (high > 1016.f);
-    const float part = power2(-less);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) c[i] = rintf(c[i] * part);
-    if (r == 0) {
-      unsigned* m = reinterpret_cast<unsigned*>(blk + kKv8Sums + 8 * g);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float* z = c + 8 * h;
-        *reinterpret_cast<u32x2*>(m + 8 * h) = u32x2{bytes_of(z[0], z[1], z[2], z[3]) ^ 0x80808080u,
-                                                     bytes_of(z[4], z[5], z[6], z[7]) ^ 0x80808080u};
-      }
-    }
-    // The last of these is the summary's scale, for means.
-    old_s = (old_s & 0xffff0000u) | half_bits(power2(e));
-    old_k[0] = half_bits(power2(e + less - 4));
-  }
-  {
-    unsigned top[4], all = 0u, marks = 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      top[i] = 0u;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) top[i] = max(top[i], magnitude(y[i][j]));
-      top[i] = max16(top[i]);
-      if (top[i] >= kInfBits) {
-        marks |= 1u << (4 * g + i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[i][j] = 0.f;
-        top[i] = 0u;
-      }
-      all = max(all, top[i]);
-    }
-    bad_v = 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) bad_v |= (unsigned)__builtin_amdgcn_readlane((int)marks, 16 * i);
-    all = rows_max(all);
-    const int need = scale_exponent(__uint_as_float(all)), before = held_exponent(old_s >> 16);
-    const int e = from > 0 ? max(need, before) : need;
-    const float down = power2(-e), shrink = power2(before - e);
-    u32x4 w;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float c[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        c[i] = 4 * g + i < from ? clamp127(rintf(code_at(old_v[j], i) * shrink)) : clamp127(rintf(y[i][j] * down));
-      w[j] = bytes_of(c[0], c[1], c[2], c[3]);
-    }
-    *reinterpret_cast<u32x4*>(blk + kKv8Values + 16 * lane) = w;
-    old_s = (old_s & 0xffffu) | half_bits(power2(e)) << 16;
-  }
-  if (lane == 0)
-    *reinterpret_cast<u32x4*>(blk + kKv8Scales) = u32x4{old_s, old_bad | bad_k | bad_v << 16, old_k[0], 0u};
+__global__ __launch_bounds__(256) void k_kv8_append(Kv4Pool P, Kv4Rows R, const void* __restrict__ k,
+                                                    const void* __restrict__ v, int type, int64_t ks, int64_t vs,
+                                                    RopeTable rope, int tiles) {
+  const int head = blockIdx.y * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (head >= P.hkv) return;
+  const unsigned sq = blockIdx.x / (unsigned)tiles;
+  const int tile = blockIdx.x - sq * tiles;
+  PageRows z;
+  z.q = load_seq(P, R, R.seq0 + sq);
+  const int lo = max(z.q.first, 0);
+  int hi = min(z.q.first + z.q.n, P.max_pages * kPage);
+  if (rope.at) hi = min(hi, rope.len);
+  z.page = lo / kPage + tile;
+  // (page * kPage may pass 31 bits.)  Without rows the page stays as it is.
+  if (lo >= hi || z.page >= (hi + kPage - 1) >> 4) return;
+  const int id = P.table[(size_t)z.q.trow * P.max_pages + z.page];
+  if ((unsigned)id >= (unsigned)P.n_pages) return;
+  z.blk = P.pool + ((size_t)id * P.hkv + head) * kKv8Block;
+  z.from = max(lo - z.page * kPage, 0);
+  z.to = min(hi - z.page * kPage, kPage);
+  z.row = (size_t)((int64_t)z.q.row0 + z.page * kPage - z.q.first);  // (that of slot `from` on is in the buffer)
+  if (blockIdx.z == 0)
+    put_keys(z, head, k, type, ks, rope);
+  else
+    put_values(z, head, v, type, vs);
 }
 
 // The same lanes the other way round.  Tiles are counted from the page of the
@@ -866,7 +890,9 @@ hipError_t kv8_append(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const 
                       int64_t k_stride, int64_t v_stride, RopeTable rope) {
   const int h = row_heads(P, R);
   return by_sequences(R, kv8_row_threads(P, R), [&](const Kv4Rows& r) {
-    return launch(k_kv8_append, row_grid(P, r, h), 64 * h, 0, st, P, r, k, v, type, k_stride, v_stride, rope, row_tiles(r));
+    dim3 grid = row_grid(P, r, h);
+    grid.z = 2;  // keys, and values
+    return launch(k_kv8_append, grid, 64 * h, 0, st, P, r, k, v, type, k_stride, v_stride, rope, row_tiles(r));
   });
 }
 
