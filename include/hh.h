@@ -74,6 +74,12 @@ enum { HH_WF_DTYPE = 0, HH_WF_Q4G32 = 1 };
  * gives HH_ERR_UNSUPPORTED.  A context is created with one or the other cache.
  */
 enum { HH_KV_Q4 = 0x100 };
+/*
+ * The same with 8 bits, in the pages of hh_kv8_append below (136 bytes a position and kv
+ * head).  A page's scale grows as its positions come, so a prompt that is evaluated in other
+ * passes may differ by what its codes are rounded again.
+ */
+enum { HH_KV_Q8 = 0x400 };
 enum { HH_LOGITS_NONE = 0, HH_LOGITS_LAST = 1, HH_LOGITS_ALL = 2 };
 
 /*
@@ -93,7 +99,7 @@ typedef struct {
   int32_t max_prefill;       /* rows per prefill pass; 0 means max_context.
                                 Longer prompts are processed in passes.      */
   int32_t weight_format;     /* HH_WF_DTYPE or HH_WF_Q4G32 (dtype HH_BF16,
-                                d_model % 32 == 0); + HH_KV_Q4               */
+                                d_model % 32 == 0); + HH_KV_Q4 or HH_KV_Q8   */
 } hh_config;
 
 typedef struct hh_ctx hh_ctx;

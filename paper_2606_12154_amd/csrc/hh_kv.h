@@ -76,6 +76,8 @@ int64_t kv8_row_threads(const Kv4Pool& P, const Kv4Rows& R);
 inline Kv8Plan kv8_plan(const Kv4Pool& P, const Kv4Rows& R, int hq, int pages) {
   return kv8_plan(Kv4Sizes{R.n_seqs, R.n_rows, R.max_rows, hq, P.hkv, pages});
 }
+// (Keys enter the products as a sixteenth: A.scale is the softmax's times this.)
+constexpr float kKv8ScoreScale = 16.f;
 hipError_t kv8_attend(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const Kv4Attend& A, const Kv8Plan& p);
 
 // Listed blocks: device [n_rows][hkv][n].

@@ -30,7 +30,7 @@ hh_status attend_args(const Kv4Pool& P, const void* q, int32_t q_dtype, int64_t 
   A->q_stride = q_stride;
   A->out_stride = out_stride;
   A->hq = n_heads;
-  A->scale = scale * 16.f;  // keys enter the products as a sixteenth
+  A->scale = scale * kKv8ScoreScale;
   A->part = static_cast<float*>(workspace);
   return HH_OK;
 }

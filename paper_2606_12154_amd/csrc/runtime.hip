@@ -63,22 +63,24 @@ struct Layout {
   // between launches; in the zero-initialised range) and row sums of squares.
   size_t nrm_cnt, nrm_ss;
   int nrm_ncnt;
-  // 4-bit caches: fp32 rows of the QKV product, the pass's sequences (row
-  // starts, first positions, streams) and the attention's split outputs.
-  bool kv4;
-  size_t qkv32, seqs, kv4_work;
+  // Quantized caches (4 bits, or kv8): fp32 rows of the QKV product, the pass's sequences
+  // (row starts, first positions, streams) and the attention's split outputs.
+  bool kvq, kv8;
+  size_t qkv32, seqs, kvq_work;
   size_t page_bytes;  // one layer's page
   size_t compact, lengths;  // hh_compact's lists, and the streams' lengths
   size_t total;
 };
 
-// The cache's format travels in weight_format (HH_KV_Q4); the rest of the runtime
-// sees the weights' format alone.
+// The cache's format travels in weight_format (HH_KV_Q4 or HH_KV_Q8); the rest of the
+// runtime sees the weights' format alone.  (Both at once are no format.)
 hh_config without_kv(hh_config c) {
-  c.weight_format &= ~HH_KV_Q4;
+  constexpr int kBoth = HH_KV_Q4 | HH_KV_Q8;
+  if ((c.weight_format & kBoth) != kBoth) c.weight_format &= ~kBoth;
   return c;
 }
-bool wants_kv4(const hh_config& c) { return (c.weight_format & HH_KV_Q4) != 0; }
+bool wants_kv8(const hh_config& c) { return (c.weight_format & HH_KV_Q8) != 0; }
+bool wants_kvq(const hh_config& c) { return (c.weight_format & HH_KV_Q4) != 0 || wants_kv8(c); }
 
 bool config_supported(const hh_config& asked, std::string& why) {
   const hh_config c = without_kv(asked);
@@ -137,7 +139,8 @@ size_t q4_tile_codes(size_t rows, size_t K) { return (rows + 15) / 16 * 16 * K /
 Layout make_layout(const hh_config& asked) {
   const hh_config c = without_kv(asked);
   Layout L{};
-  L.kv4 = wants_kv4(asked);
+  L.kvq = wants_kvq(asked);
+  L.kv8 = wants_kv8(asked);
   const bool bf = c.dtype == HH_BF16;
   L.ew = bf ? 2 : 4;
   L.ekv = bf ? 2 : 4;
@@ -224,7 +227,7 @@ Layout make_layout(const hh_config& asked) {
   }
   L.final_norm = take(d * 4);
   L.rope = take((size_t)c.max_context * 32 * sizeof(float2));
-  L.page_bytes = L.kv4 ? (size_t)c.n_kv_heads * kKv4Block : (size_t)2 * c.n_kv_heads * kPage * 64 * L.ekv;
+  L.page_bytes = L.kvq ? (size_t)c.n_kv_heads * (L.kv8 ? kKv8Block : kKv4Block) : (size_t)2 * c.n_kv_heads * kPage * 64 * L.ekv;
   L.kv = take((size_t)c.n_layers * L.n_pages * L.page_bytes);
   L.page_table = take((size_t)c.max_streams * L.max_pages * 4);
   L.pos = take((size_t)c.max_streams * 4);
@@ -267,10 +270,10 @@ Layout make_layout(const hh_config& asked) {
   L.nrm_ss = take((size_t)32 * (d / 64) * 4);
   L.compact = take(compact_workspace(L.n_pages));
   L.lengths = take((size_t)c.max_streams * 4);
-  if (L.kv4) {
+  if (L.kvq) {
     L.qkv32 = take(R * L.nqkv * 4);
     L.seqs = take((3 * (size_t)c.max_streams + 1) * 4);
-    L.kv4_work = take(kKv4Workspace);
+    L.kvq_work = take(kKv4Workspace);
   }
   L.total = off;
   return L;
@@ -372,7 +375,7 @@ WTiles head_tiles(const hh_ctx* c) {
 
 KvLayout kv_layout(const hh_ctx* c) { return KvLayout{c->L.n_pages, c->cfg.n_kv_heads, c->L.max_pages}; }
 
-// What a pass over rows of a 4-bit cache needs: the cache (layer 0), the rows'
+// What a pass over rows of a quantized cache needs: the cache (layer 0), the rows'
 // sequences on the device, and how their attention is cut up.
 struct Kv4Pass {
   Kv4Pool pool;
@@ -389,7 +392,8 @@ Kv4Pass kv4_pass(const hh_ctx* c, int n_seqs, int n_rows, int max_rows, const in
   p.pool = Kv4Pool{c->at<unsigned char>(L.kv), c->at<int>(L.page_table), L.n_pages, c->cfg.n_kv_heads, L.max_pages,
                    c->cfg.max_streams};
   p.rows = Kv4Rows{starts, first_pos, streams, n_seqs, n_rows, max_rows};
-  p.plan = kv4_plan(p.pool, p.rows, c->cfg.n_heads, std::min(pages, L.max_pages));
+  const int most = std::min(pages, L.max_pages);
+  p.plan = L.kv8 ? kv8_plan(p.pool, p.rows, c->cfg.n_heads, most) : kv4_plan(p.pool, p.rows, c->cfg.n_heads, most);
   return p;
 }
 
@@ -426,9 +430,9 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
   // reads it (RowNorm); `pending`: h holds x * gain and the row sums of
   // squares are in nrm_ss, not yet applied.  (For prompt rows the large-tile
   // kernels' arrival chain cost as much as the norm pass it replaced.)
-  // (4-bit caches take the QKV product's rows whole, without such a scale.)
+  // (Quantized caches take the QKV product's rows whole, without such a scale.)
   const bool rnorm = sizeof(TM) == 2 && !decode_gemv && prefill_stream < 0 && head_row == -1 &&
-                     !L.kv4 && L.tiled && GK::norm_fusable(d) && d % 256 == 0 && d <= 2048 && c->row_norm;
+                     !L.kvq && L.tiled && GK::norm_fusable(d) && d % 256 == 0 && d <= 2048 && c->row_norm;
   float* nss = rnorm ? c->at<float>(L.nrm_ss) : nullptr;
   int* ncnt = rnorm ? c->at<int>(L.nrm_cnt) : nullptr;
   RowNorm rn_use;
@@ -456,7 +460,7 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
       if (!fuse) DK::rmsnorm_rows(st, n, x, an, eps, d, h);
       else if (l == 0) GK::rmsnorm(st, n, x, d, an, eps, h);
       // Prefill rows of one stream with an fp16 cache use MFMA flash attention.
-      const bool flash = !L.kv4 && prefill_stream >= 0 && sizeof(TKV) == 2 &&
+      const bool flash = !L.kvq && prefill_stream >= 0 && sizeof(TKV) == 2 &&
                          flash_prefill_supported(hq / hkv, c->cfg.max_context,
                                                  (size_t)kl.n_pages * 2 * hkv * kPage * kHeadDim);
       // Flash attention reads only the fp16 queries.
@@ -472,7 +476,7 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
       // over the QKV split-K reduction, rotation and KV append.
       const bool fold = prefill_stream < 0 && head_row == -1;
       QkvFold<TKV> qf;
-      if (L.kv4) {
+      if (L.kvq) {
         // The product's rows in fp32 (it adds, so they start at zero, all layers'
         // at once where the buffer holds them); keys are rotated and quantized as
         // they go into their pages, queries rotated as the attention reads them.
@@ -484,7 +488,8 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
         pool.pool += (size_t)l * L.n_pages * L.page_bytes;
         const RopeTable rt{rope, g.max_context};
         // (Launch errors here are found as the other kernels' are, at the end of the call.)
-        (void)kv4_append(st, pool, pass->rows, rows + hq * 64, rows + (hq + hkv) * 64, kRowF32, L.nqkv, L.nqkv, rt);
+        const auto append = L.kv8 ? kv8_append : kv4_append;
+        (void)append(st, pool, pass->rows, rows + hq * 64, rows + (hq + hkv) * 64, kRowF32, L.nqkv, L.nqkv, rt);
         Kv4Attend a{};
         a.q = rows;
         a.out = oM;
@@ -493,10 +498,10 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
         a.q_type = kRowF32;
         a.out_type = sizeof(TM) == 2 ? kRowF16 : kRowF32;
         a.hq = hq;
-        a.scale = 0.125f;
+        a.scale = L.kv8 ? 0.125f * kKv8ScoreScale : 0.125f;
         a.rope = rt;
-        a.part = c->at<float>(L.kv4_work);
-        (void)kv4_attend(st, pool, pass->rows, a, pass->plan);
+        a.part = c->at<float>(L.kvq_work);
+        (void)(L.kv8 ? kv8_attend : kv4_attend)(st, pool, pass->rows, a, pass->plan);
       } else if (fold) {
         const int sp = GK::qkv_deferred(st, gws, h, n, c->at<TM>(L.wqkvM[l]), d, hq, hkv, ws, rs, rp, rope, q, kv, kl, l,
                                         pt, tq,
@@ -506,7 +511,7 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
         GK::qkv(st, gws, h, n, c->at<TM>(L.wqkvM[l]), d, hq, hkv, ws, rs, rp, rope, flash ? nullptr : q,
                 flash ? c->at<TM>(L.qM) : nullptr, kv, kl, l, pt, tq);
       }
-      if (L.kv4) {
+      if (L.kvq) {
         // (attended above)
       } else if (flash) {
         if constexpr (sizeof(TKV) == 2)
@@ -559,7 +564,7 @@ void enqueue_layers(hh_ctx* c, int n, bool decode_gemv, int s_max, int head_row,
 }
 
 // One decode step for n rows (row_stream already on the device).
-// pages: a bound of the rows' cached pages (how a 4-bit cache's attention is cut up).
+// pages: a bound of the rows' cached pages (how a quantized cache's attention is cut up).
 template <typename TW, typename TKV, typename TM>
 void enqueue_decode(hh_ctx* c, int n, bool feed, bool want_logits, int pages) {
   const Layout& L = c->L;
@@ -569,10 +574,10 @@ void enqueue_decode(hh_ctx* c, int n, bool feed, bool want_logits, int pages) {
                  c->at<unsigned long long>(L.slot), c->at<TW>(L.embed), c->at<float>(L.x), c->cfg.d_model);
   // The batch-1 GEMV kernels read the model's own (bf16) matrices, which a
   // 4-bit model does not compute with: it takes the MFMA path at one row.
-  // So do steps on a 4-bit cache, which those kernels do not read.
-  const bool gemv = n == 1 && c->cfg.weight_format == HH_WF_DTYPE && !L.kv4;
+  // So do steps on a quantized cache, which those kernels do not read.
+  const bool gemv = n == 1 && c->cfg.weight_format == HH_WF_DTYPE && !L.kvq;
   Kv4Pass pass{};
-  if (L.kv4) pass = kv4_pass(c, n, n, 1, nullptr, c->at<int>(L.row_pos), c->at<int>(L.row_stream), pages);
+  if (L.kvq) pass = kv4_pass(c, n, n, 1, nullptr, c->at<int>(L.row_pos), c->at<int>(L.row_stream), pages);
   enqueue_layers<TW, TKV, TM>(c, n, gemv, kSplitMax, -1, want_logits ? c->at<float>(L.logits) : nullptr, -1, 0, 0, &pass);
   finalize(c->stream, 0, n, c->at<int>(L.row_stream), c->at<int>(L.row_pos), c->at<unsigned long long>(L.slot),
            c->at<int>(L.pending), c->at<int>(L.hist), c->at<int>(L.pos), c->cfg.max_context);
@@ -632,7 +637,7 @@ hipError_t setup_step_tables_q4(hh_ctx* c) {
 }
 
 hipError_t setup_step_kernel(hh_ctx* c) {
-  if (c->L.kv4) return hipSuccess;  // it reads fp16 and fp32 caches
+  if (c->L.kvq) return hipSuccess;  // it reads fp16 and fp32 caches
   if (c->cfg.dtype == HH_BF16) {
     if (c->cfg.weight_format == HH_WF_Q4G32) {
       // Without the 4-bit kernel (other shapes) the fp16 one streams the
@@ -840,7 +845,7 @@ hh_status do_prefill(hh_ctx* c, int s, const int32_t* tokens, int n, int mode, f
                    c->at<int>(L.pending), c->at<unsigned long long>(L.slot), c->at<TW>(L.embed), c->at<float>(L.x),
                    c->cfg.d_model);
     Kv4Pass pass{};
-    if (L.kv4) {
+    if (L.kvq) {
       const int starts[2] = {0, P};
       put_ints(st, c->at<int>(L.seqs), starts, 2);
       pass = kv4_pass(c, 1, P, P, c->at<int>(L.seqs), c->at<int>(L.row_pos), c->at<int>(L.row_stream),
@@ -938,7 +943,7 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
     const int R = (int)rs.size(), ne = (int)last_r.size();
     // fp16 caches: MFMA attention over each stream's rows where it is the
     // faster one (flash_packed_wins).
-    if (sizeof(TKV) == 2 && !L.kv4 &&
+    if (sizeof(TKV) == 2 && !L.kvq &&
         flash_prefill_supported(g.n_heads / g.n_kv_heads, g.max_context,
                                 (size_t)L.n_pages * 2 * g.n_kv_heads * kPage * kHeadDim)) {
       PackedRows pr;
@@ -966,7 +971,7 @@ hh_status do_prefill_batch(hh_ctx* c, int n, const int32_t* ids, const int32_t* 
     DK::prep_embed(st, R, -2, c->at<int>(L.feed), row_stream, row_pos, c->at<int>(L.pos), c->at<int>(L.pending),
                    slot, c->at<TW>(L.embed), x, d);
     Kv4Pass pass{};
-    if (L.kv4) {
+    if (L.kvq) {
       int longest = 1, keys = 1;
       for (int r = 0; r < R; ++r) {
         if (r == 0 || rs[r] != rs[r - 1]) {
@@ -1039,10 +1044,10 @@ hh_status do_decode(hh_ctx* c, int n, const std::vector<int>& ids, const int32_t
   }
   if (tokens) HIPCHK(c, put_ints(st, c->at<int>(L.feed), tokens, n));
   const bool want_logits = logits != nullptr;
-  // A 4-bit cache's attention is cut up for the longest stream's pages, in
+  // A quantized cache's attention is cut up for the longest stream's pages, in
   // powers of two (a graph for each).
   int pages = 0;
-  if (L.kv4) {
+  if (L.kvq) {
     int longest = 1;
     for (int i = 0; i < n; ++i) longest = std::max(longest, c->len[ids[i]] + 1);
     for (pages = 1; pages * kPage < longest;) pages *= 2;

@@ -23,6 +23,7 @@ HH_F32, HH_BF16, HH_F16 = 0, 1, 2
 HH_LOGITS_NONE, HH_LOGITS_LAST, HH_LOGITS_ALL = 0, 1, 2
 HH_WF_DTYPE, HH_WF_Q4G32 = 0, 1
 HH_KV_Q4 = 0x100  # added to a weight format: 4-bit KV cache
+HH_KV_Q8 = 0x400  # the same with 8 bits
 HH_KV4_WORKSPACE_MOST = 16 << 20  # bound of hh_kv4_attention_workspace
 HH_KV8_BLOCK = 2176  # bytes of one page of one kv head
 HH_KV8_WORKSPACE_MOST = 16 << 20  # bound of the hh_kv8 calls' workspaces
@@ -397,7 +398,7 @@ def _check(ctx, status: int) -> None:
 def make_config(shape, max_streams: int, max_context: int, max_prefill: int = 0,
                 weight_format: int = 0) -> hh_config:
     """hh_config from a model-shape object (attributes as in synth.ModelShape);
-    weight_format: HH_WF_DTYPE or HH_WF_Q4G32, + HH_KV_Q4 for a 4-bit KV cache."""
+    weight_format: HH_WF_DTYPE or HH_WF_Q4G32, + HH_KV_Q4 or HH_KV_Q8 for a KV cache in 4 or 8 bits."""
     return hh_config(shape.n_layers, shape.d_model, shape.n_heads, shape.n_kv_heads, shape.head_dim,
                      shape.ffn_dim, shape.vocab, shape.rms_eps, shape.rope_theta, int(shape.tied),
                      int(shape.dtype), max_streams, max_context, 16, max_prefill, weight_format)

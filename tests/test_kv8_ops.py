@@ -244,3 +244,21 @@ def test_calls_too_large_for_a_launch():
     wide = pool(n_kv_heads=1)
     attention(wide, rows(n_seqs=1, n_rows=1), h=1 << 25, qs=1 << 31, os=1 << 31, status=hh.HH_ERR_UNSUPPORTED)
     listed(wide, rows(n_seqs=1, n_rows=1), h=1 << 25, qs=1 << 31, os=1 << 31, status=hh.HH_ERR_UNSUPPORTED)
+
+
+# ------------------------------------------------------------------ contexts with an 8-bit cache
+
+def test_cache_format_in_the_config():
+    import synth
+    for f in (0, hh.HH_WF_Q4G32):
+        n, c, sh = 4, 4096, synth.ONE_B
+        sizes = [hh.hh_workspace_size(hh.make_config(sh, n, c, 512, weight_format=f + k)) for k in (0, hh.HH_KV_Q4, hh.HH_KV_Q8)]
+        kv = n * c * sh.n_layers * sh.n_kv_heads
+        assert abs(sizes[2] - sizes[1] - kv * (136 - 72)) < 4096
+        extra = 512 * (sh.q_dim + 2 * sh.kv_dim) * 4 + (16 << 20)  # the pass's fp32 rows and split outputs
+        assert abs(sizes[0] - sizes[2] - (kv * (256 - 136) - extra)) < 4096
+    for bad in (hh.HH_KV_Q8 + hh.HH_KV_Q4, hh.HH_KV_Q8 + 2, hh.HH_KV_Q8 + hh.HH_WF_Q4G32, hh.HH_KV_Q8 + 0x200):
+        with pytest.raises(hh.HHError) as e:
+            hh.hh_workspace_size(hh.make_config(synth.TINY, 2, 128, weight_format=bad))
+        assert e.value.status == hh.HH_ERR_UNSUPPORTED
+    assert hh.hh_workspace_size(hh.make_config(synth.TINY, 2, 128, weight_format=hh.HH_KV_Q8)) > 0
