@@ -76,8 +76,9 @@ enum { HH_WF_DTYPE = 0, HH_WF_Q4G32 = 1 };
 enum { HH_KV_Q4 = 0x100 };
 /*
  * The same with 8 bits, in the pages of hh_kv8_append below (136 bytes a position and kv
- * head).  A page's scale grows as its positions come, so a prompt that is evaluated in other
- * passes may differ by what its codes are rounded again.
+ * head).  A page's scale grows as its positions come and stays when a stream is cut, so a prompt
+ * that is evaluated in other passes, or a stream that was longer, may differ by what its codes are
+ * rounded again.
  */
 enum { HH_KV_Q8 = 0x400 };
 enum { HH_LOGITS_NONE = 0, HH_LOGITS_LAST = 1, HH_LOGITS_ALL = 2 };
@@ -420,7 +421,7 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
  * caller's own device memory.
  *
  * 136 bytes a position and kv head (fp16 takes 256, the 4-bit cache 72), at a
- * twentieth of the 4-bit cache's error.  A block (the 16 positions of a page of one kv head)
+ * tenth of the 4-bit cache's error.  A block (the 16 positions of a page of one kv head)
  * has one scale for its keys and one for its values, and a summary of its keys, by
  * which a step over a long stream can choose the blocks that it reads.
  *
@@ -480,8 +481,11 @@ enum { HH_KV8_WORKSPACE_MOST = 16 << 20 };
 hh_status hh_kv8_attention_workspace(const hh_kv8_pool* pool, const hh_kv8_rows* rows, int32_t n_heads, size_t* bytes);
 
 /*
- * Causal grouped-query attention over the pages: arguments, masks, precision and
- * errors as in hh_kv4_attention (scale at most 2^100).
+ * Causal grouped-query attention over the pages: arguments, masks and errors as in
+ * hh_kv4_attention (scale at most 2^100).  Sums, softmax and weights are as there too, and so
+ * are the queries of calls with max_rows * (n_heads / n_kv_heads) over 16; those of others are
+ * whole numbers of 23 bits in the products, each element off by 2^-22 of the query's largest
+ * at most.
  */
 hh_status hh_kv8_attention(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const void* q, int32_t q_dtype,
                            int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len,
@@ -529,7 +533,7 @@ hh_status hh_kv8_attention_blocks_workspace(const hh_kv8_pool* pool, const hh_kv
  *  blocks  device int32 [n_rows][n_kv_heads][n_blocks], in any order; entries that
  *          are no block of the row (negative, or past p / 16) are skipped, and one
  *          that is listed twice counts twice.  A row without any gives 0.
- * Otherwise as hh_kv8_attention.  Errors: as there, INVALID_ARG (blocks NULL or
+ * Otherwise as hh_kv8_attention, queries as in its smaller calls.  Errors: as there, INVALID_ARG (blocks NULL or
  * misaligned, n_blocks < 1), UNSUPPORTED (n_blocks over 32,768).
  */
 hh_status hh_kv8_attention_blocks(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const int32_t* blocks,

@@ -13,7 +13,18 @@
 //   keys    lane l holds slot l % 16, dimensions 8 (l / 16) .. + 7 of each half;
 //   values  lane l holds dimensions 4 (l % 16) .. + 3, of each its slots 4 (l / 16) .. + 3.
 // The scores of two pages, S^T[slot][query], leave each lane with the slots of both pages
-// that its value bytes hold (see kv_attend.h for what follows).
+// that its value bytes hold (see kv_attend.h for what follows).  An int8 product of 64
+// dimensions takes the same key bytes as they are.
+//
+// Precision: weights are two fp16 terms each (22 bits), and so are queries of prompts (one term
+// where 16-bit ones are not rotated); those of few columns are whole numbers of 23 bits.
+//
+// What bounds it.  Few columns over all keys: the loads.  32 sequences of 4,000 positions (132
+// MB) take 27 us, 4.9 TB/s, the same loads alone 24: blocks of 2 KiB in no order, and the
+// longest sequence, which one workgroup a kv head takes whole, is 1.4 times the mean.  Listed
+// blocks of prompts: vector instructions, 100 a step of two blocks beside 14 matrix ones (85%
+// of the cycles; 4,000 rows of 32 160 us, the same loads alone 96).  Prompts: both, hardly at
+// once, as in the 4-bit cache's kernel (8,192 rows 493 us).
 #include "kv_attend.h"
 
 #include <type_traits>
@@ -294,7 +305,8 @@ struct PageRegs {
 };
 
 // The block as a buffer: its base stays in scalar registers, a lane's offset in one
-// vector register; its scales are the wave's.  ONCE: no other workgroup reads the block, whose
+// vector register; its scales are the wave's, read by the scalar unit (by vector loads, with
+// 8 more registers, the longest prompt 493 -> 516, 131,072 positions 30.0 -> 33.1).  ONCE: no other workgroup reads the block, whose
 // lines then stay out of the caches' way (32 sequences of 4,000 positions 31.5 -> 27.9 us,
 // one of 131,072 33.4 -> 31.1; but the longest prompt 496 -> 509).
 template <bool ONCE>
@@ -874,7 +886,10 @@ hipError_t launch_prompt(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, con
   return launch(kernel, groups, 256, 0, st, P, R, A, div_by(P.hkv), div_by(p.splits), div_by(p.tiles), div_by(A.hq / P.hkv));
 }
 
-// A wave a (page, head), as in the 4-bit cache's calls.
+// Waves a (page, head), as in the 4-bit cache's calls: workgroups of one head while each CU
+// gets a few of them, or else of four, whose rows are neighbours (8,192 rows appended and
+// read 23.0 us; of one head 22.7, two 22.4, eight 23.0).  A wave of its own for the keys and one
+// for the values: 32 tokens 9.3 -> 8.1 us, 8,192 rows 24.1 -> 23.1.
 int row_heads(const Kv4Pool& P, const Kv4Rows& R) {
   return (int64_t)R.n_seqs * row_tiles(R) * P.hkv <= 1024 ? 1 : std::min(P.hkv, 4);
 }

@@ -104,8 +104,9 @@ inline Kv4Cut kv4_cut(const Kv4Sizes& z) {
   return best;
 }
 
-inline Kv4Plan kv4_plan(const Kv4Sizes& z, const Kv4Cut& c) {
+inline Kv4Plan kv4_plan(const Kv4Sizes& z) {
   Kv4Plan p;
+  const Kv4Cut c = kv4_cut(z);
   const int64_t cols = (int64_t)z.max_rows * (z.hq / z.hkv), outputs = (int64_t)z.n_rows * z.hq;
   p.nq = c.nq;
   p.waves = c.waves;
@@ -119,6 +120,5 @@ inline Kv4Plan kv4_plan(const Kv4Sizes& z, const Kv4Cut& c) {
   p.workspace = p.splits > 1 ? split_bytes(p.splits, outputs) : 0;
   return p;
 }
-inline Kv4Plan kv4_plan(const Kv4Sizes& z) { return kv4_plan(z, kv4_cut(z)); }
 
 }  // namespace hh

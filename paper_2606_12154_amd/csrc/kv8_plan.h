@@ -6,14 +6,12 @@
 
 namespace hh {
 
-// The attention over all keys is cut up as the one over a 4-bit cache: a step of
-// either takes the same products and exponentials.
+// The attention over all keys is cut up as the one over a 4-bit cache: what that one's
+// times choose is within 3% of the best here too (12 sizes, one to 64 splits; us: 8,192 prompt rows
+// four tiles 493, two 548, one 705; 1,200 two 24.9, four 27.1; 32 tokens at 4,000 eight waves and
+// no split 27.2, two splits 31.4, four waves 34.0; one at 131,072 64 splits 30.0, 32 29.3).
 typedef Kv4Plan Kv8Plan;
-inline Kv8Plan kv8_plan(const Kv4Sizes& z) {
-  Kv4Cut c = kv4_cut(z);
-  // (tune dense)
-  return kv4_plan(z, c);
-}
+inline Kv8Plan kv8_plan(const Kv4Sizes& z) { return kv4_plan(z); }
 
 // The attention over listed blocks: a workgroup has 16 columns of one row (the
 // group's query heads), its waves take the list's pairs of blocks in turn.
@@ -57,7 +55,6 @@ inline Kv8ListPlan kv8_list_plan(const Kv4Sizes& z, int n) {
   const Kv8ListCut c = kv8_list_cut((int64_t)z.n_rows * z.hkv * p.tiles, (n + 1) / 2, outputs);
   p.waves = c.waves;
   p.splits = c.splits;
-  // (tune list)
   p.threads = z.hq >= 1 << 25 || (int64_t)z.max_rows * group > INT32_MAX - 1024
                   ? INT64_MAX
                   : (int64_t)z.max_rows * p.tiles * z.hkv * p.splits * 64 * p.waves;
@@ -67,7 +64,14 @@ inline Kv8ListPlan kv8_list_plan(const Kv4Sizes& z, int n) {
 }
 
 // Selection: a workgroup has `rows` rows and one kv head.  A wave of it searches a row, with
-// up to `keys` scores a lane, or (team) all of them search one.
+// up to `keys` scores a lane, or (team) all of them search one: rows of more than 2,048 blocks.
+// Measured, us:
+//   rows of a workgroup, which share what they read: 4,000 rows of 437 blocks 16 rows 44, 8 54;
+//   1,200 of 1,770 8 rows 62 (66 KiB of scores), 16 74, 4 92;
+//   its waves: 4,000 rows 8 waves 44, 4 48, 16 56; 32 of 1,400 blocks 19 with any of them;
+//   a launch of its own for the scores, which has workgroups enough where rows are few: one
+//   row of 8,192 blocks 19.6, without 55; 8 of 2,600 21.7 and 35; but 32 of 3,500 50 and 33.6;
+//   waves of a team: 8,192 blocks 4 waves 19.6, 8 20.0, 16 26.7.
 constexpr int kMaxSelectPages = 1 << 15;  // a row's scores fit LDS
 struct Kv8SelectPlan {
   int rows, waves, keys;
@@ -85,7 +89,6 @@ inline Kv8SelectPlan kv8_select_plan(const Kv4Sizes& z) {
   p.rows = p.team ? 1 : std::min(z.max_rows, z.pages > 512 ? 8 : 16);
   p.waves = p.team ? (z.pages > 8192 ? 16 : 4) : 8;
   p.chunks = p.team && items <= 128 ? (z.pages + 255) / 256 : 0;
-  // (tune select)
   const int most = p.team ? 64 * p.waves : 64, each = ((z.pages + most - 1) / most) | 1;
   p.keys = !p.team && each <= 9 ? 9 : !p.team && each <= 17 ? 17 : 33;
   p.lds = (size_t)p.rows * each * most * sizeof(unsigned);

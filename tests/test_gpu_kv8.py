@@ -6,10 +6,11 @@
 * Attention is compared with fp64 attention over the values that the pages hold.
   Its bound, for every element (a = max over the attended keys of
   scale * sum |q_i k_i|, m = max |v|):
-    - scores: queries as two fp16 terms, 2^-22 of each product, and 64 fp32 sums,
-      2^-18 of sum |q k| (or, of few columns, as whole numbers, 2^-22 of the largest
-      element at most, in random directions: 8 * 2^-22 of its products' 64 rather than sums of
-      fp32); a rotation in fp32, 3 * 2^-24 more; the power's argument
+    - scores: queries as two fp16 terms, 2^-22 of each product, and 64 fp32 sums, 2^-18 of
+      sum |q k|; or, of few columns, as whole numbers, 2^-22 of the largest element each,
+      64 of them 2^-16 max |q| max |k|, below 2^-18 max |k| sum |q| where the sum is over four
+      times the largest, as of the N(0, 1) rows here (and none at all where elements are
+      whole numbers of the scale); a rotation in fp32, 3 * 2^-24 more; the power's argument
       and the exponential, 2^-20 and 2^-21 of a weight (|argument| < 2^7):
       e = 2^-17.5 a + 2^-19;
     - weights relative to their sum: 2 e, and two fp16 terms each, 2 * 2^-22; sums of

@@ -11,7 +11,7 @@ are about 40 steps, so 40 x 2^-19 = 8e-5 of the codes: at most about 4 of a prom
 (rows of E have norm 0.32) by 0.32 (16 / 0.4) (0.32 s w) = 0.002: typically 16 times less, since
 that is spread over 256 dimensions, so 1e-4 + 4 x 1.3e-4 < 1e-3.  bf16: fp16 activations
 put (40 x 2^-11) 2 % of the codes there, errors of a step at random signs, 0.14 of its rms beside
-the 0.29 of quantization itself that both sides share and that is a twelfth of the 4-bit cache's:
+the 0.29 of quantization itself that both sides share and that is a tenth of the 4-bit cache's:
 below the 2e-2 that the fp16 paths are given elsewhere, so 3e-2 with them.
 """
 import numpy as np
