@@ -421,7 +421,8 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
  * caller's own device memory.
  *
  * 136 bytes a position and kv head (fp16 takes 256, the 4-bit cache 72), at a
- * tenth of the 4-bit cache's error.  A block (the 16 positions of a page of one kv head)
+ * tenth of the 4-bit cache's error where a page's rows are of like magnitude (1.0% of normal
+ * values; 1.6%, a sixth, where rows differ by factors of e^(0.3 n), n normal).  A block (the 16 positions of a page of one kv head)
  * has one scale for its keys and one for its values, and a summary of its keys, by
  * which a step over a long stream can choose the blocks that it reads.
  *
