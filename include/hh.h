@@ -422,9 +422,10 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
  *
  * 136 bytes a position and kv head (fp16 takes 256, the 4-bit cache 72), at a
  * tenth of the 4-bit cache's error where a page's rows are of like magnitude (1.0% of normal
- * values; 1.6%, a sixth, where rows differ by factors of e^(0.3 n), n normal).  A block (the 16 positions of a page of one kv head)
- * has one scale for its keys and one for its values, and a summary of its keys, by
- * which a step over a long stream can choose the blocks that it reads.
+ * values; 1.6%, a sixth, where rows differ by factors of e^(0.3 n), n normal).  A
+ * block (the 16 positions of a page of one kv head) has one scale for its keys and one for
+ * its values, and a summary of its keys, by which a step over a long stream can choose the
+ * blocks that it reads.
  *
  * Values.  A scale is 2^e, e the least integer from -20 to 9 with max|x| <=
  * 127 * 2^e over the block's keys (or values); a code is

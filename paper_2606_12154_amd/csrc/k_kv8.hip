@@ -307,8 +307,9 @@ struct PageRegs {
 // The block as a buffer: its base stays in scalar registers, a lane's offset in one
 // vector register; its scales are the wave's, read by the scalar unit (by vector loads, with
 // 8 more registers, the longest prompt 493 -> 516, 131,072 positions 30.0 -> 33.1).  ONCE:
-// no other workgroup reads the block, whose lines then stay out of the caches' way (32 sequences of 4,000 positions 31.5 -> 27.9 us,
-// one of 131,072 33.4 -> 31.1; but the longest prompt 496 -> 509).
+// no other workgroup reads the block, whose lines then stay out of the caches' way (32
+// sequences of 4,000 positions 31.5 -> 27.9 us, one of 131,072 33.4 -> 31.1; but the longest
+// prompt 501 -> 509).
 template <bool ONCE>
 __device__ __forceinline__ void load_page(PageRegs& r, const unsigned char* blk, unsigned lane) {
   constexpr int AUX = ONCE ? 2 : 0;

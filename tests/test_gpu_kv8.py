@@ -771,3 +771,113 @@ def test_equal_calls_give_equal_bits():
         attend(c, r, q, "bf16", out, "bf16", ws=torch.full((need,), fill, dtype=torch.uint8, device="cuda:0"))
         outs.append(out)
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+# ------------------------------------------------------------------ the same calls elsewhere
+#
+# Results are compared bit by bit with those of calls that the tests above hold against the
+# oracle: neither where a page or row lies nor what runs beside a call changes a result.
+
+def every_call(c, r, q, t, n=6):
+    """Attention over all keys, selection, and attention over what it selected."""
+    out = [torch.full(q.shape, 7.0, dtype=TYPES[t][1], device="cuda:0") for _ in "ab"]
+    attend(c, r, q, t, out[0], t)
+    blocks = select(c, r, q, t, n, 1, 2)
+    attend(c, r, q, t, out[1], t, blocks=blocks)
+    return out[0], blocks, out[1]
+
+
+@pytest.mark.parametrize("lens,first", [([1, 1], [299, 500]), ([70], [430])])
+def test_pools_past_32_bits_of_bytes(lens, first):
+    hkv, past = 2, [m + f for m, f in zip(lens, first)]
+    c, rng = filled(past, hkv, 8)
+    low = (1 << 32) // (hkv * kv8.BLOCK) + 1  # pages below the ones in use
+    assert low * hkv * kv8.BLOCK > 1 << 32
+    big = Cache(len(lens), hkv, c.max_pages, 8)
+    big.pool = torch.full((low + c.n_pages, hkv, kv8.BLOCK), 255, dtype=torch.uint8, device="cuda:0")
+    big.d_table = ints(big.table + low)
+    big.desc = hh.hh_kv8_pool(big.pool.data_ptr(), big.d_table.data_ptr(), low + c.n_pages, hkv, c.max_pages, len(lens))
+    again = np.random.default_rng(8)
+    x = [again.standard_normal((sum(past), hkv, 64)).astype(np.float32) for _ in "kv"]
+    big.append(past, [0] * len(past), dev(x[0]), dev(x[1]), "f32", ref=False)
+    assert torch.equal(big.pool[low:], c.pool)
+    assert (big.pool[:c.n_pages] == 255).all() and (big.pool[low - c.n_pages:low] == 255).all()
+    for a, b in zip(read(c, past, [0] * len(past), "f32"), read(big, past, [0] * len(past), "f32")):
+        assert torch.equal(a, b)
+    q = dev(rng.standard_normal((sum(lens), 8, 64)), torch.float32)
+    start = np.concatenate([[0], np.cumsum(lens)])
+    r, keep = c.rows(start, first, sum(lens))
+    for a, b in zip(every_call(c, r, q, "f32"), every_call(big, r, q, "f32")):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("lens", [[1, 1, 1, 1], [3, 2, 1, 4], [30, 20, 9, 25]])
+def test_a_table_row_of_several_sequences(lens):
+    """The same stream read at several places in one call, the same place twice among them."""
+    c, rng = filled([900, 400], 2, 17)
+    first, which = [870, 120, 120, 300], [0, 0, 0, 1]
+    start = np.concatenate([[0], np.cumsum(lens)])
+    q = dev(rng.standard_normal((sum(lens), 8, 64)), torch.float32)
+    q[start[2]:start[2] + 1] = q[start[1]:start[1] + 1]
+    r, keep = c.rows(start, first, sum(lens), which)
+    out, blocks, listed = every_call(c, r, q, "f32")
+    assert torch.equal(blocks[start[1]], blocks[start[2]]) and torch.equal(listed[start[1]], listed[start[2]])
+    if lens[1] == lens[2]:  # (how the keys are cut up depends on a sequence's last row)
+        assert torch.equal(out[start[1]], out[start[2]])
+    qf, lists = q.double().cpu().numpy(), blocks.cpu().numpy()
+    for s in range(4):
+        at = slice(start[s], start[s + 1])
+        k, v = c.ref.values(which[s], first[s] + lens[s])
+        e, half = bound(qf[at], k, v, 0.125, "f32")
+        for got, want in ((out[at], kv4.attend(qf[at], k, v, 0.125, first[s])),
+                          (listed[at], listed_reference(qf[at], k, v, 0.125, first[s], lists[at], 2))):
+            assert (np.abs(got.double().cpu().numpy() - want) <= e + half * (np.abs(want) + e)).all(), s
+        for i in range(lens[s]):
+            for h in range(2):
+                want = kv8.select(qf[start[s] + i, 4 * h:4 * h + 4], [p[h] for p in c.ref.blocks[which[s]]], first[s] + i, 6, 1, 2)
+                assert np.array_equal(lists[start[s] + i, h], want)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,first", [([1, 1], [300, 77]), ([40, 3], [200, 16])])
+def test_columns_of_a_wider_matrix(t, lens, first):
+    """Queries, keys and values as one product leaves them, and each by itself."""
+    hkv, hq, n = 2, 8, sum(lens)
+    wide = torch.randn(n, hq + 2 * hkv, 64, device="cuda:0").to(TYPES[t][1])
+    parts = wide[:, :hq], wide[:, hq:hq + hkv], wide[:, hq + hkv:]
+    start, results = np.concatenate([[0], np.cumsum(lens)]), []
+    for q, k, v in (parts, [x.contiguous() for x in parts]):
+        c, rng = filled(first, hkv, 4, max_pages=32)
+        c.append(lens, first, k, v, t, ref=False)
+        r, keep = c.rows(start, first, n)
+        results.append((c.pool, *every_call(c, r, q, t)))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_calls_on_two_streams_at_once():
+    """With outputs and workspaces of their own, on one pool."""
+    c, rng = filled([5000, 3000], 4, 23)
+    r, keep = c.rows(None, [4999, 2999], 2)
+    qs = [torch.randn(2, 16, 64, device="cuda:0") for _ in "ab"]
+    want = [every_call(c, r, q, "f32", 40) for q in qs]
+    need = hh.hh_kv8_attention_workspace(c.desc, r, 16)
+    sel = hh.hh_kv8_select_workspace(c.desc, r, 16, 40)
+    lst = hh.hh_kv8_attention_blocks_workspace(c.desc, r, 16, 40)
+    sides = [torch.cuda.Stream() for _ in qs]
+    ws = [[torch.full((max(b, 1),), 255, dtype=torch.uint8, device="cuda:0") for b in (need, sel, lst)] for _ in qs]
+    out = [[torch.zeros_like(q), torch.zeros(2, 4, 40, dtype=torch.int32, device="cuda:0"), torch.zeros_like(q)] for q in qs]
+    torch.cuda.synchronize()
+    for turn in range(10):
+        for q, s, w, o in zip(qs, sides, ws, out):
+            on = s.cuda_stream
+            hh.hh_kv8_attention(c.desc, r, q.data_ptr(), hh.HH_F32, 1024, 16, 0.125, None, 0, o[0].data_ptr(), hh.HH_F32, 1024,
+                                w[0].data_ptr(), need, on)
+            hh.hh_kv8_select(c.desc, r, q.data_ptr(), hh.HH_F32, 1024, 16, None, 0, 40, 1, 2, o[1].data_ptr(), w[1].data_ptr(),
+                             sel, on)
+            hh.hh_kv8_attention_blocks(c.desc, r, o[1].data_ptr(), 40, q.data_ptr(), hh.HH_F32, 1024, 16, 0.125, None, 0,
+                                       o[2].data_ptr(), hh.HH_F32, 1024, w[2].data_ptr(), lst, on)
+    torch.cuda.synchronize()
+    for a, b in zip(want, out):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
