@@ -487,7 +487,7 @@ hh_status hh_kv8_attention_workspace(const hh_kv8_pool* pool, const hh_kv8_rows*
  * hh_kv4_attention (scale at most 2^100).  Sums, softmax and weights are as there too, and so
  * are the queries of calls with max_rows * (n_heads / n_kv_heads) over 16; those of others are
  * whole numbers of 23 bits in the products, each element off by 2^-22 of the query's largest
- * at most.
+ * at most.  Scores past fp32 are no error: the largest takes all.
  */
 hh_status hh_kv8_attention(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const void* q, int32_t q_dtype,
                            int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len,

@@ -369,6 +369,11 @@ constexpr int kNowhere = 1 << 30;  // a listed block that is none: behind every 
 // listed blocks 177 -> 164 us, 64 sequences of 1,500 positions 22.7 -> 21.7; 16-bit queries
 // that need one term and no scaling lose 0.4 us at the start).  P = 4 takes fewer exponentials
 // a page, but 165 to 195 registers (170 and 25.6).
+// A query's factor is at most 2^80, so that scores (sums below 2^35 of codes, scales to 2^9)
+// are finite.  Where it would be more, different scores lie 2^32 apart at least, and the
+// largest takes all whatever the factor.
+constexpr float kMostFactor = 0x1p80f;
+
 template <int P>
 __device__ __forceinline__ int copy_of() { return (threadIdx.x & 15) / (16 / P); }
 
@@ -407,7 +412,8 @@ __device__ __forceinline__ float make_digits(const RawQuery& q, const Kv4Attend&
     z.d[2][w] = (int)__builtin_amdgcn_perm(d, c, 0x05040100u);
   }
   // (A query that is not finite makes every score NaN.)
-  return top < kInfBits ? fmaxf(__builtin_amdgcn_ldexpf(A.scale * (1.4426950408889634f / 16.f), -e), 1e-37f) : NAN;
+  const float f = __builtin_amdgcn_ldexpf(A.scale * (1.4426950408889634f / 16.f), -e);
+  return top < kInfBits ? __builtin_amdgcn_fmed3f(f, 1e-37f, kMostFactor) : NAN;
 }
 
 // A wave's columns: their queries, bases, sums (of a lane's own slots) and outputs.
@@ -787,6 +793,7 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   C.start(w, most);
   if constexpr (NQ == 1) {
     C.q[0] = make_query<QT>(raw, A);
+    C.q[0].qs = fminf(C.q[0].qs, kMostFactor);
   } else {
     __shared__ f16x8 made[NQ][2 * QT][64];
     __shared__ float made_qs[NQ][64];
@@ -794,7 +801,7 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
       const Query<QT> z = make_query<QT>(raw, A);
 #pragma unroll
       for (int i = 0; i < 2 * QT; ++i) made[wave][i][lane] = i < 2 ? z.h[i] : z.l[i - 2];
-      made_qs[wave][lane] = z.qs;
+      made_qs[wave][lane] = fminf(z.qs, kMostFactor);
     }
     lds_barrier();
 #pragma unroll

@@ -403,6 +403,33 @@ def test_queries_that_are_not_finite():
     assert torch.equal(nan, want)
 
 
+@pytest.mark.parametrize("t,top", [("f32", 2.0 ** 127), ("bf16", 2.0 ** 127), ("f16", 2.0 ** 15)])
+@pytest.mark.parametrize("rows", [1, 20])
+@pytest.mark.parametrize("listed", [False, True])
+def test_scores_past_fp32(t, top, rows, listed):
+    """scale * q . k above 2^128: the largest score takes all, and keys that a query does not
+    see (a product of 0) count alike.  One weight of 1, or 40 equal ones in two fp16
+    terms: 2^-22 each and in their sum, and 40 sums of 2^-24."""
+    scale, n, rng = 2.0 ** 100, 40, np.random.default_rng(2)
+    for seen in (True, False):
+        k = np.zeros((n, 1, 64), np.float32)
+        k[:, 0, 0 if seen else 1] = 7 * np.arange(n) % n - 20  # (exact in the cache, no two alike)
+        v = rng.standard_normal((n, 1, 64)).astype(np.float32)
+        c = Cache(1, 1, 3)
+        c.append([n], [0], dev(k), dev(v), "f32")
+        q = np.zeros((rows, 4, 64), np.float32)
+        q[:, :, 0] = top
+        r, keep = c.rows([0, rows], [n - rows], rows)
+        out = torch.empty(rows, 4, 64, device="cuda:0")
+        blocks = dev(np.tile(np.arange(3, dtype=np.int32), (rows, 1, 1))) if listed else None
+        attend(c, r, dev(q).to(TYPES[t][1]), t, out, "f32", scale, blocks=blocks)
+        kk, vv = c.ref.values(0, n)
+        want = kv4.attend(q.astype(np.float64), kk, vv, scale, n - rows)
+        assert np.isfinite(want).all()
+        err = np.abs(out.double().cpu().numpy() - want)
+        assert (err <= np.abs(vv).max() * (2 * 2.0 ** -22 + 40 * 2.0 ** -24 + 2.0 ** -24)).all(), (seen, err.max())
+
+
 def test_weights_far_apart():
     """One key takes nearly all of the weight and has a small value; the many others'
     weights of about 2^-20 make the sum of its other dimensions."""
