@@ -70,7 +70,8 @@ inline Kv8ListPlan kv8_list_plan(const Kv4Sizes& z, int n) {
 //   1,200 of 1,770 8 rows 62 (66 KiB of scores), 16 74, 4 92;
 //   its waves: 4,000 rows 8 waves 44, 4 48, 16 56; 32 of 1,400 blocks 19 with any of them;
 //   a launch of its own for the scores, which has workgroups enough where rows are few: one
-//   row of 8,192 blocks 19.6, without 55; 8 of 2,600 21.7 and 35; but 32 of 3,500 50 and 33.6;
+//   row of 8,192 blocks 19.6, without 55; 8 of 2,600 21.7 and 35; but 32 of 3,500 50 and 33.6
+//   (33.6 in most runs, 45 to 47 in others of the same code, for a reason not known);
 //   waves of a team: 8,192 blocks 4 waves 19.6, 8 20.0, 16 26.7.
 constexpr int kMaxSelectPages = 1 << 15;  // a row's scores fit LDS
 struct Kv8SelectPlan {
