@@ -371,8 +371,9 @@ constexpr int kNowhere = 1 << 30;  // a listed block that is none: behind every 
 // a page, but 165 to 195 registers (170 and 25.6).
 // A query's factor is at most 2^80, so that scores (sums below 2^35 of codes, scales to 2^9)
 // are finite.  Where it would be more, different scores lie 2^32 apart at least, and the
-// largest takes all whatever the factor.
-constexpr float kMostFactor = 0x1p80f;
+// largest takes all whatever the factor.  Where it would be less than 2^-100, scores are below
+// 2^-56, and all weights 1.
+constexpr float kMostFactor = 0x1p80f, kLeastFactor = 0x1p-100f;
 
 template <int P>
 __device__ __forceinline__ int copy_of() { return (threadIdx.x & 15) / (16 / P); }
@@ -381,7 +382,7 @@ struct Digits {
   i32x4 d[3];
 };
 __device__ __forceinline__ i32x4 no_digits() { return i32x4{0, 0, 0, 0}; }
-// The lane's 16 dimensions as digits, and the factor of scores to powers of two.
+// The lane's 16 dimensions as digits, and the power of two that scores take.
 __device__ __forceinline__ float make_digits(const RawQuery& q, const Kv4Attend& A, Digits& z) {
   float x[16];
   raw_values(q.row, A.q_type, x);
@@ -393,18 +394,21 @@ __device__ __forceinline__ float make_digits(const RawQuery& q, const Kv4Attend&
       x[8 + i] = v * co + u * si;
     }
   }
+  // The scores' factor to powers of two, but for a power of two itself, goes into the query: then
+  // a whole number times what is left is exact, and equal scores stay equal whatever their base.
+  const float to_powers = A.scale * (1.4426950408889634f / 16.f), part = __builtin_amdgcn_frexp_mantf(to_powers);
   unsigned top = 0u;
 #pragma unroll
   for (int i = 0; i < 16; ++i) top = max(top, magnitude(x[i]));
   top = rows_max(top);
   // The largest becomes a number from 2^21 to 2^22.
-  const int e = top > 0u && top < kInfBits ? 22 - __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
+  const int e = top > 0u && top < kInfBits ? 22 - __builtin_amdgcn_frexp_expf(__uint_as_float(top) * part) : 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     unsigned y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      y[i] = ((unsigned)(int)rintf(__builtin_amdgcn_ldexpf(top < kInfBits ? x[4 * w + i] : 0.f, e)) + 0x808080u) ^ 0x808080u;
+      y[i] = ((unsigned)(int)rintf(__builtin_amdgcn_ldexpf(top < kInfBits ? x[4 * w + i] : 0.f, e) * part) + 0x808080u) ^ 0x808080u;
     const unsigned a = __builtin_amdgcn_perm(y[1], y[0], 0x05010400u), b = __builtin_amdgcn_perm(y[3], y[2], 0x05010400u);
     const unsigned c = __builtin_amdgcn_perm(y[1], y[0], 0x0c0c0602u), d = __builtin_amdgcn_perm(y[3], y[2], 0x0c0c0602u);
     z.d[0][w] = (int)__builtin_amdgcn_perm(b, a, 0x05040100u);
@@ -412,8 +416,8 @@ __device__ __forceinline__ float make_digits(const RawQuery& q, const Kv4Attend&
     z.d[2][w] = (int)__builtin_amdgcn_perm(d, c, 0x05040100u);
   }
   // (A query that is not finite makes every score NaN.)
-  const float f = __builtin_amdgcn_ldexpf(A.scale * (1.4426950408889634f / 16.f), -e);
-  return top < kInfBits ? __builtin_amdgcn_fmed3f(f, 1e-37f, kMostFactor) : NAN;
+  const float f = __builtin_amdgcn_ldexpf(1.f, __builtin_amdgcn_frexp_expf(to_powers) - e);
+  return top < kInfBits ? __builtin_amdgcn_fmed3f(f, kLeastFactor, kMostFactor) : NAN;
 }
 
 // A wave's columns: their queries, bases, sums (of a lane's own slots) and outputs.
@@ -448,7 +452,6 @@ struct Few {
   template <bool MASK>
   __device__ __forceinline__ void step(const PageRegs (&x)[2], const Places& at) {
     const int g = (threadIdx.x & 63) >> 4, side = copy_of<P>();
-    float sc[N];
     float scale[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -467,13 +470,10 @@ struct Few {
       }
     }
     const float mine = P == 2 && side ? scale[1] : scale[0];
-    float high = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const i32x4* y = acc[P == 1 ? i >> 2 : 0];
-      const float s = fmaf((float)y[2][i & 3], 65536.f, fmaf((float)y[1][i & 3], 256.f, (float)y[0][i & 3]));
-      sc[i] = fmaf(s, P == 1 ? scale[i >> 2] : mine, -base);
-    }
+    // Scores as whole numbers, and each page's largest of those that are neither hidden nor
+    // marked.  Weights are taken against the base that these leave (see base_for).
+    float s[N], most[N / 4], high = -INFINITY;
+    bool hidden[N], marked[N];
     if constexpr (MASK) {
       unsigned bad[2];
 #pragma unroll
@@ -482,25 +482,46 @@ struct Few {
       const int from = P == 2 && side ? at.v[1] : at.v[0];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if ((P == 1 ? bad[i >> 2] : of) >> (4 * g + (i & 3)) & 1u) sc[i] = NAN;
-        if ((P == 1 ? at.v[i >> 2] : from) + 4 * g + (i & 3) >= lim) sc[i] = -INFINITY;
+        marked[i] = (P == 1 ? bad[i >> 2] : of) >> (4 * g + (i & 3)) & 1u;
+        hidden[i] = (P == 1 ? at.v[i >> 2] : from) + 4 * g + (i & 3) >= lim;
       }
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) high = fmaxf(high, sc[i]);
-    if (any_fresh || __builtin_amdgcn_ballot_w64(high > kOffset + kSlack)) {
-      const float mx = rows_max(high);
-      float up = mx > -INFINITY ? mx - kOffset : 0.f;
-      if (!fresh) up = fmaxf(up, 0.f);
-      const float f = fresh ? 1.f : __builtin_amdgcn_exp2f(-up);
-      base += up;
-      sum *= f;
+    for (int u = 0; u < N / 4; ++u) {
+      const i32x4* y = acc[u];
+      most[u] = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < N; ++i) sc[i] -= up;
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * u + j;
+        s[i] = fmaf((float)y[2][j], 65536.f, fmaf((float)y[1][j], 256.f, (float)y[0][j]));
+        most[u] = fmaxf(most[u], MASK && (hidden[i] || marked[i]) ? -INFINITY : s[i]);
+      }
+      high = fmaxf(high, fmaf(most[u], P == 1 ? scale[u] : mine, -base));
+    }
+    if (any_fresh || __builtin_amdgcn_ballot_w64(high > kOffset + kSlack)) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < N / 4; ++u) mx = fmaxf(mx, most[u] * (P == 1 ? scale[u] : mine));
+      mx = rows_max(mx);
+      float to = mx > -INFINITY ? base_for(mx) : base;
+      if (!fresh) to = fmaxf(to, base);
+      const float f = fresh ? 1.f : __builtin_amdgcn_exp2f(base - to);
+      base = to;
+      sum *= f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] *= f;
       fresh = fresh && !(mx > -INFINITY);
       any_fresh = __builtin_amdgcn_ballot_w64(fresh);
+    }
+    float sc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sc[i] = fmaf(s[i], P == 1 ? scale[i >> 2] : mine, -base);
+    if constexpr (MASK) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (marked[i]) sc[i] = NAN;
+        if (hidden[i]) sc[i] = -INFINITY;
+      }
     }
     f16x2 h[N / 2], l[N / 2];
 #pragma unroll

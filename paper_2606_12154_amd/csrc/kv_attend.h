@@ -43,6 +43,17 @@ __device__ __forceinline__ f16x8 join8(f16x4 a, f16x4 b) {
 // lanes (8,192-token prompt 513 us, as with an offset of 2^7 and a slack of 2^8).
 constexpr float kOffset = 12.f, kSlack = 3.9f;
 
+// A base decides a step's weights only as a number: it is found first, and then every
+// weight's power is one rounding of S qs - base, the same for equal scores in whatever step they
+// come.  Where the base is kLarge or more, the exact product's own last bits would pass its
+// rounding by more than the slack, so that S qs is rounded by itself, and the base is the largest.
+constexpr float kLarge = 65536.f;
+__device__ __forceinline__ float base_for(float top) { return fabsf(top) < kLarge ? top - kOffset : top; }
+__device__ __forceinline__ float rounded(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
 // Loads in flight need not land at this barrier: it orders LDS alone.
 __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -144,9 +155,11 @@ struct Columns {
   f32x4 o[NQ][4], sum[NQ];
   float base[NQ];
   bool first;
+  bool large;  // a base is kLarge or more
 
   __device__ __forceinline__ void start(const Place& w, int most) {
     first = true;
+    large = false;
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
 #pragma unroll
@@ -192,50 +205,65 @@ struct Columns {
   }
 
   // MASK: slots past a column's keys (the pages' first positions are at0 and at1), and
-  // bad ones (N bits), whose keys or values are NaN.  The check of all columns' scores is
-  // the step's only branch.
+  // bad ones (N bits), whose keys or values are NaN.  The check of all columns' largest scores
+  // is the step's only branch, but for large bases.
   template <bool MASK>
-  __device__ __forceinline__ void weights(const f32x4 (*sc)[2], int at0, int at1, unsigned bad, f16x8* ph, f16x8* pl) {
+  __device__ __forceinline__ void weights(f32x4 (*sc)[2], int at0, int at1, unsigned bad, f16x8* ph, f16x8* pl) {
     const int g = (threadIdx.x & 63) >> 4;
-    float x[NQ][N], high = -INFINITY;
+    float top[NQ], high = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < NQ; ++t)
+    for (int t = 0; t < NQ; ++t) {
+      top[t] = -INFINITY;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        x[t][i] = fmaf(sc[t][i >> 2][i & 3], q[t].qs, -base[t]);
         if constexpr (MASK) {
-          if (bad >> i & 1u) x[t][i] = NAN;
-          if (((PACK == 2 ? right() : i >> 2) ? at1 : at0) + 4 * g + (i & 3) >= lim[t]) x[t][i] = -INFINITY;
+          if (bad >> i & 1u) sc[t][i >> 2][i & 3] = NAN;
+          if (((PACK == 2 ? right() : i >> 2) ? at1 : at0) + 4 * g + (i & 3) >= lim[t]) sc[t][i >> 2][i & 3] = -INFINITY;
         }
-        high = fmaxf(high, x[t][i]);
+        top[t] = fmaxf(top[t], sc[t][i >> 2][i & 3]);
       }
+      high = fmaxf(high, fmaf(top[t], q[t].qs, -base[t]));
+    }
     // A wave's first pages set the base: a column that sees none of them sees
     // none of the later ones either.
     if (first || __builtin_amdgcn_ballot_w64(high > kOffset + kSlack)) {
+      bool is_large = false;
 #pragma unroll
       for (int t = 0; t < NQ; ++t) {
-        float mx = x[t][0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[t][i]);
-        mx = rows_max(mx);
-        float up = mx > -INFINITY ? mx - kOffset : 0.f;
-        if (!first) up = fmaxf(up, 0.f);
-        const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
-        base[t] += up;
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[t][i] -= up;
+        const float mx = rounded(rows_max(top[t]), q[t].qs);
+        float to = mx > -INFINITY ? base_for(mx) : base[t];
+        if (!first) to = fmaxf(to, base[t]);
+        const float f = first ? 1.f : __builtin_amdgcn_exp2f(base[t] - to);
+        base[t] = to;
+        is_large = is_large || !(fabsf(to) < kLarge);
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[t][j] *= f;
         sum[t] *= f;
       }
+      large = __builtin_amdgcn_ballot_w64(is_large);
     }
     first = false;
+    if (large) {
+#pragma unroll
+      for (int t = 0; t < NQ; ++t)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float x = sc[t][i >> 2][i & 3];
+          sc[t][i >> 2][i & 3] = fabsf(base[t]) < kLarge ? fmaf(x, q[t].qs, -base[t]) : rounded(x, q[t].qs) - base[t];
+        }
+    } else {
+#pragma unroll
+      for (int t = 0; t < NQ; ++t)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sc[t][i >> 2][i & 3] = fmaf(sc[t][i >> 2][i & 3], q[t].qs, -base[t]);
+    }
 #pragma unroll
     for (int t = 0; t < NQ; ++t)
 #pragma unroll
       for (int i = 0; i < N; i += 2) {
         f16x2 h, l;
-        split_weights(__builtin_amdgcn_exp2f(x[t][i]), __builtin_amdgcn_exp2f(x[t][i + 1]), h, l);
+        const float a = sc[t][i >> 2][i & 3], b = sc[t][(i + 1) >> 2][(i + 1) & 3];
+        split_weights(__builtin_amdgcn_exp2f(a), __builtin_amdgcn_exp2f(b), h, l);
         ph[t][i] = h[0];
         ph[t][i + 1] = h[1];
         pl[t][i] = l[0];
