@@ -407,6 +407,7 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
  * weights are fp16 pairs (22 bits), and so are queries, scaled by a power of two
  * (16-bit ones that are not rotated are single fp16 numbers, exactly); a weight
  * is 2^-37 of its row's largest off at most, so that smaller ones may count as 0.
+ * A query with an infinity or NaN gives NaN where its row sees a key.
  * Equal calls give equal bits.
  * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
  * UNSUPPORTED (max_rows * n_heads near 2^30 and above, n_heads from 2^25 on), HIP.
@@ -487,7 +488,8 @@ hh_status hh_kv8_attention_workspace(const hh_kv8_pool* pool, const hh_kv8_rows*
  * hh_kv4_attention (scale at most 2^100).  Sums, softmax and weights are as there too, and so
  * are the queries of calls with max_rows * (n_heads / n_kv_heads) over 16; those of others are
  * whole numbers of 23 bits in the products, each element off by 2^-22 of the query's largest
- * at most.  Scores past fp32 are no error: the largest takes all.
+ * at most.  Scores past fp32 are no error: the largest takes all.  A query with an infinity or
+ * NaN gives NaN where its row sees a key.
  */
 hh_status hh_kv8_attention(const hh_kv8_pool* pool, const hh_kv8_rows* rows, const void* q, int32_t q_dtype,
                            int64_t q_stride, int32_t n_heads, float scale, const float* rope, int32_t rope_len,

@@ -78,6 +78,8 @@ struct RawQuery {
 // rotated.  Queries (but for fp16 ones of one term) are scaled by a power of two that puts
 // a row's largest element into [2^13, 2^14), so that one term holds any 16-bit
 // query and two hold 22 bits of an fp32 one.
+// An infinity makes its query's scores NaN, as it makes their softmax: as products they could all be
+// -Inf, which stands for hidden keys.
 template <int QT>
 struct Query {
   f16x8 h[2], l[QT == 2 ? 2 : 1];
@@ -110,6 +112,10 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
   if (QT == 1 && A.q_type == kRowF16) {
     z.h[0] = __builtin_bit_cast(f16x8, q.row.w[0]);
     z.h[1] = __builtin_bit_cast(f16x8, q.row.w[1]);
+    unsigned bad = 0u;  // (a carry into the sign: exponents of infinities and NaN)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bad |= (q.row.w[i >> 2][i & 3] & 0x7fff7fffu) + 0x04000400u;
+    if (bad & 0x80008000u) z.h[0][0] = (_Float16)NAN;
     z.qs = fmaxf(A.scale * 1.4426950408889634f, 1e-37f);
     return z;
   }
@@ -137,6 +143,7 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
     z.h[i >> 3][i & 7] = h;
     if constexpr (QT == 2) z.l[i >> 3][i & 7] = (_Float16)(y - (float)h);
   }
+  if (top == INFINITY) z.h[0][0] = (_Float16)NAN;
   return z;
 }
 
