@@ -398,8 +398,10 @@ hipError_t kv8_select(hipStream_t st, const Kv4Pool& P, const Kv4Rows& R, const 
                         : p.keys == 17 ? k_kv8_select<17, false, false>
                                        : k_kv8_select<33, false, false>;
   if (p.lds > 64 << 10) {
-    // More LDS than a kernel may have unasked.
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds);
+    // More LDS than a kernel may have unasked.  The limit is the process's, so that it is set to the
+    // kernel's most: a call on another thread may have one of its own between this one's and its launch.
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)(p.team ? kMostTeamLds : kMostRowsLds));
     if (e != hipSuccess) return e;
   }
   const int tiles = (R.max_rows + p.rows - 1) / p.rows;

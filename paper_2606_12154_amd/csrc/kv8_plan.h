@@ -82,6 +82,8 @@ struct Kv8SelectPlan {
   int64_t threads;   // of a sequence's larger grid
   size_t workspace;  // bytes
 };
+// The most that a call asks for: 33 scores of each thread, of a team of 1,024 or of 8 waves.
+constexpr size_t kMostTeamLds = (size_t)33 * 1024 * sizeof(unsigned), kMostRowsLds = (size_t)33 * 512 * sizeof(unsigned);
 inline int kv8_score_pitch(int pages) { return (pages + 15) / 16 * 16; }
 inline Kv8SelectPlan kv8_select_plan(const Kv4Sizes& z) {
   Kv8SelectPlan p;
