@@ -455,7 +455,9 @@ struct Few {
     float scale[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const unsigned s = !MASK && x[i].s[1] ? 0x7e00u : x[i].s[0] & 0xffffu;  // (as in operands)
+      // (Marks as in operands.  Where a block is none, whatever is read in its place may have any scale.)
+      const unsigned held = MASK && at.v[i] == kNowhere ? 0u : x[i].s[0];
+      const unsigned s = !MASK && x[i].s[1] ? 0x7e00u : held & 0xffffu;
       scale[i] = qs * from_half(s);
     }
     i32x4 acc[P == 1 ? 2 : 1][3];
@@ -540,7 +542,6 @@ struct Few {
     Scale vs[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      // (A block that is none has no values: what is read in its place may have any scale.)
       const unsigned s = MASK && at.v[i] == kNowhere ? 0u : x[i].s[0];
       vs[i] = scale_of(__builtin_amdgcn_perm(s, s, 0x03020302u));
     }

@@ -18,7 +18,7 @@ from kv4_cases import CASES
 from kv8_cases import LISTS, LONG
 from paper_2606_12154_amd import hh
 from test_gpu_kv4_forms import HALF_STEP, check
-from test_gpu_kv8 import TYPES, Cache, attend, dev, ints, read, rope_table, select, stream
+from test_gpu_kv8 import TYPES, Cache, attend, bound, dev, ints, listed_reference, read, rope_table, select, stream
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -281,3 +281,25 @@ def test_captured_selections_replay(pages, rows, n):
         call()
         torch.cuda.synchronize()
         assert torch.equal(got, out) and (got >= 0).all() and (got[..., 1:] > got[..., :-1]).all()
+
+
+# ------------------------------------------------------------------ whatever lies in pages that no row sees
+
+@pytest.mark.parametrize("bits", [0xffff, 0xbc00, 0x3c00, 0x7c00, 0xfc00, 0x0000, 0x8000, 0xfbff, 0x7bff])
+@pytest.mark.parametrize("group", [4, 12])
+def test_entries_that_are_none_beside_any_bytes(bits, group):
+    """A sequence whose first pages were never written, and lists of its others with entries that are none:
+    the page that is read in their place may have any scale, negative and infinite ones too."""
+    torch.manual_seed(1)
+    c = Cache(1, 1, 6)
+    c.pool.view(torch.int16).fill_(bits - (bits >> 15 << 16))
+    k, v = (torch.randn(64, 1, 64, device="cuda:0") for _ in "kv")
+    c.append([64], [32], k, v, "f32")
+    lists = np.array([[2, -1, -1, 3, 5, -1, -1, -1], [-1, -1, 4, -1, -1, 99, 2, -1], [5, -1, -1, -1, -1, -1, -1, -1]], np.int32)[:, None]
+    q = torch.randn(3, group, 64, device="cuda:0")
+    out = torch.full(q.shape, 3.0, device="cuda:0")
+    r, keep = c.rows([0, 3], [93], 3)
+    attend(c, r, q, "f32", out, "f32", blocks=ints(lists))
+    want = listed_reference(q.double().cpu().numpy(), *c.ref.values(0, 96), 0.125, 93, lists, 1)
+    e, half = bound(q.double().cpu().numpy(), *(x[32:] for x in c.ref.values(0, 96)), 0.125, "f32")
+    assert (np.abs(out.double().cpu().numpy() - want) <= e + half * (np.abs(want) + e)).all()
