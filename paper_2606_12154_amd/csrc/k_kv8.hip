@@ -429,6 +429,7 @@ struct Few {
   };
   Digits q[P];
   float qs, base, sum;
+  float limit;  // scores above it raise the base
   int lim;  // keys that the column sees
   f32x4 o[4];
   bool fresh;      // the column has seen no key yet
@@ -441,7 +442,7 @@ struct Few {
     for (int i = 0; i < P; ++i)
 #pragma unroll
       for (int j = 0; j < 3; ++j) q[i].d[j] = P == 1 || copy_of<P>() == i ? z.d[j] : no_digits();
-    base = sum = 0.f;
+    base = sum = limit = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     lim = min(max(w.s.first + column_row(w, w.c0 + column_of<P>()) + 1, 0), most);
@@ -472,9 +473,9 @@ struct Few {
       }
     }
     const float mine = P == 2 && side ? scale[1] : scale[0];
-    // Scores as whole numbers, and each page's largest of those that are neither hidden nor
-    // marked.  Weights are taken against the base that these leave (see base_for).
-    float s[N], most[N / 4], high = -INFINITY;
+    // Scores as whole numbers, and the largest of those that are neither hidden nor marked.
+    // Weights are taken against the base that it leaves (see base_for).
+    float s[N], high = -INFINITY;
     bool hidden[N], marked[N];
     if constexpr (MASK) {
       unsigned bad[2];
@@ -491,24 +492,22 @@ struct Few {
 #pragma unroll
     for (int u = 0; u < N / 4; ++u) {
       const i32x4* y = acc[u];
-      most[u] = -INFINITY;
+      float most = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int i = 4 * u + j;
         s[i] = fmaf((float)y[2][j], 65536.f, fmaf((float)y[1][j], 256.f, (float)y[0][j]));
-        most[u] = fmaxf(most[u], MASK && (hidden[i] || marked[i]) ? -INFINITY : s[i]);
+        most = fmaxf(most, MASK && (hidden[i] || marked[i]) ? -INFINITY : s[i]);
       }
-      high = fmaxf(high, fmaf(most[u], P == 1 ? scale[u] : mine, -base));
+      high = u ? fmaxf(high, most * scale[u]) : most * (P == 1 ? scale[0] : mine);
     }
-    if (any_fresh || __builtin_amdgcn_ballot_w64(high > kOffset + kSlack)) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < N / 4; ++u) mx = fmaxf(mx, most[u] * (P == 1 ? scale[u] : mine));
-      mx = rows_max(mx);
+    if (any_fresh || __builtin_amdgcn_ballot_w64(high > limit)) {
+      const float mx = rows_max(fmaxf(high, -INFINITY));  // (NaN, of what is not finite, counts as none)
       float to = mx > -INFINITY ? base_for(mx) : base;
       if (!fresh) to = fmaxf(to, base);
       const float f = fresh ? 1.f : __builtin_amdgcn_exp2f(base - to);
       base = to;
+      limit = fabsf(base) < kLarge ? base + (kOffset + kSlack) : base;
       sum *= f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] *= f;
