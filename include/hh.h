@@ -407,8 +407,8 @@ hh_status hh_kv4_attention_workspace(const hh_kv4_pool* pool, const hh_kv4_rows*
  * weights are fp16 pairs (22 bits), and so are queries, scaled by a power of two
  * (16-bit ones that are not rotated are single fp16 numbers, exactly); a weight
  * is 2^-37 of its row's largest off at most, so that smaller ones may count as 0.
- * A query with an infinity or NaN gives NaN where its row sees a key.
- * Equal calls give equal bits.
+ * Scores past fp32 are no error: the largest takes all.  A query with an infinity
+ * or NaN gives NaN where its row sees a key.  Equal calls give equal bits.
  * Errors: INVALID_ARG (as above; a workspace that is too small; scale),
  * UNSUPPORTED (max_rows * n_heads near 2^30 and above, n_heads from 2^25 on), HIP.
  */

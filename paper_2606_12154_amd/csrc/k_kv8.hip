@@ -369,11 +369,8 @@ constexpr int kNowhere = 1 << 30;  // a listed block that is none: behind every 
 // listed blocks 177 -> 164 us, 64 sequences of 1,500 positions 22.7 -> 21.7; 16-bit queries
 // that need one term and no scaling lose 0.4 us at the start).  P = 4 takes fewer exponentials
 // a page, but 165 to 195 registers (170 and 25.6).
-// A query's factor is at most 2^80, so that scores (sums below 2^35 of codes, scales to 2^9)
-// are finite.  Where it would be more, different scores lie 2^32 apart at least, and the
-// largest takes all whatever the factor.  Where it would be less than 2^-100, scores are below
-// 2^-56, and all weights 1.
-constexpr float kMostFactor = 0x1p80f, kLeastFactor = 0x1p-100f;
+// Where a query's factor would be less than 2^-100, scores are below 2^-56, and all weights 1.
+constexpr float kLeastFactor = 0x1p-100f;
 
 template <int P>
 __device__ __forceinline__ int copy_of() { return (threadIdx.x & 15) / (16 / P); }
@@ -814,7 +811,6 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   C.start(w, most);
   if constexpr (NQ == 1) {
     C.q[0] = make_query<QT>(raw, A);
-    C.q[0].qs = fminf(C.q[0].qs, kMostFactor);
   } else {
     __shared__ f16x8 made[NQ][2 * QT][64];
     __shared__ float made_qs[NQ][64];
@@ -822,7 +818,7 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
       const Query<QT> z = make_query<QT>(raw, A);
 #pragma unroll
       for (int i = 0; i < 2 * QT; ++i) made[wave][i][lane] = i < 2 ? z.h[i] : z.l[i - 2];
-      made_qs[wave][lane] = fminf(z.qs, kMostFactor);
+      made_qs[wave][lane] = z.qs;
     }
     lds_barrier();
 #pragma unroll

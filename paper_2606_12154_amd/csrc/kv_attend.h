@@ -78,6 +78,11 @@ struct RawQuery {
 // rotated.  Queries (but for fp16 ones of one term) are scaled by a power of two that puts
 // a row's largest element into [2^13, 2^14), so that one term holds any 16-bit
 // query and two hold 22 bits of an fp32 one.
+// Scores' factor to powers of two is at most 2^80, so that they (sums below 2^37) are finite.
+// Where it would be more, different scores lie 2^32 apart at least (queries and keys are
+// multiples of 2^-24, whole ones in few columns on the 8-bit cache of 2^-20), and the largest takes all
+// whatever the factor.
+constexpr float kMostFactor = 0x1p80f;
 // An infinity makes its query's scores NaN, as it makes their softmax: as products they could all be
 // -Inf, which stands for hidden keys.
 template <int QT>
@@ -116,7 +121,7 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
 #pragma unroll
     for (int i = 0; i < 8; ++i) bad |= (q.row.w[i >> 2][i & 3] & 0x7fff7fffu) + 0x04000400u;
     if (bad & 0x80008000u) z.h[0][0] = (_Float16)NAN;
-    z.qs = fmaxf(A.scale * 1.4426950408889634f, 1e-37f);
+    z.qs = __builtin_amdgcn_fmed3f(A.scale * 1.4426950408889634f, 1e-37f, kMostFactor);
     return z;
   }
   float x[16];
@@ -135,7 +140,7 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
   top = rows_max(top);
   int e = 0;
   if (top > 0.f && top < INFINITY) e = 14 - __builtin_amdgcn_frexp_expf(top);
-  z.qs = fmaxf(__builtin_amdgcn_ldexpf(A.scale * 1.4426950408889634f, -e), 1e-37f);
+  z.qs = __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(A.scale * 1.4426950408889634f, -e), 1e-37f, kMostFactor);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float y = __builtin_amdgcn_ldexpf(x[i], e);

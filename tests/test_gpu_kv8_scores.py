@@ -84,3 +84,35 @@ def test_equal_scores_of_a_4_bit_cache(t, rows, n, order, size):
     out = torch.empty(rows, 4, 64, device="cuda:0")
     four.attend(c, r, q, t, out, "f32", 0.125)
     compare(out, back[1].double().cpu().numpy(), low, rows)
+
+
+@pytest.mark.parametrize("t,top", [("f32", 2.0 ** 127), ("bf16", 2.0 ** 127), ("f16", 2.0 ** 15)])
+@pytest.mark.parametrize("rows", [1, 3, 20, 200])
+def test_scores_past_fp32_of_a_4_bit_cache(t, top, rows):
+    """scale * q . k above 2^128: the largest score takes all, and keys that a query does not see (a product of 0)
+    count alike. Weights as in test_gpu_kv8.py: two fp16 terms, 2^-22 each and in their sum, and sums of 2^-24."""
+    scale, n = 2.0 ** 100, 205
+    rng = np.random.default_rng(2)
+    for seen in (True, False):
+        k = np.zeros((n, 1, 64), np.float32)
+        k[:, 0, 0 if seen else 1] = np.repeat(np.arange(n // 5), 5)[:n] % 41 + 1.0
+        k[::7, 0, 0 if seen else 1] *= -1
+        k[100, 0, 0 if seen else 1] = 50.0
+        v = rng.standard_normal((n, 1, 64)).astype(np.float32)
+        c = four.Cache(1, 1, (n + 15) // 16, 0)
+        r, keep = c.rows([0, n], [0], n)
+        four.append(c, r, dev(k), dev(v), "f32")
+        back = [torch.empty(n, 1, 64, device="cuda:0") for _ in "kv"]
+        hh.hh_kv4_read(c.desc, r, back[0].data_ptr(), back[1].data_ptr(), hh.HH_F32, 64, 64, torch.cuda.current_stream().cuda_stream)
+        q = torch.zeros(rows, 4, 64, device="cuda:0")
+        q[:, :, 0] = top
+        r, keep = c.rows([0, rows], [n - rows], rows)
+        out = torch.empty(rows, 4, 64, device="cuda:0")
+        four.attend(c, r, q.to(TYPES[t][1]), t, out, "f32", scale)
+        kk, vv = (a.double().cpu().numpy()[:, 0] for a in back)
+        for i in range(rows):
+            m = n - rows + i + 1
+            best = np.flatnonzero(kk[:m, 0] == kk[:m, 0].max())
+            want = vv[best].mean(0)
+            err = np.abs(out[i].double().cpu().numpy() - want)
+            assert (err <= np.abs(vv).max() * (2 * 2.0 ** -22 + (m / 32 + 16) * 2.0 ** -23 + 3 * 2.0 ** -19)).all(), (seen, i, err.max())
