@@ -778,6 +778,7 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
   const int* row = P.table + (size_t)s.trow * P.max_pages;
   constexpr int STEP = 2 * W;
   int p = p0 + 2 * wave;
+  const int from = p < p1 ? p * kPage : INT_MAX - kPage;
   const int last = max(p + (p1 - 1 - p) / STEP * STEP, 0);
   unsigned ids[2];
   auto load_ids = [&](int q) {
@@ -873,6 +874,8 @@ k_kv8_attend(Kv4Pool P, Kv4Rows R, Kv4Attend A, Div heads, Div splits_, Div tile
     a[1] = c[1];
     p += STEP;
   }
+
+  C.finish(from);
 
   // Join the waves: wave v takes dimensions 16 g + 4 v .. + 3.
   __shared__ f32x4 lo[W][4][64];

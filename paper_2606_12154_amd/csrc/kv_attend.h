@@ -83,8 +83,6 @@ struct RawQuery {
 // multiples of 2^-24, whole ones in few columns on the 8-bit cache of 2^-20), and the largest takes all
 // whatever the factor.
 constexpr float kMostFactor = 0x1p80f;
-// An infinity makes its query's scores NaN, as it makes their softmax: as products they could all be
-// -Inf, which stands for hidden keys.
 template <int QT>
 struct Query {
   f16x8 h[2], l[QT == 2 ? 2 : 1];
@@ -117,10 +115,6 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
   if (QT == 1 && A.q_type == kRowF16) {
     z.h[0] = __builtin_bit_cast(f16x8, q.row.w[0]);
     z.h[1] = __builtin_bit_cast(f16x8, q.row.w[1]);
-    unsigned bad = 0u;  // (a carry into the sign: exponents of infinities and NaN)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) bad |= (q.row.w[i >> 2][i & 3] & 0x7fff7fffu) + 0x04000400u;
-    if (bad & 0x80008000u) z.h[0][0] = (_Float16)NAN;
     z.qs = __builtin_amdgcn_fmed3f(A.scale * 1.4426950408889634f, 1e-37f, kMostFactor);
     return z;
   }
@@ -148,7 +142,6 @@ __device__ __forceinline__ Query<QT> make_query(const RawQuery& q, const Kv4Atte
     z.h[i >> 3][i & 7] = h;
     if constexpr (QT == 2) z.l[i >> 3][i & 7] = (_Float16)(y - (float)h);
   }
-  if (top == INFINITY) z.h[0][0] = (_Float16)NAN;
   return z;
 }
 
@@ -303,6 +296,17 @@ struct Columns {
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j], ph[t], o[t][j], 0, 0, 0);
       sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph[t], sum[t], 0, 0, 0);
+    }
+  }
+
+  // Behind a wave's steps, the first of which began at position `from`.  An infinity in a query of
+  // one term can make every score -Inf, which stands for hidden keys; the softmax of such is NaN.
+  // (With two terms the second one is Inf - Inf.)
+  __device__ __forceinline__ void finish(int from) {
+    if constexpr (QT == 1) {
+#pragma unroll
+      for (int t = 0; t < NQ; ++t)
+        if (sum[t][0] == 0.f && lim[t] > (PACK == 2 && right() ? from + kPage : from)) sum[t][0] = NAN;
     }
   }
 
