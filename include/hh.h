@@ -79,6 +79,9 @@ enum { HH_KV_Q4 = 0x100 };
  * head).  A page's scale grows as its positions come and stays when a stream is cut, so a prompt
  * that is evaluated in other passes, or a stream that was longer, may differ by what its codes are
  * rounded again.
+ * Either cache pays where streams are many or long; a single stream's steps are slower than with a
+ * 16-bit one (1B decoder, 8 bits: 0.93 ms for 0.63 at 256 positions, 0.99 for 0.74 at 8,192; 32
+ * streams at 4,000 1.34 for 1.68).
  */
 enum { HH_KV_Q8 = 0x400 };
 enum { HH_LOGITS_NONE = 0, HH_LOGITS_LAST = 1, HH_LOGITS_ALL = 2 };
@@ -453,6 +456,11 @@ hh_status hh_kv4_attention(const hh_kv4_pool* pool, const hh_kv4_rows* rows, con
  *
  * The descriptions are those of the 4-bit cache, with these blocks, and so is what
  * is said there of streams, devices, captures and pointers.
+ * Positions live on the device, so that how a call over all keys, or a selection, is cut up goes by
+ * max_pages, as if every sequence filled its row of the page table. A table that is as
+ * wide as the longest sequence of a call is the fastest: behind one of 8,192 columns a selection for
+ * 4,000 rows of 437 blocks takes 458 us (44 behind 438 columns), for 32 rows of 1,400 22 (19), and
+ * attention of 32 tokens at 4,000 30 (27), of 6 at 200 9 (5.4). Lists do not depend on it.
  * ------------------------------------------------------------------------ */
 
 enum { HH_KV8_BLOCK = 2176 };

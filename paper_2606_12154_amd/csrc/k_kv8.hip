@@ -22,9 +22,10 @@
 // What bounds it.  Few columns over all keys: the loads.  32 sequences of 4,000 positions (132
 // MB) take 27 us, 4.9 TB/s, the same loads alone 24: blocks of 2 KiB in no order, and the
 // longest sequence, which one workgroup a kv head takes whole, is 1.4 times the mean.  Listed
-// blocks of prompts: vector instructions, 100 a step of two blocks beside 14 matrix ones (85%
+// blocks of prompts: vector instructions, 106 a step of two blocks beside 14 matrix ones (85%
 // of the cycles; 4,000 rows of 32 160 us, the same loads alone 96).  Prompts: both, hardly at
-// once, as in the 4-bit cache's kernel (8,192 rows 493 us).
+// once, as in the 4-bit cache's kernel (8,192 rows 488 us).  There four column tiles of queries of two
+// terms take all 256 registers that two waves a SIMD leave each, and 20 bytes of scratch a lane.
 #include "kv_attend.h"
 
 #include <type_traits>
@@ -364,7 +365,10 @@ constexpr int kNowhere = 1 << 30;  // a listed block that is none: behind every 
 // four scores of a step of two pages are of both, not of one and half of them of no column.
 //
 // Scores are products of whole numbers: a query in three signed digits of 8 bits (23 bits of
-// its largest element) times the page's codes as they lie, mfma_i32_16x16x64_i8; three
+// its largest element: a score is off by 2^-16 of the largest |q| times the block's largest |k| at
+// most, where a code's own rounding, half a step of |k| / 127, is worth 2^-8 of that in the largest
+// |q|'s dimension alone; a fourth digit took 28.8 us for 26.6 at 32 tokens of 4,000 positions, 33.0 for
+// 28.9 at one of 131,072) times the page's codes as they lie, mfma_i32_16x16x64_i8; three
 // conversions and two FMAs a score take the place of unpacking the keys (4,000 prompt rows of 32
 // listed blocks 177 -> 164 us, 64 sequences of 1,500 positions 22.7 -> 21.7; 16-bit queries
 // that need one term and no scaling lose 0.4 us at the start).  P = 4 takes fewer exponentials

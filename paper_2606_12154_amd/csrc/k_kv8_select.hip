@@ -13,7 +13,7 @@
 // the integers takes 14, and 30 among equal scores).  What is above it is selected, and of what
 // equals it the first blocks; a sum over lanes gives their places.
 //
-// What bounds it: 32 rows of 1,400 blocks take 19 us, 10 of them reading 45,000 x 8 lines of
+// What bounds it: 32 rows of 600 to 1,400 blocks take 19 us, 10 of them reading 32,000 x 8 lines of
 // 128 bytes, of which 80 are used, 6 searching, by one wave of each workgroup alone.  4,000 prompt
 // rows of 437 blocks: 44, of which the scores 25 (112 MB of lines out of L2), the search 15, places 4.
 // Measured and not kept: a histogram of the scores in LDS before the first guess (2 counts, but 44 ->
@@ -27,7 +27,8 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ queries and scores
 
-// A pair's rotation: x c - y s and y c + x s, the products exact, each rounded once.
+// A pair's rotation, x c - y s and y c + x s, in 64 bits: one product of each is rounded (and
+// exact where a query is not the sum of several, 24 bits by 24), then the sum.
 __device__ __forceinline__ void turn(double& x, double& y, float2 t) {
   const double c = t.x, s = t.y, u = fma(x, c, -(y * s));
   y = fma(y, c, x * s);

@@ -73,6 +73,8 @@ inline Kv8ListPlan kv8_list_plan(const Kv4Sizes& z, int n) {
 //   row of 8,192 blocks 19.6, without 55; 8 of 2,600 21.7 and 35; but 32 of 3,500 50 and 33.6
 //   (33.6 in most runs, 45 to 47 in others of the same code, for a reason not known);
 //   waves of a team: 8,192 blocks 4 waves 19.6, 8 20.0, 16 26.7.
+// All of this goes by the table's width, as if rows had that many blocks: the 4,000 rows of 437 take
+// 73 us behind a table of 1,024 columns, 114 behind 2,048 and 458 behind 8,192; the 32 rows 22.
 constexpr int kMaxSelectPages = 1 << 15;  // a row's scores fit LDS
 struct Kv8SelectPlan {
   int rows, waves, keys;

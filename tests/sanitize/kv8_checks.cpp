@@ -1,8 +1,9 @@
 // The 8-bit cache's calls on the CPU, built with AddressSanitizer and UndefinedBehaviorSanitizer
 // by tests/test_host_kv8.py: what they refuse, and that their launches cover every sequence,
 // row, kv head and split once, with fewer than 2^32 threads each and no more LDS than the kernel
-// may have.  HIP's calls are fake_hip.h's, but for the limit of a kernel's LDS, which is kept
-// here; no launch touches the memory that it is given.
+// may have; and that split outputs are joined, on the 4-bit cache too.  HIP's calls are
+// fake_hip.h's, but for the limit of a kernel's LDS, which is kept here; no launch touches the
+// memory that it is given.
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
@@ -71,6 +72,7 @@ static void run_kernel(const std::string& k, dim3 grid, dim3 block, void** a) {
     CHECK(is("k_kv_join_rows") ? arg<int>(a, 4) <= 16 : arg<int>(a, 4) <= 64);
     return;
   }
+  if (is("k_kv4_attend")) return;  // (kv_checks.cpp's)
   CHECK(grid.x % r.n_seqs == 0);
   const int64_t each = grid.x / r.n_seqs, page_tiles = (r.max_rows + 14) / 16 + 1;
   auto divides = [&](Div d, unsigned by) { return d.d == by && over(grid.x - 1, d) == (grid.x - 1) / by; };
@@ -211,6 +213,22 @@ static void check_limits() {
     }
 }
 
+// The kernels that join split outputs are both caches'.
+static void check_4_bit_joins() {
+  const struct { int n_seqs, max_rows, max_pages; bool split; } cases[] = {
+      {1, 1, 8192, true}, {1, 1, 300, true}, {32, 1, 8192, true}, {3, 150, 450, true}, {1, 128, 8192, true}, {1, 1, 20, false}, {64, 300, 20, false}};
+  for (const auto& c : cases)
+    for (int type : {(int)HH_F32, (int)HH_F16}) {
+      const hh_kv4_pool pool{at, ints, 1000, 8, c.max_pages, 70};
+      const hh_kv4_rows rows{ints, ints, nullptr, c.n_seqs, c.n_seqs * c.max_rows, c.max_rows};
+      size_t need = 0;
+      CHECK(hh_kv4_attention_workspace(&pool, &rows, 32, &need) == HH_OK && (need > 0) == c.split);
+      joins = 0;
+      CHECK(hh_kv4_attention(&pool, &rows, at, type, 2048, 32, 1.f, nullptr, 0, at, type, 2048, at, need, nullptr) == HH_OK);
+      CHECK(joins == (c.split ? 1 : 0));
+    }
+}
+
 static void check_refusals() {
   size_t n = 0;
   hh_kv8_pool pool{at, ints, 9, 2, 4, 3};
@@ -265,6 +283,7 @@ int main() {
   check_refusals();
   check_launches();
   check_limits();
+  check_4_bit_joins();
   if (failures) {
     std::fprintf(stderr, "%d checks of the 8-bit cache's calls failed\n", failures);
     return 1;
