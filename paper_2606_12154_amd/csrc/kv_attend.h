@@ -45,10 +45,12 @@ constexpr float kOffset = 12.f, kSlack = 3.9f;
 
 // A base decides a step's weights only as a number: it is found first, and then every
 // weight's power is one rounding of S qs - base, the same for equal scores in whatever step they
-// come.  Where the base is kLarge or more, the exact product's own last bits would pass its
-// rounding by more than the slack, so that S qs is rounded by itself, and the base is the largest.
-constexpr float kLarge = 65536.f;
-__device__ __forceinline__ float base_for(float top) { return fabsf(top) < kLarge ? top - kOffset : top; }
+// come.  From kLarge on the exact product's last bits would show in the weights, and S qs is
+// rounded by itself.  Rounding may then lift a power past the slack, so that such bases are looked
+// at in every step; from kWhole on a base is the largest score, since the offset would be rounded
+// too.
+constexpr float kLarge = 0x1p16f, kWhole = 0x1p22f;
+__device__ __forceinline__ float base_for(float top) { return fabsf(top) < kWhole ? top - kOffset : top; }
 __device__ __forceinline__ float rounded(float a, float b) {
 #pragma clang fp contract(off)
   return a * b;
@@ -160,11 +162,14 @@ struct Columns {
   f32x4 o[NQ][4], sum[NQ];
   float base[NQ];
   bool first;
-  bool large;  // a base is kLarge or more
+  // Bits of what a score has to pass, against its base, for bases to be looked at: kAny (-Inf) at
+  // first, and once a base is large.
+  static constexpr int kAny = (int)0xff800000, kSome = __builtin_bit_cast(int, kOffset + kSlack);
+  int limit;
 
   __device__ __forceinline__ void start(const Place& w, int most) {
     first = true;
-    large = false;
+    limit = kAny;
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
 #pragma unroll
@@ -231,7 +236,7 @@ struct Columns {
     }
     // A wave's first pages set the base: a column that sees none of them sees
     // none of the later ones either.
-    if (first || __builtin_amdgcn_ballot_w64(high > kOffset + kSlack)) {
+    if (__builtin_amdgcn_ballot_w64(high > __int_as_float(limit))) {
       bool is_large = false;
 #pragma unroll
       for (int t = 0; t < NQ; ++t) {
@@ -245,10 +250,10 @@ struct Columns {
         for (int j = 0; j < 4; ++j) o[t][j] *= f;
         sum[t] *= f;
       }
-      large = __builtin_amdgcn_ballot_w64(is_large);
+      limit = __builtin_amdgcn_ballot_w64(is_large) ? kAny : kSome;
     }
     first = false;
-    if (large) {
+    if (limit == kAny) {
 #pragma unroll
       for (int t = 0; t < NQ; ++t)
 #pragma unroll

@@ -116,3 +116,42 @@ def test_scores_past_fp32_of_a_4_bit_cache(t, top, rows):
             want = vv[best].mean(0)
             err = np.abs(out[i].double().cpu().numpy() - want)
             assert (err <= np.abs(vv).max() * (2 * 2.0 ** -22 + (m / 32 + 16) * 2.0 ** -23 + 3 * 2.0 ** -19)).all(), (seen, i, err.max())
+
+
+@pytest.mark.parametrize("t,rope", [("f32", False), ("f16", False), ("bf16", False), ("f32", True)])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("rows", [1, 4, 40, 300])
+def test_large_scores_that_differ_by_little(t, rope, bits, rows):
+    """Scores of 2^18 to 2^30 as a power of two, which rise by 1/4 to 100 from page to page (a dimension of small
+    queries whose keys rise): beside the rounding of such scores any of the higher ones may take all, but weights
+    stay finite, and results a mean of the values.  The bound: a mean's, and of its two fp16 terms and sums."""
+    torch.manual_seed(0)
+    n = 700
+    sizes = torch.exp2(torch.linspace(8, 14.5, 4 * rows)).reshape(rows, 4, 1)  # |q| = |k| times a constant
+    steps = torch.exp2(torch.rand(rows, 4) * 9 - 3)
+    k, v = torch.full((n, 1, 64), 512.0), torch.randn(n, 1, 64).abs() + 0.5
+    k[:, 0, 31] = (torch.arange(n) // 16 % 5 * 128).float()
+    k[:, 0, 63] = 0.0
+    # (A rise of 128 in the 31st dimension: steps as a power of two; the pair's other dimension is 0.)
+    q = (sizes.square() / 512).expand(rows, 4, 64).clone()
+    q[..., 31], q[..., 63] = steps / (128 * 0.125 * 1.4427), 0.0
+    if t == "f16":
+        q = q.clamp(max=60000.0)
+    tab = torch.tensor([1.0, 0.0]).expand(n, 32, 2).contiguous().cuda() if rope else None
+    q, k, v = (x.cuda().contiguous() for x in (q.to(TYPES[t][1]), k, v))
+    out = torch.empty(rows, 4, 64, device="cuda:0")
+    if bits == 8:
+        c = Cache(1, 1, (n + 15) // 16)
+        c.append([n], [0], k, v, "f32", ref=False)
+        r, keep = c.rows([0, rows], [n - rows], rows)
+        attend(c, r, q, t, out, "f32", rope=None if tab is None else tab.cpu().numpy())
+    else:
+        c = four.Cache(1, 1, (n + 15) // 16, 0)
+        r, keep = c.rows([0, n], [0], n)
+        four.append(c, r, k, v, "f32")
+        r, keep = c.rows([0, rows], [n - rows], rows)
+        four.attend(c, r, q, t, out, "f32", 0.125, tab)
+    most, least = v.max() * (1 + (1 / 14 if bits == 4 else 1 / 250)), v.min() - v.max() / (14 if bits == 4 else 250)
+    slack = v.max() * (2.0 ** -21 + (n / 32 + 16) * 2.0 ** -23)
+    assert torch.isfinite(out).all()
+    assert (out <= most + slack).all() and (out >= least - slack).all()
